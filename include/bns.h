@@ -351,6 +351,111 @@ bns_status bns_workspace_status(const void* workspace, uint32_t* flags, void* cu
 int bns_slab_plan(const bns_shape* shape, const bns_sampling* sampling, int backward, int32_t* plan);
 bns_status bns_wait_timeouts(uint32_t* count, void* cuda_stream);
 
+/* ==== operators at the end of a language model's step =============================================
+ *
+ * Residual add + root-mean-square norm, linear head + softmax cross entropy, distillation from a
+ * teacher's top logits.  The conventions at the top of this file hold, except for what is said here:
+ * the large tensors are matrices whose rows are dense and may lie apart (strides in elements, at least
+ * the row's length); outputs of the caller's type are dense unless a stride is passed for them.
+ * rows = 0 is allowed: nothing is read, gradients of weights are set to zero, row pointers may be NULL.
+ */
+typedef struct {
+    int rows, columns;
+    int dtype;                  /* bns_dtype */
+} bns_rows;
+
+/*
+ * Residual add + root-mean-square norm of the rows.
+ *   s = x + residual (fp32; residual may be NULL: s = x)      h = s in the tensor's type
+ *   rstd_t = 1 / sqrt(mean_i s_ti^2 + eps)                     y_ti = s_ti rstd_t weight_i
+ * The sum is not rounded before it is normalised.  h may be NULL.  weight is float[columns], rstd
+ * float[rows].  Any alignment of the element type: rows whose addresses and strides are multiples of 16
+ * bytes are moved in 16-byte words, others in the widest words that they allow.
+ */
+bns_status bns_rms_norm_forward(const bns_rows* shape, const void* x, int64_t x_stride, const void* residual,
+                                int64_t residual_stride, const float* weight, float eps, void* y, void* h,
+                                float* rstd, void* cuda_stream);
+
+/*
+ * The same with y in 8 bits (e4m3: 4 bits of exponent, 3 of fraction, largest value 448) and scales:
+ *   a = max |y| over a group of columns     scale = a / 448, 1 where a = 0     q = e4m3(y / scale)
+ * group = 0: one scale per row, scales is float[rows]; group = 128: one per 128 columns (the last group
+ * may be shorter), scales is float[rows][ceil(columns / 128)].  q is a dense byte matrix.
+ */
+bns_status bns_rms_norm_forward_quantized(const bns_rows* shape, const void* x, int64_t x_stride,
+                                          const void* residual, int64_t residual_stride, const float* weight,
+                                          float eps, int group, void* q, float* scales, void* h, float* rstd,
+                                          void* cuda_stream);
+
+/*
+ * Gradient at the stored sum h:   c_t = mean_i weight_i dy_ti h_ti rstd_t
+ *   dx_ti = rstd_t (weight_i dy_ti - h_ti rstd_t c_t) + dh_ti        dweight_i = sum_t dy_ti h_ti rstd_t
+ * dh (may be NULL) is the gradient that reaches h along the residual path; dx is the gradient of x and of
+ * the residual alike.  dweight is float[columns], summed in fp32 in a fixed order.
+ */
+size_t bns_rms_norm_workspace_bytes(const bns_rows* shape);
+bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t dy_stride, const void* h,
+                                 int64_t h_stride, const float* weight, const float* rstd, const void* dh,
+                                 int64_t dh_stride, void* dx, float* dweight, void* workspace,
+                                 size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Linear head + softmax cross entropy, without keeping the logits.
+ *   z = x w^T (x: rows x width, w: vocabulary x width)       lse_t = log sum_v exp z_tv
+ *   loss_t = lse_t - z_{t, target_t}, and 0 where target_t is not in [0, vocabulary)
+ * A negative target leaves its row out; one at or above the vocabulary's size does too, and sets
+ * BNS_FLAG_BAD_TARGET in the workspace's status word (see bns_workspace_status).
+ * Backward, with dloss float[rows] the gradient of each row's loss (rows that are left out: ignored):
+ *   G_tv = dloss_t (exp(z_tv - lse_t) - [v = target_t])      dx = G w      dw = G^T x
+ * The logits are computed again, one piece of the vocabulary at a time; G of a piece is held in the
+ * workspace (bf16 for bf16 tensors: half an ulp of the gradients' own type per term).
+ * loss, lse: float[rows].  dx, dw: the type of x and w, dense.  x and w must be 16-byte aligned; bf16
+ * rows whose stride or width is no multiple of 8 elements are copied piece by piece, and fp32 tensors are
+ * split into three bf16 terms whose products are added up in fp32 (the result is that of an fp32 product).
+ * rows <= 2^24, vocabulary <= 2^28, width <= 2^20.
+ */
+typedef struct {
+    int rows, vocabulary, width;
+    int dtype;                  /* bns_dtype of x, w, dx, dw          */
+    int64_t x_stride, w_stride; /* elements from one row to the next  */
+    int target_is_int64;        /* 0: target is int32_t[rows]         */
+} bns_head;
+#define BNS_FLAG_BAD_TARGET 2u
+size_t bns_linear_cross_entropy_workspace_bytes(const bns_head* shape, int backward);
+bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x, const void* w, const void* target,
+                                            float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                                            void* cuda_stream);
+bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* x, const void* w, const void* target,
+                                             const float* lse, const float* dloss, void* dx, void* dw,
+                                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Distillation: divergence of the student's distribution from a teacher's top logits.
+ *   teacher [rows][entries] logits at index [rows][entries]; an index outside [0, vocabulary) is no entry
+ *   p = softmax over the row's entries of teacher / temperature     q = softmax of logits / temperature
+ *   loss_t = temperature^2 sum_k p_k (log p_k - log q_{index_k})     lse_t = log sum_v exp(logits_tv / temperature)
+ *   dlogits_tv = dloss_t temperature (q_v - sum over k with index_k = v of p_k)
+ * A row without entries (or whose entries are all -inf) has loss 0 and gradient 0.  _backward takes the
+ * lse of _forward; _step gives loss and gradient in one launch where dloss is known beforehand.
+ * 1 <= entries <= 1024.  Any alignment of the element type.
+ */
+typedef struct {
+    int rows, vocabulary, entries;
+    int dtype;                  /* bns_dtype of logits and dlogits    */
+    int64_t stride;             /* elements from one row of logits to the next */
+    int teacher_dtype;          /* bns_dtype of teacher               */
+    int index_is_int64;         /* 0: index is int32_t                */
+    float temperature;
+} bns_distillation;
+bns_status bns_topk_distillation_forward(const bns_distillation* shape, const void* logits, const void* teacher,
+                                         const void* index, float* loss, float* lse, void* cuda_stream);
+bns_status bns_topk_distillation_backward(const bns_distillation* shape, const void* logits, const void* teacher,
+                                          const void* index, const float* lse, const float* dloss, void* dlogits,
+                                          int64_t dlogits_stride, void* cuda_stream);
+bns_status bns_topk_distillation_step(const bns_distillation* shape, const void* logits, const void* teacher,
+                                      const void* index, const float* dloss, float* loss, void* dlogits,
+                                      int64_t dlogits_stride, void* cuda_stream);
+
 const char* bns_status_string(bns_status status);
 
 /* ---- measurement hooks (process-wide, not thread-safe; off by default) ---------------------- */
@@ -369,7 +474,14 @@ typedef enum {
     BNS_KERNEL_VECTOR = 11,        /* C-length kernels: mixing of statistics, moving average          */
     BNS_KERNEL_SLAB_FORWARD = 12,  /* whole forward of a layer whose channel data fits on chip        */
     BNS_KERNEL_SLAB_BACKWARD = 13, /* whole backward of such a layer                                   */
-    BNS_KERNEL_KINDS = 14
+    BNS_KERNEL_RMS_FORWARD = 14,   /* residual add + root-mean-square norm                             */
+    BNS_KERNEL_RMS_BACKWARD = 15,
+    BNS_KERNEL_HEAD_LOGITS = 16,   /* head: logits' statistics                                         */
+    BNS_KERNEL_HEAD_GRADIENT = 17, /* head: logits again, their gradient                               */
+    BNS_KERNEL_HEAD_PRODUCT = 18,  /* head: dx and dw                                                  */
+    BNS_KERNEL_HEAD_VECTOR = 19,   /* head: joining of partial results, copies of operands             */
+    BNS_KERNEL_DISTILL = 20,       /* distillation: loss, gradient                                     */
+    BNS_KERNEL_KINDS = 21
 } bns_kernel_kind;
 
 /* Number of kernels this library has launched in this process since load (or since reset). */
@@ -396,7 +508,8 @@ const char* bns_kernel_name(int kernel_kind);
  * the streaming kernels), "slab_small_sets": 0/1 take that path also when the sampled set is small (default 0: the
  * streaming path is then two short kernels per direction and measured faster), "slab_cluster_max": largest cluster (1..8);
  * "per_channel_min_hw": map size H*W from which backward pass 1 keeps its sums per channel instead of per position;
- * "host_pipeline": 0/1 row-chunk pipelining of bns_forward_backward_host; "fold_finalize": 0/1 let the second
+ * "head_piece": most columns of the vocabulary that bns_linear_cross_entropy_* hold in the workspace at a time (0 = as many as
+ * make 256 MiB); "host_pipeline": 0/1 row-chunk pipelining of bns_forward_backward_host; "fold_finalize": 0/1 let the second
  * backward pass over a sampled set finish the sums of Eq. 5 itself; "pdl": 0/1 programmatic dependent launch; "l2_order": 0/1 visit rows in an
  * order that lets a kernel find in L2 what the previous one read.  Returns BNS_OK,
  * BNS_ERR_RULE for an unknown name or BNS_ERR_SHAPE for a value < 1. */

@@ -23,10 +23,11 @@ RULE_FULL, RULE_BATCH, RULE_FEATURE, RULE_VIRTUAL = 0, 1, 2, 3
 OFF_SHARED, OFF_PER_SAMPLE, OFF_PER_MAP = 0, 1, 2
 FLAG_BAD_OFFSET = 1
 
-KERNEL_KINDS = 14
+KERNEL_KINDS = 21
 (KERNEL_COL_MOMENTS, KERNEL_PATCH_MOMENTS, KERNEL_FINALIZE_STATS, KERNEL_NORMALIZE, KERNEL_BWD_REDUCE,
  KERNEL_FINALIZE_BWD, KERNEL_COL_FIXUP, KERNEL_PATCH_FIXUP, KERNEL_MASK, KERNEL_DIRECT_MOMENTS,
- KERNEL_DIRECT_FIXUP, KERNEL_VECTOR, KERNEL_SLAB_FORWARD, KERNEL_SLAB_BACKWARD) = range(KERNEL_KINDS)
+ KERNEL_DIRECT_FIXUP, KERNEL_VECTOR, KERNEL_SLAB_FORWARD, KERNEL_SLAB_BACKWARD, KERNEL_RMS_FORWARD, KERNEL_RMS_BACKWARD,
+ KERNEL_HEAD_LOGITS, KERNEL_HEAD_GRADIENT, KERNEL_HEAD_PRODUCT, KERNEL_HEAD_VECTOR, KERNEL_DISTILL) = range(KERNEL_KINDS)
 
 EXPORTS = [
     "bns_workspace_bytes", "bns_forward", "bns_forward_static", "bns_static_workspace_bytes", "bns_backward", "bns_full_bn", "bns_host_arena_bytes",
@@ -39,6 +40,10 @@ EXPORTS = [
     "bns_sync_backward_apply",
     "bns_forward_relu", "bns_backward_relu",
     "bns_workspace_bytes_nhwc", "bns_forward_nhwc", "bns_backward_nhwc",
+    # bound in lm.py
+    "bns_rms_norm_forward", "bns_rms_norm_forward_quantized", "bns_rms_norm_workspace_bytes", "bns_rms_norm_backward",
+    "bns_linear_cross_entropy_workspace_bytes", "bns_linear_cross_entropy_forward", "bns_linear_cross_entropy_backward",
+    "bns_topk_distillation_forward", "bns_topk_distillation_backward", "bns_topk_distillation_step",
 ]
 
 

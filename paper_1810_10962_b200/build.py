@@ -8,13 +8,15 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIBRARY = os.path.join(HERE, "libbns.so")
-SOURCES = [os.path.join(CSRC, "bns_api.cu")]
-HEADERS = [os.path.join(CSRC, "bns_kernels.cuh"), os.path.join(CSRC, "bns_nhwc_kernels.cuh"), os.path.join(CSRC, "bns_slab_kernels.cuh"), os.path.join(ROOT, "include", "bns.h")]
+SOURCES = [os.path.join(CSRC, name) for name in ("bns_api.cu", "bns_lm_api.cu")]
+HEADERS = [os.path.join(CSRC, name) for name in (
+    "bns_host.h", "bns_elements.cuh", "bns_kernels.cuh", "bns_nhwc_kernels.cuh", "bns_slab_kernels.cuh",
+    "bns_rms_kernels.cuh", "bns_head_kernels.cuh", "bns_distill_kernels.cuh")] + [os.path.join(ROOT, "include", "bns.h")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-O3", "-lineinfo", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared",
+    "-Xcompiler", "-fPIC", "-shared", "--threads", "0",
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 

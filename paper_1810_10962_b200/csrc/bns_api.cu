@@ -9,18 +9,16 @@
 #include <mutex>
 #include <vector>
 
+#include "bns_host.h"
 #include "bns_kernels.cuh"
 #include "bns_nhwc_kernels.cuh"
 #include "bns_slab_kernels.cuh"
 
+namespace bns {
+
 namespace {
-
-using namespace bns;
-
-constexpr size_t kAlign = 256;
-constexpr size_t kHeaderBytes = 256;  // status word lives at the start of the workspace
-constexpr int kMaxDevices = 64;
 constexpr int kSmCountFallback = 148;     // B200; used only if the device cannot be queried
+}
 
 // Streaming multiprocessors of the current device (queried once per device).
 int sm_count() {
@@ -37,11 +35,8 @@ int sm_count() {
     return n;
 }
 
-size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
-int elem_bytes(int dtype) { return dtype == BNS_F32 ? 4 : 2; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // ------------------------------------------------------------------------------------ measurement hooks
+namespace {
 std::atomic<uint64_t> g_launches{0};
 bool g_profile = false;
 constexpr int kEventPool = 8192;
@@ -63,29 +58,61 @@ cudaEvent_t take_event() {
     return e;
 }
 
-struct LaunchScope {
-    cudaStream_t stream;
-    bool timed = false;
-    TimedLaunch rec{};
-    LaunchScope(int kind, cudaStream_t s) : stream(s) {
-        g_launches.fetch_add(1, std::memory_order_relaxed);
-        if (g_profile && static_cast<int>(g_timed.size()) < kEventPool) {
-            rec.kind = kind;
-            rec.start = take_event();
-            rec.stop = take_event();
-            if (rec.start && rec.stop) {
-                timed = true;
-                cudaEventRecord(rec.start, stream);
-            }
+}  // namespace
+
+LaunchScope::LaunchScope(int kind_, cudaStream_t s) : stream(s), kind(kind_) {
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    if (g_profile && static_cast<int>(g_timed.size()) < kEventPool) {
+        start = take_event();
+        stop = take_event();
+        if (start && stop) {
+            timed = true;
+            cudaEventRecord(start, stream);
         }
     }
-    ~LaunchScope() {
-        if (timed) {
-            cudaEventRecord(rec.stop, stream);
-            g_timed.push_back(rec);
-        }
+}
+
+LaunchScope::~LaunchScope() {
+    if (timed) {
+        cudaEventRecord(stop, stream);
+        g_timed.push_back(TimedLaunch{kind, start, stop});
     }
-};
+}
+
+// Launch failures of the current call, on this host thread: every launch helper records the return code
+// of its own cudaLaunchKernelEx, so an error that some other code left in the runtime is neither
+// reported as ours nor cleared.
+namespace {
+thread_local bool t_launch_failed = false;
+}
+
+void note_launch(cudaError_t err) {
+    if (err != cudaSuccess) {
+        t_launch_failed = true;
+        cudaGetLastError();  // a failed launch leaves its error behind: take it back out
+    }
+}
+
+bns_status last_error() {
+    const bool failed = t_launch_failed;
+    t_launch_failed = false;
+    return failed ? BNS_ERR_CUDA : BNS_OK;
+}
+
+bool g_pdl = true;
+
+}  // namespace bns
+
+namespace {
+
+using namespace bns;
+
+constexpr size_t kAlign = 256;
+constexpr size_t kHeaderBytes = 256;  // status word lives at the start of the workspace
+
+size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+int elem_bytes(int dtype) { return dtype == BNS_F32 ? 4 : 2; }
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // ------------------------------------------------------------------------------------ planning
 // How a streaming kernel covers `rows` rows of P positions: vector width, tiles per row, rows per block.
@@ -401,24 +428,6 @@ T* ws_at(void* ws, size_t off) {
     return reinterpret_cast<T*>(static_cast<char*>(ws) + off);
 }
 
-// Launch failures of the current call, on this host thread: every launch helper records the return code
-// of its own cudaLaunchKernelEx, so an error that some other code left in the runtime is neither
-// reported as ours nor cleared.
-thread_local bool t_launch_failed = false;
-
-void note_launch(cudaError_t err) {
-    if (err != cudaSuccess) {
-        t_launch_failed = true;
-        cudaGetLastError();  // a failed launch leaves its error behind: take it back out
-    }
-}
-
-bns_status last_error() {
-    const bool failed = t_launch_failed;
-    t_launch_failed = false;
-    return failed ? BNS_ERR_CUDA : BNS_OK;
-}
-
 // Copies a non-contiguous sample list into the workspace; returns the device list or NULL.
 bns_status stage_list(const Problem& pb, const bns_sampling* sp, void* ws, cudaStream_t stream, const int** list) {
     *list = nullptr;
@@ -440,7 +449,6 @@ bns_status clear_status(const Problem& pb, void* ws, cudaStream_t stream, unsign
 }
 
 // ------------------------------------------------------------------------------------ launches
-bool g_pdl = true;    // ask for programmatic dependent launch (blocks may be scheduled while the previous kernel drains)
 bool g_fold_finalize = true;  // let the second backward pass finish the sums of Eq. 5 itself where it can
 bool g_l2_order = true;  // order rows so that a kernel re-reads what the previous one left in L2
 
@@ -1612,6 +1620,7 @@ int bns_set_tuning(const char* name, int value) {
                  {"per_channel_min_hw", &g_per_channel_min_hw, nullptr, false},
                  {"fold_finalize", nullptr, &g_fold_finalize, false},
                  {"host_pipeline", nullptr, &g_host_pipeline, false},
+                 {"head_piece", &g_head_piece, nullptr, true},
                  {"pdl", nullptr, &g_pdl, false},
                  {"l2_order", nullptr, &g_l2_order, false}};
     for (const Knob& k : knobs) {
@@ -1646,9 +1655,14 @@ int bns_slab_plan(const bns_shape* shape, const bns_sampling* sampling, int back
 bns_status bns_wait_timeouts(uint32_t* count, void* cuda_stream) {
     if (!count) return BNS_ERR_NULL;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    uint32_t head = 0;
+    bns_status st = head_wait_timeouts(&head, stream);
+    if (st != BNS_OK) return st;
     if (cudaMemcpyFromSymbolAsync(count, g_wait_timeouts, sizeof(uint32_t), 0, cudaMemcpyDeviceToHost, stream) != cudaSuccess)
         return BNS_ERR_CUDA;
-    return cudaStreamSynchronize(stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
+    if (cudaStreamSynchronize(stream) != cudaSuccess) return BNS_ERR_CUDA;
+    *count += head;
+    return BNS_OK;
 }
 
 const char* bns_kernel_name(int kernel_kind) {
@@ -1667,6 +1681,13 @@ const char* bns_kernel_name(int kernel_kind) {
     case BNS_KERNEL_VECTOR: return "per-channel vector kernels";
     case BNS_KERNEL_SLAB_FORWARD: return "slab_forward_kernel";
     case BNS_KERNEL_SLAB_BACKWARD: return "slab_backward_kernel";
+    case BNS_KERNEL_RMS_FORWARD: return "rms_forward_kernel";
+    case BNS_KERNEL_RMS_BACKWARD: return "rms_backward_kernel";
+    case BNS_KERNEL_HEAD_LOGITS: return "head_gemm_kernel (statistics)";
+    case BNS_KERNEL_HEAD_GRADIENT: return "head_gemm_kernel (gradient of the logits)";
+    case BNS_KERNEL_HEAD_PRODUCT: return "head_gemm_kernel (gradients)";
+    case BNS_KERNEL_HEAD_VECTOR: return "head: joining and layout kernels";
+    case BNS_KERNEL_DISTILL: return "distill_kernel";
     }
     return "unknown";
 }

@@ -1,0 +1,578 @@
+// Host side of the language-model operators declared in include/bns.h: residual add + root-mean-square norm,
+// linear head + cross entropy, top-k distillation.  Checks, plans, workspace layout and launches; nothing here allocates
+// device memory or synchronises the host.
+#include <algorithm>
+#include <atomic>
+
+#include "bns_distill_kernels.cuh"
+#include "bns_head_kernels.cuh"
+#include "bns_host.h"
+#include "bns_rms_kernels.cuh"
+
+namespace {
+
+using namespace bns;
+
+constexpr size_t kAlign = 256;
+constexpr size_t kHeaderBytes = 256;   // the status word
+
+size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+template <typename N>
+N divide_up(N a, N b) {
+    return (a + b - 1) / b;
+}
+int elem_bytes(int dtype) { return dtype == BNS_F32 ? 4 : 2; }
+bool known(int dtype) { return dtype == BNS_F32 || dtype == BNS_BF16; }
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+bool workspace_fits(const void* ws, size_t bytes, size_t need) { return ws && aligned(ws, kAlign) && bytes >= need; }
+
+template <typename... KArgs, typename... Args>
+void launch(int kind, void (*kernel)(KArgs...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s, Args&&... args) {
+    LaunchScope scope(kind, s);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = g_pdl ? 1 : 0;
+    note_launch(cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...));
+}
+
+// The widest vector (up to 16 bytes) that divides the row, the strides and the addresses.
+struct VectorRule {
+    int V;
+    explicit VectorRule(int columns, int ebytes) : V(16 / ebytes) {
+        while (columns % V) V >>= 1;
+        eb = ebytes;
+    }
+    void tensor(const void* p, int64_t stride) {
+        if (!p) return;
+        while (stride % V || !aligned(p, static_cast<size_t>(V) * eb)) V >>= 1;
+    }
+
+private:
+    int eb;
+};
+
+// ------------------------------------------------------------------------------------ root-mean-square norm
+bns_status check_rows(const bns_rows* sh) {
+    if (!sh) return BNS_ERR_NULL;
+    if (sh->rows < 0 || sh->columns <= 0) return BNS_ERR_SHAPE;
+    if (!known(sh->dtype)) return BNS_ERR_DTYPE;
+    return BNS_OK;
+}
+
+struct RmsPlan {
+    int threads;
+    bool wide;       // the row does not fit the block's registers
+    unsigned grid;
+};
+
+RmsPlan plan_rms(int rows, int columns, int V, bool backward) {
+    RmsPlan pl;
+    const int per_thread = std::min(kRmsElements / V, 8), vectors = columns / V;
+    const int threads = divide_up(divide_up(vectors, per_thread), 32) * 32;
+    pl.wide = threads > kRmsMaxThreads;
+    pl.threads = pl.wide ? kRmsMaxThreads : threads;
+    const int blocks_per_sm = std::max(1, std::min(16, 1024 / pl.threads));
+    pl.grid = static_cast<unsigned>(std::min<int64_t>(rows, static_cast<int64_t>(sm_count()) * blocks_per_sm));
+    return pl;
+}
+
+#define BNS_LM_BY_TYPE_V(dtype, V_, CALL)                   \
+    do {                                                    \
+        if ((dtype) == BNS_F32) {                           \
+            using T = F32;                                  \
+            switch (V_) {                                   \
+            case 4: { constexpr int V = 4; CALL; } break;   \
+            case 2: { constexpr int V = 2; CALL; } break;   \
+            default: { constexpr int V = 1; CALL; } break;  \
+            }                                               \
+        } else {                                            \
+            using T = BF16;                                 \
+            switch (V_) {                                   \
+            case 8: { constexpr int V = 8; CALL; } break;   \
+            case 4: { constexpr int V = 4; CALL; } break;   \
+            case 2: { constexpr int V = 2; CALL; } break;   \
+            default: { constexpr int V = 1; CALL; } break;  \
+            }                                               \
+        }                                                   \
+    } while (0)
+
+#define BNS_LM_BY_TYPE(dtype, CALL) \
+    do {                            \
+        if ((dtype) == BNS_F32) {   \
+            using T = F32;          \
+            CALL;                   \
+        } else {                    \
+            using T = BF16;         \
+            CALL;                   \
+        }                           \
+    } while (0)
+
+template <typename OUT>
+bns_status rms_forward(const bns_rows* sh, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                       const float* weight, float eps, void* y, float* scales, void* h, float* rstd, void* cuda_stream) {
+    constexpr bool quantized = !__is_same(OUT, RmsNone);
+    if (sh->rows == 0) return BNS_OK;
+    if (!x || !weight || !y || !rstd || (quantized && !scales)) return BNS_ERR_NULL;
+    if (!(eps > 0.f) || x_stride < sh->columns || (residual && residual_stride < sh->columns)) return BNS_ERR_SHAPE;
+    const size_t eb = elem_bytes(sh->dtype);
+    if (!aligned(x, eb) || !aligned(residual, eb) || !aligned(h, eb) || !aligned(weight, 4) || !aligned(rstd, 4) ||
+        !aligned(scales, 4) || !(quantized || aligned(y, eb)))
+        return BNS_ERR_ALIGN;
+    VectorRule rule(sh->columns, static_cast<int>(eb));
+    rule.tensor(x, x_stride);
+    rule.tensor(residual, residual_stride);
+    rule.tensor(h, sh->columns);
+    if (!quantized) rule.tensor(y, sh->columns);
+    while (quantized && !aligned(y, static_cast<size_t>(rule.V))) rule.V >>= 1;
+    const RmsPlan pl = plan_rms(sh->rows, sh->columns, rule.V, false);
+    const RmsForward a{x, residual, weight, y, scales, h, rstd, sh->rows, x_stride, residual_stride, sh->columns, eps,
+                       1.f / static_cast<float>(sh->columns)};
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const size_t smem = __is_same(OUT, RmsGroupScale) && rule.V < 4 ? pl.threads / 32 * 8 * sizeof(float) : 0;
+    if (pl.wide)
+        BNS_LM_BY_TYPE_V(sh->dtype, rule.V, (launch(BNS_KERNEL_RMS_FORWARD, rms_forward_wide_kernel<T, V, OUT>, pl.grid,
+                                                    pl.threads, 0, stream, a)));
+    else
+        BNS_LM_BY_TYPE_V(sh->dtype, rule.V, (launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, OUT>, pl.grid, pl.threads,
+                                                    smem, stream, a)));
+    return last_error();
+}
+
+// Blocks of the gradient kernel, at the most: each leaves a row of partial sums.
+int rms_backward_blocks(int rows) { return std::min(rows, sm_count() * 16); }
+
+// ------------------------------------------------------------------------------------ head
+constexpr size_t kHeadPieceBytes = size_t{256} << 20;   // aimed at for G of a piece, and for a piece's operand in bf16 terms
+constexpr int kHeadPieceLeast = 4096;
+
+struct HeadProblem {
+    int T, V, D, dtype;
+    bool f32, copy_x, copy_w;       // operands laid out anew in the workspace
+    int terms, pairs;
+    int pitch;                      // of a copied row's term
+    int piece, pieces;              // columns of the vocabulary at a time
+    int G_pitch;
+    int splits;                     // of dx along the vocabulary
+    size_t off_x, off_w, off_G, off_partial, off_logit, off_sums, total;
+};
+
+bns_status check_head(const bns_head* sh) {
+    if (!sh) return BNS_ERR_NULL;
+    if (sh->rows < 0 || sh->vocabulary <= 0 || sh->width <= 0 || sh->rows > 1 << 24 || sh->vocabulary > 1 << 28 ||
+        sh->width > 1 << 20 || sh->x_stride < sh->width || sh->w_stride < sh->width)
+        return BNS_ERR_SHAPE;
+    if (!known(sh->dtype)) return BNS_ERR_DTYPE;
+    return BNS_OK;
+}
+
+bool tma_rows(int64_t stride) { return stride % 8 == 0 && stride < int64_t{1} << 38; }
+
+HeadProblem plan_head(const bns_head* sh, bool backward) {
+    HeadProblem p{};
+    p.T = sh->rows;
+    p.V = sh->vocabulary;
+    p.D = sh->width;
+    p.dtype = sh->dtype;
+    p.f32 = sh->dtype == BNS_F32;
+    p.copy_x = p.f32 || !tma_rows(sh->x_stride);
+    p.copy_w = p.f32 || !tma_rows(sh->w_stride);
+    p.terms = p.f32 ? 3 : 1;
+    p.pairs = p.f32 ? 6 : 1;
+    p.pitch = divide_up(p.D, kHeadK) * kHeadK;
+    size_t column = 0;              // workspace bytes per column of the vocabulary
+    if (p.copy_w) column = static_cast<size_t>(p.terms) * p.pitch * 2;
+    if (backward) column = std::max(column, static_cast<size_t>(p.T) * p.terms * 2);
+    int64_t piece = p.V;
+    if (column) piece = std::max<int64_t>(kHeadPieceLeast, static_cast<int64_t>(kHeadPieceBytes / column) / kHeadN * kHeadN);
+    if (g_head_piece > 0 && (p.copy_w || backward)) piece = std::min<int64_t>(piece, g_head_piece);
+    p.pieces = static_cast<int>(divide_up<int64_t>(p.V, piece));
+    // equal pieces of whole tiles
+    p.piece = static_cast<int>(std::min<int64_t>(p.V, divide_up(divide_up(p.V, p.pieces), kHeadN) * static_cast<int64_t>(kHeadN)));
+    p.pieces = divide_up(p.V, p.piece);
+    p.G_pitch = divide_up(p.piece, kHeadK) * kHeadK;
+    // few rows: dx is a product with few tiles and a long sum, which is split over the SMs
+    const int64_t tiles = static_cast<int64_t>(divide_up(p.T, kHeadM)) * divide_up(p.D, kHeadN);
+    const int64_t steps = static_cast<int64_t>(divide_up(p.piece, kHeadK)) * p.pairs;
+    p.splits = static_cast<int>(std::max<int64_t>(1, std::min(tiles ? sm_count() / tiles : 1, steps / 4)));
+    size_t at = kHeaderBytes;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at = align_up(at + bytes);
+        return here;
+    };
+    const size_t T = p.T;
+    if (p.copy_x) p.off_x = take(T * p.terms * p.pitch * 2);
+    if (p.copy_w) p.off_w = take(static_cast<size_t>(p.piece) * p.terms * p.pitch * 2);
+    if (backward) {
+        p.off_G = take(T * p.terms * p.G_pitch * 2);
+        if (p.splits > 1 || p.pieces > 1) p.off_sums = take(T * p.splits * p.D * 4);
+    } else {
+        p.off_partial = take(T * divide_up(p.V, kHeadN) * sizeof(float2) + T * p.pieces * sizeof(float2));
+        p.off_logit = take(T * 4);
+    }
+    p.total = at;
+    return p;
+}
+
+// Tensor map of a matrix of bf16 rows; the box is 64 elements (128 bytes, swizzled) by `box_rows`.
+bool make_map(CUtensorMap* map, const void* base, uint64_t columns, uint64_t rows, uint64_t stride_elements, unsigned box_rows) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<void*> entry{nullptr};
+    void* fn = entry.load(std::memory_order_relaxed);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess || !fn)
+            return false;
+        entry.store(fn, std::memory_order_relaxed);
+    }
+    const cuuint64_t dims[2] = {columns, rows}, strides[1] = {stride_elements * 2};
+    const cuuint32_t box[2] = {kHeadK, box_rows}, steps[2] = {1, 1};
+    return reinterpret_cast<Encode>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
+                                        steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A matrix operand: `terms` bf16 terms a row, `pitch` elements apart.
+struct Operand {
+    const void* base;
+    int64_t stride;     // elements from one row to the next
+    int rows, columns;  // that exist; with several terms a term's padding exists too
+    int terms, pitch;
+    bool map(CUtensorMap* m, unsigned box_rows) const {
+        return make_map(m, base, terms > 1 ? static_cast<uint64_t>(terms) * pitch : columns, rows, stride, box_rows);
+    }
+};
+
+template <int KIND, bool A_K, bool B_K, typename T>
+bns_status head_gemm(int kind, const Operand& a, const Operand& b, HeadGemm g, int K, cudaStream_t stream) {
+    static std::atomic<bool> raised[kMaxDevices];
+    int device = -1;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= kMaxDevices) return BNS_ERR_CUDA;
+    auto kernel = head_gemm_kernel<KIND, A_K, B_K, T>;
+    if (!raised[device].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem) != cudaSuccess) {
+            cudaGetLastError();
+            return BNS_ERR_CUDA;
+        }
+        raised[device].store(true, std::memory_order_relaxed);
+    }
+    CUtensorMap ma, mb;
+    if (!a.map(&ma, A_K ? kHeadM : 64) || !b.map(&mb, B_K ? kHeadN : 64)) return BNS_ERR_CUDA;
+    g.tiles_m = divide_up(g.M, kHeadM);
+    g.tiles_n = divide_up(g.N, kHeadN);
+    g.k_blocks = divide_up(K, kHeadK);
+    g.pairs = a.terms > 1 ? 6 : 1;
+    g.a_pitch = a.pitch;
+    g.b_pitch = b.pitch;
+    const int64_t tiles = static_cast<int64_t>(g.tiles_m) * g.tiles_n * g.splits;
+    if (tiles >= int64_t{1} << 31) return BNS_ERR_SHAPE;
+    launch(kind, kernel, static_cast<unsigned>(std::min<int64_t>(tiles, sm_count())), kHeadThreads, kHeadSmem, stream, ma, mb, g);
+    return last_error();
+}
+
+void lay_out(int dtype, const void* src, int64_t stride, int rows, int D, int terms, int pitch, void* dst, cudaStream_t stream) {
+    const int64_t blocks = divide_up<int64_t>(static_cast<int64_t>(rows) * pitch, 256);
+    BNS_LM_BY_TYPE(dtype, (launch(BNS_KERNEL_HEAD_VECTOR, head_terms_kernel<T>,
+                                  static_cast<unsigned>(std::min<int64_t>(blocks, sm_count() * 16)), 256, 0, stream, src, stride,
+                                  rows, D, terms, pitch, static_cast<unsigned short*>(dst))));
+}
+
+Operand rows_of_x(const HeadProblem& p, const bns_head* sh, const void* x, char* ws) {
+    if (p.copy_x) return {ws + p.off_x, static_cast<int64_t>(p.terms) * p.pitch, p.T, p.pitch, p.terms, p.pitch};
+    return {x, sh->x_stride, p.T, p.D, 1, 0};
+}
+
+// Rows [first, first + count) of w; copied ones are laid out here.
+Operand rows_of_w(const HeadProblem& p, const bns_head* sh, const void* w, int first, int count, char* ws, cudaStream_t stream) {
+    const char* from = static_cast<const char*>(w) + static_cast<int64_t>(first) * sh->w_stride * elem_bytes(p.dtype);
+    if (!p.copy_w) return {from, sh->w_stride, count, p.D, 1, 0};
+    lay_out(p.dtype, from, sh->w_stride, count, p.D, p.terms, p.pitch, ws + p.off_w, stream);
+    return {ws + p.off_w, static_cast<int64_t>(p.terms) * p.pitch, count, p.pitch, p.terms, p.pitch};
+}
+
+// ------------------------------------------------------------------------------------ distillation
+bns_status check_distillation(const bns_distillation* sh) {
+    if (!sh) return BNS_ERR_NULL;
+    if (sh->rows < 0 || sh->vocabulary <= 0 || sh->vocabulary > 1 << 30 || sh->entries < 1 || sh->entries > kDistillMaxEntries ||
+        sh->stride < sh->vocabulary || !(sh->temperature > 0.f) || sh->temperature > 1e30f)
+        return BNS_ERR_SHAPE;
+    if (!known(sh->dtype) || !known(sh->teacher_dtype)) return BNS_ERR_DTYPE;
+    return BNS_OK;
+}
+
+template <typename WHAT>
+bns_status distill(const bns_distillation* sh, Distill a, cudaStream_t stream) {
+    const size_t eb = elem_bytes(sh->dtype);
+    if (!aligned(a.z, eb) || !aligned(a.dz, eb) || !aligned(a.teacher, elem_bytes(sh->teacher_dtype)) ||
+        !aligned(a.index, sh->index_is_int64 ? 8 : 4) || !aligned(a.loss, 4) || !aligned(a.lse, 4) || !aligned(a.dloss, 4) ||
+        !aligned(a.lse_in, 4))
+        return BNS_ERR_ALIGN;
+    a.z_stride = sh->stride;
+    a.rows = sh->rows;
+    a.V = sh->vocabulary;
+    a.K = sh->entries;
+    a.index64 = sh->index_is_int64;
+    a.teacher_bf16 = sh->teacher_dtype == BNS_BF16;
+    a.tau = sh->temperature;
+    a.c = static_cast<float>(1.4426950408889634 / static_cast<double>(sh->temperature));
+    BNS_LM_BY_TYPE(sh->dtype, (launch(BNS_KERNEL_DISTILL, distill_kernel<T, WHAT>, static_cast<unsigned>(sh->rows),
+                                      kDistillThreads, 0, stream, a)));
+    return last_error();
+}
+
+}  // namespace
+
+namespace bns {
+
+int g_head_piece = 0;
+
+bns_status head_wait_timeouts(uint32_t* count, cudaStream_t stream) {
+    if (cudaMemcpyFromSymbolAsync(count, g_head_timeouts, sizeof(uint32_t), 0, cudaMemcpyDeviceToHost, stream) != cudaSuccess)
+        return BNS_ERR_CUDA;
+    return cudaStreamSynchronize(stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
+}
+
+}  // namespace bns
+
+extern "C" {
+
+bns_status bns_rms_norm_forward(const bns_rows* shape, const void* x, int64_t x_stride, const void* residual,
+                                int64_t residual_stride, const float* weight, float eps, void* y, void* h, float* rstd,
+                                void* cuda_stream) {
+    const bns_status st = check_rows(shape);
+    if (st != BNS_OK) return st;
+    return rms_forward<RmsNone>(shape, x, x_stride, residual, residual_stride, weight, eps, y, nullptr, h, rstd, cuda_stream);
+}
+
+bns_status bns_rms_norm_forward_quantized(const bns_rows* shape, const void* x, int64_t x_stride, const void* residual,
+                                          int64_t residual_stride, const float* weight, float eps, int group, void* q,
+                                          float* scales, void* h, float* rstd, void* cuda_stream) {
+    const bns_status st = check_rows(shape);
+    if (st != BNS_OK) return st;
+    if (group != 0 && group != kRmsGroup) return BNS_ERR_RULE;
+    if (group == 0)
+        return rms_forward<RmsRowScale>(shape, x, x_stride, residual, residual_stride, weight, eps, q, scales, h, rstd, cuda_stream);
+    return rms_forward<RmsGroupScale>(shape, x, x_stride, residual, residual_stride, weight, eps, q, scales, h, rstd, cuda_stream);
+}
+
+size_t bns_rms_norm_workspace_bytes(const bns_rows* shape) {
+    if (check_rows(shape) != BNS_OK) return 0;
+    return kHeaderBytes + align_up(static_cast<size_t>(rms_backward_blocks(shape->rows)) * shape->columns * sizeof(float));
+}
+
+bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t dy_stride, const void* h, int64_t h_stride,
+                                 const float* weight, const float* rstd, const void* dh, int64_t dh_stride, void* dx,
+                                 float* dweight, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    const bns_status st = check_rows(shape);
+    if (st != BNS_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!dweight) return BNS_ERR_NULL;
+    if (shape->rows == 0)
+        return cudaMemsetAsync(dweight, 0, sizeof(float) * shape->columns, stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
+    if (!dy || !h || !weight || !rstd || !dx) return BNS_ERR_NULL;
+    if (dy_stride < shape->columns || h_stride < shape->columns || (dh && dh_stride < shape->columns)) return BNS_ERR_SHAPE;
+    const size_t eb = elem_bytes(shape->dtype);
+    if (!aligned(dy, eb) || !aligned(h, eb) || !aligned(dh, eb) || !aligned(dx, eb) || !aligned(weight, 4) ||
+        !aligned(rstd, 4) || !aligned(dweight, 4))
+        return BNS_ERR_ALIGN;
+    if (!workspace_fits(workspace, workspace_bytes, bns_rms_norm_workspace_bytes(shape))) return BNS_ERR_WORKSPACE;
+    VectorRule rule(shape->columns, static_cast<int>(eb));
+    rule.tensor(dy, dy_stride);
+    rule.tensor(h, h_stride);
+    rule.tensor(dh, dh_stride);
+    rule.tensor(dx, shape->columns);
+    const RmsPlan pl = plan_rms(shape->rows, shape->columns, rule.V, true);
+    float* partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kHeaderBytes);
+    const RmsBackward a{dy, h, dh, weight, rstd, dx, partial, shape->rows, dy_stride, h_stride, dh_stride, shape->columns,
+                        1.f / static_cast<float>(shape->columns)};
+    if (pl.wide)
+        BNS_LM_BY_TYPE_V(shape->dtype, rule.V, (launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_wide_kernel<T, V>, pl.grid,
+                                                       pl.threads, 0, stream, a)));
+    else
+        BNS_LM_BY_TYPE_V(shape->dtype, rule.V, (launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V>, pl.grid, pl.threads, 0,
+                                                       stream, a)));
+    launch(BNS_KERNEL_RMS_BACKWARD, rms_dweight_kernel, static_cast<unsigned>(divide_up(shape->columns, 32)), 256, 0, stream,
+           partial, static_cast<int>(pl.grid), shape->columns, dweight);
+    return last_error();
+}
+
+size_t bns_linear_cross_entropy_workspace_bytes(const bns_head* shape, int backward) {
+    if (check_head(shape) != BNS_OK) return 0;
+    return plan_head(shape, backward != 0).total;
+}
+
+bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x, const void* w, const void* target, float* loss,
+                                            float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    bns_status st = check_head(shape);
+    if (st != BNS_OK) return st;
+    if (!w) return BNS_ERR_NULL;
+    if (shape->rows > 0 && (!x || !target || !loss || !lse)) return BNS_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(w, 16) || !aligned(target, shape->target_is_int64 ? 8 : 4) || !aligned(loss, 4) ||
+        !aligned(lse, 4))
+        return BNS_ERR_ALIGN;
+    const HeadProblem p = plan_head(shape, false);
+    if (!workspace_fits(workspace, workspace_bytes, p.total)) return BNS_ERR_WORKSPACE;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    char* ws = static_cast<char*>(workspace);
+    if (p.T == 0) return cudaMemsetAsync(ws, 0, sizeof(uint32_t), stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
+    if (p.copy_x) lay_out(p.dtype, x, shape->x_stride, p.T, p.D, p.terms, p.pitch, ws + p.off_x, stream);
+    const Operand xs = rows_of_x(p, shape, x, ws);
+    float2* partial = reinterpret_cast<float2*>(ws + p.off_partial);
+    int tiles = 0;
+    for (int first = 0; first < p.V; first += p.piece) {
+        const int count = std::min(p.piece, p.V - first);
+        const Operand rows = rows_of_w(p, shape, w, first, count, ws, stream);
+        HeadGemm g{};
+        g.M = p.T;
+        g.N = count;
+        g.splits = 1;
+        g.target = target;
+        g.target64 = shape->target_is_int64;
+        g.first = first;
+        g.V = p.V;
+        g.partial = partial + static_cast<size_t>(tiles) * p.T;
+        g.target_logit = reinterpret_cast<float*>(ws + p.off_logit);
+        g.status = first == 0 ? reinterpret_cast<unsigned*>(ws) : nullptr;
+        st = head_gemm<kHeadLse, true, true, BF16>(BNS_KERNEL_HEAD_LOGITS, xs, rows, g, p.D, stream);
+        if (st != BNS_OK) return st;
+        tiles += divide_up(count, kHeadN);
+    }
+    launch(BNS_KERNEL_HEAD_VECTOR, head_join_kernel, static_cast<unsigned>(divide_up(p.T, 32)), 256, 0, stream, partial, tiles, p.T,
+           reinterpret_cast<const float*>(ws + p.off_logit), target, shape->target_is_int64, p.V, loss, lse,
+           reinterpret_cast<unsigned*>(ws));
+    return last_error();
+}
+
+bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* x, const void* w, const void* target,
+                                             const float* lse, const float* dloss, void* dx, void* dw, void* workspace,
+                                             size_t workspace_bytes, void* cuda_stream) {
+    bns_status st = check_head(shape);
+    if (st != BNS_OK) return st;
+    if (!w || !dw) return BNS_ERR_NULL;
+    if (shape->rows > 0 && (!x || !target || !lse || !dloss || !dx)) return BNS_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(w, 16) || !aligned(dx, 16) || !aligned(dw, 16) ||
+        !aligned(target, shape->target_is_int64 ? 8 : 4) || !aligned(lse, 4) || !aligned(dloss, 4))
+        return BNS_ERR_ALIGN;
+    const HeadProblem p = plan_head(shape, true);
+    if (!workspace_fits(workspace, workspace_bytes, p.total)) return BNS_ERR_WORKSPACE;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    char* ws = static_cast<char*>(workspace);
+    const size_t eb = elem_bytes(p.dtype);
+    if (p.T == 0)
+        return cudaMemsetAsync(dw, 0, eb * p.V * p.D, stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
+    if (p.copy_x) lay_out(p.dtype, x, shape->x_stride, p.T, p.D, p.terms, p.pitch, ws + p.off_x, stream);
+    const Operand xs = rows_of_x(p, shape, x, ws);
+    float* sums = p.splits > 1 || p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sums) : nullptr;
+    for (int first = 0; first < p.V; first += p.piece) {
+        const int count = std::min(p.piece, p.V - first);
+        const Operand rows = rows_of_w(p, shape, w, first, count, ws, stream);
+        HeadGemm g{};
+        g.M = p.T;
+        g.N = count;
+        g.splits = 1;
+        g.target = target;
+        g.target64 = shape->target_is_int64;
+        g.first = first;
+        g.V = p.V;
+        g.lse = lse;
+        g.dloss = dloss;
+        g.G = reinterpret_cast<unsigned short*>(ws + p.off_G);
+        g.G_stride = static_cast<int64_t>(p.terms) * p.G_pitch;
+        g.G_pitch = p.G_pitch;
+        g.terms = p.terms;
+        st = head_gemm<kHeadGrad, true, true, BF16>(BNS_KERNEL_HEAD_GRADIENT, xs, rows, g, p.D, stream);
+        if (st != BNS_OK) return st;
+        const Operand G{g.G, g.G_stride, p.T, count, p.terms, p.G_pitch};
+        HeadGemm o{};
+        o.M = p.T;
+        o.N = p.D;
+        o.splits = p.splits;
+        o.out = dx;
+        o.out_stride = p.D;
+        o.sums = sums;
+        o.add = first > 0;
+        o.last = p.splits == 1 && first + count == p.V;
+        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, true, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, rows, o, count, stream)));
+        if (st != BNS_OK) return st;
+        HeadGemm q{};
+        q.M = count;
+        q.N = p.D;
+        q.splits = 1;
+        q.out = static_cast<char*>(dw) + static_cast<size_t>(first) * p.D * eb;
+        q.out_stride = p.D;
+        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, false, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, xs, q, p.T, stream)));
+        if (st != BNS_OK) return st;
+    }
+    if (p.splits > 1) {
+        const int64_t blocks = divide_up<int64_t>(static_cast<int64_t>(p.T) * p.D, 256);
+        BNS_LM_BY_TYPE(p.dtype, (launch(BNS_KERNEL_HEAD_VECTOR, head_sum_kernel<T>,
+                                        static_cast<unsigned>(std::min<int64_t>(blocks, sm_count() * 16)), 256, 0, stream,
+                                        static_cast<const float*>(sums), p.splits, p.T, p.D, dx, static_cast<int64_t>(p.D))));
+    }
+    return last_error();
+}
+
+bns_status bns_topk_distillation_forward(const bns_distillation* shape, const void* logits, const void* teacher, const void* index,
+                                         float* loss, float* lse, void* cuda_stream) {
+    const bns_status st = check_distillation(shape);
+    if (st != BNS_OK) return st;
+    if (shape->rows == 0) return BNS_OK;
+    if (!logits || !teacher || !index || !loss || !lse) return BNS_ERR_NULL;
+    Distill a{};
+    a.z = logits;
+    a.teacher = teacher;
+    a.index = index;
+    a.loss = loss;
+    a.lse = lse;
+    return distill<DistillForward>(shape, a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+bns_status bns_topk_distillation_backward(const bns_distillation* shape, const void* logits, const void* teacher, const void* index,
+                                          const float* lse, const float* dloss, void* dlogits, int64_t dlogits_stride,
+                                          void* cuda_stream) {
+    const bns_status st = check_distillation(shape);
+    if (st != BNS_OK) return st;
+    if (shape->rows == 0) return BNS_OK;
+    if (!logits || !teacher || !index || !lse || !dloss || !dlogits) return BNS_ERR_NULL;
+    if (dlogits_stride < shape->vocabulary) return BNS_ERR_SHAPE;
+    Distill a{};
+    a.z = logits;
+    a.teacher = teacher;
+    a.index = index;
+    a.lse_in = lse;
+    a.dloss = dloss;
+    a.dz = dlogits;
+    a.dz_stride = dlogits_stride;
+    return distill<DistillBackward>(shape, a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+bns_status bns_topk_distillation_step(const bns_distillation* shape, const void* logits, const void* teacher, const void* index,
+                                      const float* dloss, float* loss, void* dlogits, int64_t dlogits_stride,
+                                      void* cuda_stream) {
+    const bns_status st = check_distillation(shape);
+    if (st != BNS_OK) return st;
+    if (shape->rows == 0) return BNS_OK;
+    if (!logits || !teacher || !index || !dloss || !loss || !dlogits) return BNS_ERR_NULL;
+    if (dlogits_stride < shape->vocabulary) return BNS_ERR_SHAPE;
+    Distill a{};
+    a.z = logits;
+    a.teacher = teacher;
+    a.index = index;
+    a.dloss = dloss;
+    a.loss = loss;
+    a.dz = dlogits;
+    a.dz_stride = dlogits_stride;
+    return distill<DistillStep>(shape, a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,469 @@
+// Root-mean-square norm of the rows of a [rows, D] tensor with the residual's addition, and its gradient.
+//
+//   s = x + residual (fp32, not rounded before it is normalised); h = s in the tensor's type
+//   rstd = 1 / sqrt(mean(s^2) + eps);  y = s rstd w
+//   8-bit output: a = max |y| over a group of columns, scale = a / 448 (1 where a = 0), q = e4m3(y / scale)
+//   gradient at the stored h: c = mean(w dy h rstd);  dx = rstd (w dy - h rstd c) + dh;  dw = sum over rows of dy h rstd
+//
+// Bound by HBM: a row is read once and lives in registers (EPT elements a thread), so every tensor crosses the
+// memory system once.  A block owns a row at a time and walks down the rows with a grid stride, which keeps its
+// columns' weights (and, in the gradient, its columns' sums over the rows) in registers as well.
+#pragma once
+
+#include "bns_elements.cuh"
+
+namespace bns {
+
+constexpr int kRmsElements = 16;      // elements of a row that a thread holds
+constexpr int kRmsMaxThreads = 1024;
+constexpr int kRmsGroup = 128;        // columns of a scale in the grouped 8-bit form
+
+struct RmsNone {};                    // output forms of the forward kernel
+struct RmsRowScale {};
+struct RmsGroupScale {};
+
+// Sum and maximum over the block in one exchange; every thread gets both.  `turn` alternates between two buffers,
+// so that one barrier per row is enough.  Warps' partial results are combined in warp order by everybody.
+struct BlockExchange {
+    float sum[2][32];
+    float top[2][32];
+};
+
+// |a| and |b| joined by the larger, NaN winning: on the bits of non-negative floats NaN lies above infinity.
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+}
+
+template <bool TOP>
+__device__ __forceinline__ void block_exchange(float& sum, float& top, BlockExchange& ex, int turn) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if constexpr (TOP) top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+    const int warps = blockDim.x >> 5;
+    if (warps == 1) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) {
+        ex.sum[turn][warp] = sum;
+        if constexpr (TOP) ex.top[turn][warp] = top;
+    }
+    __syncthreads();
+    sum = lane < warps ? ex.sum[turn][lane] : 0.f;
+    if constexpr (TOP) top = lane < warps ? ex.top[turn][lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if constexpr (TOP) top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+}
+
+__device__ __forceinline__ unsigned short e4m3_pair(float lo, float hi) {
+    unsigned short r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <int V>
+__device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&f)[V]) {
+    if constexpr (V == 1) {
+        *p = static_cast<uint8_t>(e4m3_pair(f[0], 0.f));
+    } else {
+        typename RawWord<V>::type raw;
+        unsigned short* half = reinterpret_cast<unsigned short*>(&raw);
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) half[j] = e4m3_pair(f[2 * j], f[2 * j + 1]);
+        *reinterpret_cast<typename RawWord<V>::type*>(p) = raw;
+    }
+}
+
+// What multiplies s w to give y / scale, from the largest |s w| of the group.  y = s rstd w, so rstd cancels in
+// y / scale = s w 448 / max|s w|: the 8-bit values carry no rounding of rstd or of the scale.  A group of zeros has
+// scale 1; infinities and NaN give NaN, as the formula does.  `lift` keeps 448 / max finite for groups below 2^-100.
+struct Quant {
+    float scale, lift, factor;
+    __device__ __forceinline__ Quant(float top, float rstd) {
+        const float a = top * rstd, inf = __int_as_float(0x7f800000);
+        scale = a == 0.f ? 1.f : a / 448.f;
+        lift = top < 0x1p-100f ? 0x1p100f : 1.f;
+        factor = a == 0.f ? 0.f : top < inf && a < inf ? 448.f / (top * lift) : __int_as_float(0x7fffffff);
+    }
+    __device__ __forceinline__ float operator()(float sw) const { return sw * lift * factor; }
+};
+
+struct RmsForward {
+    const void* x;
+    const void* residual;  // or NULL
+    const float* weight;
+    void* y;               // the tensor's type, or e4m3
+    float* scales;         // [rows] or [rows][ceil(D / 128)]
+    void* h;               // or NULL
+    float* rstd;
+    int64_t rows, x_stride, residual_stride;
+    int D;
+    float eps, inv_D;
+};
+
+// One row in registers: thread t holds vectors t, t + blockDim, ... of V elements.
+template <typename T, int V, typename OUT>
+__global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsForward a) {
+    using S = typename T::storage;
+    constexpr int NV = kRmsElements / V < 8 ? kRmsElements / V : 8;
+    constexpr bool kRow = __is_same(OUT, RmsRowScale), kGroup = __is_same(OUT, RmsGroupScale);
+    __shared__ BlockExchange ex;
+    extern __shared__ float segment[];    // grouped form with V < 4: largest |s w| of every 32 V columns
+    const int B = blockDim.x, vectors = a.D / V;
+    grid_dependency_wait();
+    grid_dependency_launch();
+
+    float w[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = threadIdx.x + i * B;
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[i][j] = v < vectors ? a.weight[v * V + j] : 0.f;
+    }
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const S* x = static_cast<const S*>(a.x) + row * a.x_stride;
+        const S* r = static_cast<const S*>(a.residual) + (a.residual ? row * a.residual_stride : 0);
+        Vec<T, V> vx[NV], vr[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = threadIdx.x + i * B;
+            if (v < vectors) {
+                vx[i].load(x + static_cast<int64_t>(v) * V);
+                if (a.residual) vr[i].load(r + static_cast<int64_t>(v) * V);
+            }
+        }
+        float s[NV][V], sum = 0.f, top = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = threadIdx.x + i * B;
+            if (v < vectors) {
+                vx[i].unpack(s[i]);
+                if (a.residual) {
+                    float f[V];
+                    vr[i].unpack(f);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) s[i][j] += f[j];
+                }
+                if (a.h) {
+                    Vec<T, V> o;
+                    o.pack(s[i]);
+                    o.store(static_cast<S*>(a.h) + row * a.D + static_cast<int64_t>(v) * V);
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    sum = fmaf(s[i][j], s[i][j], sum);
+                    if constexpr (kRow) top = max_or_nan(top, fabsf(s[i][j] * w[i][j]));
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[i][j] = 0.f;
+            }
+        }
+        if constexpr (kGroup && V < 4) {
+            // a warp's 32 V columns lie inside one group: their maximum goes through shared memory
+            __syncthreads();   // the previous row's readers are done
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float m = 0.f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) m = max_or_nan(m, fabsf(s[i][j] * w[i][j]));
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+                if ((threadIdx.x & 31) == 0) segment[(threadIdx.x + i * B) >> 5] = m;
+            }
+            __syncthreads();
+        }
+        block_exchange<kRow>(sum, top, ex, turn);
+        const float rstd = 1.f / sqrtf(fmaf(sum, a.inv_D, a.eps));
+        if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+        if constexpr (!kRow && !kGroup) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = threadIdx.x + i * B;
+                if (v >= vectors) continue;
+                float f[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[j] = s[i][j] * rstd * w[i][j];
+                Vec<T, V> o;
+                o.pack(f);
+                o.store(static_cast<S*>(a.y) + row * a.D + static_cast<int64_t>(v) * V);
+            }
+        } else if constexpr (kRow) {
+            const Quant quant(top, rstd);
+            if (threadIdx.x == 0) a.scales[row] = quant.scale;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = threadIdx.x + i * B;
+                if (v >= vectors) continue;
+                float f[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[j] = quant(s[i][j] * w[i][j]);
+                store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, f);
+            }
+        } else {
+            const int groups = (a.D + kRmsGroup - 1) / kRmsGroup;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = threadIdx.x + i * B;
+                float m = 0.f;
+                if constexpr (V >= 4) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) m = max_or_nan(m, fabsf(s[i][j] * w[i][j]));
+#pragma unroll
+                    for (int o = kRmsGroup / V / 2; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+                } else {
+                    constexpr int kSegments = kRmsGroup / (32 * V);
+                    const int first = (v >> 5) / kSegments * kSegments;
+#pragma unroll
+                    for (int q = 0; q < kSegments; ++q)
+                        if (first + q < (vectors + 31) >> 5) m = max_or_nan(m, segment[first + q]);
+                }
+                if (v >= vectors) continue;
+                const Quant quant(m, rstd);
+                float f[V];
+                if (v % (kRmsGroup / V) == 0) a.scales[row * groups + v / (kRmsGroup / V)] = quant.scale;
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[j] = quant(s[i][j] * w[i][j]);
+                store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, f);
+            }
+        }
+    }
+}
+
+// Rows wider than a block's registers: the same arithmetic in two walks over the row, the second mostly out of L2.
+template <typename T, int V, typename OUT>
+__global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_wide_kernel(const RmsForward a) {
+    using S = typename T::storage;
+    constexpr bool kRow = __is_same(OUT, RmsRowScale), kGroup = __is_same(OUT, RmsGroupScale);
+    __shared__ BlockExchange ex;
+    grid_dependency_wait();
+    grid_dependency_launch();
+    const int B = blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = B >> 5;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const S* x = static_cast<const S*>(a.x) + row * a.x_stride;
+        const S* r = static_cast<const S*>(a.residual) + (a.residual ? row * a.residual_stride : 0);
+        auto element = [&](int i) { return to_float<T>(x[i]) + (a.residual ? to_float<T>(r[i]) : 0.f); };
+        float sum = 0.f, top = 0.f;
+        const int vectors = a.D / V;
+        for (int v = threadIdx.x; v < vectors; v += B) {
+            Vec<T, V> vx;
+            float s[V];
+            vx.load(x + static_cast<int64_t>(v) * V);
+            vx.unpack(s);
+            if (a.residual) {
+                Vec<T, V> vr;
+                float f[V];
+                vr.load(r + static_cast<int64_t>(v) * V);
+                vr.unpack(f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[j] += f[j];
+            }
+            if (a.h) {
+                Vec<T, V> o;
+                o.pack(s);
+                o.store(static_cast<S*>(a.h) + row * a.D + static_cast<int64_t>(v) * V);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                sum = fmaf(s[j], s[j], sum);
+                if constexpr (kRow) top = max_or_nan(top, fabsf(s[j] * a.weight[v * V + j]));
+            }
+        }
+        block_exchange<kRow>(sum, top, ex, turn);
+        const float rstd = 1.f / sqrtf(fmaf(sum, a.inv_D, a.eps));
+        if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+        if constexpr (kGroup) {
+            // a warp per group, four columns a lane
+            const int groups = (a.D + kRmsGroup - 1) / kRmsGroup;
+            for (int g = warp; g < groups; g += warps) {
+                float p[4], m = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = g * kRmsGroup + j * 32 + lane;
+                    p[j] = i < a.D ? element(i) * a.weight[i] : 0.f;
+                    m = max_or_nan(m, fabsf(p[j]));
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const Quant quant(m, rstd);
+                if (lane == 0) a.scales[row * groups + g] = quant.scale;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = g * kRmsGroup + j * 32 + lane;
+                    if (i < a.D)
+                        static_cast<uint8_t*>(a.y)[row * a.D + i] = static_cast<uint8_t>(e4m3_pair(quant(p[j]), 0.f));
+                }
+            }
+        } else {
+            const Quant quant(top, rstd);
+            if constexpr (kRow) {
+                if (threadIdx.x == 0) a.scales[row] = quant.scale;
+            }
+            for (int v = threadIdx.x; v < vectors; v += B) {
+                float f[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float s = element(v * V + j), w = a.weight[v * V + j];
+                    f[j] = kRow ? quant(s * w) : s * rstd * w;
+                }
+                if constexpr (kRow) {
+                    store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, f);
+                } else {
+                    Vec<T, V> o;
+                    o.pack(f);
+                    o.store(static_cast<S*>(a.y) + row * a.D + static_cast<int64_t>(v) * V);
+                }
+            }
+        }
+    }
+}
+
+struct RmsBackward {
+    const void *dy, *h, *dh;  // dh or NULL
+    const float *weight, *rstd;
+    void* dx;
+    float* partial;           // [blocks][D]: a block's sums for dweight
+    int64_t rows, dy_stride, h_stride, dh_stride;
+    int D;
+    float inv_D;
+};
+
+template <typename T, int V>
+__global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsBackward a) {
+    using S = typename T::storage;
+    constexpr int NV = kRmsElements / V < 8 ? kRmsElements / V : 8;
+    __shared__ BlockExchange ex;
+    const int B = blockDim.x, vectors = a.D / V;
+    grid_dependency_wait();
+    grid_dependency_launch();
+    float w[NV][V], dw[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = threadIdx.x + i * B;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            w[i][j] = v < vectors ? a.weight[v * V + j] : 0.f;
+            dw[i][j] = 0.f;
+        }
+    }
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const S* dy = static_cast<const S*>(a.dy) + row * a.dy_stride;
+        const S* h = static_cast<const S*>(a.h) + row * a.h_stride;
+        const S* dh = static_cast<const S*>(a.dh) + (a.dh ? row * a.dh_stride : 0);
+        const float rstd = a.rstd[row];
+        Vec<T, V> vy[NV], vh[NV], vd[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = threadIdx.x + i * B;
+            if (v < vectors) {
+                vy[i].load(dy + static_cast<int64_t>(v) * V);
+                vh[i].load(h + static_cast<int64_t>(v) * V);
+                if (a.dh) vd[i].load(dh + static_cast<int64_t>(v) * V);
+            }
+        }
+        float sum = 0.f, none = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (threadIdx.x + i * B < vectors) {
+                float fy[V], fh[V];
+                vy[i].unpack(fy);
+                vh[i].unpack(fh);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float xhat = fh[j] * rstd;
+                    dw[i][j] = fmaf(fy[j], xhat, dw[i][j]);
+                    sum = fmaf(w[i][j] * fy[j], xhat, sum);
+                }
+            }
+        }
+        block_exchange<false>(sum, none, ex, turn);
+        const float c = sum * a.inv_D;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = threadIdx.x + i * B;
+            if (v >= vectors) continue;
+            float fy[V], fh[V], f[V];
+            vy[i].unpack(fy);
+            vh[i].unpack(fh);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[j] = rstd * fmaf(-fh[j] * rstd, c, w[i][j] * fy[j]);
+            if (a.dh) {
+                float fd[V];
+                vd[i].unpack(fd);
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[j] += fd[j];
+            }
+            Vec<T, V> o;
+            o.pack(f);
+            o.store(static_cast<S*>(a.dx) + row * a.D + static_cast<int64_t>(v) * V);
+        }
+    }
+    float* p = a.partial + static_cast<int64_t>(blockIdx.x) * a.D;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = threadIdx.x + i * B;
+        if (v >= vectors) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) p[v * V + j] = dw[i][j];
+    }
+}
+
+// Rows wider than a block's registers.  The block's sums for dweight stay in its own row of `partial`, which only
+// the thread that owns the column touches.
+template <typename T, int V>
+__global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_wide_kernel(const RmsBackward a) {
+    using S = typename T::storage;
+    __shared__ BlockExchange ex;
+    grid_dependency_wait();
+    grid_dependency_launch();
+    const int B = blockDim.x;
+    float* p = a.partial + static_cast<int64_t>(blockIdx.x) * a.D;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const S* dy = static_cast<const S*>(a.dy) + row * a.dy_stride;
+        const S* h = static_cast<const S*>(a.h) + row * a.h_stride;
+        const S* dh = static_cast<const S*>(a.dh) + (a.dh ? row * a.dh_stride : 0);
+        const float rstd = a.rstd[row];
+        const bool first = row == blockIdx.x;
+        float sum = 0.f, none = 0.f;
+        for (int i = threadIdx.x; i < a.D; i += B) {
+            const float fy = to_float<T>(dy[i]), xhat = to_float<T>(h[i]) * rstd;
+            p[i] = fmaf(fy, xhat, first ? 0.f : p[i]);
+            sum = fmaf(a.weight[i] * fy, xhat, sum);
+        }
+        block_exchange<false>(sum, none, ex, turn);
+        const float c = sum * a.inv_D;
+        for (int i = threadIdx.x; i < a.D; i += B) {
+            const float fy = to_float<T>(dy[i]), xhat = to_float<T>(h[i]) * rstd;
+            float f = rstd * fmaf(-xhat, c, a.weight[i] * fy);
+            if (a.dh) f += to_float<T>(dh[i]);
+            static_cast<S*>(a.dx)[row * a.D + i] = from_float<T>(f);
+        }
+    }
+}
+
+// dweight: 32 columns a block, 8 threads a column over the blocks' sums, joined in a fixed order.
+__global__ void __launch_bounds__(256) rms_dweight_kernel(const float* partial, int blocks, int D, float* dweight) {
+    __shared__ float fold[8][33];
+    grid_dependency_wait();
+    grid_dependency_launch();
+    const int column = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    float sum = 0.f;
+    if (column < D)
+        for (int b = part; b < blocks; b += 8) sum += partial[static_cast<int64_t>(b) * D + column];
+    fold[part][threadIdx.x & 31] = sum;
+    __syncthreads();
+    if (part == 0 && column < D) {
+#pragma unroll
+        for (int q = 1; q < 8; ++q) sum += fold[q][threadIdx.x & 31];
+        dweight[column] = sum;
+    }
+}
+
+}  // namespace bns
