@@ -9,12 +9,18 @@
 //   GRAD  z tile -> G tile, bf16, into a buffer that holds one piece of the vocabulary
 //   OUT   dx and dW tiles -> the gradient in the tensor's type, or fp32 partial sums
 //
-// One CTA per SM; a tile is 128 x 256 with its fp32 accumulator in tensor memory (two of them, so that the epilogue of
-// one tile runs under the products of the next).  Warp 0 feeds a ring of shared-memory stages by TMA (64 elements of
-// K a stage, 128-byte swizzle), warp 1 issues tcgen05.mma, warps 4-7 read the accumulator back.  Operands are bf16; either
-// may be stored with K or with its other dimension contiguous (G^T, and W and x as the right-hand sides of the
-// gradients), so no tensor is transposed.  fp32 tensors are split into three bf16 terms (8 + 8 + 8 bits) and the six
-// products that matter in fp32 are added up in the same accumulator, smallest first.
+// A CTA pair (two SMs) owns a 256 x 256 tile: each CTA keeps 128 rows of it in its tensor memory and half of either
+// operand's stage in its shared memory, so that a stage's bytes per product are half of what two single CTAs would
+// move.  Products with at most 128 rows run the same kernel with single CTAs (128 x 256).  Warp 0 feeds a ring of stages
+// by TMA (64 elements of K, 128-byte swizzle), warp 1 of the first CTA issues tcgen05.mma, warps 4-11 read the
+// accumulator back, 128 columns of a row a thread; the accumulator is double buffered.  Operands are bf16; either may be
+// stored with K or with its other dimension contiguous (G^T, and W and x as the right-hand sides of the gradients),
+// so no tensor is transposed.  fp32 tensors are split into three bf16 terms (8 + 8 + 8 bits) and the six products
+// that matter in fp32 are added up, smallest first.
+//
+// The tensor core truncates as it accumulates: after n steps of 16 a sum has lost some n 2^-25 of itself, always towards
+// zero.  Where the result is an fp32 number (the logits' statistics, everything of fp32 tensors) the sum is therefore
+// taken in segments of 512 elements of K, which the epilogue's threads add up in registers, rounding to nearest.
 //
 // Every wait is bounded: one that runs out is counted, and the block ends without touching memory further.
 #pragma once
@@ -26,11 +32,19 @@
 
 namespace bns {
 
-constexpr int kHeadM = 128, kHeadN = 256, kHeadK = 64;   // tile, and K per stage
-constexpr int kHeadStages = 4;
-constexpr int kHeadThreads = 256;
-constexpr unsigned kHeadStageA = kHeadM * kHeadK * 2, kHeadStageB = kHeadN * kHeadK * 2;
-constexpr unsigned kHeadSmem = kHeadStages * (kHeadStageA + kHeadStageB) + 1024;
+constexpr int kHeadM = 128, kHeadN = 256, kHeadK = 64;   // rows of a CTA, columns of a tile, K per stage
+constexpr int kHeadSegment = 8;                          // stages of K per segment
+constexpr int kHeadThreads = 384;
+constexpr unsigned kHeadStageA = kHeadM * kHeadK * 2;
+
+// Ring of a CTA that works alone (CTAS = 1) or as half of a pair (2): 192 KB either way.
+template <int CTAS>
+struct HeadRing {
+    static constexpr int kStages = CTAS == 2 ? 6 : 4;
+    static constexpr int kColumns = kHeadN / CTAS;       // of B in this CTA's stage
+    static constexpr unsigned kStageB = kColumns * kHeadK * 2, kStage = kHeadStageA + kStageB;
+    static constexpr unsigned kSmem = kStages * kStage + 1024;
+};
 constexpr int kHeadRaster = 16;        // row tiles that are swept together, so that their operand stays in L2
 constexpr unsigned kHeadPolls = 1u << 22;
 constexpr float kHeadLog2e = 1.4426950408889634f, kHeadLn2 = 0.6931471805599453f;
@@ -48,8 +62,20 @@ __device__ __forceinline__ void barrier_init(unsigned bar, unsigned arrivals) {
 __device__ __forceinline__ void barrier_expect(unsigned bar, unsigned bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void barrier_arrive(unsigned bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+// The same shared-memory place in the pair's first CTA.
+template <int CTAS>
+__device__ __forceinline__ unsigned in_first(unsigned address) {
+    if constexpr (CTAS == 1) return address;
+    unsigned r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(address));
+    return r;
+}
+template <int CTAS>
+__device__ __forceinline__ void arrive_in_first(unsigned bar) {
+    if constexpr (CTAS == 1)
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+    else
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first<CTAS>(bar)) : "memory");
 }
 __device__ __forceinline__ bool barrier_try(unsigned bar, unsigned parity) {
     unsigned done;
@@ -72,24 +98,77 @@ __device__ __forceinline__ bool wait(unsigned bar, unsigned parity, volatile int
     atomicAdd(&g_head_timeouts, 1u);
     return false;
 }
+// `bar` lies in the pair's first CTA, the data goes to this one.
+template <int CTAS>
 __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(bar)
-        : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+            "[%4];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
 }
+// Arrives on `bar` (in both CTAs of a pair) when the products issued so far have ended.
+template <int CTAS>
 __device__ __forceinline__ void commit(unsigned bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    else
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+            "h"(static_cast<unsigned short>(3))
+            : "memory");
 }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+template <int CTAS>
 __device__ __forceinline__ void mma(unsigned d, uint64_t a, uint64_t b, unsigned idesc, bool accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(static_cast<unsigned>(accumulate))
-        : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(static_cast<unsigned>(accumulate))
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(static_cast<unsigned>(accumulate))
+            : "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void tensor_memory_alloc(unsigned where) {
+    if constexpr (CTAS == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(where) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(where) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+}
+template <int CTAS>
+__device__ __forceinline__ void tensor_memory_free(unsigned base) {
+    if constexpr (CTAS == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(base));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(base));
+}
+// Barrier over the CTAs of a pair (or the block).
+template <int CTAS>
+__device__ __forceinline__ void sync_all() {
+    if constexpr (CTAS == 1) {
+        __syncthreads();
+    } else {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
 }
 __device__ __forceinline__ void load32(unsigned address, float (&f)[32]) {
     __syncwarp();
@@ -97,13 +176,26 @@ __device__ __forceinline__ void load32(unsigned address, float (&f)[32]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
           "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
           "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(address));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        : "r"(address)
+        : "memory");
+}
+__device__ __forceinline__ void load16(unsigned address, float (&f)[16]) {
+    __syncwarp();
+    unsigned* r = reinterpret_cast<unsigned*>(f);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(address)
+        : "memory");
 }
 __device__ __forceinline__ float exp2_fast(float x) {
     float r;
@@ -143,13 +235,14 @@ struct HeadGemm {
     int target64;
     int first;                   // vocabulary index of column 0
     int V;
-    float2* partial;             // LSE: [tiles_n][M] maximum (base 2) and sum
+    float2* partial;             // LSE: [2 tiles_n][M] maximum (base 2) and sum of half a tile's columns
     float* target_logit;         // LSE: [M]
     unsigned* status;            // LSE: cleared here, set by the kernel that joins the partial sums
     const float *lse, *dloss;    // GRAD: [M]
-    unsigned short* G;           // GRAD: [M][terms][pitch]
+    const float* unit;           // GRAD: G holds the gradient divided by this; OUT: multiplied in again
+    unsigned short* G;           // GRAD: [M][1 or 3 terms][pitch]
     int64_t G_stride;
-    int G_pitch, terms;
+    int G_pitch;
     // OUT
     void* out;                   // the tensor's type
     int64_t out_stride;
@@ -183,25 +276,163 @@ struct HeadTile {
     }
 };
 
-template <int KIND, bool A_K, bool B_K, typename T>
+// What a thread of the epilogue does with its 128 columns of a row, 32 at a time.
+template <int KIND, typename T>
+struct HeadEpilogue {
+    using S = typename T::storage;
+    const HeadGemm& g;
+    const HeadTile& t;
+    int row, column0, columns;   // first column, and how many of the 128 exist
+    bool in;
+    // LSE and GRAD
+    int mine = -1;               // the target's place among the 128
+    bool counts = false;
+    float m, s;                  // LSE
+    float shift, factor, one;    // GRAD
+    int half;
+
+    __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_)
+        : g(g_), t(t_), row(row_), column0(t_.n * kHeadN + half_ * (kHeadN / 2)), in(row_ < g_.M), half(half_) {
+        columns = min(kHeadN / 2, g.N - column0);
+        if constexpr (KIND != kHeadOut) {
+            const int64_t y = in ? head::load_index(g.target, row, g.target64) : -1;
+            counts = y >= 0 && y < g.V;
+            const int64_t place = y - g.first - column0;
+            if (counts && place >= 0 && place < columns) mine = static_cast<int>(place);
+        }
+        if constexpr (KIND == kHeadLse) {
+            m = __int_as_float(0xff800000);
+            s = 0.f;
+        } else if constexpr (KIND == kHeadGrad) {
+            const float lse = counts ? g.lse[row] : 0.f;
+            one = counts ? g.dloss[row] / *g.unit : 0.f;
+            // lse log2(e) = shift + rest, log2(e) being the same fp32 number as in z log2(e), so that only the
+            // difference z - lse feels its rounding; rest goes into the factor
+            shift = lse * kHeadLog2e;
+            factor = one * head::exp2_fast(-fmaf(lse, kHeadLog2e, -shift));
+        } else {
+            factor = g.unit ? *g.unit : 1.f;
+        }
+    }
+    // Columns that the accumulator has to be read for: G is written up to whole stages of K, zeros where nothing is.
+    __device__ __forceinline__ int extent() const {
+        if constexpr (KIND == kHeadGrad) return min(kHeadN / 2, (max(columns, 0) + kHeadK - 1) / kHeadK * kHeadK);
+        return columns;
+    }
+    __device__ __forceinline__ void chunk(int c, float* f) {
+        if constexpr (KIND == kHeadLse) {
+            const float inf = __int_as_float(0x7f800000);
+            if (columns - c < 32) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (c + j >= columns) f[j] = -inf;
+            }
+            float top = f[0];
+#pragma unroll
+            for (int j = 1; j < 32; ++j) top = fmaxf(top, f[j]);
+            top = fmaxf(top * kHeadLog2e, m);
+            const float ref = top == -inf ? 0.f : top;
+            s *= head::exp2_fast(m - ref);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s += head::exp2_fast(fmaf(f[j], kHeadLog2e, -ref));
+            m = top;
+            if (mine >= c && mine < c + 32) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (mine == c + j) g.target_logit[row] = f[j];
+            }
+        } else if constexpr (KIND == kHeadGrad) {
+            if (!in) return;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                f[j] = counts && c + j < columns ? head::exp2_fast(fmaf(f[j], kHeadLog2e, -shift)) * factor : 0.f;
+                if (mine == c + j) f[j] -= one;
+            }
+            unsigned short* to = g.G + row * g.G_stride + column0 + c;
+            constexpr int kTerms = sizeof(S) == 4 ? 3 : 1;
+#pragma unroll
+            for (int term = 0; term < kTerms; ++term) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    Vec<BF16, 8> o;
+                    float e[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) e[j] = f[q * 8 + j];
+                    o.pack(e);
+                    o.store(to + term * static_cast<int64_t>(g.G_pitch) + q * 8);
+                    if (term + 1 < kTerms) {
+                        o.unpack(e);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[q * 8 + j] -= e[j];   // what the term leaves for the next
+                    }
+                }
+            }
+        } else {
+            if (!in) return;
+            const int left = columns - c;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) f[j] *= factor;
+            if (g.sums) {
+                float* p = g.sums + (static_cast<int64_t>(t.split) * g.M + row) * g.N + column0 + c;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    if (j < left) {
+                        if (g.add) f[j] += p[j];
+                        if (!g.last) p[j] = f[j];
+                    }
+                }
+                if (!g.last) return;
+            }
+            S* to = static_cast<S*>(g.out) + row * g.out_stride + column0 + c;
+            constexpr int V = 16 / sizeof(S);
+            if (left >= 32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+#pragma unroll
+                for (int q = 0; q < 32 / V; ++q) {
+                    Vec<T, V> o;
+                    float e[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) e[j] = f[q * V + j];
+                    o.pack(e);
+                    o.store(to + q * V);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j < left) to[j] = from_float<T>(f[j]);
+            }
+        }
+    }
+    __device__ __forceinline__ void finish() {
+        if constexpr (KIND == kHeadLse) {
+            if (in) g.partial[static_cast<int64_t>(t.n * 2 + half) * g.M + row] = make_float2(m, s);
+        }
+    }
+};
+
+template <int KIND, bool A_K, bool B_K, typename T, int CTAS>
 __global__ void __launch_bounds__(kHeadThreads, 1)
     head_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const HeadGemm g) {
+    using Ring = HeadRing<CTAS>;
+    constexpr int kStages = Ring::kStages;
+    constexpr bool kSegments = KIND == kHeadLse || sizeof(typename T::storage) == 4;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kHeadStages + 5];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
     __shared__ unsigned tmem_base;
-    __shared__ int gave_up;
+    __shared__ volatile int gave_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = CTAS == 1 ? 0 : static_cast<int>(blockIdx.x & 1);      // in the pair
+    const int worker = blockIdx.x / CTAS, workers = gridDim.x / CTAS;
     const unsigned ring = (head::smem(raw) + 1023) & ~1023u;
-    const unsigned full = head::smem(bars), empty = full + 8 * kHeadStages, ready = empty + 8 * kHeadStages,
-                   drained = ready + 16, flush = drained + 16;
+    const unsigned full = head::smem(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16,
+                   flush = drained + 16;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kHeadStages; ++s) {
+        for (int s = 0; s < kStages; ++s) {
             head::barrier_init(full + 8 * s, 1);
             head::barrier_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
             head::barrier_init(ready + 8 * b, 1);
-            head::barrier_init(drained + 8 * b, 128);
+            head::barrier_init(drained + 8 * b, 8 * CTAS);
         }
         head::barrier_init(flush, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -210,12 +441,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
     }
-    if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(head::smem(&tmem_base)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
+    if (warp == 2) head::tensor_memory_alloc<CTAS>(head::smem(&tmem_base));
     head::fence_before();
     __syncthreads();
+    if constexpr (CTAS == 2) head::sync_all<CTAS>();      // the other CTA's barriers exist
     head::fence_after();
     const unsigned tmem = tmem_base;
     grid_dependency_wait();
@@ -223,206 +452,174 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
 
     const int tiles = g.tiles_m * g.tiles_n * g.splits;
     int issued = 0;   // stages that thread 0 has asked TMA to fill
-    if (warp == 0) {
-        if (lane == 0) {
+    if (warp < 4) {
+        if (warp == 0 && lane == 0) {
             int it = 0;
             bool ok = true;
-            for (int id = blockIdx.x; ok && id < tiles; id += gridDim.x) {
+            for (int id = worker; ok && id < tiles; id += workers) {
                 const HeadTile t(g, id);
+                const int row = (t.m * CTAS + rank) * kHeadM, column = t.n * kHeadN + rank * Ring::kColumns;
                 for (int k = t.k0; k < t.k1; ++k, ++it) {
-                    const int s = it % kHeadStages;
-                    if (it >= kHeadStages && !(ok = head::wait(empty + 8 * s, (it / kHeadStages - 1) & 1, &gave_up))) break;
-                    const unsigned bar = full + 8 * s, sa = ring + s * (kHeadStageA + kHeadStageB), sb = sa + kHeadStageA;
-                    head::barrier_expect(bar, kHeadStageA + kHeadStageB);
+                    const int s = it % kStages;
+                    if (it >= kStages && !(ok = head::wait(empty + 8 * s, (it / kStages - 1) & 1, &gave_up))) break;
+                    const unsigned bar = head::in_first<CTAS>(full + 8 * s), sa = ring + s * Ring::kStage, sb = sa + kHeadStageA;
+                    if (rank == 0) head::barrier_expect(full + 8 * s, CTAS * Ring::kStage);
                     int ta, tb;
                     const int pair = k / g.k_blocks, kk = (k - pair * g.k_blocks) * kHeadK;
                     head_pair(pair, g.pairs, ta, tb);
                     if constexpr (A_K) {
-                        head::tma_load(sa, &map_a, ta * g.a_pitch + kk, t.m * kHeadM, bar);
+                        head::tma_load<CTAS>(sa, &map_a, ta * g.a_pitch + kk, row, bar);
                     } else {
 #pragma unroll
                         for (int q = 0; q < kHeadM / 64; ++q)
-                            head::tma_load(sa + q * 8192, &map_a, ta * g.a_pitch + t.m * kHeadM + q * 64, kk, bar);
+                            head::tma_load<CTAS>(sa + q * 8192, &map_a, ta * g.a_pitch + row + q * 64, kk, bar);
                     }
                     if constexpr (B_K) {
-                        head::tma_load(sb, &map_b, tb * g.b_pitch + kk, t.n * kHeadN, bar);
+                        head::tma_load<CTAS>(sb, &map_b, tb * g.b_pitch + kk, column, bar);
                     } else {
 #pragma unroll
-                        for (int q = 0; q < kHeadN / 64; ++q)
-                            head::tma_load(sb + q * 8192, &map_b, tb * g.b_pitch + t.n * kHeadN + q * 64, kk, bar);
+                        for (int q = 0; q < Ring::kColumns / 64; ++q)
+                            head::tma_load<CTAS>(sb + q * 8192, &map_b, tb * g.b_pitch + column + q * 64, kk, bar);
                     }
                 }
             }
+            // the products have read every stage: nothing arrives here any more once the block ends
+            for (int i = max(0, it - kStages); ok && i < it; ++i)
+                ok = head::wait(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up);
             issued = it;
-        }
-    } else if (warp == 1) {
-        if (lane == 0) {
+        } else if (warp == 1 && lane == 0 && rank == 0) {
             constexpr unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_K ? 0u : 1u << 15) | (B_K ? 0u : 1u << 16) |
-                                       ((kHeadN >> 3) << 17) | ((kHeadM >> 4) << 24);
+                                       ((kHeadN >> 3) << 17) | ((CTAS * kHeadM >> 4) << 24);
             int it = 0, n = 0;
             bool ok = true;
-            for (int id = blockIdx.x; ok && id < tiles; id += gridDim.x, ++n) {
+            for (int id = worker; ok && id < tiles; id += workers) {
                 const HeadTile t(g, id);
-                const int buffer = n & 1;
-                if (n >= 2 && !(ok = head::wait(drained + 8 * buffer, (n / 2 - 1) & 1, &gave_up))) break;
-                head::fence_after();
-                const unsigned d = tmem + buffer * kHeadN;
-                for (int k = t.k0; k < t.k1; ++k, ++it) {
-                    const int s = it % kHeadStages;
-                    if (!(ok = head::wait(full + 8 * s, (it / kHeadStages) & 1, &gave_up))) break;
+                const int step = kSegments ? kHeadSegment : t.k1 - t.k0;
+                for (int k = t.k0; ok && k < t.k1; k += step, ++n) {
+                    const int buffer = n & 1, end = min(t.k1, k + step);
+                    if (n >= 2 && !(ok = head::wait(drained + 8 * buffer, (n / 2 - 1) & 1, &gave_up))) break;
                     head::fence_after();
-                    const unsigned sa = ring + s * (kHeadStageA + kHeadStageB);
-                    const uint64_t da = head::descriptor<A_K>(sa), db = head::descriptor<B_K>(sa + kHeadStageA);
+                    const unsigned d = tmem + buffer * kHeadN;
+                    for (int kk = k; kk < end; ++kk, ++it) {
+                        const int s = it % kStages;
+                        if (!(ok = head::wait(full + 8 * s, (it / kStages) & 1, &gave_up))) break;
+                        head::fence_after();
+                        const unsigned sa = ring + s * Ring::kStage;
+                        const uint64_t da = head::descriptor<A_K>(sa), db = head::descriptor<B_K>(sa + kHeadStageA);
 #pragma unroll
-                    for (int q = 0; q < kHeadK / 16; ++q)
-                        head::mma(d, da + q * head::descriptor_step<A_K>(), db + q * head::descriptor_step<B_K>(), idesc,
-                                  k > t.k0 || q > 0);
-                    head::commit(empty + 8 * s);
+                        for (int q = 0; q < kHeadK / 16; ++q)
+                            head::mma<CTAS>(d, da + q * head::descriptor_step<A_K>(), db + q * head::descriptor_step<B_K>(), idesc,
+                                            kk > k || q > 0);
+                        head::commit<CTAS>(empty + 8 * s);
+                    }
+                    if (!ok) break;
+                    head::commit<CTAS>(ready + 8 * buffer);
                 }
-                if (!ok) break;
-                head::commit(ready + 8 * buffer);
             }
         }
-    } else if (warp >= 4) {
-        using S = typename T::storage;
-        const int slot = warp & 3;
+        __syncwarp();
+    } else {
+        const int slot = warp & 3, half = (warp - 4) >> 2;
         if (KIND == kHeadLse && blockIdx.x == 0 && threadIdx.x == 128 && g.status) *g.status = 0;
         int n = 0;
-        for (int id = blockIdx.x; id < tiles; id += gridDim.x, ++n) {
+        bool ok = true;
+        for (int id = worker; ok && id < tiles; id += workers) {
             const HeadTile t(g, id);
-            const int buffer = n & 1;
-            if (!__all_sync(0xffffffffu, head::wait(ready + 8 * buffer, (n / 2) & 1, &gave_up))) break;
-            head::fence_after();
-            const unsigned src = tmem + buffer * kHeadN + (static_cast<unsigned>(slot * 32) << 16);
-            const int row = t.m * kHeadM + slot * 32 + lane, column0 = t.n * kHeadN;
-            const bool in = row < g.M;
-            const int columns = min(kHeadN, g.N - column0);     // that exist
-            if constexpr (KIND == kHeadLse) {
-                const float inf = __int_as_float(0x7f800000);
-                const int64_t y = in ? head::load_index(g.target, row, g.target64) : -1;
-                const int64_t mine = y - g.first - column0;     // the target's place in this tile, if it is in it
-                float m = -inf, s = 0.f;
-                for (int c = 0; c < columns; c += 32) {
-                    float f[32];
-                    head::load32(src + c, f);
-                    if (columns - c < 32) {
+            HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half);
+            const unsigned lanes = tmem + (static_cast<unsigned>(slot * 32) << 16) + half * (kHeadN / 2);
+            auto wait_ready = [&]() {
+                ok = __all_sync(0xffffffffu, head::wait(ready + 8 * (n & 1), (n / 2) & 1, &gave_up));
+                head::fence_after();
+                return ok;
+            };
+            auto give_back = [&]() {
+                head::fence_before();
+                __syncwarp();
+                if (lane == 0) head::arrive_in_first<CTAS>(drained + 8 * (n & 1));
+                ++n;
+            };
+            if constexpr (kSegments) {
+                float acc[kHeadN / 2];
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (c + j >= columns) f[j] = -inf;
+                for (int j = 0; j < kHeadN / 2; ++j) acc[j] = 0.f;
+                for (int k = t.k0; k < t.k1; k += kHeadSegment) {
+                    if (!wait_ready()) break;
+#pragma unroll
+                    for (int c = 0; c < kHeadN / 2; c += 16) {
+                        float f[16];
+                        head::load16(lanes + (n & 1) * kHeadN + c, f);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) acc[c + j] += f[j];
                     }
-                    float top = f[0];
-#pragma unroll
-                    for (int j = 1; j < 32; ++j) top = fmaxf(top, f[j]);
-                    top = fmaxf(top * kHeadLog2e, m);
-                    const float ref = top == -inf ? 0.f : top;
-                    s *= head::exp2_fast(m - ref);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) s += head::exp2_fast(fmaf(f[j], kHeadLog2e, -ref));
-                    m = top;
-                    if (mine >= c && mine < c + 32 && mine < columns) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (mine == c + j) g.target_logit[row] = f[j];
-                    }
+                    give_back();
                 }
-                if (in) g.partial[static_cast<int64_t>(t.n) * g.M + row] = make_float2(m, s);
-            } else if constexpr (KIND == kHeadGrad) {
-                const int64_t y = in ? head::load_index(g.target, row, g.target64) : -1;
-                const int64_t mine = y - g.first - column0;
-                const bool counts = y >= 0 && y < g.V;
-                const float lse = counts ? g.lse[row] : 0.f, scale = counts ? g.dloss[row] : 0.f;
-                // lse log2(e) = shift + rest, log2(e) being the same fp32 number as in z log2(e), so that only the
-                // difference z - lse feels its rounding; rest goes into the factor
-                const float shift = lse * kHeadLog2e;
-                const float factor = scale * head::exp2_fast(-fmaf(lse, kHeadLog2e, -shift));
-                const int padded = (columns + kHeadK - 1) / kHeadK * kHeadK;   // zeros up to whole stages of K
-                for (int c = 0; c < padded; c += 32) {
-                    float f[32];
-                    head::load32(src + c, f);
-                    if (in) {
+                if (!ok) break;
+                const int extent = e.extent();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            f[j] = counts && c + j < columns ? head::exp2_fast(fmaf(f[j], kHeadLog2e, -shift)) * factor : 0.f;
-                            if (mine == c + j && c + j < columns) f[j] -= scale;
-                        }
-                        unsigned short* to = g.G + row * g.G_stride + column0 + c;
-                        for (int term = 0; term < g.terms; ++term) {
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                Vec<BF16, 8> o;
-                                float e[8];
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) e[j] = f[q * 8 + j];
-                                o.pack(e);
-                                o.store(to + term * static_cast<int64_t>(g.G_pitch) + q * 8);
-                                o.unpack(e);
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) f[q * 8 + j] -= e[j];   // what the term leaves for the next
-                            }
-                        }
-                    }
-                }
+                for (int c = 0; c < kHeadN / 2; c += 32)
+                    if (c < extent) e.chunk(c, acc + c);
+                e.finish();
             } else {
-                for (int c = 0; c < columns; c += 32) {
+                if (!wait_ready()) break;
+                const int extent = e.extent();
+                for (int c = 0; c < extent; c += 32) {
                     float f[32];
-                    head::load32(src + c, f);
-                    const int left = columns - c;
-                    float* p = g.sums + (static_cast<int64_t>(t.split) * g.M + row) * g.N + column0 + c;
-                    if (in && g.sums) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            if (j < left) {
-                                if (g.add) f[j] += p[j];
-                                if (!g.last) p[j] = f[j];
-                            }
-                        }
-                    }
-                    if (in && (!g.sums || g.last)) {
-                        S* to = static_cast<S*>(g.out) + row * g.out_stride + column0 + c;
-                        constexpr int V = 16 / sizeof(S);
-                        if (left >= 32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
-#pragma unroll
-                            for (int q = 0; q < 32 / V; ++q) {
-                                Vec<T, V> o;
-                                float e[V];
-#pragma unroll
-                                for (int j = 0; j < V; ++j) e[j] = f[q * V + j];
-                                o.pack(e);
-                                o.store(to + q * V);
-                            }
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j < left) to[j] = from_float<T>(f[j]);
-                        }
-                    }
+                    head::load32(lanes + (n & 1) * kHeadN + c, f);
+                    e.chunk(c, f);
                 }
+                e.finish();
+                give_back();
             }
-            head::fence_before();
-            head::barrier_arrive(drained + 8 * buffer);
         }
     }
     __syncthreads();
     if (gave_up) {
         // a block that gave up leaves only when its copies have landed and its products have ended
-        if (threadIdx.x == 0)
-            for (int i = max(0, issued - kHeadStages); i < issued; ++i)
-                for (unsigned n = 0; n < kHeadPolls && !head::barrier_try(full + 8 * (i % kHeadStages), (i / kHeadStages) & 1); ++n) {
+        if (threadIdx.x == 0 && rank == 0)
+            for (int i = max(0, issued - kStages); i < issued; ++i)
+                for (unsigned n = 0; n < kHeadPolls && !head::barrier_try(full + 8 * (i % kStages), (i / kStages) & 1); ++n) {
                 }
-        if (threadIdx.x == 32) {
-            head::commit(flush);
+        if (threadIdx.x == 32 && rank == 0) {
+            head::commit<CTAS>(flush);
             for (unsigned n = 0; n < kHeadPolls && !head::barrier_try(flush, 0); ++n) {
             }
         }
         __syncthreads();
     }
+    if constexpr (CTAS == 2) head::sync_all<CTAS>();
     if (warp == 2) {
         head::fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+        head::tensor_memory_free<CTAS>(tmem);
     }
 }
 
 // ------------------------------------------------------------------------------------ around the products
+// The largest |dloss| of the rows that count (1 if that is zero): G is kept in units of it.  With one weight for all
+// rows, as a mean has, the largest entry of a row of G is then p - 1 itself; its rounding to bf16 does not carry that
+// of the weight, which would be the same in every row and add up.
+__global__ void __launch_bounds__(1024) head_unit_kernel(const void* target, int target64, const float* dloss, int rows, int V,
+                                                         float* unit) {
+    __shared__ float fold[32];
+    grid_dependency_wait();
+    grid_dependency_launch();
+    float top = 0.f;
+    for (int t = threadIdx.x; t < rows; t += 1024) {
+        const int64_t y = head::load_index(target, t, target64);
+        const float g = fabsf(dloss[t]);
+        if (y >= 0 && y < V && g < __int_as_float(0x7f800000)) top = fmaxf(top, g);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if ((threadIdx.x & 31) == 0) fold[threadIdx.x >> 5] = top;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        top = fold[threadIdx.x];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (threadIdx.x == 0) *unit = top > 0.f ? top : 1.f;
+    }
+}
+
 // Rows into bf16 terms: the first is the value rounded, the next what that leaves, and so on; each term's row is padded
 // with zeros to `pitch` elements.  One term lays out bf16 rows whose stride TMA cannot take.
 template <typename T>
@@ -443,7 +640,7 @@ __global__ void __launch_bounds__(256) head_terms_kernel(const void* src, int64_
     }
 }
 
-// Joins the tiles' maxima and sums of a row: 32 rows a block, eight threads a row, in a fixed order.
+// Joins the half tiles' maxima and sums of a row: 32 rows a block, eight threads a row, in a fixed order.
 __global__ void __launch_bounds__(256) head_join_kernel(const float2* partial, int tiles, int rows, const float* target_logit,
                                                         const void* target, int target64, int V, float* loss, float* lse,
                                                         unsigned* status) {

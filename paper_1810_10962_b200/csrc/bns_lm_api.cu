@@ -26,19 +26,32 @@ bool known(int dtype) { return dtype == BNS_F32 || dtype == BNS_BF16; }
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 bool workspace_fits(const void* ws, size_t bytes, size_t need) { return ws && aligned(ws, kAlign) && bytes >= need; }
 
+struct Shape {
+    unsigned grid, threads, cluster = 1;
+};
+
 template <typename... KArgs, typename... Args>
-void launch(int kind, void (*kernel)(KArgs...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s, Args&&... args) {
+void launch(int kind, void (*kernel)(KArgs...), Shape shape, size_t smem, cudaStream_t s, Args&&... args) {
     LaunchScope scope(kind, s);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
+    cfg.gridDim = dim3(shape.grid);
+    cfg.blockDim = dim3(shape.threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (g_pdl) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (shape.cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = shape.cluster;
+        attr[n].val.clusterDim.y = 1;
+        attr[n++].val.clusterDim.z = 1;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = g_pdl ? 1 : 0;
+    cfg.numAttrs = n;
     note_launch(cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...));
 }
 
@@ -67,7 +80,7 @@ bns_status check_rows(const bns_rows* sh) {
 }
 
 struct RmsPlan {
-    int threads;
+    unsigned threads;
     bool wide;       // the row does not fit the block's registers
     unsigned grid;
 };
@@ -77,8 +90,8 @@ RmsPlan plan_rms(int rows, int columns, int V, bool backward) {
     const int per_thread = std::min(kRmsElements / V, 8), vectors = columns / V;
     const int threads = divide_up(divide_up(vectors, per_thread), 32) * 32;
     pl.wide = threads > kRmsMaxThreads;
-    pl.threads = pl.wide ? kRmsMaxThreads : threads;
-    const int blocks_per_sm = std::max(1, std::min(16, 1024 / pl.threads));
+    pl.threads = static_cast<unsigned>(pl.wide ? kRmsMaxThreads : threads);
+    const int blocks_per_sm = std::max(1, std::min(16, 1024 / static_cast<int>(pl.threads)));
     pl.grid = static_cast<unsigned>(std::min<int64_t>(rows, static_cast<int64_t>(sm_count()) * blocks_per_sm));
     return pl;
 }
@@ -137,11 +150,11 @@ bns_status rms_forward(const bns_rows* sh, const void* x, int64_t x_stride, cons
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const size_t smem = __is_same(OUT, RmsGroupScale) && rule.V < 4 ? pl.threads / 32 * 8 * sizeof(float) : 0;
     if (pl.wide)
-        BNS_LM_BY_TYPE_V(sh->dtype, rule.V, (launch(BNS_KERNEL_RMS_FORWARD, rms_forward_wide_kernel<T, V, OUT>, pl.grid,
-                                                    pl.threads, 0, stream, a)));
+        BNS_LM_BY_TYPE_V(sh->dtype, rule.V, (launch(BNS_KERNEL_RMS_FORWARD, rms_forward_wide_kernel<T, V, OUT>,
+                                                    Shape{pl.grid, pl.threads}, 0, stream, a)));
     else
-        BNS_LM_BY_TYPE_V(sh->dtype, rule.V, (launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, OUT>, pl.grid, pl.threads,
-                                                    smem, stream, a)));
+        BNS_LM_BY_TYPE_V(sh->dtype, rule.V, (launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, OUT>,
+                                                    Shape{pl.grid, pl.threads}, smem, stream, a)));
     return last_error();
 }
 
@@ -160,7 +173,7 @@ struct HeadProblem {
     int piece, pieces;              // columns of the vocabulary at a time
     int G_pitch;
     int splits;                     // of dx along the vocabulary
-    size_t off_x, off_w, off_G, off_partial, off_logit, off_sums, total;
+    size_t off_unit, off_x, off_w, off_G, off_partial, off_logit, off_sums, total;
 };
 
 bns_status check_head(const bns_head* sh) {
@@ -171,6 +184,9 @@ bns_status check_head(const bns_head* sh) {
     if (!known(sh->dtype)) return BNS_ERR_DTYPE;
     return BNS_OK;
 }
+
+// CTAs that work on a tile of a product with M rows.
+int head_ctas(int M) { return M <= kHeadM ? 1 : 2; }
 
 bool tma_rows(int64_t stride) { return stride % 8 == 0 && stride < int64_t{1} << 38; }
 
@@ -198,9 +214,10 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     p.pieces = divide_up(p.V, p.piece);
     p.G_pitch = divide_up(p.piece, kHeadK) * kHeadK;
     // few rows: dx is a product with few tiles and a long sum, which is split over the SMs
-    const int64_t tiles = static_cast<int64_t>(divide_up(p.T, kHeadM)) * divide_up(p.D, kHeadN);
+    const int ctas = head_ctas(p.T);
+    const int64_t tiles = static_cast<int64_t>(divide_up(p.T, kHeadM * ctas)) * divide_up(p.D, kHeadN);
     const int64_t steps = static_cast<int64_t>(divide_up(p.piece, kHeadK)) * p.pairs;
-    p.splits = static_cast<int>(std::max<int64_t>(1, std::min(tiles ? sm_count() / tiles : 1, steps / 4)));
+    p.splits = static_cast<int>(std::max<int64_t>(1, std::min(tiles ? sm_count() / ctas / tiles : 1, steps / 4)));
     size_t at = kHeaderBytes;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -211,10 +228,11 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     if (p.copy_x) p.off_x = take(T * p.terms * p.pitch * 2);
     if (p.copy_w) p.off_w = take(static_cast<size_t>(p.piece) * p.terms * p.pitch * 2);
     if (backward) {
+        p.off_unit = take(sizeof(float));
         p.off_G = take(T * p.terms * p.G_pitch * 2);
         if (p.splits > 1 || p.pieces > 1) p.off_sums = take(T * p.splits * p.D * 4);
     } else {
-        p.off_partial = take(T * divide_up(p.V, kHeadN) * sizeof(float2) + T * p.pieces * sizeof(float2));
+        p.off_partial = take(2 * T * (divide_up(p.V, kHeadN) + p.pieces) * sizeof(float2));
         p.off_logit = take(T * 4);
     }
     p.total = at;
@@ -253,37 +271,47 @@ struct Operand {
     }
 };
 
-template <int KIND, bool A_K, bool B_K, typename T>
-bns_status head_gemm(int kind, const Operand& a, const Operand& b, HeadGemm g, int K, cudaStream_t stream) {
+template <int KIND, bool A_K, bool B_K, typename T, int CTAS>
+bns_status head_gemm_on(int kind, const CUtensorMap& ma, const CUtensorMap& mb, const HeadGemm& g, cudaStream_t stream) {
     static std::atomic<bool> raised[kMaxDevices];
     int device = -1;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= kMaxDevices) return BNS_ERR_CUDA;
-    auto kernel = head_gemm_kernel<KIND, A_K, B_K, T>;
+    auto kernel = head_gemm_kernel<KIND, A_K, B_K, T, CTAS>;
+    constexpr unsigned smem = HeadRing<CTAS>::kSmem;
     if (!raised[device].load(std::memory_order_relaxed)) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem) != cudaSuccess) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
             cudaGetLastError();
             return BNS_ERR_CUDA;
         }
         raised[device].store(true, std::memory_order_relaxed);
     }
+    const int64_t tiles = static_cast<int64_t>(g.tiles_m) * g.tiles_n * g.splits;
+    if (tiles >= int64_t{1} << 30) return BNS_ERR_SHAPE;
+    launch(kind, kernel, Shape{static_cast<unsigned>(std::min<int64_t>(tiles, sm_count() / CTAS)) * CTAS, kHeadThreads, CTAS}, smem,
+           stream, ma, mb, g);
+    return last_error();
+}
+
+// CTA pairs with 256 x 256 tiles; single CTAs where the product has no more rows than one of them holds.
+template <int KIND, bool A_K, bool B_K, typename T>
+bns_status head_gemm(int kind, const Operand& a, const Operand& b, HeadGemm g, int K, cudaStream_t stream) {
+    const int ctas = head_ctas(g.M);
     CUtensorMap ma, mb;
-    if (!a.map(&ma, A_K ? kHeadM : 64) || !b.map(&mb, B_K ? kHeadN : 64)) return BNS_ERR_CUDA;
-    g.tiles_m = divide_up(g.M, kHeadM);
+    if (!a.map(&ma, A_K ? kHeadM : 64) || !b.map(&mb, B_K ? kHeadN / ctas : 64)) return BNS_ERR_CUDA;
+    g.tiles_m = divide_up(g.M, kHeadM * ctas);
     g.tiles_n = divide_up(g.N, kHeadN);
     g.k_blocks = divide_up(K, kHeadK);
     g.pairs = a.terms > 1 ? 6 : 1;
     g.a_pitch = a.pitch;
     g.b_pitch = b.pitch;
-    const int64_t tiles = static_cast<int64_t>(g.tiles_m) * g.tiles_n * g.splits;
-    if (tiles >= int64_t{1} << 31) return BNS_ERR_SHAPE;
-    launch(kind, kernel, static_cast<unsigned>(std::min<int64_t>(tiles, sm_count())), kHeadThreads, kHeadSmem, stream, ma, mb, g);
-    return last_error();
+    return ctas == 2 ? head_gemm_on<KIND, A_K, B_K, T, 2>(kind, ma, mb, g, stream)
+                     : head_gemm_on<KIND, A_K, B_K, T, 1>(kind, ma, mb, g, stream);
 }
 
 void lay_out(int dtype, const void* src, int64_t stride, int rows, int D, int terms, int pitch, void* dst, cudaStream_t stream) {
     const int64_t blocks = divide_up<int64_t>(static_cast<int64_t>(rows) * pitch, 256);
     BNS_LM_BY_TYPE(dtype, (launch(BNS_KERNEL_HEAD_VECTOR, head_terms_kernel<T>,
-                                  static_cast<unsigned>(std::min<int64_t>(blocks, sm_count() * 16)), 256, 0, stream, src, stride,
+                                  Shape{static_cast<unsigned>(std::min<int64_t>(blocks, sm_count() * 16)), 256}, 0, stream, src, stride,
                                   rows, D, terms, pitch, static_cast<unsigned short*>(dst))));
 }
 
@@ -325,8 +353,8 @@ bns_status distill(const bns_distillation* sh, Distill a, cudaStream_t stream) {
     a.teacher_bf16 = sh->teacher_dtype == BNS_BF16;
     a.tau = sh->temperature;
     a.c = static_cast<float>(1.4426950408889634 / static_cast<double>(sh->temperature));
-    BNS_LM_BY_TYPE(sh->dtype, (launch(BNS_KERNEL_DISTILL, distill_kernel<T, WHAT>, static_cast<unsigned>(sh->rows),
-                                      kDistillThreads, 0, stream, a)));
+    BNS_LM_BY_TYPE(sh->dtype, (launch(BNS_KERNEL_DISTILL, distill_kernel<T, WHAT>,
+                                      Shape{static_cast<unsigned>(sh->rows), kDistillThreads}, 0, stream, a)));
     return last_error();
 }
 
@@ -396,12 +424,12 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
     const RmsBackward a{dy, h, dh, weight, rstd, dx, partial, shape->rows, dy_stride, h_stride, dh_stride, shape->columns,
                         1.f / static_cast<float>(shape->columns)};
     if (pl.wide)
-        BNS_LM_BY_TYPE_V(shape->dtype, rule.V, (launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_wide_kernel<T, V>, pl.grid,
-                                                       pl.threads, 0, stream, a)));
+        BNS_LM_BY_TYPE_V(shape->dtype, rule.V, (launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_wide_kernel<T, V>,
+                                                       Shape{pl.grid, pl.threads}, 0, stream, a)));
     else
-        BNS_LM_BY_TYPE_V(shape->dtype, rule.V, (launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V>, pl.grid, pl.threads, 0,
-                                                       stream, a)));
-    launch(BNS_KERNEL_RMS_BACKWARD, rms_dweight_kernel, static_cast<unsigned>(divide_up(shape->columns, 32)), 256, 0, stream,
+        BNS_LM_BY_TYPE_V(shape->dtype, rule.V, (launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V>,
+                                                       Shape{pl.grid, pl.threads}, 0, stream, a)));
+    launch(BNS_KERNEL_RMS_BACKWARD, rms_dweight_kernel, Shape{static_cast<unsigned>(divide_up(shape->columns, 32)), 256}, 0, stream,
            partial, static_cast<int>(pl.grid), shape->columns, dweight);
     return last_error();
 }
@@ -445,9 +473,9 @@ bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x
         g.status = first == 0 ? reinterpret_cast<unsigned*>(ws) : nullptr;
         st = head_gemm<kHeadLse, true, true, BF16>(BNS_KERNEL_HEAD_LOGITS, xs, rows, g, p.D, stream);
         if (st != BNS_OK) return st;
-        tiles += divide_up(count, kHeadN);
+        tiles += 2 * divide_up(count, kHeadN);
     }
-    launch(BNS_KERNEL_HEAD_VECTOR, head_join_kernel, static_cast<unsigned>(divide_up(p.T, 32)), 256, 0, stream, partial, tiles, p.T,
+    launch(BNS_KERNEL_HEAD_VECTOR, head_join_kernel, Shape{static_cast<unsigned>(divide_up(p.T, 32)), 256}, 0, stream, partial, tiles, p.T,
            reinterpret_cast<const float*>(ws + p.off_logit), target, shape->target_is_int64, p.V, loss, lse,
            reinterpret_cast<unsigned*>(ws));
     return last_error();
@@ -472,6 +500,8 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         return cudaMemsetAsync(dw, 0, eb * p.V * p.D, stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
     if (p.copy_x) lay_out(p.dtype, x, shape->x_stride, p.T, p.D, p.terms, p.pitch, ws + p.off_x, stream);
     const Operand xs = rows_of_x(p, shape, x, ws);
+    float* unit = reinterpret_cast<float*>(ws + p.off_unit);
+    launch(BNS_KERNEL_HEAD_VECTOR, head_unit_kernel, Shape{1, 1024}, 0, stream, target, shape->target_is_int64, dloss, p.T, p.V, unit);
     float* sums = p.splits > 1 || p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sums) : nullptr;
     for (int first = 0; first < p.V; first += p.piece) {
         const int count = std::min(p.piece, p.V - first);
@@ -486,17 +516,18 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         g.V = p.V;
         g.lse = lse;
         g.dloss = dloss;
+        g.unit = unit;
         g.G = reinterpret_cast<unsigned short*>(ws + p.off_G);
         g.G_stride = static_cast<int64_t>(p.terms) * p.G_pitch;
         g.G_pitch = p.G_pitch;
-        g.terms = p.terms;
-        st = head_gemm<kHeadGrad, true, true, BF16>(BNS_KERNEL_HEAD_GRADIENT, xs, rows, g, p.D, stream);
+        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadGrad, true, true, T>(BNS_KERNEL_HEAD_GRADIENT, xs, rows, g, p.D, stream)));
         if (st != BNS_OK) return st;
         const Operand G{g.G, g.G_stride, p.T, count, p.terms, p.G_pitch};
         HeadGemm o{};
         o.M = p.T;
         o.N = p.D;
         o.splits = p.splits;
+        o.unit = unit;
         o.out = dx;
         o.out_stride = p.D;
         o.sums = sums;
@@ -508,6 +539,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         q.M = count;
         q.N = p.D;
         q.splits = 1;
+        q.unit = unit;
         q.out = static_cast<char*>(dw) + static_cast<size_t>(first) * p.D * eb;
         q.out_stride = p.D;
         BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, false, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, xs, q, p.T, stream)));
@@ -516,7 +548,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
     if (p.splits > 1) {
         const int64_t blocks = divide_up<int64_t>(static_cast<int64_t>(p.T) * p.D, 256);
         BNS_LM_BY_TYPE(p.dtype, (launch(BNS_KERNEL_HEAD_VECTOR, head_sum_kernel<T>,
-                                        static_cast<unsigned>(std::min<int64_t>(blocks, sm_count() * 16)), 256, 0, stream,
+                                        Shape{static_cast<unsigned>(std::min<int64_t>(blocks, sm_count() * 16)), 256}, 0, stream,
                                         static_cast<const float*>(sums), p.splits, p.T, p.D, dx, static_cast<int64_t>(p.D))));
     }
     return last_error();
