@@ -81,17 +81,27 @@ bns_status check_rows(const bns_rows* sh) {
 
 struct RmsPlan {
     unsigned threads;
-    bool wide;       // the row does not fit the block's registers
+    int elements;    // of a row that a thread holds: 8 or 16; 0 = the row does not fit the block's registers
     unsigned grid;
 };
 
-RmsPlan plan_rms(int rows, int columns, int V, bool backward) {
+// Both kernels are compiled for 64 registers a thread, so 1024 threads an SM.  Eight elements a thread leave room for
+// the next row's loads of fp32 tensors and for the gradient's column sums; sixteen of bf16 fit the forward kernel
+// (8192 x 4096: 49 us against 52 with eight).  Few rows take more threads per row, as nothing else fills the SM.
+RmsPlan plan_rms(int rows, int columns, int V, bool eight) {
     RmsPlan pl;
-    const int per_thread = std::min(kRmsElements / V, 8), vectors = columns / V;
-    const int threads = divide_up(divide_up(vectors, per_thread), 32) * 32;
-    pl.wide = threads > kRmsMaxThreads;
-    pl.threads = static_cast<unsigned>(pl.wide ? kRmsMaxThreads : threads);
-    const int blocks_per_sm = std::max(1, std::min(16, 1024 / static_cast<int>(pl.threads)));
+    const int vectors = columns / V;
+    for (pl.elements = eight || rows <= sm_count() ? 8 : 16; pl.elements <= 16; pl.elements *= 2) {
+        const int per_thread = std::min(std::max(1, pl.elements / V), 8);
+        const int threads = divide_up(divide_up(vectors, per_thread), 32) * 32;
+        pl.threads = static_cast<unsigned>(threads);
+        if (threads <= kRmsMaxThreads) break;
+    }
+    if (pl.elements > 16) {
+        pl.elements = 0;
+        pl.threads = kRmsMaxThreads;
+    }
+    const int blocks_per_sm = std::max(1, std::min(32, kRmsMaxThreads / static_cast<int>(pl.threads)));
     pl.grid = static_cast<unsigned>(std::min<int64_t>(rows, static_cast<int64_t>(sm_count()) * blocks_per_sm));
     return pl;
 }
@@ -144,22 +154,25 @@ bns_status rms_forward(const bns_rows* sh, const void* x, int64_t x_stride, cons
     rule.tensor(h, sh->columns);
     if (!quantized) rule.tensor(y, sh->columns);
     while (quantized && !aligned(y, static_cast<size_t>(rule.V))) rule.V >>= 1;
-    const RmsPlan pl = plan_rms(sh->rows, sh->columns, rule.V, false);
+    const RmsPlan pl = plan_rms(sh->rows, sh->columns, rule.V, sh->dtype == BNS_F32);
     const RmsForward a{x, residual, weight, y, scales, h, rstd, sh->rows, x_stride, residual_stride, sh->columns, eps,
                        1.f / static_cast<float>(sh->columns)};
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const Shape shape{pl.grid, pl.threads};
     const size_t smem = __is_same(OUT, RmsGroupScale) && rule.V < 4 ? pl.threads / 32 * 8 * sizeof(float) : 0;
-    if (pl.wide)
-        BNS_LM_BY_TYPE_V(sh->dtype, rule.V, (launch(BNS_KERNEL_RMS_FORWARD, rms_forward_wide_kernel<T, V, OUT>,
-                                                    Shape{pl.grid, pl.threads}, 0, stream, a)));
-    else
-        BNS_LM_BY_TYPE_V(sh->dtype, rule.V, (launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, OUT>,
-                                                    Shape{pl.grid, pl.threads}, smem, stream, a)));
+    BNS_LM_BY_TYPE_V(sh->dtype, rule.V, {
+        if (pl.elements == 8)
+            launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, 8, OUT>, shape, smem, stream, a);
+        else if (pl.elements == 16)
+            launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, 16, OUT>, shape, smem, stream, a);
+        else
+            launch(BNS_KERNEL_RMS_FORWARD, rms_forward_wide_kernel<T, V, OUT>, shape, 0, stream, a);
+    });
     return last_error();
 }
 
 // Blocks of the gradient kernel, at the most: each leaves a row of partial sums.
-int rms_backward_blocks(int rows) { return std::min(rows, sm_count() * 16); }
+int rms_backward_blocks(int rows) { return std::min(rows, sm_count() * 32); }
 
 // ------------------------------------------------------------------------------------ head
 constexpr size_t kHeadPieceBytes = size_t{256} << 20;   // aimed at for G of a piece, and for a piece's operand in bf16 terms
@@ -423,12 +436,15 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
     float* partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kHeaderBytes);
     const RmsBackward a{dy, h, dh, weight, rstd, dx, partial, shape->rows, dy_stride, h_stride, dh_stride, shape->columns,
                         1.f / static_cast<float>(shape->columns)};
-    if (pl.wide)
-        BNS_LM_BY_TYPE_V(shape->dtype, rule.V, (launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_wide_kernel<T, V>,
-                                                       Shape{pl.grid, pl.threads}, 0, stream, a)));
-    else
-        BNS_LM_BY_TYPE_V(shape->dtype, rule.V, (launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V>,
-                                                       Shape{pl.grid, pl.threads}, 0, stream, a)));
+    const Shape grid{pl.grid, pl.threads};
+    BNS_LM_BY_TYPE_V(shape->dtype, rule.V, {
+        if (pl.elements == 8)
+            launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V, 8>, grid, 0, stream, a);
+        else if (pl.elements == 16)
+            launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V, 16>, grid, 0, stream, a);
+        else
+            launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_wide_kernel<T, V>, grid, 0, stream, a);
+    });
     launch(BNS_KERNEL_RMS_BACKWARD, rms_dweight_kernel, Shape{static_cast<unsigned>(divide_up(shape->columns, 32)), 256}, 0, stream,
            partial, static_cast<int>(pl.grid), shape->columns, dweight);
     return last_error();

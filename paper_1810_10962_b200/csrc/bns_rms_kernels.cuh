@@ -6,15 +6,16 @@
 //   gradient at the stored h: c = mean(w dy h rstd);  dx = rstd (w dy - h rstd c) + dh;  dw = sum over rows of dy h rstd
 //
 // Bound by HBM: a row is read once and lives in registers (EPT elements a thread), so every tensor crosses the
-// memory system once.  A block owns a row at a time and walks down the rows with a grid stride, which keeps its
-// columns' weights (and, in the gradient, its columns' sums over the rows) in registers as well.
+// memory system once.  A block owns a row at a time and walks down the rows with a grid stride; the next row's loads are
+// issued before this row's sums are joined, so that loads stay in flight across the block's barriers.  The weights are read
+// from L1 for every row (they would cost as many registers as the row).  The gradient keeps its columns' sums over the rows in
+// registers and leaves them once, one row of partial sums per block.
 #pragma once
 
 #include "bns_elements.cuh"
 
 namespace bns {
 
-constexpr int kRmsElements = 16;      // elements of a row that a thread holds
 constexpr int kRmsMaxThreads = 1024;
 constexpr int kRmsGroup = 128;        // columns of a scale in the grouped 8-bit form
 
@@ -104,73 +105,115 @@ struct RmsForward {
     float eps, inv_D;
 };
 
-// One row in registers: thread t holds vectors t, t + blockDim, ... of V elements.
-template <typename T, int V, typename OUT>
+// Vectors of V elements that a thread holds.
+template <int V, int EPT>
+constexpr int kRmsVectors = EPT / V < 1 ? 1 : EPT / V < 8 ? EPT / V : 8;
+
+// A thread's vectors t, t + blockDim, ... of a row.
+template <typename T, int V, int NV>
+struct RowPiece {
+    Vec<T, V> v[NV];
+    __device__ __forceinline__ void load(const typename T::storage* row, int vectors) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = threadIdx.x + i * blockDim.x;
+            if (at < vectors) v[i].raw = __ldcs(reinterpret_cast<const typename Vec<T, V>::raw_t*>(row + static_cast<int64_t>(at) * V));
+        }
+    }
+};
+
+// V weights; rows of weights are only as aligned as floats are.
+template <int V>
+__device__ __forceinline__ void load_weights(const float* weight, int at, bool aligned, float (&w)[V]) {
+    if constexpr (V >= 4) {
+        if (aligned) {
+#pragma unroll
+            for (int j = 0; j < V; j += 4) {
+                const float4 q = __ldg(reinterpret_cast<const float4*>(weight + at * V + j));
+                w[j] = q.x;
+                w[j + 1] = q.y;
+                w[j + 2] = q.z;
+                w[j + 3] = q.w;
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) w[j] = __ldg(weight + at * V + j);
+}
+
+template <typename T, int V, int EPT, typename OUT>
 __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsForward a) {
     using S = typename T::storage;
-    constexpr int NV = kRmsElements / V < 8 ? kRmsElements / V : 8;
+    constexpr int NV = kRmsVectors<V, EPT>;
     constexpr bool kRow = __is_same(OUT, RmsRowScale), kGroup = __is_same(OUT, RmsGroupScale);
     __shared__ BlockExchange ex;
     extern __shared__ float segment[];    // grouped form with V < 4: largest |s w| of every 32 V columns
     const int B = blockDim.x, vectors = a.D / V;
+    const bool aligned = (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     grid_dependency_wait();
     grid_dependency_launch();
 
-    float w[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int v = threadIdx.x + i * B;
-#pragma unroll
-        for (int j = 0; j < V; ++j) w[i][j] = v < vectors ? a.weight[v * V + j] : 0.f;
-    }
+    RowPiece<T, V, NV> vx, vr;
+    auto fetch = [&](int64_t row) {
+        vx.load(static_cast<const S*>(a.x) + row * a.x_stride, vectors);
+        if (a.residual) vr.load(static_cast<const S*>(a.residual) + row * a.residual_stride, vectors);
+    };
     int turn = 0;
+    if (blockIdx.x < a.rows) fetch(blockIdx.x);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        const S* x = static_cast<const S*>(a.x) + row * a.x_stride;
-        const S* r = static_cast<const S*>(a.residual) + (a.residual ? row * a.residual_stride : 0);
-        Vec<T, V> vx[NV], vr[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = threadIdx.x + i * B;
-            if (v < vectors) {
-                vx[i].load(x + static_cast<int64_t>(v) * V);
-                if (a.residual) vr[i].load(r + static_cast<int64_t>(v) * V);
-            }
-        }
         float s[NV][V], sum = 0.f, top = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+            vx.v[i].unpack(s[i]);
+            if (a.residual) {
+                float f[V];
+                vr.v[i].unpack(f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[i][j] += f[j];
+            }
+        }
+        if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
             if (v < vectors) {
-                vx[i].unpack(s[i]);
-                if (a.residual) {
-                    float f[V];
-                    vr[i].unpack(f);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) s[i][j] += f[j];
-                }
                 if (a.h) {
                     Vec<T, V> o;
                     o.pack(s[i]);
                     o.store(static_cast<S*>(a.h) + row * a.D + static_cast<int64_t>(v) * V);
                 }
+                if constexpr (kRow) {
+                    float w[V];
+                    load_weights<V>(a.weight, v, aligned, w);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    sum = fmaf(s[i][j], s[i][j], sum);
-                    if constexpr (kRow) top = max_or_nan(top, fabsf(s[i][j] * w[i][j]));
+                    for (int j = 0; j < V; ++j) top = max_or_nan(top, fabsf(s[i][j] * w[j]));
                 }
-            } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) s[i][j] = 0.f;
+                for (int j = 0; j < V; ++j) sum = fmaf(s[i][j], s[i][j], sum);
             }
         }
+        // s w of vector i, zeros past the row's end
+        auto product = [&](int i, float (&p)[V]) {
+            const int v = threadIdx.x + i * B;
+            if (v < vectors) {
+                load_weights<V>(a.weight, v, aligned, p);
+#pragma unroll
+                for (int j = 0; j < V; ++j) p[j] *= s[i][j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) p[j] = 0.f;
+            }
+        };
         if constexpr (kGroup && V < 4) {
             // a warp's 32 V columns lie inside one group: their maximum goes through shared memory
             __syncthreads();   // the previous row's readers are done
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                float m = 0.f;
+                float m = 0.f, p[V];
+                product(i, p);
 #pragma unroll
-                for (int j = 0; j < V; ++j) m = max_or_nan(m, fabsf(s[i][j] * w[i][j]));
+                for (int j = 0; j < V; ++j) m = max_or_nan(m, fabsf(p[j]));
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
                 if ((threadIdx.x & 31) == 0) segment[(threadIdx.x + i * B) >> 5] = m;
@@ -179,56 +222,52 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
         }
         block_exchange<kRow>(sum, top, ex, turn);
         const float rstd = 1.f / sqrtf(fmaf(sum, a.inv_D, a.eps));
-        if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+        if (threadIdx.x == 0) a.rstd[row] = rstd;
         if constexpr (!kRow && !kGroup) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int v = threadIdx.x + i * B;
                 if (v >= vectors) continue;
                 float f[V];
+                load_weights<V>(a.weight, v, aligned, f);
 #pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = s[i][j] * rstd * w[i][j];
+                for (int j = 0; j < V; ++j) f[j] *= s[i][j] * rstd;
                 Vec<T, V> o;
                 o.pack(f);
                 o.store(static_cast<S*>(a.y) + row * a.D + static_cast<int64_t>(v) * V);
             }
-        } else if constexpr (kRow) {
-            const Quant quant(top, rstd);
-            if (threadIdx.x == 0) a.scales[row] = quant.scale;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int v = threadIdx.x + i * B;
-                if (v >= vectors) continue;
-                float f[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = quant(s[i][j] * w[i][j]);
-                store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, f);
-            }
         } else {
             const int groups = (a.D + kRmsGroup - 1) / kRmsGroup;
+            const Quant of_row(top, rstd);
+            if (kRow && threadIdx.x == 0) a.scales[row] = of_row.scale;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int v = threadIdx.x + i * B;
-                float m = 0.f;
-                if constexpr (V >= 4) {
+                float p[V];
+                product(i, p);
+                if constexpr (kRow) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) m = max_or_nan(m, fabsf(s[i][j] * w[i][j]));
-#pragma unroll
-                    for (int o = kRmsGroup / V / 2; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    for (int j = 0; j < V; ++j) p[j] = of_row(p[j]);
                 } else {
-                    constexpr int kSegments = kRmsGroup / (32 * V);
-                    const int first = (v >> 5) / kSegments * kSegments;
+                    float m = 0.f;
+                    if constexpr (V >= 4) {
 #pragma unroll
-                    for (int q = 0; q < kSegments; ++q)
-                        if (first + q < (vectors + 31) >> 5) m = max_or_nan(m, segment[first + q]);
+                        for (int j = 0; j < V; ++j) m = max_or_nan(m, fabsf(p[j]));
+#pragma unroll
+                        for (int o = kRmsGroup / V / 2; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    } else {
+                        constexpr int kSegments = kRmsGroup / (32 * V);
+                        const int first = (v >> 5) / kSegments * kSegments;
+#pragma unroll
+                        for (int q = 0; q < kSegments; ++q)
+                            if (first + q < (vectors + 31) >> 5) m = max_or_nan(m, segment[first + q]);
+                    }
+                    const Quant quant(m, rstd);
+                    if (v < vectors && v % (kRmsGroup / V) == 0) a.scales[row * groups + v / (kRmsGroup / V)] = quant.scale;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) p[j] = quant(p[j]);
                 }
-                if (v >= vectors) continue;
-                const Quant quant(m, rstd);
-                float f[V];
-                if (v % (kRmsGroup / V) == 0) a.scales[row * groups + v / (kRmsGroup / V)] = quant.scale;
-#pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = quant(s[i][j] * w[i][j]);
-                store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, f);
+                if (v < vectors) store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, p);
             }
         }
     }
@@ -276,7 +315,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_wide_kernel(const 
         }
         block_exchange<kRow>(sum, top, ex, turn);
         const float rstd = 1.f / sqrtf(fmaf(sum, a.inv_D, a.eps));
-        if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+        if (threadIdx.x == 0) a.rstd[row] = rstd;
         if constexpr (kGroup) {
             // a warp per group, four columns a lane
             const int groups = (a.D + kRmsGroup - 1) / kRmsGroup;
@@ -333,69 +372,63 @@ struct RmsBackward {
     float inv_D;
 };
 
-template <typename T, int V>
+template <typename T, int V, int EPT>
 __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsBackward a) {
     using S = typename T::storage;
-    constexpr int NV = kRmsElements / V < 8 ? kRmsElements / V : 8;
+    constexpr int NV = kRmsVectors<V, EPT>;
     __shared__ BlockExchange ex;
     const int B = blockDim.x, vectors = a.D / V;
+    const bool aligned = (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     grid_dependency_wait();
     grid_dependency_launch();
-    float w[NV][V], dw[NV][V];
+    float dw[NV][V];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int v = threadIdx.x + i * B;
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            w[i][j] = v < vectors ? a.weight[v * V + j] : 0.f;
-            dw[i][j] = 0.f;
-        }
-    }
+        for (int j = 0; j < V; ++j) dw[i][j] = 0.f;
+    RowPiece<T, V, NV> vy, vh, vd;
+    float next_rstd = 0.f;
+    auto fetch = [&](int64_t row) {
+        vy.load(static_cast<const S*>(a.dy) + row * a.dy_stride, vectors);
+        vh.load(static_cast<const S*>(a.h) + row * a.h_stride, vectors);
+        next_rstd = a.rstd[row];
+    };
     int turn = 0;
+    if (blockIdx.x < a.rows) fetch(blockIdx.x);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        const S* dy = static_cast<const S*>(a.dy) + row * a.dy_stride;
-        const S* h = static_cast<const S*>(a.h) + row * a.h_stride;
-        const S* dh = static_cast<const S*>(a.dh) + (a.dh ? row * a.dh_stride : 0);
-        const float rstd = a.rstd[row];
-        Vec<T, V> vy[NV], vh[NV], vd[NV];
+        const float rstd = next_rstd;
+        if (a.dh) vd.load(static_cast<const S*>(a.dh) + row * a.dh_stride, vectors);
+        float sum = 0.f, none = 0.f, xhat[NV][V], wdy[NV][V];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
             if (v < vectors) {
-                vy[i].load(dy + static_cast<int64_t>(v) * V);
-                vh[i].load(h + static_cast<int64_t>(v) * V);
-                if (a.dh) vd[i].load(dh + static_cast<int64_t>(v) * V);
-            }
-        }
-        float sum = 0.f, none = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (threadIdx.x + i * B < vectors) {
-                float fy[V], fh[V];
-                vy[i].unpack(fy);
-                vh[i].unpack(fh);
+                float w[V];
+                load_weights<V>(a.weight, v, aligned, w);
+                vy.v[i].unpack(wdy[i]);
+                vh.v[i].unpack(xhat[i]);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float xhat = fh[j] * rstd;
-                    dw[i][j] = fmaf(fy[j], xhat, dw[i][j]);
-                    sum = fmaf(w[i][j] * fy[j], xhat, sum);
+                    xhat[i][j] *= rstd;
+                    dw[i][j] = fmaf(wdy[i][j], xhat[i][j], dw[i][j]);
+                    wdy[i][j] *= w[j];
+                    sum = fmaf(wdy[i][j], xhat[i][j], sum);
                 }
             }
         }
+        if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
         block_exchange<false>(sum, none, ex, turn);
         const float c = sum * a.inv_D;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
             if (v >= vectors) continue;
-            float fy[V], fh[V], f[V];
-            vy[i].unpack(fy);
-            vh[i].unpack(fh);
+            float f[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) f[j] = rstd * fmaf(-fh[j] * rstd, c, w[i][j] * fy[j]);
+            for (int j = 0; j < V; ++j) f[j] = rstd * fmaf(-xhat[i][j], c, wdy[i][j]);
             if (a.dh) {
                 float fd[V];
-                vd[i].unpack(fd);
+                vd.v[i].unpack(fd);
 #pragma unroll
                 for (int j = 0; j < V; ++j) f[j] += fd[j];
             }

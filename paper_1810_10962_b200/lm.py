@@ -10,6 +10,7 @@ of the wrong kind.
 from __future__ import annotations
 
 import ctypes
+from functools import lru_cache
 from typing import Optional
 
 import torch
@@ -37,6 +38,13 @@ class _Distillation(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int), ("vocabulary", ctypes.c_int), ("entries", ctypes.c_int), ("dtype", ctypes.c_int),
                 ("stride", ctypes.c_int64), ("teacher_dtype", ctypes.c_int), ("index_is_int64", ctypes.c_int),
                 ("temperature", ctypes.c_float)]
+
+
+@lru_cache(maxsize=4096)
+def _shape(kind, *fields):
+    """(structure, reference to it) for these values; the library only reads it."""
+    struct = kind(*fields)
+    return struct, ctypes.byref(struct)
 
 
 _lib = None
@@ -111,14 +119,27 @@ def _indices(t, shape, name: str, device):
 
 def _stream(device) -> int:
     """The current stream, of the tensors' device: kernels are launched on the device that is current."""
-    if device.index != torch.cuda.current_device():
+    index = device.index
+    if index != torch.cuda.current_device():
         raise TypeError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(index)      # torch.cuda.current_stream() builds a Stream object first: 3 us
 
 
 def _check(status: int, what: str) -> None:
     if status != 0:
         raise BnsError(status, what)
+
+
+def _like(t, dtype=None):
+    """A new dense tensor of t's shape."""
+    if t.is_contiguous():
+        return torch.empty_like(t, dtype=dtype)
+    return torch.empty(t.shape, dtype=dtype or t.dtype, device=t.device)
+
+
+def _vector_of(t):
+    """A new fp32 tensor with a value for each row of t."""
+    return t.new_empty(t.shape[:-1], dtype=torch.float32)
 
 
 def _scratch(workspace, need: int, device):
@@ -136,7 +157,7 @@ def _norm_inputs(x, residual, weight):
     if residual is not None:
         residual_stride = _matrix(residual, "residual", x)[2]
         residual_at = residual.data_ptr()
-    shape = _Rows(rows, columns, _code(x))
+    shape = _shape(_Rows, rows, columns, _code(x))[1]
     return shape, x.data_ptr(), stride, residual_at, residual_stride, _vector(weight, columns, "weight", x.device)
 
 
@@ -144,10 +165,10 @@ def rms_norm_forward(x, residual, weight, eps):
     """bns_rms_norm_forward: returns (y, h, rstd) with h = x + residual and y = h rstd weight.  ``residual`` may be
     None; h is then x itself.  weight and rstd are float32."""
     shape, xp, xs, rp, rs, wp = _norm_inputs(x, residual, weight)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    h = x if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    _check(_load().bns_rms_norm_forward(ctypes.byref(shape), xp, xs, rp, rs, wp, float(eps), y.data_ptr(),
+    y = _like(x)
+    h = x if residual is None else _like(x)
+    rstd = _vector_of(x)
+    _check(_load().bns_rms_norm_forward(shape, xp, xs, rp, rs, wp, float(eps), y.data_ptr(),
                                         None if residual is None else h.data_ptr(), rstd.data_ptr(), _stream(x.device)),
            "bns_rms_norm_forward")
     return y, h, rstd
@@ -157,12 +178,12 @@ def rms_norm_forward_fp8(x, residual, weight, eps, group=0):
     """bns_rms_norm_forward_quantized: returns (q, scales, h, rstd); q is float8_e4m3fn, y = q * scale.  ``group``: 0 for
     one scale a row (scales [..., 1]), 128 for one per 128 columns (scales [..., ceil(columns / 128)])."""
     shape, xp, xs, rp, rs, wp = _norm_inputs(x, residual, weight)
-    groups = 1 if group == 0 else -(-shape.columns // GROUP)
-    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
-    scales = torch.empty((*x.shape[:-1], groups), dtype=torch.float32, device=x.device)
-    h = x if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    _check(_load().bns_rms_norm_forward_quantized(ctypes.byref(shape), xp, xs, rp, rs, wp, float(eps), int(group),
+    groups = 1 if group == 0 else -(-x.shape[-1] // GROUP)
+    q = _like(x, torch.float8_e4m3fn)
+    scales = x.new_empty((*x.shape[:-1], groups), dtype=torch.float32)
+    h = x if residual is None else _like(x)
+    rstd = _vector_of(x)
+    _check(_load().bns_rms_norm_forward_quantized(shape, xp, xs, rp, rs, wp, float(eps), int(group),
                                                   q.data_ptr(), scales.data_ptr(),
                                                   None if residual is None else h.data_ptr(), rstd.data_ptr(),
                                                   _stream(x.device)), "bns_rms_norm_forward_quantized")
@@ -178,12 +199,13 @@ def rms_norm_backward(dy, h, weight, rstd, dh=None, workspace=None):
     if dh is not None:
         dh_stride, dh_at = _matrix(dh, "dh", h)[2], dh.data_ptr()
     device, lib = h.device, _load()
-    shape = _Rows(rows, columns, _code(h))
-    dx = torch.empty(h.shape, dtype=h.dtype, device=device)
-    dweight = torch.empty(columns, dtype=torch.float32, device=device)
-    workspace = _scratch(workspace, lib.bns_rms_norm_workspace_bytes(ctypes.byref(shape)), device)
-    _check(lib.bns_rms_norm_backward(ctypes.byref(shape), dy.data_ptr(), dy_stride, h.data_ptr(), h_stride,
-                                     _vector(weight, columns, "weight", device), _vector(rstd, rows, "rstd", device), dh_at,
+    weight_at = _vector(weight, columns, "weight", device)
+    shape = _shape(_Rows, rows, columns, _code(h))[1]
+    dx = _like(h)
+    dweight = torch.empty_like(weight)
+    workspace = _scratch(workspace, lib.bns_rms_norm_workspace_bytes(shape), device)
+    _check(lib.bns_rms_norm_backward(shape, dy.data_ptr(), dy_stride, h.data_ptr(), h_stride,
+                                     weight_at, _vector(rstd, rows, "rstd", device), dh_at,
                                      dh_stride, dx.data_ptr(), dweight.data_ptr(), workspace.data_ptr(), workspace.nbytes,
                                      _stream(device)), "bns_rms_norm_backward")
     return dx, dweight
@@ -196,12 +218,12 @@ def _head_inputs(x, w, target):
     if w.dim() != 2 or w_width != width or w.dtype != x.dtype or w.device != x.device:
         raise TypeError("w must be [vocabulary, width] with the width, dtype and device of x")
     at, wide = _indices(target, x.shape[:-1], "target", x.device)
-    return _Head(rows, vocabulary, width, _code(x), x_stride, w_stride, wide), at
+    return (*_shape(_Head, rows, vocabulary, width, _code(x), x_stride, w_stride, wide), at)
 
 
 def linear_cross_entropy_workspace_bytes(x, w, target, backward=False) -> int:
-    shape, _ = _head_inputs(x, w, target)
-    need = _load().bns_linear_cross_entropy_workspace_bytes(ctypes.byref(shape), 1 if backward else 0)
+    _, shape, _ = _head_inputs(x, w, target)
+    need = _load().bns_linear_cross_entropy_workspace_bytes(shape, 1 if backward else 0)
     if need == 0:
         raise BnsError(-2, "bns_linear_cross_entropy_workspace_bytes")
     return int(need)
@@ -210,12 +232,11 @@ def linear_cross_entropy_workspace_bytes(x, w, target, backward=False) -> int:
 def linear_cross_entropy_forward(x, w, target, workspace=None):
     """bns_linear_cross_entropy_forward: returns (loss, lse), float32 of target's shape.  Rows whose target is negative
     are left out: their loss is 0.  The caller takes the mean, or whatever it wants, of the losses."""
-    shape, at = _head_inputs(x, w, target)
+    _, shape, at = _head_inputs(x, w, target)
     device, lib = x.device, _load()
-    loss = torch.empty(target.shape, dtype=torch.float32, device=device)
-    lse = torch.empty(target.shape, dtype=torch.float32, device=device)
-    workspace = _scratch(workspace, lib.bns_linear_cross_entropy_workspace_bytes(ctypes.byref(shape), 0), device)
-    _check(lib.bns_linear_cross_entropy_forward(ctypes.byref(shape), x.data_ptr(), w.data_ptr(), at, loss.data_ptr(),
+    loss, lse = _vector_of(x), _vector_of(x)
+    workspace = _scratch(workspace, lib.bns_linear_cross_entropy_workspace_bytes(shape, 0), device)
+    _check(lib.bns_linear_cross_entropy_forward(shape, x.data_ptr(), w.data_ptr(), at, loss.data_ptr(),
                                                 lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(device)),
            "bns_linear_cross_entropy_forward")
     return loss, lse
@@ -223,14 +244,13 @@ def linear_cross_entropy_forward(x, w, target, workspace=None):
 
 def linear_cross_entropy_backward(x, w, target, lse, dloss, workspace=None):
     """bns_linear_cross_entropy_backward: returns (dx, dw); dloss is the gradient of every row's loss, float32."""
-    shape, at = _head_inputs(x, w, target)
+    fields, shape, at = _head_inputs(x, w, target)
     device, lib = x.device, _load()
-    dx = torch.empty(x.shape, dtype=x.dtype, device=device)
-    dw = torch.empty(w.shape, dtype=w.dtype, device=device)
-    workspace = _scratch(workspace, lib.bns_linear_cross_entropy_workspace_bytes(ctypes.byref(shape), 1), device)
-    _check(lib.bns_linear_cross_entropy_backward(ctypes.byref(shape), x.data_ptr(), w.data_ptr(), at,
-                                                 _vector(lse, shape.rows, "lse", device),
-                                                 _vector(dloss, shape.rows, "dloss", device), dx.data_ptr(), dw.data_ptr(),
+    dx, dw = _like(x), _like(w)
+    workspace = _scratch(workspace, lib.bns_linear_cross_entropy_workspace_bytes(shape, 1), device)
+    _check(lib.bns_linear_cross_entropy_backward(shape, x.data_ptr(), w.data_ptr(), at,
+                                                 _vector(lse, fields.rows, "lse", device),
+                                                 _vector(dloss, fields.rows, "dloss", device), dx.data_ptr(), dw.data_ptr(),
                                                  workspace.data_ptr(), workspace.nbytes, _stream(device)),
            "bns_linear_cross_entropy_backward")
     return dx, dw
@@ -243,17 +263,16 @@ def _distillation_inputs(logits, teacher, index, temperature):
             or teacher.shape[:-1] != logits.shape[:-1] or not teacher.is_contiguous()):
         raise TypeError("teacher must be a contiguous tensor [..., entries] next to the logits")
     at, wide = _indices(index, teacher.shape, "index", logits.device)
-    shape = _Distillation(rows, vocabulary, teacher.shape[-1], _code(logits), stride, _code(teacher), wide, float(temperature))
-    return shape, at
+    return (*_shape(_Distillation, rows, vocabulary, teacher.shape[-1], _code(logits), stride, _code(teacher), wide,
+                    float(temperature)), at)
 
 
 def topk_distillation_forward(logits, teacher, index, temperature=1.0):
     """bns_topk_distillation_forward: returns (loss, lse), float32 per row.  ``teacher`` holds the teacher's logits at the
     places ``index``; a negative index is no entry."""
-    shape, at = _distillation_inputs(logits, teacher, index, temperature)
-    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
-    lse = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
-    _check(_load().bns_topk_distillation_forward(ctypes.byref(shape), logits.data_ptr(), teacher.data_ptr(), at,
+    _, shape, at = _distillation_inputs(logits, teacher, index, temperature)
+    loss, lse = _vector_of(logits), _vector_of(logits)
+    _check(_load().bns_topk_distillation_forward(shape, logits.data_ptr(), teacher.data_ptr(), at,
                                                  loss.data_ptr(), lse.data_ptr(), _stream(logits.device)),
            "bns_topk_distillation_forward")
     return loss, lse
@@ -262,25 +281,25 @@ def topk_distillation_forward(logits, teacher, index, temperature=1.0):
 def topk_distillation_backward(logits, teacher, index, lse, dloss, temperature=1.0):
     """bns_topk_distillation_backward: the gradient of the logits; lse is what the forward call returned, dloss the gradient
     of every row's loss."""
-    shape, at = _distillation_inputs(logits, teacher, index, temperature)
+    fields, shape, at = _distillation_inputs(logits, teacher, index, temperature)
     device = logits.device
-    dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=device)
-    _check(_load().bns_topk_distillation_backward(ctypes.byref(shape), logits.data_ptr(), teacher.data_ptr(), at,
-                                                  _vector(lse, shape.rows, "lse", device),
-                                                  _vector(dloss, shape.rows, "dloss", device), dlogits.data_ptr(),
-                                                  shape.vocabulary, _stream(device)), "bns_topk_distillation_backward")
+    dlogits = _like(logits)
+    _check(_load().bns_topk_distillation_backward(shape, logits.data_ptr(), teacher.data_ptr(), at,
+                                                  _vector(lse, fields.rows, "lse", device),
+                                                  _vector(dloss, fields.rows, "dloss", device), dlogits.data_ptr(),
+                                                  fields.vocabulary, _stream(device)), "bns_topk_distillation_backward")
     return dlogits
 
 
 def topk_distillation_step(logits, teacher, index, dloss, temperature=1.0):
     """bns_topk_distillation_step: returns (loss, dlogits) in one launch, for a dloss that is known beforehand (a mean over
     the rows, say)."""
-    shape, at = _distillation_inputs(logits, teacher, index, temperature)
+    fields, shape, at = _distillation_inputs(logits, teacher, index, temperature)
     device = logits.device
-    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=device)
-    dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=device)
-    _check(_load().bns_topk_distillation_step(ctypes.byref(shape), logits.data_ptr(), teacher.data_ptr(), at,
-                                              _vector(dloss, shape.rows, "dloss", device), loss.data_ptr(),
-                                              dlogits.data_ptr(), shape.vocabulary, _stream(device)),
+    loss = _vector_of(logits)
+    dlogits = _like(logits)
+    _check(_load().bns_topk_distillation_step(shape, logits.data_ptr(), teacher.data_ptr(), at,
+                                              _vector(dloss, fields.rows, "dloss", device), loss.data_ptr(),
+                                              dlogits.data_ptr(), fields.vocabulary, _stream(device)),
            "bns_topk_distillation_step")
     return loss, dlogits
