@@ -1655,13 +1655,13 @@ int bns_slab_plan(const bns_shape* shape, const bns_sampling* sampling, int back
 bns_status bns_wait_timeouts(uint32_t* count, void* cuda_stream) {
     if (!count) return BNS_ERR_NULL;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    uint32_t head = 0;
-    bns_status st = head_wait_timeouts(&head, stream);
+    uint32_t lm = 0;
+    bns_status st = lm_wait_timeouts(&lm, stream);
     if (st != BNS_OK) return st;
     if (cudaMemcpyFromSymbolAsync(count, g_wait_timeouts, sizeof(uint32_t), 0, cudaMemcpyDeviceToHost, stream) != cudaSuccess)
         return BNS_ERR_CUDA;
     if (cudaStreamSynchronize(stream) != cudaSuccess) return BNS_ERR_CUDA;
-    *count += head;
+    *count += lm;
     return BNS_OK;
 }
 

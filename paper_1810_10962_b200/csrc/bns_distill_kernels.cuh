@@ -3,26 +3,28 @@
 //   p = softmax over the row's entries of teacher / tau;  q = softmax over the vocabulary of z / tau
 //   loss = tau^2 sum_k p_k (log p_k - log q_{i_k});   dz_v = dloss tau (q_v [row has entries] - sum over k with i_k = v of p_k)
 //
-// Bound by HBM: the logits are read once (forward), or read once and the gradient written once.  A block owns a row;
-// the pass that writes the gradient reads the row again, out of L2 (148 SMs hold a few rows of some 100 KB each).
-// The statistics are one pass with a running maximum and sum a thread, joined in a fixed order.
+// Bound by HBM: the logits have to be read once (forward), or read once and the gradient written once.  A row is walked by
+// the blocks of a cluster, each on its part: a pass with a running maximum and sum, an exchange over the cluster through
+// distributed shared memory, and for the gradient a second pass that finds part of the row in L2.  What a row needs
+// besides its logits (entries, the logits at their places, its weight) is asked for before the first pass, so that its
+// latencies, some 8 us in a row when each is waited for in turn, lie under the stream.
+//
+// Eight 16-byte loads in flight a thread and 1024 threads an SM: with four loads and 2048 threads the rows in flight
+// (592 of 256 KB at 131072 bf16 values) leave nothing of a row in L2 (4096 rows: 416 us against 509).
+// Measured and not kept: rows held on the chip between the passes, in registers and shared memory of one block per SM or
+// of a cluster (4096 x 131072: 480 and 620 us; the phases of a row no longer overlap those of others).
 //
 // All exponentials are 2^x: with c = log2(e) / tau, exp(z / tau - max) = 2^(z c - max c) is one multiply-add.
 #pragma once
 
-#include "bns_elements.cuh"
+#include <type_traits>
+
+#include "bns_async.cuh"
 
 namespace bns {
 
-constexpr int kDistillThreads = 512;
 constexpr int kDistillMaxEntries = 1024;
 constexpr float kLn2 = 0.6931471805599453f;
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));   // 2 ulp, 2^-126 and below give 0
-    return r;
-}
 
 // Maximum m of a set of values times c (rounded once: it is only the reference) and sum of 2^(value c - m).
 struct TopSum {
@@ -39,6 +41,76 @@ __device__ __forceinline__ TopSum join(TopSum a, TopSum b) {
     return {m, a.s * exp2_fast(a.m - ref) + b.s * exp2_fast(b.m - ref)};
 }
 
+// ---- arithmetic on 16-byte vectors of logits.  The kernels issue some nine instructions an element where memory leaves
+// time for twelve, so pairs go through packed fp32 arithmetic, and bf16 maxima are taken on the stored pairs.
+template <typename T>
+struct TopOf;
+template <>
+struct TopOf<F32> {
+    float v;
+    __device__ __forceinline__ TopOf() : v(-__builtin_huge_valf()) {}
+    __device__ __forceinline__ void add(const uint4& raw) {
+        const float* f = reinterpret_cast<const float*>(&raw);
+        v = fmaxf(v, fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])));
+    }
+    __device__ __forceinline__ float get() const { return v; }
+};
+template <>
+struct TopOf<BF16> {
+    __nv_bfloat162 v;
+    __device__ __forceinline__ TopOf() { *reinterpret_cast<unsigned*>(&v) = 0xff80ff80u; }
+    __device__ __forceinline__ void add(const uint4& raw) {
+        const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&raw);
+        v = __hmax2(v, __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3])));
+    }
+    __device__ __forceinline__ float get() const { return fmaxf(__low2float(v), __high2float(v)); }
+};
+
+// 2^(c value - ref) of a vector's pairs.
+template <typename T>
+__device__ __forceinline__ void exp_pairs(const uint4& raw, pair_t c, pair_t minus_ref, pair_t (&e)[8 / sizeof(typename T::storage)]) {
+    constexpr int V = 16 / sizeof(typename T::storage);
+    Vec<T, V> x;
+    x.raw = raw;
+#pragma unroll
+    for (int q = 0; q < V / 2; ++q) {
+        float lo, hi;
+        split_pair(fma2(vec_pair<T, V>(x, q), c, minus_ref), lo, hi);
+        e[q] = make_pair(exp2_fast(lo), exp2_fast(hi));
+    }
+}
+template <typename T>
+__device__ __forceinline__ void add_exps(const uint4& raw, pair_t c, pair_t minus_ref, pair_t& sum) {
+    constexpr int P = 8 / sizeof(typename T::storage);
+    pair_t e[P];
+    exp_pairs<T>(raw, c, minus_ref, e);
+#pragma unroll
+    for (int q = 0; q < P; ++q) sum = add2(sum, e[q]);
+}
+// Writes 2^(c value - shift) factor; `vectors`: the place is 16-byte aligned.
+template <typename T, bool VECTORS>
+__device__ __forceinline__ void write_exps(typename T::storage* to, const uint4& raw, pair_t c, pair_t minus_shift, pair_t factor) {
+    constexpr int V = 16 / sizeof(typename T::storage), P = V / 2;
+    pair_t e[P];
+    exp_pairs<T>(raw, c, minus_shift, e);
+    Vec<T, V> o;
+#pragma unroll
+    for (int q = 0; q < P; ++q) set_vec_pair<T, V>(o, q, mul2(e[q], factor));
+    if constexpr (VECTORS) {
+        __stcs(reinterpret_cast<uint4*>(to), o.raw);
+    } else {
+        const typename T::storage* f = reinterpret_cast<const typename T::storage*>(&o.raw);
+#pragma unroll
+        for (int j = 0; j < V; ++j) to[j] = f[j];
+    }
+}
+__device__ __forceinline__ pair_t twice(float v) { return make_pair(v, v); }
+__device__ __forceinline__ float both(pair_t v) {
+    float lo, hi;
+    split_pair(v, lo, hi);
+    return lo + hi;
+}
+
 struct Distill {
     const void* z;
     const void* teacher;
@@ -53,162 +125,219 @@ struct Distill {
     int V, K;
     int index64, teacher_bf16;
     float tau, c;         // c = log2(e) / tau
+    int parts, per;       // blocks a row is split over, vectors of each
 };
 
 struct DistillForward {};   // loss and log-sum
 struct DistillBackward {};  // gradient, from the log-sum of the forward call
 struct DistillStep {};      // both in one launch
 
-template <typename T, typename WHAT>
-__global__ void __launch_bounds__(kDistillThreads) distill_kernel(const Distill a) {
+constexpr int kDistillThreads = 512, kDistillSmall = 128;      // of a block; the second for short rows
+constexpr int kDistillParts = 8;                                    // most blocks a row is split over
+constexpr int kDistillOwn = 2;                                      // entries that a thread looks after
+static_assert(kDistillThreads * kDistillOwn == kDistillMaxEntries);
+constexpr int kDistillDepth = 8;                                    // vectors in flight per thread
+
+// The student's maximum and sum as the forward call's log-sum tells them: lse tau c = m + rest with the same c as in
+// z c, so that only z - lse tau feels its rounding; 2^rest stands in for the sum.
+__device__ __forceinline__ TopSum student_of(const Distill& a, float lse) {
+    const double exponent = static_cast<double>(lse) * a.tau * a.c;
+    const float m = static_cast<float>(exponent);
+    return {m, exp2_fast(static_cast<float>(exponent - m))};
+}
+
+// Both pairs of all lanes joined: the maximum first, so that each sum is scaled once.
+__device__ __forceinline__ void warp_join(TopSum& a, TopSum& b) {
+    float ma = a.m, mb = b.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        ma = fmaxf(ma, __shfl_xor_sync(0xffffffffu, ma, o));
+        mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, o));
+    }
+    const float inf = __int_as_float(0x7f800000);
+    a.s *= exp2_fast(a.m - (ma == -inf ? 0.f : ma));
+    b.s *= exp2_fast(b.m - (mb == -inf ? 0.f : mb));
+    a.m = ma;
+    b.m = mb;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+        b.s += __shfl_xor_sync(0xffffffffu, b.s, o);
+    }
+}
+
+// Part blockIdx % parts of row blockIdx / parts: `per` vectors, and the loose elements at either end of the row.
+template <typename T, typename WHAT, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const Distill a) {
     using S = typename T::storage;
-    constexpr int V = 16 / sizeof(S);
+    constexpr int V = 16 / sizeof(S), kWarps = THREADS / 32, kMost = THREADS * kDistillOwn;
     constexpr bool kLoss = !__is_same(WHAT, DistillBackward), kGrad = !__is_same(WHAT, DistillForward);
-    constexpr int kWarpsHere = kDistillThreads / 32;
-    __shared__ float p[kDistillMaxEntries];
-    __shared__ int place[kDistillMaxEntries];
-    __shared__ TopSum fold[kWarpsHere];
-    __shared__ float fold2[kWarpsHere];
+    __shared__ __align__(16) float p[kMost];      // filled up to a multiple of four with no entries
+    __shared__ __align__(16) int place[kMost];
+    __shared__ TopSum fold[2][kWarps];                  // teacher, student
+    __shared__ TopSum of_part[kDistillParts];
+    __shared__ float sums[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float inf = __int_as_float(0x7f800000);
     grid_dependency_wait();
     grid_dependency_launch();
-    const int64_t row = blockIdx.x;
+    const int64_t row = blockIdx.x / a.parts;
+    const int part = blockIdx.x - static_cast<int>(row) * a.parts;
     const S* z = static_cast<const S*>(a.z) + row * a.z_stride;
 
-    // the teacher's distribution: places outside the vocabulary (or negative: no entry) carry nothing
-    TopSum t{-inf, 0.f};
-    for (int k = tid; k < a.K; k += kDistillThreads) {
-        const int64_t e = row * a.K + k;
-        const int64_t i = a.index64 ? static_cast<const long long*>(a.index)[e] : static_cast<const int*>(a.index)[e];
-        const bool there = i >= 0 && i < a.V;
-        const float v = a.teacher_bf16 ? to_float<BF16>(static_cast<const unsigned short*>(a.teacher)[e])
-                                       : static_cast<const float*>(a.teacher)[e];
-        place[k] = there ? static_cast<int>(i) : -1;
-        p[k] = there ? v : -inf;
-        if (there) t = join(t, top_of(v, a.c));
+    // asked for first: the entries (places outside the vocabulary, or negative ones, are none), the row's scalars, loose elements
+    int64_t own_index[kDistillOwn];
+    float own_value[kDistillOwn], own_z[kDistillOwn];
+#pragma unroll
+    for (int o = 0; o < kDistillOwn; ++o) {
+        const int k = tid + o * THREADS;
+        own_index[o] = -1;
+        own_value[o] = -inf;
+        if (k < a.K) {
+            const int64_t e = row * a.K + k;
+            own_index[o] = a.index64 ? static_cast<const long long*>(a.index)[e] : static_cast<const int*>(a.index)[e];
+            own_value[o] = a.teacher_bf16 ? to_float<BF16>(static_cast<const unsigned short*>(a.teacher)[e])
+                                          : static_cast<const float*>(a.teacher)[e];
+        }
     }
-    auto block_join = [&](TopSum v) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const TopSum w{__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o)};
-            v = join(v, w);
-        }
-        __syncthreads();
-        if (lane == 0) fold[warp] = v;
-        __syncthreads();
-        v = lane < kWarpsHere ? fold[lane] : TopSum{-inf, 0.f};
-#pragma unroll
-        for (int o = kWarpsHere / 2; o > 0; o >>= 1) {
-            const TopSum w{__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o)};
-            v = join(v, w);
-        }
-        return TopSum{__shfl_sync(0xffffffffu, v.m, 0), __shfl_sync(0xffffffffu, v.s, 0)};
-    };
-    const TopSum teacher = block_join(t);
-    const bool any = teacher.s != 0.f;            // false: no entry, or all at -inf
-
-    // head: elements before the row's first 16-byte boundary; then whole vectors; then the tail
+    float g = 0.f, lse = 0.f;
+    if constexpr (kGrad) g = a.dloss[row] * a.tau;
+    if constexpr (!kLoss) lse = a.lse_in[row];
     const int head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(S)));
     const int vectors = (a.V - head) / V, tail = head + vectors * V;
-    const S* body = z + head;
+    const int begin = min(vectors, part * a.per), end = min(vectors, begin + a.per);
+    // elements outside whole vectors: those before them belong to the first part, those after them to the last
+    const int loose = part == 0 && tid < head ? tid : part == a.parts - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
+    const float loose_z = loose >= 0 ? to_float<T>(z[loose]) : -inf;
+    const uint4* body = reinterpret_cast<const uint4*>(z + head);
+    uint4 x[kDistillDepth];
+    auto fetch = [&](int v0) {
+#pragma unroll
+        for (int i = 0; i < kDistillDepth; ++i)
+            if (v0 + i * THREADS < end) x[i] = body[v0 + i * THREADS];
+    };
+    fetch(begin + tid);
+    TopSum teacher{-inf, 0.f}, st{-inf, 0.f};
+#pragma unroll
+    for (int o = 0; o < kDistillOwn; ++o) {
+        const int k = tid + o * THREADS;
+        if (own_index[o] < 0 || own_index[o] >= a.V) {
+            own_index[o] = -1;
+            own_value[o] = -inf;
+        } else {
+            teacher = join(teacher, top_of(own_value[o], a.c));
+        }
+        own_z[o] = own_index[o] >= 0 ? to_float<T>(z[own_index[o]]) : 0.f;
+        if (k < (a.K + 3) / 4 * 4) place[k] = static_cast<int>(own_index[o]);
+    }
 
-    TopSum st{-inf, 0.f};
     if constexpr (kLoss) {
-        auto take = [&](float v) { st = join(st, top_of(v, a.c)); };
-        if (tid < head) take(to_float<T>(z[tid]));
-        if (tid < a.V - tail) take(to_float<T>(z[tail + tid]));
-        for (int v = tid; v < vectors; v += kDistillThreads) {
-            Vec<T, V> x;
-            float f[V];
-            x.load(body + static_cast<int64_t>(v) * V);
-            x.unpack(f);
-            float m = f[0];
+        if (loose >= 0) st = top_of(loose_z, a.c);
+        for (int v0 = begin + tid; v0 < end; v0 += THREADS * kDistillDepth) {
+            if (v0 != begin + tid) fetch(v0);
+            TopOf<T> top;
 #pragma unroll
-            for (int j = 1; j < V; ++j) m = fmaxf(m, f[j]);
-            m = fmaxf(m * a.c, st.m);
+            for (int i = 0; i < kDistillDepth; ++i)
+                if (v0 + i * THREADS < end) top.add(x[i]);
+            const float m = fmaxf(top.get() * a.c, st.m);
             const float ref = m == -inf ? 0.f : m;
-            float s = st.s * exp2_fast(st.m - ref);
+            pair_t sum = make_pair(st.s * exp2_fast(st.m - ref), 0.f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) s += exp2_fast(fmaf(f[j], a.c, -ref));
-            st = TopSum{m, s};
+            for (int i = 0; i < kDistillDepth; ++i)
+                if (v0 + i * THREADS < end) add_exps<T>(x[i], twice(a.c), twice(-ref), sum);
+            st = TopSum{m, both(sum)};
         }
-        st = block_join(st);
     }
-    // q_v = 2^(z_v c - shift) scale
-    float shift, scale;
+    // one exchange for both: every warp joins all warps' pairs, in the same order
+    warp_join(teacher, st);
+    if (lane == 0) {
+        fold[0][warp] = teacher;
+        fold[1][warp] = st;
+    }
+    __syncthreads();
+    teacher = lane < kWarps ? fold[0][lane] : TopSum{-inf, 0.f};
+    st = lane < kWarps ? fold[1][lane] : TopSum{-inf, 0.f};
+    warp_join(teacher, st);
     if constexpr (kLoss) {
-        shift = st.m == -inf ? 0.f : st.m;
-        scale = 1.f / st.s;
-        if (tid == 0 && a.lse) a.lse[row] = (st.m + log2f(st.s)) * kLn2;
-    } else {
-        // lse tau c = shift + rest, with the same c as in z c, so that only z - lse tau feels its rounding; rest goes
-        // into the factor
-        const double exponent = static_cast<double>(a.lse_in[row]) * a.tau * a.c;
-        shift = static_cast<float>(exponent);
-        scale = exp2_fast(static_cast<float>(shift - exponent));
-    }
-    // p_k, and the loss
-    float loss = 0.f, between = 0.f;               // between: log-sum of the student minus the teacher's
-    if constexpr (kLoss) between = ((st.m - teacher.m) + (log2f(st.s) - log2f(teacher.s))) * kLn2;
-    for (int k = tid; k < a.K; k += kDistillThreads) {
-        float pk = 0.f;
-        if (place[k] >= 0 && any) {
-            const float v = p[k];
-            pk = v == -inf ? 0.f : exp2_fast(fmaf(v, a.c, -teacher.m)) / teacher.s;
-            if constexpr (kLoss) {
-                if (pk != 0.f) loss = fmaf(pk, (v - to_float<T>(z[place[k]])) / a.tau + between, loss);
+        if (a.parts > 1) {      // every block of the cluster gets every block's pair, and joins them in the same order
+            if (tid < a.parts) {
+                unsigned to;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_address(&of_part[part])), "r"(tid));
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(st.m), "f"(st.s) : "memory");
             }
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            st = of_part[0];
+            for (int q = 1; q < a.parts; ++q) st = join(st, of_part[q]);
         }
-        p[k] = pk;
+        if (tid == 0 && part == 0 && a.lse) a.lse[row] = (st.m + log2f(st.s)) * kLn2;
+    } else {
+        st = student_of(a, lse);
+    }
+    const bool any = teacher.s != 0.f;             // false: no entry, or all at -inf
+
+    // p_k, and the loss: log-sum of the student minus the teacher's, plus the difference of the logits
+    float loss = 0.f;
+    const float between = kLoss ? ((st.m - teacher.m) + (log2f(st.s) - log2f(teacher.s))) * kLn2 : 0.f;
+#pragma unroll
+    for (int o = 0; o < kDistillOwn; ++o) {
+        const int k = tid + o * THREADS;
+        const float v = own_value[o];
+        const float pk = any && v != -inf ? exp2_fast(fmaf(v, a.c, -teacher.m)) / teacher.s : 0.f;
+        if (kLoss && pk != 0.f) loss = fmaf(pk, (v - own_z[o]) / a.tau + between, loss);
+        if (k < (a.K + 3) / 4 * 4) p[k] = pk;
     }
     if constexpr (kLoss) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-        if (lane == 0) fold2[warp] = loss;
-        __syncthreads();
-        if (tid == 0) {
-            float sum = 0.f;
-            for (int w = 0; w < kWarpsHere; ++w) sum += fold2[w];
-            a.loss[row] = a.tau * a.tau * sum;
+        if (lane == 0) sums[warp] = loss;
+    }
+    if constexpr (kGrad) {
+        // q_v g = 2^(z_v c - shift) factor
+        const float shift = st.m == -inf ? 0.f : st.m, factor = g / st.s;
+        S* dz = static_cast<S*>(a.dz) + row * a.dz_stride;
+        if (loose >= 0) dz[loose] = from_float<T>(any ? exp2_fast(fmaf(loose_z, a.c, -shift)) * factor : 0.f);
+        auto write = [&](auto aligned) {
+            for (int v0 = begin + tid; v0 < end; v0 += THREADS * kDistillDepth) {
+                if (kLoss || v0 != begin + tid) fetch(v0);
+                S* to = dz + head + static_cast<int64_t>(v0) * V;
+#pragma unroll
+                for (int i = 0; i < kDistillDepth; ++i)
+                    if (v0 + i * THREADS < end)
+                        write_exps<T, aligned.value>(to + i * THREADS * V, x[i], twice(a.c), twice(-shift), twice(factor));
+            }
+        };
+        if (!any)
+            for (int v = begin * V + tid; v < end * V; v += THREADS) dz[head + v] = from_float<T>(0.f);
+        else if (((reinterpret_cast<uintptr_t>(dz) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0)
+            write(std::true_type{});
+        else
+            write(std::false_type{});
+        __syncthreads();     // the places of the entries in this part have their q: now q minus the teacher's share, the sum
+                             // over all entries there in the list's order, the same for every repetition of a place
+        const int first = part == 0 ? 0 : head + begin * V, last = part == a.parts - 1 ? a.V : head + end * V;
+#pragma unroll
+        for (int o = 0; o < kDistillOwn; ++o) {
+            const int i = static_cast<int>(own_index[o]);
+            if (i < first || i >= last || !any) continue;
+            float share = 0.f;
+            for (int j = 0; j < a.K; j += 4) {
+                const int4 at = *reinterpret_cast<const int4*>(place + j);
+                const float4 pj = *reinterpret_cast<const float4*>(p + j);
+                share += at.x == i ? pj.x : 0.f;
+                share += at.y == i ? pj.y : 0.f;
+                share += at.z == i ? pj.z : 0.f;
+                share += at.w == i ? pj.w : 0.f;
+            }
+            dz[i] = from_float<T>(exp2_fast(fmaf(own_z[o], a.c, -shift)) * factor - g * share);
         }
     } else {
         __syncthreads();
     }
-    if constexpr (kGrad) {
-        S* dz = static_cast<S*>(a.dz) + row * a.dz_stride;
-        const float g = a.dloss[row] * a.tau;
-        const float factor = any ? g * scale : 0.f;
-        auto q = [&](float v) { return any ? exp2_fast(fmaf(v, a.c, -shift)) * factor : 0.f; };
-        if (tid < head) dz[tid] = from_float<T>(q(to_float<T>(z[tid])));
-        if (tid < a.V - tail) dz[tail + tid] = from_float<T>(q(to_float<T>(z[tail + tid])));
-        const bool same_phase = ((reinterpret_cast<uintptr_t>(dz) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
-        for (int v = tid; v < vectors; v += kDistillThreads) {
-            Vec<T, V> x;
-            float f[V];
-            x.load(body + static_cast<int64_t>(v) * V);
-            x.unpack(f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) f[j] = q(f[j]);
-            S* to = dz + head + static_cast<int64_t>(v) * V;
-            if (same_phase) {
-                x.pack(f);
-                x.store(to);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) to[j] = from_float<T>(f[j]);
-            }
-        }
-        __syncthreads();   // the entries' places have their q: now q minus the teacher's share (every repetition of a
-                           // place writes the same value, the sum over all of them in the list's order)
-        for (int k = tid; k < a.K; k += kDistillThreads) {
-            const int i = place[k];
-            if (i < 0 || !any) continue;
-            float share = 0.f;
-            for (int j = 0; j < a.K; ++j)
-                if (place[j] == i) share += p[j];
-            dz[i] = from_float<T>(q(to_float<T>(z[i])) - g * share);
-        }
+    if (kLoss && tid == 0 && part == 0) {
+        float sum = 0.f;
+        for (int w = 0; w < kWarps; ++w) sum += sums[w];
+        a.loss[row] = a.tau * a.tau * sum;
     }
 }
 

@@ -28,7 +28,7 @@
 #include <cuda.h>
 
 #include "bns.h"
-#include "bns_elements.cuh"
+#include "bns_async.cuh"
 
 namespace bns {
 
@@ -46,22 +46,11 @@ struct HeadRing {
     static constexpr unsigned kSmem = kStages * kStage + 1024;
 };
 constexpr int kHeadRaster = 16;        // row tiles that are swept together, so that their operand stays in L2
-constexpr unsigned kHeadPolls = 1u << 22;
 constexpr float kHeadLog2e = 1.4426950408889634f, kHeadLn2 = 0.6931471805599453f;
-
-// Bounded waits that ran out since the library was loaded.
-__device__ unsigned g_head_timeouts;
 
 // ------------------------------------------------------------------------------------ PTX wrappers
 namespace head {
 
-__device__ __forceinline__ unsigned smem(const void* p) { return static_cast<unsigned>(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ void barrier_init(unsigned bar, unsigned arrivals) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(arrivals) : "memory");
-}
-__device__ __forceinline__ void barrier_expect(unsigned bar, unsigned bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 // The same shared-memory place in the pair's first CTA.
 template <int CTAS>
 __device__ __forceinline__ unsigned in_first(unsigned address) {
@@ -76,27 +65,6 @@ __device__ __forceinline__ void arrive_in_first(unsigned bar) {
         asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
     else
         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first<CTAS>(bar)) : "memory");
-}
-__device__ __forceinline__ bool barrier_try(unsigned bar, unsigned parity) {
-    unsigned done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return done != 0;
-}
-// False once this wait, or another one of the block, has run out.
-__device__ __forceinline__ bool wait(unsigned bar, unsigned parity, volatile int* gave_up) {
-    for (unsigned i = 0; i < kHeadPolls; ++i) {
-        if (barrier_try(bar, parity)) return true;
-        if ((i & 255) == 255 && *gave_up) return false;
-    }
-    *gave_up = 1;
-    atomicAdd(&g_head_timeouts, 1u);
-    return false;
 }
 // `bar` lies in the pair's first CTA, the data goes to this one.
 template <int CTAS>
@@ -197,12 +165,6 @@ __device__ __forceinline__ void load16(unsigned address, float (&f)[16]) {
         : "r"(address)
         : "memory");
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
 // Shared-memory matrix descriptor, 128-byte swizzle.  K contiguous: rows of 128 bytes, groups of eight rows 1024
 // bytes apart.  Other dimension contiguous: 64 elements of it by eight of K are 1024 bytes, the next eight of K
 // follow, the next 64 elements are one TMA box (64 x 64, 8192 bytes) away.
@@ -309,7 +271,7 @@ struct HeadEpilogue {
             // lse log2(e) = shift + rest, log2(e) being the same fp32 number as in z log2(e), so that only the
             // difference z - lse feels its rounding; rest goes into the factor
             shift = lse * kHeadLog2e;
-            factor = one * head::exp2_fast(-fmaf(lse, kHeadLog2e, -shift));
+            factor = one * exp2_fast(-fmaf(lse, kHeadLog2e, -shift));
         } else {
             factor = g.unit ? *g.unit : 1.f;
         }
@@ -332,9 +294,9 @@ struct HeadEpilogue {
             for (int j = 1; j < 32; ++j) top = fmaxf(top, f[j]);
             top = fmaxf(top * kHeadLog2e, m);
             const float ref = top == -inf ? 0.f : top;
-            s *= head::exp2_fast(m - ref);
+            s *= exp2_fast(m - ref);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) s += head::exp2_fast(fmaf(f[j], kHeadLog2e, -ref));
+            for (int j = 0; j < 32; ++j) s += exp2_fast(fmaf(f[j], kHeadLog2e, -ref));
             m = top;
             if (mine >= c && mine < c + 32) {
 #pragma unroll
@@ -345,7 +307,7 @@ struct HeadEpilogue {
             if (!in) return;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                f[j] = counts && c + j < columns ? head::exp2_fast(fmaf(f[j], kHeadLog2e, -shift)) * factor : 0.f;
+                f[j] = counts && c + j < columns ? exp2_fast(fmaf(f[j], kHeadLog2e, -shift)) * factor : 0.f;
                 if (mine == c + j) f[j] -= one;
             }
             unsigned short* to = g.G + row * g.G_stride + column0 + c;
@@ -422,26 +384,26 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CTAS == 1 ? 0 : static_cast<int>(blockIdx.x & 1);      // in the pair
     const int worker = blockIdx.x / CTAS, workers = gridDim.x / CTAS;
-    const unsigned ring = (head::smem(raw) + 1023) & ~1023u;
-    const unsigned full = head::smem(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16,
+    const unsigned ring = (smem_address(raw) + 1023) & ~1023u;
+    const unsigned full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16,
                    flush = drained + 16;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            head::barrier_init(full + 8 * s, 1);
-            head::barrier_init(empty + 8 * s, 1);
+            barrier_init(full + 8 * s, 1);
+            barrier_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
-            head::barrier_init(ready + 8 * b, 1);
-            head::barrier_init(drained + 8 * b, 8 * CTAS);
+            barrier_init(ready + 8 * b, 1);
+            barrier_init(drained + 8 * b, 8 * CTAS);
         }
-        head::barrier_init(flush, 1);
+        barrier_init(flush, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         gave_up = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
     }
-    if (warp == 2) head::tensor_memory_alloc<CTAS>(head::smem(&tmem_base));
+    if (warp == 2) head::tensor_memory_alloc<CTAS>(smem_address(&tmem_base));
     head::fence_before();
     __syncthreads();
     if constexpr (CTAS == 2) head::sync_all<CTAS>();      // the other CTA's barriers exist
@@ -461,9 +423,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 const int row = (t.m * CTAS + rank) * kHeadM, column = t.n * kHeadN + rank * Ring::kColumns;
                 for (int k = t.k0; k < t.k1; ++k, ++it) {
                     const int s = it % kStages;
-                    if (it >= kStages && !(ok = head::wait(empty + 8 * s, (it / kStages - 1) & 1, &gave_up))) break;
+                    if (it >= kStages && !(ok = wait_bounded(empty + 8 * s, (it / kStages - 1) & 1, &gave_up))) break;
                     const unsigned bar = head::in_first<CTAS>(full + 8 * s), sa = ring + s * Ring::kStage, sb = sa + kHeadStageA;
-                    if (rank == 0) head::barrier_expect(full + 8 * s, CTAS * Ring::kStage);
+                    if (rank == 0) barrier_expect(full + 8 * s, CTAS * Ring::kStage);
                     int ta, tb;
                     const int pair = k / g.k_blocks, kk = (k - pair * g.k_blocks) * kHeadK;
                     head_pair(pair, g.pairs, ta, tb);
@@ -485,7 +447,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             }
             // the products have read every stage: nothing arrives here any more once the block ends
             for (int i = max(0, it - kStages); ok && i < it; ++i)
-                ok = head::wait(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up);
+                ok = wait_bounded(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up);
             issued = it;
         } else if (warp == 1 && lane == 0 && rank == 0) {
             constexpr unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_K ? 0u : 1u << 15) | (B_K ? 0u : 1u << 16) |
@@ -497,12 +459,12 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 const int step = kSegments ? kHeadSegment : t.k1 - t.k0;
                 for (int k = t.k0; ok && k < t.k1; k += step, ++n) {
                     const int buffer = n & 1, end = min(t.k1, k + step);
-                    if (n >= 2 && !(ok = head::wait(drained + 8 * buffer, (n / 2 - 1) & 1, &gave_up))) break;
+                    if (n >= 2 && !(ok = wait_bounded(drained + 8 * buffer, (n / 2 - 1) & 1, &gave_up))) break;
                     head::fence_after();
                     const unsigned d = tmem + buffer * kHeadN;
                     for (int kk = k; kk < end; ++kk, ++it) {
                         const int s = it % kStages;
-                        if (!(ok = head::wait(full + 8 * s, (it / kStages) & 1, &gave_up))) break;
+                        if (!(ok = wait_bounded(full + 8 * s, (it / kStages) & 1, &gave_up))) break;
                         head::fence_after();
                         const unsigned sa = ring + s * Ring::kStage;
                         const uint64_t da = head::descriptor<A_K>(sa), db = head::descriptor<B_K>(sa + kHeadStageA);
@@ -528,7 +490,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half);
             const unsigned lanes = tmem + (static_cast<unsigned>(slot * 32) << 16) + half * (kHeadN / 2);
             auto wait_ready = [&]() {
-                ok = __all_sync(0xffffffffu, head::wait(ready + 8 * (n & 1), (n / 2) & 1, &gave_up));
+                ok = __all_sync(0xffffffffu, wait_bounded(ready + 8 * (n & 1), (n / 2) & 1, &gave_up));
                 head::fence_after();
                 return ok;
             };
@@ -577,11 +539,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         // a block that gave up leaves only when its copies have landed and its products have ended
         if (threadIdx.x == 0 && rank == 0)
             for (int i = max(0, issued - kStages); i < issued; ++i)
-                for (unsigned n = 0; n < kHeadPolls && !head::barrier_try(full + 8 * (i % kStages), (i / kStages) & 1); ++n) {
+                for (unsigned n = 0; n < kPolls && !barrier_try(full + 8 * (i % kStages), (i / kStages) & 1); ++n) {
                 }
         if (threadIdx.x == 32 && rank == 0) {
             head::commit<CTAS>(flush);
-            for (unsigned n = 0; n < kHeadPolls && !head::barrier_try(flush, 0); ++n) {
+            for (unsigned n = 0; n < kPolls && !barrier_try(flush, 0); ++n) {
             }
         }
         __syncthreads();
@@ -651,7 +613,7 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float2* partial, i
     const int row = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
     auto join = [&](float2 a, float2 b) {
         const float m = fmaxf(a.x, b.x), ref = m == -inf ? 0.f : m;
-        return make_float2(m, a.y * head::exp2_fast(a.x - ref) + b.y * head::exp2_fast(b.x - ref));
+        return make_float2(m, a.y * exp2_fast(a.x - ref) + b.y * exp2_fast(b.x - ref));
     };
     float2 v = make_float2(-inf, 0.f);
     if (row < rows)

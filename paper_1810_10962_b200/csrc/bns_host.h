@@ -35,7 +35,7 @@ extern bool g_pdl;
 // Most columns of the vocabulary that the head's gradient holds at a time; 0 = as many as its memory aim allows.
 extern int g_head_piece;
 
-// Adds the bounded waits that ran out in the head kernels on the current device (synchronises the stream).
-bns_status head_wait_timeouts(uint32_t* count, cudaStream_t stream);
+// Adds the bounded waits that ran out in the language-model kernels on the current device (synchronises the stream).
+bns_status lm_wait_timeouts(uint32_t* count, cudaStream_t stream);
 
 }  // namespace bns

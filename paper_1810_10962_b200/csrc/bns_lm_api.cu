@@ -366,8 +366,26 @@ bns_status distill(const bns_distillation* sh, Distill a, cudaStream_t stream) {
     a.teacher_bf16 = sh->teacher_dtype == BNS_BF16;
     a.tau = sh->temperature;
     a.c = static_cast<float>(1.4426950408889634 / static_cast<double>(sh->temperature));
-    BNS_LM_BY_TYPE(sh->dtype, (launch(BNS_KERNEL_DISTILL, distill_kernel<T, WHAT>,
-                                      Shape{static_cast<unsigned>(sh->rows), kDistillThreads}, 0, stream, a)));
+    constexpr bool backward = __is_same(WHAT, DistillBackward);
+    const int vectors = std::max(1, a.V / (16 / static_cast<int>(eb)));
+    const int64_t rows = sh->rows;
+    // short rows take small blocks (8192 x 1000 bf16: 38 us against 100)
+    const bool small = vectors <= kDistillSmall * 8 && a.K <= kDistillSmall * kDistillOwn && rows > 2 * sm_count();
+    // A row that is read twice should still be in L2 the second time: long ones go over two blocks, so that half as many
+    // are in flight (131072 bf16 values: 456 -> 416 us per 4096 rows; 50257, 100 KB: 184 us with one, 246 with two).
+    const size_t row_bytes = static_cast<size_t>(a.V) * eb;
+    a.parts = __is_same(WHAT, DistillStep) && row_bytes > (size_t{192} << 10) ? 2 : 1;
+    // few rows are spread over the SMs
+    while (a.parts < kDistillParts && rows * (a.parts + 1) <= 2 * sm_count() && vectors > a.parts * kDistillThreads) ++a.parts;
+    a.per = divide_up(vectors, a.parts);
+    if (rows * a.parts >= int64_t{1} << 31) return BNS_ERR_SHAPE;
+    const unsigned parts = static_cast<unsigned>(a.parts), grid = static_cast<unsigned>(rows) * parts, cluster = backward ? 1 : parts;
+    BNS_LM_BY_TYPE(sh->dtype, {
+        if (small)
+            launch(BNS_KERNEL_DISTILL, distill_kernel<T, WHAT, kDistillSmall>, Shape{grid, kDistillSmall, cluster}, 0, stream, a);
+        else
+            launch(BNS_KERNEL_DISTILL, distill_kernel<T, WHAT, kDistillThreads>, Shape{grid, kDistillThreads, cluster}, 0, stream, a);
+    });
     return last_error();
 }
 
@@ -377,8 +395,8 @@ namespace bns {
 
 int g_head_piece = 0;
 
-bns_status head_wait_timeouts(uint32_t* count, cudaStream_t stream) {
-    if (cudaMemcpyFromSymbolAsync(count, g_head_timeouts, sizeof(uint32_t), 0, cudaMemcpyDeviceToHost, stream) != cudaSuccess)
+bns_status lm_wait_timeouts(uint32_t* count, cudaStream_t stream) {
+    if (cudaMemcpyFromSymbolAsync(count, g_lm_timeouts, sizeof(uint32_t), 0, cudaMemcpyDeviceToHost, stream) != cudaSuccess)
         return BNS_ERR_CUDA;
     return cudaStreamSynchronize(stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
 }
@@ -445,7 +463,7 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
         else
             launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_wide_kernel<T, V>, grid, 0, stream, a);
     });
-    launch(BNS_KERNEL_RMS_BACKWARD, rms_dweight_kernel, Shape{static_cast<unsigned>(divide_up(shape->columns, 32)), 256}, 0, stream,
+    launch(BNS_KERNEL_RMS_BACKWARD, rms_dweight_kernel, Shape{static_cast<unsigned>(divide_up(shape->columns, 32)), 1024}, 0, stream,
            partial, static_cast<int>(pl.grid), shape->columns, dweight);
     return last_error();
 }

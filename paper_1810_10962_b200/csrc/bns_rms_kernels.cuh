@@ -30,9 +30,58 @@ struct BlockExchange {
     float top[2][32];
 };
 
-// |a| and |b| joined by the larger, NaN winning: on the bits of non-negative floats NaN lies above infinity.
+// The larger magnitude, NaN winning.
 __device__ __forceinline__ float max_or_nan(float a, float b) {
-    return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+
+// Elementwise arithmetic on a thread's vector, two elements an instruction where it has them.
+template <int V>
+__device__ __forceinline__ void add_to(float (&a)[V], const float (&b)[V]) {
+    if constexpr (V == 1) {
+        a[0] += b[0];
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) split_pair(add2(make_pair(a[j], a[j + 1]), make_pair(b[j], b[j + 1])), a[j], a[j + 1]);
+    }
+}
+template <int V>
+__device__ __forceinline__ void multiply_by(float (&a)[V], const float (&b)[V]) {
+    if constexpr (V == 1) {
+        a[0] *= b[0];
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) split_pair(mul2(make_pair(a[j], a[j + 1]), make_pair(b[j], b[j + 1])), a[j], a[j + 1]);
+    }
+}
+template <int V>
+__device__ __forceinline__ void multiply_by(float (&a)[V], float b) {
+    if constexpr (V == 1) {
+        a[0] *= b;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) split_pair(mul2(make_pair(a[j], a[j + 1]), make_pair(b, b)), a[j], a[j + 1]);
+    }
+}
+// acc += a b: two partial sums where V allows it
+template <int V>
+__device__ __forceinline__ void add_products(float (&acc)[2], const float (&a)[V], const float (&b)[V]) {
+    if constexpr (V == 1) {
+        acc[0] = fmaf(a[0], b[0], acc[0]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; j += 2)
+            split_pair(fma2(make_pair(a[j], a[j + 1]), make_pair(b[j], b[j + 1]), make_pair(acc[0], acc[1])), acc[0], acc[1]);
+    }
+}
+template <int V>
+__device__ __forceinline__ float top_of_vector(const float (&a)[V]) {
+    float m = fabsf(a[0]);
+#pragma unroll
+    for (int j = 1; j < V; ++j) m = max_or_nan(m, a[j]);
+    return m;
 }
 
 template <bool TOP>
@@ -82,14 +131,21 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&f)[V]) {
 // y / scale = s w 448 / max|s w|: the 8-bit values carry no rounding of rstd or of the scale.  A group of zeros has
 // scale 1; infinities and NaN give NaN, as the formula does.  `lift` keeps 448 / max finite for groups below 2^-100.
 struct Quant {
-    float scale, lift, factor;
+    float a, lift, factor;
     __device__ __forceinline__ Quant(float top, float rstd) {
-        const float a = top * rstd, inf = __int_as_float(0x7f800000);
-        scale = a == 0.f ? 1.f : a / 448.f;
+        const float inf = __int_as_float(0x7f800000);
+        a = top * rstd;
         lift = top < 0x1p-100f ? 0x1p100f : 1.f;
-        factor = a == 0.f ? 0.f : top < inf && a < inf ? 448.f / (top * lift) : __int_as_float(0x7fffffff);
+        float inverse;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(top * lift));   // 1 ulp
+        factor = a == 0.f ? 0.f : top < inf && a < inf ? 448.f * inverse : __int_as_float(0x7fffffff);
     }
-    __device__ __forceinline__ float operator()(float sw) const { return sw * lift * factor; }
+    __device__ __forceinline__ float scale() const { return a == 0.f ? 1.f : a / 448.f; }
+    template <int V>
+    __device__ __forceinline__ void apply(float (&sw)[V]) const {
+        if (lift != 1.f) multiply_by<V>(sw, lift);
+        multiply_by<V>(sw, factor);
+    }
 };
 
 struct RmsForward {
@@ -162,15 +218,14 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
     int turn = 0;
     if (blockIdx.x < a.rows) fetch(blockIdx.x);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        float s[NV][V], sum = 0.f, top = 0.f;
+        float s[NV][V], squares[2] = {0.f, 0.f}, top = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             vx.v[i].unpack(s[i]);
             if (a.residual) {
                 float f[V];
                 vr.v[i].unpack(f);
-#pragma unroll
-                for (int j = 0; j < V; ++j) s[i][j] += f[j];
+                add_to<V>(s[i], f);
             }
         }
         if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
@@ -186,20 +241,19 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
                 if constexpr (kRow) {
                     float w[V];
                     load_weights<V>(a.weight, v, aligned, w);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) top = max_or_nan(top, fabsf(s[i][j] * w[j]));
+                    multiply_by<V>(w, s[i]);
+                    top = max_or_nan(top, top_of_vector<V>(w));
                 }
-#pragma unroll
-                for (int j = 0; j < V; ++j) sum = fmaf(s[i][j], s[i][j], sum);
+                add_products<V>(squares, s[i], s[i]);
             }
         }
+        float sum = squares[0] + squares[1];
         // s w of vector i, zeros past the row's end
         auto product = [&](int i, float (&p)[V]) {
             const int v = threadIdx.x + i * B;
             if (v < vectors) {
                 load_weights<V>(a.weight, v, aligned, p);
-#pragma unroll
-                for (int j = 0; j < V; ++j) p[j] *= s[i][j];
+                multiply_by<V>(p, s[i]);
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j) p[j] = 0.f;
@@ -210,10 +264,9 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
             __syncthreads();   // the previous row's readers are done
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                float m = 0.f, p[V];
+                float p[V];
                 product(i, p);
-#pragma unroll
-                for (int j = 0; j < V; ++j) m = max_or_nan(m, fabsf(p[j]));
+                float m = top_of_vector<V>(p);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
                 if ((threadIdx.x & 31) == 0) segment[(threadIdx.x + i * B) >> 5] = m;
@@ -230,8 +283,8 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
                 if (v >= vectors) continue;
                 float f[V];
                 load_weights<V>(a.weight, v, aligned, f);
-#pragma unroll
-                for (int j = 0; j < V; ++j) f[j] *= s[i][j] * rstd;
+                multiply_by<V>(s[i], rstd);
+                multiply_by<V>(f, s[i]);
                 Vec<T, V> o;
                 o.pack(f);
                 o.store(static_cast<S*>(a.y) + row * a.D + static_cast<int64_t>(v) * V);
@@ -239,20 +292,18 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
         } else {
             const int groups = (a.D + kRmsGroup - 1) / kRmsGroup;
             const Quant of_row(top, rstd);
-            if (kRow && threadIdx.x == 0) a.scales[row] = of_row.scale;
+            if (kRow && threadIdx.x == 0) a.scales[row] = of_row.scale();
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int v = threadIdx.x + i * B;
                 float p[V];
                 product(i, p);
                 if constexpr (kRow) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) p[j] = of_row(p[j]);
+                    of_row.template apply<V>(p);
                 } else {
                     float m = 0.f;
                     if constexpr (V >= 4) {
-#pragma unroll
-                        for (int j = 0; j < V; ++j) m = max_or_nan(m, fabsf(p[j]));
+                        m = top_of_vector<V>(p);
 #pragma unroll
                         for (int o = kRmsGroup / V / 2; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
                     } else {
@@ -263,9 +314,8 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
                             if (first + q < (vectors + 31) >> 5) m = max_or_nan(m, segment[first + q]);
                     }
                     const Quant quant(m, rstd);
-                    if (v < vectors && v % (kRmsGroup / V) == 0) a.scales[row * groups + v / (kRmsGroup / V)] = quant.scale;
-#pragma unroll
-                    for (int j = 0; j < V; ++j) p[j] = quant(p[j]);
+                    if (v < vectors && v % (kRmsGroup / V) == 0) a.scales[row * groups + v / (kRmsGroup / V)] = quant.scale();
+                    quant.template apply<V>(p);
                 }
                 if (v < vectors) store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, p);
             }
@@ -330,27 +380,29 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_wide_kernel(const 
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
                 const Quant quant(m, rstd);
-                if (lane == 0) a.scales[row * groups + g] = quant.scale;
+                if (lane == 0) a.scales[row * groups + g] = quant.scale();
+                quant.template apply<4>(p);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = g * kRmsGroup + j * 32 + lane;
                     if (i < a.D)
-                        static_cast<uint8_t*>(a.y)[row * a.D + i] = static_cast<uint8_t>(e4m3_pair(quant(p[j]), 0.f));
+                        static_cast<uint8_t*>(a.y)[row * a.D + i] = static_cast<uint8_t>(e4m3_pair(p[j], 0.f));
                 }
             }
         } else {
             const Quant quant(top, rstd);
             if constexpr (kRow) {
-                if (threadIdx.x == 0) a.scales[row] = quant.scale;
+                if (threadIdx.x == 0) a.scales[row] = quant.scale();
             }
             for (int v = threadIdx.x; v < vectors; v += B) {
                 float f[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     const float s = element(v * V + j), w = a.weight[v * V + j];
-                    f[j] = kRow ? quant(s * w) : s * rstd * w;
+                    f[j] = kRow ? s * w : s * rstd * w;
                 }
                 if constexpr (kRow) {
+                    quant.template apply<V>(f);
                     store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, f);
                 } else {
                     Vec<T, V> o;
@@ -398,7 +450,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const float rstd = next_rstd;
         if (a.dh) vd.load(static_cast<const S*>(a.dh) + row * a.dh_stride, vectors);
-        float sum = 0.f, none = 0.f, xhat[NV][V], wdy[NV][V];
+        float inner[2] = {0.f, 0.f}, xhat[NV][V], wdy[NV][V];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
@@ -407,15 +459,20 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
                 load_weights<V>(a.weight, v, aligned, w);
                 vy.v[i].unpack(wdy[i]);
                 vh.v[i].unpack(xhat[i]);
+                multiply_by<V>(xhat[i], rstd);
+                if constexpr (V == 1) {
+                    dw[i][0] = fmaf(wdy[i][0], xhat[i][0], dw[i][0]);
+                } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    xhat[i][j] *= rstd;
-                    dw[i][j] = fmaf(wdy[i][j], xhat[i][j], dw[i][j]);
-                    wdy[i][j] *= w[j];
-                    sum = fmaf(wdy[i][j], xhat[i][j], sum);
+                    for (int j = 0; j < V; j += 2)
+                        split_pair(fma2(make_pair(wdy[i][j], wdy[i][j + 1]), make_pair(xhat[i][j], xhat[i][j + 1]),
+                                        make_pair(dw[i][j], dw[i][j + 1])), dw[i][j], dw[i][j + 1]);
                 }
+                multiply_by<V>(wdy[i], w);
+                add_products<V>(inner, wdy[i], xhat[i]);
             }
         }
+        float sum = inner[0] + inner[1], none = 0.f;
         if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
         block_exchange<false>(sum, none, ex, turn);
         const float c = sum * a.inv_D;
@@ -423,17 +480,16 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
         for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
             if (v >= vectors) continue;
-            float f[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) f[j] = rstd * fmaf(-xhat[i][j], c, wdy[i][j]);
+            multiply_by<V>(xhat[i], -c);
+            add_to<V>(wdy[i], xhat[i]);
+            multiply_by<V>(wdy[i], rstd);
             if (a.dh) {
                 float fd[V];
                 vd.v[i].unpack(fd);
-#pragma unroll
-                for (int j = 0; j < V; ++j) f[j] += fd[j];
+                add_to<V>(wdy[i], fd);
             }
             Vec<T, V> o;
-            o.pack(f);
+            o.pack(wdy[i]);
             o.store(static_cast<S*>(a.dx) + row * a.D + static_cast<int64_t>(v) * V);
         }
     }
@@ -481,22 +537,23 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_wide_kernel(const
     }
 }
 
-// dweight: 32 columns a block, 8 threads a column over the blocks' sums, joined in a fixed order.
-__global__ void __launch_bounds__(256) rms_dweight_kernel(const float* partial, int blocks, int D, float* dweight) {
-    __shared__ float fold[8][33];
+// dweight: 32 columns a block, 32 threads a column over the blocks' sums, joined in a fixed order.
+__global__ void __launch_bounds__(1024) rms_dweight_kernel(const float* partial, int blocks, int D, float* dweight) {
+    __shared__ float fold[32][33];
     grid_dependency_wait();
     grid_dependency_launch();
-    const int column = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, column = blockIdx.x * 32 + lane;
     float sum = 0.f;
-    if (column < D)
-        for (int b = part; b < blocks; b += 8) sum += partial[static_cast<int64_t>(b) * D + column];
-    fold[part][threadIdx.x & 31] = sum;
-    __syncthreads();
-    if (part == 0 && column < D) {
-#pragma unroll
-        for (int q = 1; q < 8; ++q) sum += fold[q][threadIdx.x & 31];
-        dweight[column] = sum;
+    if (column < D) {
+#pragma unroll 8
+        for (int b = part; b < blocks; b += 32) sum += partial[static_cast<int64_t>(b) * D + column];
     }
+    fold[part][lane] = sum;
+    __syncthreads();
+    sum = fold[lane][part];     // now a warp has a column
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0 && blockIdx.x * 32 + part < D) dweight[blockIdx.x * 32 + part] = sum;
 }
 
 }  // namespace bns
