@@ -55,20 +55,33 @@ void launch(int kind, void (*kernel)(KArgs...), Shape shape, size_t smem, cudaSt
     note_launch(cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...));
 }
 
-// The widest vector (up to 16 bytes) that divides the row, the strides and the addresses.
+// How the rows of several tensors may be moved: in 16-byte vectors from the first column on, in such vectors from a column
+// that depends on the row's phase (the same for all tensors in every row), or element by element.
 struct VectorRule {
-    int V;
-    explicit VectorRule(int columns, int ebytes) : V(16 / ebytes) {
-        while (columns % V) V >>= 1;
-        eb = ebytes;
+    enum Kind { kAligned, kPhase, kElements } kind = kAligned;
+    VectorRule(int columns, int ebytes) : V(16 / ebytes), D(columns), eb(ebytes) {
+        if (columns % V) kind = kPhase;
     }
-    void tensor(const void* p, int64_t stride) {
-        if (!p) return;
-        while (stride % V || !aligned(p, static_cast<size_t>(V) * eb)) V >>= 1;
-    }
+    void tensor(const void* p, int64_t stride) { add(p, stride, eb); }
+    void bytes(const void* p) { add(p, D, 1); }    // the dense 8-bit output: V elements are V bytes
 
 private:
-    int eb;
+    int V, D, eb;
+    bool first = true;
+    uint64_t phase = 0, step = 0;
+    void add(const void* p, int64_t stride, int size) {
+        if (!p || kind == kElements) return;
+        const uint64_t here = reinterpret_cast<uintptr_t>(p) / size % V, next = static_cast<uint64_t>(stride) % V;
+        if (first) {
+            phase = here;
+            step = next;
+            first = false;
+        }
+        if (here != phase || next != step)
+            kind = kElements;
+        else if (here || next)
+            kind = kPhase;
+    }
 };
 
 // ------------------------------------------------------------------------------------ root-mean-square norm
@@ -80,48 +93,60 @@ bns_status check_rows(const bns_rows* sh) {
 }
 
 struct RmsPlan {
+    int V;
+    bool loose;      // rows at any phase
     unsigned threads;
     int elements;    // of a row that a thread holds: 8 or 16; 0 = the row does not fit the block's registers
     unsigned grid;
 };
 
 // Both kernels are compiled for 64 registers a thread, so 1024 threads an SM.  Eight elements a thread leave room for
-// the next row's loads of fp32 tensors and for the gradient's column sums; sixteen of bf16 fit the forward kernel
-// (8192 x 4096: 49 us against 52 with eight).  Few rows take more threads per row, as nothing else fills the SM.
-RmsPlan plan_rms(int rows, int columns, int V, bool eight) {
+// the next row's loads of fp32 tensors and for the gradient's column sums; sixteen of bf16 fit the forward kernel.
+// Few rows take more threads per row, as nothing else fills the SM.
+RmsPlan plan_rms(int rows, int columns, int dtype, VectorRule::Kind kind, bool eight) {
     RmsPlan pl;
-    const int vectors = columns / V;
-    for (pl.elements = eight || rows <= sm_count() ? 8 : 16; pl.elements <= 16; pl.elements *= 2) {
-        const int per_thread = std::min(std::max(1, pl.elements / V), 8);
-        const int threads = divide_up(divide_up(vectors, per_thread), 32) * 32;
+    const int full = 16 / elem_bytes(dtype);
+    pl.loose = kind == VectorRule::kPhase;
+    if (pl.loose && columns > kRmsMaxThreads * 8) kind = VectorRule::kElements;   // phases come with eight elements a thread
+    pl.loose = kind == VectorRule::kPhase;
+    pl.V = kind == VectorRule::kElements ? 1 : full;
+    const int vectors = divide_up(columns, pl.V);
+    for (pl.elements = eight || pl.V == 1 || pl.loose || rows <= sm_count() ? 8 : 16; pl.elements <= 16; pl.elements *= 2) {
+        const int threads = divide_up(divide_up(vectors, std::max(1, pl.elements / pl.V)), 32) * 32;
         pl.threads = static_cast<unsigned>(threads);
-        if (threads <= kRmsMaxThreads) break;
+        if (threads <= kRmsMaxThreads || pl.V == 1) break;
     }
-    if (pl.elements > 16) {
+    if (pl.threads > kRmsMaxThreads) {
         pl.elements = 0;
         pl.threads = kRmsMaxThreads;
     }
     const int blocks_per_sm = std::max(1, std::min(32, kRmsMaxThreads / static_cast<int>(pl.threads)));
-    pl.grid = static_cast<unsigned>(std::min<int64_t>(rows, static_cast<int64_t>(sm_count()) * blocks_per_sm));
+    int64_t grid = static_cast<int64_t>(sm_count()) * blocks_per_sm;
+    grid -= grid % full;             // a block meets one phase
+    pl.grid = static_cast<unsigned>(std::min<int64_t>(rows, grid));
     return pl;
 }
 
+// V is a vector's elements, or 1.
 #define BNS_LM_BY_TYPE_V(dtype, V_, CALL)                   \
     do {                                                    \
         if ((dtype) == BNS_F32) {                           \
             using T = F32;                                  \
-            switch (V_) {                                   \
-            case 4: { constexpr int V = 4; CALL; } break;   \
-            case 2: { constexpr int V = 2; CALL; } break;   \
-            default: { constexpr int V = 1; CALL; } break;  \
+            if ((V_) == 1) {                                \
+                constexpr int V = 1;                        \
+                CALL;                                       \
+            } else {                                        \
+                constexpr int V = 4;                        \
+                CALL;                                       \
             }                                               \
         } else {                                            \
             using T = BF16;                                 \
-            switch (V_) {                                   \
-            case 8: { constexpr int V = 8; CALL; } break;   \
-            case 4: { constexpr int V = 4; CALL; } break;   \
-            case 2: { constexpr int V = 2; CALL; } break;   \
-            default: { constexpr int V = 1; CALL; } break;  \
+            if ((V_) == 1) {                                \
+                constexpr int V = 1;                        \
+                CALL;                                       \
+            } else {                                        \
+                constexpr int V = 8;                        \
+                CALL;                                       \
             }                                               \
         }                                                   \
     } while (0)
@@ -148,25 +173,39 @@ bns_status rms_forward(const bns_rows* sh, const void* x, int64_t x_stride, cons
     if (!aligned(x, eb) || !aligned(residual, eb) || !aligned(h, eb) || !aligned(weight, 4) || !aligned(rstd, 4) ||
         !aligned(scales, 4) || !(quantized || aligned(y, eb)))
         return BNS_ERR_ALIGN;
+    constexpr bool grouped = __is_same(OUT, RmsGroupScale);
     VectorRule rule(sh->columns, static_cast<int>(eb));
     rule.tensor(x, x_stride);
     rule.tensor(residual, residual_stride);
     rule.tensor(h, sh->columns);
-    if (!quantized) rule.tensor(y, sh->columns);
-    while (quantized && !aligned(y, static_cast<size_t>(rule.V))) rule.V >>= 1;
-    const RmsPlan pl = plan_rms(sh->rows, sh->columns, rule.V, sh->dtype == BNS_F32);
+    if (quantized)
+        rule.bytes(y);
+    else
+        rule.tensor(y, sh->columns);
+    if (grouped && rule.kind == VectorRule::kPhase) rule.kind = VectorRule::kElements;   // groups begin at whole vectors
+    const RmsPlan pl = plan_rms(sh->rows, sh->columns, sh->dtype, rule.kind, sh->dtype == BNS_F32);
     const RmsForward a{x, residual, weight, y, scales, h, rstd, sh->rows, x_stride, residual_stride, sh->columns, eps,
                        1.f / static_cast<float>(sh->columns)};
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const Shape shape{pl.grid, pl.threads};
-    const size_t smem = __is_same(OUT, RmsGroupScale) && rule.V < 4 ? pl.threads / 32 * 8 * sizeof(float) : 0;
-    BNS_LM_BY_TYPE_V(sh->dtype, rule.V, {
-        if (pl.elements == 8)
-            launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, 8, OUT>, shape, smem, stream, a);
-        else if (pl.elements == 16)
-            launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, 16, OUT>, shape, smem, stream, a);
-        else
+    const size_t smem = grouped && pl.V == 1 ? pl.threads / 32 * 8 * sizeof(float) : 0;
+    BNS_LM_BY_TYPE_V(sh->dtype, pl.V, {
+        if (pl.elements == 0) {
             launch(BNS_KERNEL_RMS_FORWARD, rms_forward_wide_kernel<T, V, OUT>, shape, 0, stream, a);
+        } else if constexpr (V == 1) {
+            launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, 1, 8, false, OUT>, shape, smem, stream, a);
+        } else {
+            if constexpr (!grouped) {
+                if (pl.loose) {
+                    launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, 8, true, OUT>, shape, 0, stream, a);
+                    return last_error();
+                }
+            }
+            if (pl.elements == 8)
+                launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, 8, false, OUT>, shape, 0, stream, a);
+            else
+                launch(BNS_KERNEL_RMS_FORWARD, rms_forward_kernel<T, V, 16, false, OUT>, shape, 0, stream, a);
+        }
     });
     return last_error();
 }
@@ -450,18 +489,24 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
     rule.tensor(h, h_stride);
     rule.tensor(dh, dh_stride);
     rule.tensor(dx, shape->columns);
-    const RmsPlan pl = plan_rms(shape->rows, shape->columns, rule.V, true);
+    const RmsPlan pl = plan_rms(shape->rows, shape->columns, shape->dtype, rule.kind, true);
     float* partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kHeaderBytes);
     const RmsBackward a{dy, h, dh, weight, rstd, dx, partial, shape->rows, dy_stride, h_stride, dh_stride, shape->columns,
                         1.f / static_cast<float>(shape->columns)};
     const Shape grid{pl.grid, pl.threads};
-    BNS_LM_BY_TYPE_V(shape->dtype, rule.V, {
-        if (pl.elements == 8)
-            launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V, 8>, grid, 0, stream, a);
-        else if (pl.elements == 16)
-            launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V, 16>, grid, 0, stream, a);
-        else
-            launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_wide_kernel<T, V>, grid, 0, stream, a);
+    BNS_LM_BY_TYPE_V(shape->dtype, pl.V, {
+        if (pl.elements == 0) {
+            launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_wide_kernel<T>, grid, 0, stream, a);
+        } else if constexpr (V == 1) {
+            launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, 1, 8, false>, grid, 0, stream, a);
+        } else {
+            if (pl.loose)
+                launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V, 8, true>, grid, 0, stream, a);
+            else if (pl.elements == 8)
+                launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V, 8, false>, grid, 0, stream, a);
+            else
+                launch(BNS_KERNEL_RMS_BACKWARD, rms_backward_kernel<T, V, 16, false>, grid, 0, stream, a);
+        }
     });
     launch(BNS_KERNEL_RMS_BACKWARD, rms_dweight_kernel, Shape{static_cast<unsigned>(divide_up(shape->columns, 32)), 1024}, 0, stream,
            partial, static_cast<int>(pl.grid), shape->columns, dweight);

@@ -198,27 +198,71 @@ __device__ __forceinline__ void load_weights(const float* weight, int at, bool a
     for (int j = 0; j < V; ++j) w[j] = __ldg(weight + at * V + j);
 }
 
-template <typename T, int V, int EPT, typename OUT>
+// Rows whose stride is no multiple of a vector begin at any phase.  The blocks of a launch are a multiple of V then, so
+// that a block meets one phase only: the whole vectors of its rows begin at column `head`, its threads keep the same columns
+// in every row, and the up to 2 V - 2 columns outside whole vectors are the first threads' extra ones.
+template <typename S, int V, bool LOOSE>
+struct RowPhase {
+    int head = 0, vectors, extra = -1;   // extra: this thread's column outside whole vectors
+    __device__ __forceinline__ RowPhase(const void* first_row, int D) {
+        if constexpr (LOOSE) {
+            head = min(D, static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(first_row) & 15)) & 15) / sizeof(S)));
+            vectors = (D - head) / V;
+            const int t = threadIdx.x, tail = head + vectors * V;
+            extra = t < head ? t : t >= 16 && t < 32 && tail + t - 16 < D ? tail + t - 16 : -1;
+        } else {
+            vectors = D / V;
+        }
+    }
+};
+
+template <typename T, int V, int EPT, bool LOOSE, typename OUT>
 __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsForward a) {
     using S = typename T::storage;
     constexpr int NV = kRmsVectors<V, EPT>;
     constexpr bool kRow = __is_same(OUT, RmsRowScale), kGroup = __is_same(OUT, RmsGroupScale);
+    static_assert(!(LOOSE && kGroup), "groups of columns begin at whole vectors");
     __shared__ BlockExchange ex;
     extern __shared__ float segment[];    // grouped form with V < 4: largest |s w| of every 32 V columns
-    const int B = blockDim.x, vectors = a.D / V;
-    const bool aligned = (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
+    const int B = blockDim.x;
+    const RowPhase<S, V, LOOSE> at(static_cast<const S*>(a.x) + blockIdx.x * a.x_stride, a.D);
+    const int vectors = at.vectors;
+    const bool aligned = !LOOSE && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     grid_dependency_wait();
     grid_dependency_launch();
 
+    // at a phase the weights have no vectors: a thread keeps its own
+    float kept[LOOSE ? NV : 1][V], extra_w = 0.f;
+    if constexpr (LOOSE) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = threadIdx.x + i * B;
+            if (v < vectors) load_weights<V>(a.weight + at.head, v, false, kept[i]);
+        }
+        if (at.extra >= 0) extra_w = a.weight[at.extra];
+    }
+    auto weights = [&](int i, float (&w)[V]) {
+        if constexpr (LOOSE) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) w[j] = kept[i][j];
+        } else {
+            load_weights<V>(a.weight, threadIdx.x + i * B, aligned, w);
+        }
+    };
     RowPiece<T, V, NV> vx, vr;
+    float next_extra = 0.f;
     auto fetch = [&](int64_t row) {
-        vx.load(static_cast<const S*>(a.x) + row * a.x_stride, vectors);
-        if (a.residual) vr.load(static_cast<const S*>(a.residual) + row * a.residual_stride, vectors);
+        const S* x = static_cast<const S*>(a.x) + row * a.x_stride;
+        const S* r = static_cast<const S*>(a.residual) + (a.residual ? row * a.residual_stride : 0);
+        vx.load(x + at.head, vectors);
+        if (a.residual) vr.load(r + at.head, vectors);
+        if (LOOSE && at.extra >= 0) next_extra = to_float<T>(x[at.extra]) + (a.residual ? to_float<T>(r[at.extra]) : 0.f);
     };
     int turn = 0;
     if (blockIdx.x < a.rows) fetch(blockIdx.x);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         float s[NV][V], squares[2] = {0.f, 0.f}, top = 0.f;
+        const float extra = next_extra;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             vx.v[i].unpack(s[i]);
@@ -229,6 +273,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
             }
         }
         if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
+        S* h = static_cast<S*>(a.h) + row * a.D;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
@@ -236,11 +281,11 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
                 if (a.h) {
                     Vec<T, V> o;
                     o.pack(s[i]);
-                    o.store(static_cast<S*>(a.h) + row * a.D + static_cast<int64_t>(v) * V);
+                    o.store(h + at.head + static_cast<int64_t>(v) * V);
                 }
                 if constexpr (kRow) {
                     float w[V];
-                    load_weights<V>(a.weight, v, aligned, w);
+                    weights(i, w);
                     multiply_by<V>(w, s[i]);
                     top = max_or_nan(top, top_of_vector<V>(w));
                 }
@@ -248,11 +293,15 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
             }
         }
         float sum = squares[0] + squares[1];
+        if (LOOSE && at.extra >= 0) {
+            if (a.h) h[at.extra] = from_float<T>(extra);
+            sum = fmaf(extra, extra, sum);
+            if constexpr (kRow) top = max_or_nan(top, extra * extra_w);
+        }
         // s w of vector i, zeros past the row's end
         auto product = [&](int i, float (&p)[V]) {
-            const int v = threadIdx.x + i * B;
-            if (v < vectors) {
-                load_weights<V>(a.weight, v, aligned, p);
+            if (threadIdx.x + i * B < vectors) {
+                weights(i, p);
                 multiply_by<V>(p, s[i]);
             } else {
 #pragma unroll
@@ -277,20 +326,23 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
         const float rstd = 1.f / sqrtf(fmaf(sum, a.inv_D, a.eps));
         if (threadIdx.x == 0) a.rstd[row] = rstd;
         if constexpr (!kRow && !kGroup) {
+            S* y = static_cast<S*>(a.y) + row * a.D;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int v = threadIdx.x + i * B;
                 if (v >= vectors) continue;
                 float f[V];
-                load_weights<V>(a.weight, v, aligned, f);
+                weights(i, f);
                 multiply_by<V>(s[i], rstd);
                 multiply_by<V>(f, s[i]);
                 Vec<T, V> o;
                 o.pack(f);
-                o.store(static_cast<S*>(a.y) + row * a.D + static_cast<int64_t>(v) * V);
+                o.store(y + at.head + static_cast<int64_t>(v) * V);
             }
+            if (LOOSE && at.extra >= 0) y[at.extra] = from_float<T>(extra * rstd * extra_w);
         } else {
             const int groups = (a.D + kRmsGroup - 1) / kRmsGroup;
+            uint8_t* q = static_cast<uint8_t*>(a.y) + row * a.D;
             const Quant of_row(top, rstd);
             if (kRow && threadIdx.x == 0) a.scales[row] = of_row.scale();
 #pragma unroll
@@ -310,14 +362,19 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
                         constexpr int kSegments = kRmsGroup / (32 * V);
                         const int first = (v >> 5) / kSegments * kSegments;
 #pragma unroll
-                        for (int q = 0; q < kSegments; ++q)
-                            if (first + q < (vectors + 31) >> 5) m = max_or_nan(m, segment[first + q]);
+                        for (int k = 0; k < kSegments; ++k)
+                            if (first + k < (vectors + 31) >> 5) m = max_or_nan(m, segment[first + k]);
                     }
                     const Quant quant(m, rstd);
                     if (v < vectors && v % (kRmsGroup / V) == 0) a.scales[row * groups + v / (kRmsGroup / V)] = quant.scale();
                     quant.template apply<V>(p);
                 }
-                if (v < vectors) store_e4m3<V>(static_cast<uint8_t*>(a.y) + row * a.D + static_cast<int64_t>(v) * V, p);
+                if (v < vectors) store_e4m3<V>(q + at.head + static_cast<int64_t>(v) * V, p);
+            }
+            if (LOOSE && at.extra >= 0) {
+                float p[1] = {extra * extra_w};
+                of_row.template apply<1>(p);
+                store_e4m3<1>(q + at.extra, p);
             }
         }
     }
@@ -424,39 +481,49 @@ struct RmsBackward {
     float inv_D;
 };
 
-template <typename T, int V, int EPT>
+template <typename T, int V, int EPT, bool LOOSE>
 __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsBackward a) {
     using S = typename T::storage;
     constexpr int NV = kRmsVectors<V, EPT>;
     __shared__ BlockExchange ex;
-    const int B = blockDim.x, vectors = a.D / V;
-    const bool aligned = (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
+    const int B = blockDim.x;
+    const RowPhase<S, V, LOOSE> at(static_cast<const S*>(a.h) + blockIdx.x * a.h_stride, a.D);
+    const int vectors = at.vectors;
+    const bool aligned = !LOOSE && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     grid_dependency_wait();
     grid_dependency_launch();
-    float dw[NV][V];
+    float dw[NV][V], extra_dw = 0.f, extra_w = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) dw[i][j] = 0.f;
+    if (LOOSE && at.extra >= 0) extra_w = a.weight[at.extra];
     RowPiece<T, V, NV> vy, vh, vd;
-    float next_rstd = 0.f;
+    float next_rstd = 0.f, next_extra_y = 0.f, next_extra_h = 0.f;
     auto fetch = [&](int64_t row) {
-        vy.load(static_cast<const S*>(a.dy) + row * a.dy_stride, vectors);
-        vh.load(static_cast<const S*>(a.h) + row * a.h_stride, vectors);
+        const S* dy = static_cast<const S*>(a.dy) + row * a.dy_stride;
+        const S* h = static_cast<const S*>(a.h) + row * a.h_stride;
+        vy.load(dy + at.head, vectors);
+        vh.load(h + at.head, vectors);
+        if (LOOSE && at.extra >= 0) {
+            next_extra_y = to_float<T>(dy[at.extra]);
+            next_extra_h = to_float<T>(h[at.extra]);
+        }
         next_rstd = a.rstd[row];
     };
     int turn = 0;
     if (blockIdx.x < a.rows) fetch(blockIdx.x);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        const float rstd = next_rstd;
-        if (a.dh) vd.load(static_cast<const S*>(a.dh) + row * a.dh_stride, vectors);
+        const float rstd = next_rstd, extra_y = next_extra_y * extra_w, extra_xhat = next_extra_h * rstd;
+        const S* dh = static_cast<const S*>(a.dh) + (a.dh ? row * a.dh_stride : 0);
+        if (a.dh) vd.load(dh + at.head, vectors);
         float inner[2] = {0.f, 0.f}, xhat[NV][V], wdy[NV][V];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
             if (v < vectors) {
                 float w[V];
-                load_weights<V>(a.weight, v, aligned, w);
+                load_weights<V>(a.weight + at.head, v, aligned, w);
                 vy.v[i].unpack(wdy[i]);
                 vh.v[i].unpack(xhat[i]);
                 multiply_by<V>(xhat[i], rstd);
@@ -473,9 +540,14 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
             }
         }
         float sum = inner[0] + inner[1], none = 0.f;
+        if (LOOSE && at.extra >= 0) {
+            extra_dw = fmaf(next_extra_y, extra_xhat, extra_dw);
+            sum = fmaf(extra_y, extra_xhat, sum);
+        }
         if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
         block_exchange<false>(sum, none, ex, turn);
         const float c = sum * a.inv_D;
+        S* dx = static_cast<S*>(a.dx) + row * a.D;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
@@ -490,7 +562,12 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
             }
             Vec<T, V> o;
             o.pack(wdy[i]);
-            o.store(static_cast<S*>(a.dx) + row * a.D + static_cast<int64_t>(v) * V);
+            o.store(dx + at.head + static_cast<int64_t>(v) * V);
+        }
+        if (LOOSE && at.extra >= 0) {
+            float f = rstd * fmaf(-extra_xhat, c, extra_y);
+            if (a.dh) f += to_float<T>(dh[at.extra]);
+            dx[at.extra] = from_float<T>(f);
         }
     }
     float* p = a.partial + static_cast<int64_t>(blockIdx.x) * a.D;
@@ -499,13 +576,14 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
         const int v = threadIdx.x + i * B;
         if (v >= vectors) continue;
 #pragma unroll
-        for (int j = 0; j < V; ++j) p[v * V + j] = dw[i][j];
+        for (int j = 0; j < V; ++j) p[at.head + v * V + j] = dw[i][j];
     }
+    if (LOOSE && at.extra >= 0) p[at.extra] = extra_dw;
 }
 
 // Rows wider than a block's registers.  The block's sums for dweight stay in its own row of `partial`, which only
 // the thread that owns the column touches.
-template <typename T, int V>
+template <typename T>
 __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_wide_kernel(const RmsBackward a) {
     using S = typename T::storage;
     __shared__ BlockExchange ex;
