@@ -6,7 +6,9 @@
 // Three matrix products on the tensor cores (2 T V D operations each, the logits twice: once per direction), all
 // run by one persistent kernel with different operand layouts and epilogues:
 //   LSE   z tile -> per row maximum and sum of exponentials of the tile's columns, and the target's logit
-//   GRAD  z tile -> G tile, bf16, into a buffer that holds one piece of the vocabulary
+//   GRAD  z tile -> G tile, bf16, into a buffer that holds one piece of the vocabulary, a tile's 256 columns together
+//         (with whole rows of G instead, whose 64 KB strides put each row of a box of G^T in another page, the product
+//         G^T x ran at two thirds of the tensor cores' cycles instead of four fifths)
 //   OUT   dx and dW tiles -> the gradient in the tensor's type, or fp32 partial sums
 //
 // A CTA pair (two SMs) owns a 256 x 256 tile: each CTA keeps 128 rows of it in its tensor memory and half of either
@@ -79,6 +81,21 @@ __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, i
             "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
             "[%4];" ::"r"(dst),
             "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                dst),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
+            "[%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
             : "memory");
 }
 // Arrives on `bar` (in both CTAs of a pair) when the products issued so far have ended.
@@ -202,9 +219,7 @@ struct HeadGemm {
     unsigned* status;            // LSE: cleared here, set by the kernel that joins the partial sums
     const float *lse, *dloss;    // GRAD: [M]
     const float* unit;           // GRAD: G holds the gradient divided by this; OUT: multiplied in again
-    unsigned short* G;           // GRAD: [M][1 or 3 terms][pitch]
-    int64_t G_stride;
-    int G_pitch;
+    unsigned short* G;           // GRAD: [tiles_n][M][1 or 3 terms][256 columns]
     // OUT
     void* out;                   // the tensor's type
     int64_t out_stride;
@@ -310,8 +325,8 @@ struct HeadEpilogue {
                 f[j] = counts && c + j < columns ? exp2_fast(fmaf(f[j], kHeadLog2e, -shift)) * factor : 0.f;
                 if (mine == c + j) f[j] -= one;
             }
-            unsigned short* to = g.G + row * g.G_stride + column0 + c;
             constexpr int kTerms = sizeof(S) == 4 ? 3 : 1;
+            unsigned short* to = g.G + (static_cast<int64_t>(t.n) * g.M + row) * (kTerms * kHeadN) + half * (kHeadN / 2) + c;
 #pragma unroll
             for (int term = 0; term < kTerms; ++term) {
 #pragma unroll
@@ -321,7 +336,7 @@ struct HeadEpilogue {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) e[j] = f[q * 8 + j];
                     o.pack(e);
-                    o.store(to + term * static_cast<int64_t>(g.G_pitch) + q * 8);
+                    o.store(to + term * kHeadN + q * 8);
                     if (term + 1 < kTerms) {
                         o.unpack(e);
 #pragma unroll
@@ -429,12 +444,17 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                     int ta, tb;
                     const int pair = k / g.k_blocks, kk = (k - pair * g.k_blocks) * kHeadK;
                     head_pair(pair, g.pairs, ta, tb);
-                    if constexpr (A_K) {
-                        head::tma_load<CTAS>(sa, &map_a, ta * g.a_pitch + kk, row, bar);
-                    } else {
+                    if constexpr (KIND == kHeadOut) {       // A is G, in blocks of 256 columns
+                        if constexpr (A_K) {
+                            head::tma_load<CTAS>(sa, &map_a, ta * kHeadN + kk % kHeadN, row, kk / kHeadN, bar);
+                        } else {
 #pragma unroll
-                        for (int q = 0; q < kHeadM / 64; ++q)
-                            head::tma_load<CTAS>(sa + q * 8192, &map_a, ta * g.a_pitch + row + q * 64, kk, bar);
+                            for (int q = 0; q < kHeadM / 64; ++q)
+                                head::tma_load<CTAS>(sa + q * 8192, &map_a, ta * kHeadN + (row + q * 64) % kHeadN, kk,
+                                                     (row + q * 64) / kHeadN, bar);
+                        }
+                    } else {
+                        head::tma_load<CTAS>(sa, &map_a, ta * g.a_pitch + kk, row, bar);
                     }
                     if constexpr (B_K) {
                         head::tma_load<CTAS>(sb, &map_b, tb * g.b_pitch + kk, column, bar);

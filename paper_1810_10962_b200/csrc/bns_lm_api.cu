@@ -242,6 +242,28 @@ int head_ctas(int M) { return M <= kHeadM ? 1 : 2; }
 
 bool tma_rows(int64_t stride) { return stride % 8 == 0 && stride < int64_t{1} << 38; }
 
+// Parts that dx's sum over the vocabulary is taken in.  With few rows it has few tiles and a long sum: the parts fill the
+// SMs.  With many the last round of tiles leaves SMs idle: parts even the rounds out (4096 x 4096: 256 tiles on 74 pairs
+// are 4 rounds, in halves 3.5).  Each part costs a write and a read of fp32 sums.
+int split_head(const HeadProblem& p) {
+    const int ctas = head_ctas(p.T);
+    const int64_t workers = sm_count() / ctas;
+    const int64_t tiles = static_cast<int64_t>(divide_up(p.T, kHeadM * ctas)) * divide_up(p.D, kHeadN);
+    const int64_t steps = static_cast<int64_t>(divide_up(p.piece, kHeadK)) * p.pairs;
+    const double step_us = 0.32 * p.pieces, sums_us = static_cast<double>(p.T) * p.D * 8 / 5e6;   // of all pieces; of a part
+    int best = 1;
+    double least = 1e300;
+    for (int s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
+        const double cost = static_cast<double>(divide_up(tiles * s, workers)) * static_cast<double>(divide_up<int64_t>(steps, s)) * step_us +
+                            (s > 1 ? s * sums_us * p.pieces + 3.0 : 0.0);
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
 HeadProblem plan_head(const bns_head* sh, bool backward) {
     HeadProblem p{};
     p.T = sh->rows;
@@ -264,12 +286,9 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     // equal pieces of whole tiles
     p.piece = static_cast<int>(std::min<int64_t>(p.V, divide_up(divide_up(p.V, p.pieces), kHeadN) * static_cast<int64_t>(kHeadN)));
     p.pieces = divide_up(p.V, p.piece);
-    p.G_pitch = divide_up(p.piece, kHeadK) * kHeadK;
-    // few rows: dx is a product with few tiles and a long sum, which is split over the SMs
-    const int ctas = head_ctas(p.T);
-    const int64_t tiles = static_cast<int64_t>(divide_up(p.T, kHeadM * ctas)) * divide_up(p.D, kHeadN);
-    const int64_t steps = static_cast<int64_t>(divide_up(p.piece, kHeadK)) * p.pairs;
-    p.splits = static_cast<int>(std::max<int64_t>(1, std::min(tiles ? sm_count() / ctas / tiles : 1, steps / 4)));
+    p.splits = 1;
+    p.G_pitch = divide_up(p.piece, kHeadN) * kHeadN;
+    if (backward) p.splits = split_head(p);
     size_t at = kHeaderBytes;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -291,35 +310,37 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     return p;
 }
 
-// Tensor map of a matrix of bf16 rows; the box is 64 elements (128 bytes, swizzled) by `box_rows`.
-bool make_map(CUtensorMap* map, const void* base, uint64_t columns, uint64_t rows, uint64_t stride_elements, unsigned box_rows) {
-    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static std::atomic<void*> entry{nullptr};
-    void* fn = entry.load(std::memory_order_relaxed);
-    if (!fn) {
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess || !fn)
-            return false;
-        entry.store(fn, std::memory_order_relaxed);
-    }
-    const cuuint64_t dims[2] = {columns, rows}, strides[1] = {stride_elements * 2};
-    const cuuint32_t box[2] = {kHeadK, box_rows}, steps[2] = {1, 1};
-    return reinterpret_cast<Encode>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
-                                        steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// A matrix operand: `terms` bf16 terms a row, `pitch` elements apart.
+// A matrix operand: `terms` bf16 terms a row, `pitch` elements apart.  With `blocks`, blocks of `columns` columns of all rows
+// after one another.
 struct Operand {
     const void* base;
     int64_t stride;     // elements from one row to the next
     int rows, columns;  // that exist; with several terms a term's padding exists too
     int terms, pitch;
+    int blocks = 0;
+
+    // The tensor map; the box is 64 elements (128 bytes, swizzled) by `box_rows`.
     bool map(CUtensorMap* m, unsigned box_rows) const {
-        return make_map(m, base, terms > 1 ? static_cast<uint64_t>(terms) * pitch : columns, rows, stride, box_rows);
+        using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                    const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                    CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+        static std::atomic<void*> entry{nullptr};
+        void* fn = entry.load(std::memory_order_relaxed);
+        if (!fn) {
+            cudaDriverEntryPointQueryResult found;
+            if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+                found != cudaDriverEntryPointSuccess || !fn)
+                return false;
+            entry.store(fn, std::memory_order_relaxed);
+        }
+        const cuuint64_t wide = static_cast<cuuint64_t>(terms > 1 ? terms * static_cast<int64_t>(pitch) : columns);
+        const cuuint64_t dims[3] = {wide, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(blocks)};
+        const cuuint64_t strides[2] = {static_cast<cuuint64_t>(stride) * 2, static_cast<cuuint64_t>(stride) * 2 * rows};
+        const cuuint32_t box[3] = {kHeadK, box_rows, 1}, steps[3] = {1, 1, 1};
+        return reinterpret_cast<Encode>(fn)(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, blocks ? 3 : 2, const_cast<void*>(base), dims,
+                                            strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+               CUDA_SUCCESS;
     }
 };
 
@@ -597,11 +618,9 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         g.dloss = dloss;
         g.unit = unit;
         g.G = reinterpret_cast<unsigned short*>(ws + p.off_G);
-        g.G_stride = static_cast<int64_t>(p.terms) * p.G_pitch;
-        g.G_pitch = p.G_pitch;
         BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadGrad, true, true, T>(BNS_KERNEL_HEAD_GRADIENT, xs, rows, g, p.D, stream)));
         if (st != BNS_OK) return st;
-        const Operand G{g.G, g.G_stride, p.T, count, p.terms, p.G_pitch};
+        const Operand G{g.G, static_cast<int64_t>(p.terms) * kHeadN, p.T, kHeadN, p.terms, kHeadN, divide_up(count, kHeadN)};
         HeadGemm o{};
         o.M = p.T;
         o.N = p.D;
