@@ -45,7 +45,8 @@ struct HeadRing {
     static constexpr int kStages = CTAS == 2 ? 6 : 4;
     static constexpr int kColumns = kHeadN / CTAS;       // of B in this CTA's stage
     static constexpr unsigned kStageB = kColumns * kHeadK * 2, kStage = kHeadStageA + kStageB;
-    static constexpr unsigned kSmem = kStages * kStage + 1024;
+    static constexpr unsigned kStaging = 8 * 32 * 128;   // 32 rows of 32 fp32 values for each warp of the epilogue
+    static constexpr unsigned kSmem = kStages * kStage + kStaging + 1024;
 };
 constexpr int kHeadRaster = 16;        // row tiles that are swept together, so that their operand stays in L2
 constexpr float kHeadLog2e = 1.4426950408889634f, kHeadLn2 = 0.6931471805599453f;
@@ -266,10 +267,12 @@ struct HeadEpilogue {
     bool counts = false;
     float m, s;                  // LSE
     float shift, factor, one;    // GRAD
-    int half;
+    int half, lane;
+    float4* stage;               // the warp's 32 x 128 bytes
 
-    __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_)
-        : g(g_), t(t_), row(row_), column0(t_.n * kHeadN + half_ * (kHeadN / 2)), in(row_ < g_.M), half(half_) {
+    __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_, float4* stage_)
+        : g(g_), t(t_), row(row_), column0(t_.n * kHeadN + half_ * (kHeadN / 2)), in(row_ < g_.M), half(half_),
+          lane(threadIdx.x & 31), stage(stage_) {
         columns = min(kHeadN / 2, g.N - column0);
         if constexpr (KIND != kHeadOut) {
             const int64_t y = in ? head::load_index(g.target, row, g.target64) : -1;
@@ -319,64 +322,92 @@ struct HeadEpilogue {
                     if (mine == c + j) g.target_logit[row] = f[j];
             }
         } else if constexpr (KIND == kHeadGrad) {
-            if (!in) return;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
                 f[j] = counts && c + j < columns ? exp2_fast(fmaf(f[j], kHeadLog2e, -shift)) * factor : 0.f;
                 if (mine == c + j) f[j] -= one;
             }
-            constexpr int kTerms = sizeof(S) == 4 ? 3 : 1;
-            unsigned short* to = g.G + (static_cast<int64_t>(t.n) * g.M + row) * (kTerms * kHeadN) + half * (kHeadN / 2) + c;
+            spread(f, [&](int r, int u, float (&v)[4]) {
+                if (row - lane + r >= g.M) return;
+                constexpr int kTerms = sizeof(S) == 4 ? 3 : 1;
+                unsigned short* to = g.G + (static_cast<int64_t>(t.n) * g.M + row - lane + r) * (kTerms * kHeadN) +
+                                     half * (kHeadN / 2) + c + 4 * u;
 #pragma unroll
-            for (int term = 0; term < kTerms; ++term) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    Vec<BF16, 8> o;
-                    float e[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) e[j] = f[q * 8 + j];
-                    o.pack(e);
-                    o.store(to + term * kHeadN + q * 8);
+                for (int term = 0; term < kTerms; ++term) {
+                    Vec<BF16, 4> o;
+                    o.pack(v);
+                    o.store(to + term * kHeadN);
                     if (term + 1 < kTerms) {
-                        o.unpack(e);
+                        float back[4];
+                        o.unpack(back);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) f[q * 8 + j] -= e[j];   // what the term leaves for the next
+                        for (int j = 0; j < 4; ++j) v[j] -= back[j];   // what the term leaves for the next
                     }
                 }
-            }
+            });
         } else {
-            if (!in) return;
-            const int left = columns - c;
+            const bool whole = g.N % 4 == 0;     // rows of sums and of the output begin at whole vectors
+            spread(f, [&](int r, int u, float (&v)[4]) {
+                const int left = columns - c - 4 * u;
+                const int64_t at = static_cast<int64_t>(row - lane + r);
+                if (at >= g.M || left <= 0) return;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) f[j] *= factor;
-            if (g.sums) {
-                float* p = g.sums + (static_cast<int64_t>(t.split) * g.M + row) * g.N + column0 + c;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    if (j < left) {
-                        if (g.add) f[j] += p[j];
-                        if (!g.last) p[j] = f[j];
-                    }
+                for (int j = 0; j < 4; ++j) v[j] *= factor;
+                if (g.sums) {
+                    float* p = g.sums + (t.split * static_cast<int64_t>(g.M) + at) * g.N + column0 + c + 4 * u;
+                    put_or_add(p, v, left, whole);
+                    if (!g.last) return;
                 }
-                if (!g.last) return;
-            }
-            S* to = static_cast<S*>(g.out) + row * g.out_stride + column0 + c;
-            constexpr int V = 16 / sizeof(S);
-            if (left >= 32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+                S* to = static_cast<S*>(g.out) + at * g.out_stride + column0 + c + 4 * u;
+                if (whole) {
+                    Vec<T, 4> o;
+                    o.pack(v);
+                    o.store(to);
+                } else {
 #pragma unroll
-                for (int q = 0; q < 32 / V; ++q) {
-                    Vec<T, V> o;
-                    float e[V];
-#pragma unroll
-                    for (int j = 0; j < V; ++j) e[j] = f[q * V + j];
-                    o.pack(e);
-                    o.store(to + q * V);
+                    for (int j = 0; j < 4; ++j)
+                        if (j < left) to[j] = from_float<T>(v[j]);
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (j < left) to[j] = from_float<T>(f[j]);
+            });
+        }
+    }
+    // Adds what is there, and writes the sum back unless it is the last.
+    __device__ __forceinline__ void put_or_add(float* p, float (&v)[4], int left, bool whole) const {
+        if (whole) {
+            float4* q = reinterpret_cast<float4*>(p);
+            if (g.add) {
+                const float4 old = *q;
+                v[0] += old.x;
+                v[1] += old.y;
+                v[2] += old.z;
+                v[3] += old.w;
             }
+            if (!g.last) *q = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j >= left) continue;
+                if (g.add) v[j] += p[j];
+                if (!g.last) p[j] = v[j];
+            }
+        }
+    }
+    // Turns the warp's 32 rows x 32 columns, a row a lane, through shared memory into eight lanes a row: put(r, u, v) gets
+    // columns 4 u .. 4 u + 3 of the warp's row r, so that a store covers 64 or 128 contiguous bytes of a row.  (A row a
+    // lane writes half sectors: dW of 24 rows, 32768 x 1024, took 34 us instead of 20.)
+    template <typename Put>
+    __device__ __forceinline__ void spread(const float* f, Put&& put) const {
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            stage[lane * 8 + (u ^ (lane & 7))] = make_float4(f[4 * u], f[4 * u + 1], f[4 * u + 2], f[4 * u + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3), u = lane & 7;
+            const float4 q = stage[r * 8 + (u ^ (r & 7))];
+            float v[4] = {q.x, q.y, q.z, q.w};
+            put(r, u, v);
         }
     }
     __device__ __forceinline__ void finish() {
@@ -399,7 +430,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CTAS == 1 ? 0 : static_cast<int>(blockIdx.x & 1);      // in the pair
     const int worker = blockIdx.x / CTAS, workers = gridDim.x / CTAS;
-    const unsigned ring = (smem_address(raw) + 1023) & ~1023u;
+    const unsigned head_raw = smem_address(raw), ring = (head_raw + 1023) & ~1023u;
     const unsigned full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16,
                    flush = drained + 16;
     if (threadIdx.x == 0) {
@@ -502,12 +533,13 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         __syncwarp();
     } else {
         const int slot = warp & 3, half = (warp - 4) >> 2;
+        float4* stage = reinterpret_cast<float4*>(raw + (ring - head_raw) + kStages * Ring::kStage) + (warp - 4) * 256;
         if (KIND == kHeadLse && blockIdx.x == 0 && threadIdx.x == 128 && g.status) *g.status = 0;
         int n = 0;
         bool ok = true;
         for (int id = worker; ok && id < tiles; id += workers) {
             const HeadTile t(g, id);
-            HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half);
+            HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half, stage);
             const unsigned lanes = tmem + (static_cast<unsigned>(slot * 32) << 16) + half * (kHeadN / 2);
             auto wait_ready = [&]() {
                 ok = __all_sync(0xffffffffu, wait_bounded(ready + 8 * (n & 1), (n / 2) & 1, &gave_up));
@@ -603,45 +635,77 @@ __global__ void __launch_bounds__(1024) head_unit_kernel(const void* target, int
 }
 
 // Rows into bf16 terms: the first is the value rounded, the next what that leaves, and so on; each term's row is padded
-// with zeros to `pitch` elements.  One term lays out bf16 rows whose stride TMA cannot take.
+// with zeros to `pitch` elements.  One term lays out bf16 rows whose stride TMA cannot take.  Eight columns a thread.
 template <typename T>
 __global__ void __launch_bounds__(256) head_terms_kernel(const void* src, int64_t stride, int rows, int D, int terms, int pitch,
                                                          unsigned short* dst) {
+    using S = typename T::storage;
+    constexpr int kWord = 16 / sizeof(S);
     grid_dependency_wait();
     grid_dependency_launch();
-    const int64_t total = static_cast<int64_t>(rows) * pitch;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-        const int64_t row = i / pitch;
-        const int column = static_cast<int>(i - row * pitch);
-        float v = column < D ? to_float<T>(static_cast<const typename T::storage*>(src)[row * stride + column]) : 0.f;
+    const int units = pitch / 8, unit = blockIdx.x * 32 + (threadIdx.x & 31);
+    if (unit >= units) return;
+    for (int64_t row = blockIdx.y * 8 + (threadIdx.x >> 5); row < rows; row += gridDim.y * 8) {
+        const S* from = static_cast<const S*>(src) + row * stride + unit * 8;
+        float v[8];
+        if (unit * 8 + 8 <= D && stride % kWord == 0) {
+#pragma unroll
+            for (int j = 0; j < 8; j += kWord) {
+                Vec<T, kWord> x;
+                float f[kWord];
+                x.load(from + j);
+                x.unpack(f);
+#pragma unroll
+                for (int i = 0; i < kWord; ++i) v[j + i] = f[i];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = unit * 8 + j < D ? to_float<T>(from[j]) : 0.f;
+        }
         for (int t = 0; t < terms; ++t) {
-            const unsigned short b = from_float<BF16>(v);
-            dst[(row * terms + t) * pitch + column] = b;
-            v -= to_float<BF16>(b);
+            Vec<BF16, 8> o;
+            float back[8];
+            o.pack(v);
+            o.store(dst + (row * terms + t) * pitch + unit * 8);
+            o.unpack(back);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] -= back[j];
         }
     }
 }
 
-// Joins the half tiles' maxima and sums of a row: 32 rows a block, eight threads a row, in a fixed order.
-__global__ void __launch_bounds__(256) head_join_kernel(const float2* partial, int tiles, int rows, const float* target_logit,
-                                                        const void* target, int target64, int V, float* loss, float* lse,
-                                                        unsigned* status) {
-    __shared__ float2 fold[8][32];
+// Joins the half tiles' maxima and sums of a row: 32 rows a block, 32 threads a row, in a fixed order.
+__global__ void __launch_bounds__(1024) head_join_kernel(const float2* partial, int strips, int rows, const float* target_logit,
+                                                         const void* target, int target64, int V, float* loss, float* lse,
+                                                         unsigned* status) {
+    __shared__ float2 fold[32][33];
     grid_dependency_wait();
     grid_dependency_launch();
     const float inf = __int_as_float(0x7f800000);
-    const int row = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+    int row = blockIdx.x * 32 + lane;
     auto join = [&](float2 a, float2 b) {
         const float m = fmaxf(a.x, b.x), ref = m == -inf ? 0.f : m;
         return make_float2(m, a.y * exp2_fast(a.x - ref) + b.y * exp2_fast(b.x - ref));
     };
     float2 v = make_float2(-inf, 0.f);
-    if (row < rows)
-        for (int t = part; t < tiles; t += 8) v = join(v, partial[static_cast<int64_t>(t) * rows + row]);
-    fold[part][threadIdx.x & 31] = v;
+    if (row < rows) {
+        for (int t0 = part; t0 < strips; t0 += 128) {
+            float2 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[i] = t0 + i * 32 < strips ? partial[static_cast<int64_t>(t0 + i * 32) * rows + row] : make_float2(-inf, 0.f);
+            v = join(v, join(join(x[0], x[1]), join(x[2], x[3])));
+        }
+    }
+    fold[part][lane] = v;
     __syncthreads();
-    if (part || row >= rows) return;
-    for (int q = 1; q < 8; ++q) v = join(v, fold[q][threadIdx.x]);
+    v = fold[lane][part];       // now a warp has a row
+    row = blockIdx.x * 32 + part;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+    if (lane || row >= rows) return;
     const float rest = log2f(v.y);
     lse[row] = (v.x + rest) * kHeadLn2;
     const int64_t y = head::load_index(target, row, target64);
@@ -650,18 +714,25 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float2* partial, i
     if (y >= V) atomicOr(status, BNS_FLAG_BAD_TARGET);
 }
 
-// Adds up the splits of a product, in order, and rounds once.
-template <typename T>
-__global__ void __launch_bounds__(256) head_sum_kernel(const float* sums, int splits, int rows, int columns, void* out,
-                                                       int64_t stride) {
+// Adds up the parts of a product, in order, and rounds once.  `total` elements a part, V at a time.
+template <typename T, int V>
+__global__ void __launch_bounds__(256) head_sum_kernel(const float* sums, int parts, int64_t total, void* out) {
     grid_dependency_wait();
     grid_dependency_launch();
-    const int64_t total = static_cast<int64_t>(rows) * columns;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-        float v = 0.f;
-        for (int s = 0; s < splits; ++s) v += sums[s * total + i];
-        const int64_t row = i / columns;
-        static_cast<typename T::storage*>(out)[row * stride + (i - row * columns)] = from_float<T>(v);
+    for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * V; i < total; i += gridDim.x * 256ll * V) {
+        float v[V] = {};
+#pragma unroll 8
+        for (int s = 0; s < parts; ++s) {
+            Vec<F32, V> x;
+            float f[V];
+            x.load(sums + s * total + i);
+            x.unpack(f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] += f[j];
+        }
+        Vec<T, V> o;
+        o.pack(v);
+        o.store(static_cast<typename T::storage*>(out) + i);
     }
 }
 

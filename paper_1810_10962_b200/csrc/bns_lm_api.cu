@@ -27,14 +27,14 @@ bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) %
 bool workspace_fits(const void* ws, size_t bytes, size_t need) { return ws && aligned(ws, kAlign) && bytes >= need; }
 
 struct Shape {
-    unsigned grid, threads, cluster = 1;
+    unsigned grid, threads, cluster = 1, grid_y = 1;
 };
 
 template <typename... KArgs, typename... Args>
 void launch(int kind, void (*kernel)(KArgs...), Shape shape, size_t smem, cudaStream_t s, Args&&... args) {
     LaunchScope scope(kind, s);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(shape.grid);
+    cfg.gridDim = dim3(shape.grid, shape.grid_y);
     cfg.blockDim = dim3(shape.threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -382,10 +382,9 @@ bns_status head_gemm(int kind, const Operand& a, const Operand& b, HeadGemm g, i
 }
 
 void lay_out(int dtype, const void* src, int64_t stride, int rows, int D, int terms, int pitch, void* dst, cudaStream_t stream) {
-    const int64_t blocks = divide_up<int64_t>(static_cast<int64_t>(rows) * pitch, 256);
-    BNS_LM_BY_TYPE(dtype, (launch(BNS_KERNEL_HEAD_VECTOR, head_terms_kernel<T>,
-                                  Shape{static_cast<unsigned>(std::min<int64_t>(blocks, sm_count() * 16)), 256}, 0, stream, src, stride,
-                                  rows, D, terms, pitch, static_cast<unsigned short*>(dst))));
+    const Shape grid{static_cast<unsigned>(divide_up(pitch / 8, 32)), 256, 1, static_cast<unsigned>(std::min(divide_up(rows, 8), 65535))};
+    BNS_LM_BY_TYPE(dtype, (launch(BNS_KERNEL_HEAD_VECTOR, head_terms_kernel<T>, grid, 0, stream, src, stride, rows, D, terms, pitch,
+                                  static_cast<unsigned short*>(dst))));
 }
 
 Operand rows_of_x(const HeadProblem& p, const bns_head* sh, const void* x, char* ws) {
@@ -575,7 +574,7 @@ bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x
         if (st != BNS_OK) return st;
         tiles += 2 * divide_up(count, kHeadN);
     }
-    launch(BNS_KERNEL_HEAD_VECTOR, head_join_kernel, Shape{static_cast<unsigned>(divide_up(p.T, 32)), 256}, 0, stream, partial, tiles, p.T,
+    launch(BNS_KERNEL_HEAD_VECTOR, head_join_kernel, Shape{static_cast<unsigned>(divide_up(p.T, 32)), 1024}, 0, stream, partial, tiles, p.T,
            reinterpret_cast<const float*>(ws + p.off_logit), target, shape->target_is_int64, p.V, loss, lse,
            reinterpret_cast<unsigned*>(ws));
     return last_error();
@@ -644,10 +643,15 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         if (st != BNS_OK) return st;
     }
     if (p.splits > 1) {
-        const int64_t blocks = divide_up<int64_t>(static_cast<int64_t>(p.T) * p.D, 256);
-        BNS_LM_BY_TYPE(p.dtype, (launch(BNS_KERNEL_HEAD_VECTOR, head_sum_kernel<T>,
-                                        Shape{static_cast<unsigned>(std::min<int64_t>(blocks, sm_count() * 16)), 256}, 0, stream,
-                                        static_cast<const float*>(sums), p.splits, p.T, p.D, dx, static_cast<int64_t>(p.D))));
+        const int64_t total = static_cast<int64_t>(p.T) * p.D;
+        const int V = total % 4 ? 1 : 4;         // a part begins at a 16-byte boundary
+        const Shape grid{static_cast<unsigned>(std::min<int64_t>(divide_up<int64_t>(total, 256 * V), sm_count() * 16)), 256};
+        BNS_LM_BY_TYPE(p.dtype, {
+            if (V == 4)
+                launch(BNS_KERNEL_HEAD_VECTOR, head_sum_kernel<T, 4>, grid, 0, stream, static_cast<const float*>(sums), p.splits, total, dx);
+            else
+                launch(BNS_KERNEL_HEAD_VECTOR, head_sum_kernel<T, 1>, grid, 0, stream, static_cast<const float*>(sums), p.splits, total, dx);
+        });
     }
     return last_error();
 }

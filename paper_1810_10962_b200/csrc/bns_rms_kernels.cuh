@@ -498,7 +498,9 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
 #pragma unroll
         for (int j = 0; j < V; ++j) dw[i][j] = 0.f;
     if (LOOSE && at.extra >= 0) extra_w = a.weight[at.extra];
-    RowPiece<T, V, NV> vy, vh, vd;
+    // two-byte rows have the registers for dh a row ahead as well
+    constexpr bool kAhead = sizeof(S) == 2 && EPT == 8;
+    RowPiece<T, V, NV> vy, vh, vd, ahead;
     float next_rstd = 0.f, next_extra_y = 0.f, next_extra_h = 0.f;
     auto fetch = [&](int64_t row) {
         const S* dy = static_cast<const S*>(a.dy) + row * a.dy_stride;
@@ -509,6 +511,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
             next_extra_y = to_float<T>(dy[at.extra]);
             next_extra_h = to_float<T>(h[at.extra]);
         }
+        if (kAhead && a.dh) ahead.load(static_cast<const S*>(a.dh) + row * a.dh_stride + at.head, vectors);
         next_rstd = a.rstd[row];
     };
     int turn = 0;
@@ -516,7 +519,10 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const float rstd = next_rstd, extra_y = next_extra_y * extra_w, extra_xhat = next_extra_h * rstd;
         const S* dh = static_cast<const S*>(a.dh) + (a.dh ? row * a.dh_stride : 0);
-        if (a.dh) vd.load(dh + at.head, vectors);
+        if (kAhead)
+            vd = ahead;
+        else if (a.dh)
+            vd.load(dh + at.head, vectors);
         float inner[2] = {0.f, 0.f}, xhat[NV][V], wdy[NV][V];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
