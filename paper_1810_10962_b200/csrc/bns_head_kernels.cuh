@@ -67,7 +67,9 @@ __device__ __forceinline__ void arrive_in_first(unsigned bar) {
     if constexpr (CTAS == 1)
         asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
     else
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first<CTAS>(bar)) : "memory");
+        // release at the block's scope only: at the cluster's it would wait for the epilogue's stores to reach L2, and what
+        // is handed over is tensor memory, ordered by the tcgen05 fence before
+        asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_first<CTAS>(bar)) : "memory");
 }
 // `bar` lies in the pair's first CTA, the data goes to this one.
 template <int CTAS>
@@ -248,9 +250,13 @@ struct HeadTile {
         const int rows = min(kHeadRaster, g.tiles_m - first), q = r - first * g.tiles_n;
         m = first + q % rows;
         n = q / rows;
-        const int total = g.k_blocks * g.pairs;
-        k0 = static_cast<int>(static_cast<int64_t>(total) * split / g.splits);
-        k1 = static_cast<int>(static_cast<int64_t>(total) * (split + 1) / g.splits);
+        k0 = 0;
+        k1 = g.k_blocks * g.pairs;
+        if (g.splits > 1) {
+            const int64_t total = k1;
+            k0 = static_cast<int>(total * split / g.splits);
+            k1 = static_cast<int>(total * (split + 1) / g.splits);
+        }
     }
 };
 
@@ -269,10 +275,18 @@ struct HeadEpilogue {
     float shift, factor, one;    // GRAD
     int half, lane;
     float4* stage;               // the warp's 32 x 128 bytes
+    // where the lane's four columns of the warp's row lane / 8 go, the step to four rows below, and rows that exist
+    int rows_left;
+    unsigned short* G_at = nullptr;
+    float* sums_at = nullptr;
+    S* out_at = nullptr;
+    int64_t sums_step = 0, out_step = 0;
 
     __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_, float4* stage_)
         : g(g_), t(t_), row(row_), column0(t_.n * kHeadN + half_ * (kHeadN / 2)), in(row_ < g_.M), half(half_),
           lane(threadIdx.x & 31), stage(stage_) {
+        const int64_t first = row - lane + (lane >> 3);
+        rows_left = static_cast<int>(g.M - first);
         columns = min(kHeadN / 2, g.N - column0);
         if constexpr (KIND != kHeadOut) {
             const int64_t y = in ? head::load_index(g.target, row, g.target64) : -1;
@@ -290,8 +304,15 @@ struct HeadEpilogue {
             // difference z - lse feels its rounding; rest goes into the factor
             shift = lse * kHeadLog2e;
             factor = one * exp2_fast(-fmaf(lse, kHeadLog2e, -shift));
+            constexpr int kTerms = sizeof(S) == 4 ? 3 : 1;
+            G_at = g.G + (static_cast<int64_t>(t.n) * g.M + first) * (kTerms * kHeadN) + half * (kHeadN / 2) + 4 * (lane & 7);
         } else {
-            factor = g.unit ? *g.unit : 1.f;
+            factor = *g.unit;
+            const int at = column0 + 4 * (lane & 7);
+            if (g.sums) sums_at = g.sums + (t.split * static_cast<int64_t>(g.M) + first) * g.N + at;
+            sums_step = 4 * static_cast<int64_t>(g.N);
+            out_at = static_cast<S*>(g.out) + first * g.out_stride + at;
+            out_step = 4 * g.out_stride;
         }
     }
     // Columns that the accumulator has to be read for: G is written up to whole stages of K, zeros where nothing is.
@@ -327,16 +348,14 @@ struct HeadEpilogue {
                 f[j] = counts && c + j < columns ? exp2_fast(fmaf(f[j], kHeadLog2e, -shift)) * factor : 0.f;
                 if (mine == c + j) f[j] -= one;
             }
-            spread(f, [&](int r, int u, float (&v)[4]) {
-                if (row - lane + r >= g.M) return;
-                constexpr int kTerms = sizeof(S) == 4 ? 3 : 1;
-                unsigned short* to = g.G + (static_cast<int64_t>(t.n) * g.M + row - lane + r) * (kTerms * kHeadN) +
-                                     half * (kHeadN / 2) + c + 4 * u;
+            constexpr int kTerms = sizeof(S) == 4 ? 3 : 1, kStep = 4 * kTerms * kHeadN;
+            unsigned short* to = G_at + c;
+            spread(f, [&](int i, float (&v)[4]) {
 #pragma unroll
                 for (int term = 0; term < kTerms; ++term) {
                     Vec<BF16, 4> o;
                     o.pack(v);
-                    o.store(to + term * kHeadN);
+                    o.store(to + i * kStep + term * kHeadN);
                     if (term + 1 < kTerms) {
                         float back[4];
                         o.unpack(back);
@@ -346,30 +365,45 @@ struct HeadEpilogue {
                 }
             });
         } else {
+            const int left = columns - c - 4 * (lane & 7);
             const bool whole = g.N % 4 == 0;     // rows of sums and of the output begin at whole vectors
-            spread(f, [&](int r, int u, float (&v)[4]) {
-                const int left = columns - c - 4 * u;
-                const int64_t at = static_cast<int64_t>(row - lane + r);
-                if (at >= g.M || left <= 0) return;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] *= factor;
-                if (g.sums) {
-                    float* p = g.sums + (t.split * static_cast<int64_t>(g.M) + at) * g.N + column0 + c + 4 * u;
-                    put_or_add(p, v, left, whole);
-                    if (!g.last) return;
-                }
-                S* to = static_cast<S*>(g.out) + at * g.out_stride + column0 + c + 4 * u;
-                if (whole) {
+            S* to = out_at + c;
+            if (!g.sums && whole) {
+                spread(f, [&](int, float (&v)[4]) {
+                    scale(v);
                     Vec<T, 4> o;
                     o.pack(v);
-                    o.store(to);
-                } else {
+                    if (left > 0) o.store(to);
+                    to += out_step;
+                });
+                return;
+            }
+            float* sums = sums_at + c;
+            spread(f, [&](int, float (&v)[4]) {
+                if (left > 0) {
+                    scale(v);
+                    if (g.sums) put_or_add(sums, v, left, whole);
+                    if (!g.sums || g.last) {
+                        if (whole) {
+                            Vec<T, 4> o;
+                            o.pack(v);
+                            o.store(to);
+                        } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (j < left) to[j] = from_float<T>(v[j]);
+                            for (int j = 0; j < 4; ++j)
+                                if (j < left) to[j] = from_float<T>(v[j]);
+                        }
+                    }
                 }
+                sums += sums_step;
+                to += out_step;
             });
         }
+    }
+    __device__ __forceinline__ void scale(float (&v)[4]) const {
+        const pair_t by = make_pair(factor, factor);
+        split_pair(mul2(make_pair(v[0], v[1]), by), v[0], v[1]);
+        split_pair(mul2(make_pair(v[2], v[3]), by), v[2], v[3]);
     }
     // Adds what is there, and writes the sum back unless it is the last.
     __device__ __forceinline__ void put_or_add(float* p, float (&v)[4], int left, bool whole) const {
@@ -392,9 +426,9 @@ struct HeadEpilogue {
             }
         }
     }
-    // Turns the warp's 32 rows x 32 columns, a row a lane, through shared memory into eight lanes a row: put(r, u, v) gets
-    // columns 4 u .. 4 u + 3 of the warp's row r, so that a store covers 64 or 128 contiguous bytes of a row.  (A row a
-    // lane writes half sectors: dW of 24 rows, 32768 x 1024, took 34 us instead of 20.)
+    // Turns the warp's 32 rows x 32 columns, a row a lane, through shared memory into eight lanes a row: put(i, v) gets
+    // columns 4 (lane % 8) .. + 3 of the warp's row 4 i + lane / 8, so that a store covers 64 or 128 contiguous bytes of a
+    // row (a row a lane writes half sectors).
     template <typename Put>
     __device__ __forceinline__ void spread(const float* f, Put&& put) const {
         __syncwarp();
@@ -402,12 +436,17 @@ struct HeadEpilogue {
         for (int u = 0; u < 8; ++u)
             stage[lane * 8 + (u ^ (lane & 7))] = make_float4(f[4 * u], f[4 * u + 1], f[4 * u + 2], f[4 * u + 3]);
         __syncwarp();
+        float4 q[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int r = 4 * i + (lane >> 3), u = lane & 7;
-            const float4 q = stage[r * 8 + (u ^ (r & 7))];
-            float v[4] = {q.x, q.y, q.z, q.w};
-            put(r, u, v);
+            const int r = 4 * i + (lane >> 3);
+            q[i] = stage[r * 8 + ((lane & 7) ^ (r & 7))];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (4 * i >= rows_left) break;
+            float v[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+            put(i, v);
         }
     }
     __device__ __forceinline__ void finish() {
@@ -714,25 +753,45 @@ __global__ void __launch_bounds__(1024) head_join_kernel(const float2* partial, 
     if (y >= V) atomicOr(status, BNS_FLAG_BAD_TARGET);
 }
 
-// Adds up the parts of a product, in order, and rounds once.  `total` elements a part, V at a time.
-template <typename T, int V>
+// Adds up the parts of a product in a fixed order, and rounds once.  `total` elements a part, V at a time; GROUPS threads an
+// element each take every GROUPS-th part (many parts come with few elements: four threads shorten the chain of loads).
+template <typename T, int V, int GROUPS>
 __global__ void __launch_bounds__(256) head_sum_kernel(const float* sums, int parts, int64_t total, void* out) {
+    constexpr int kPer = 256 / GROUPS;
+    __shared__ float fold[GROUPS][kPer][V];
     grid_dependency_wait();
     grid_dependency_launch();
-    for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * V; i < total; i += gridDim.x * 256ll * V) {
+    const int at = threadIdx.x % kPer, group = threadIdx.x / kPer;
+    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kPer * V; i0 < total; i0 += static_cast<int64_t>(gridDim.x) * kPer * V) {
+        const int64_t i = i0 + at * V;
         float v[V] = {};
-#pragma unroll 8
-        for (int s = 0; s < parts; ++s) {
-            Vec<F32, V> x;
-            float f[V];
-            x.load(sums + s * total + i);
-            x.unpack(f);
+        if (i < total) {
+#pragma unroll 10
+            for (int s = group; s < parts; s += GROUPS) {
+                Vec<F32, V> x;
+                float f[V];
+                x.load(sums + s * total + i);
+                x.unpack(f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] += f[j];
+                for (int j = 0; j < V; ++j) v[j] += f[j];
+            }
         }
-        Vec<T, V> o;
-        o.pack(v);
-        o.store(static_cast<typename T::storage*>(out) + i);
+        if constexpr (GROUPS > 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) fold[group][at][j] = v[j];
+            __syncthreads();
+            if (group == 0) {
+                for (int q = 1; q < GROUPS; ++q)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) v[j] += fold[q][at][j];
+            }
+            __syncthreads();
+        }
+        if (group == 0 && i < total) {
+            Vec<T, V> o;
+            o.pack(v);
+            o.store(static_cast<typename T::storage*>(out) + i);
+        }
     }
 }
 

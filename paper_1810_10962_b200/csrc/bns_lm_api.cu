@@ -645,12 +645,13 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
     if (p.splits > 1) {
         const int64_t total = static_cast<int64_t>(p.T) * p.D;
         const int V = total % 4 ? 1 : 4;         // a part begins at a 16-byte boundary
-        const Shape grid{static_cast<unsigned>(std::min<int64_t>(divide_up<int64_t>(total, 256 * V), sm_count() * 16)), 256};
+        const int groups = p.splits > 8 ? 4 : 1;
+        const Shape grid{static_cast<unsigned>(std::min<int64_t>(divide_up<int64_t>(total, 256 / groups * V), sm_count() * 16)), 256};
+        const float* parts = sums;
         BNS_LM_BY_TYPE(p.dtype, {
-            if (V == 4)
-                launch(BNS_KERNEL_HEAD_VECTOR, head_sum_kernel<T, 4>, grid, 0, stream, static_cast<const float*>(sums), p.splits, total, dx);
-            else
-                launch(BNS_KERNEL_HEAD_VECTOR, head_sum_kernel<T, 1>, grid, 0, stream, static_cast<const float*>(sums), p.splits, total, dx);
+            auto kernel = V == 4 ? (groups == 4 ? head_sum_kernel<T, 4, 4> : head_sum_kernel<T, 4, 1>)
+                                 : (groups == 4 ? head_sum_kernel<T, 1, 4> : head_sum_kernel<T, 1, 1>);
+            launch(BNS_KERNEL_HEAD_VECTOR, kernel, grid, 0, stream, parts, p.splits, total, dx);
         });
     }
     return last_error();
