@@ -101,6 +101,21 @@ __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, i
             "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
             : "memory");
 }
+template <int CTAS>
+__device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int x, int y, int z, int w, unsigned bar) {
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+                dst),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
+            "[%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+            : "memory");
+}
 // Arrives on `bar` (in both CTAs of a pair) when the products issued so far have ended.
 template <int CTAS>
 __device__ __forceinline__ void commit(unsigned bar) {
@@ -212,6 +227,7 @@ struct HeadGemm {
     int tiles_m, tiles_n, splits;
     int k_blocks, pairs;         // stages of K per pair of terms; 1 pair, or 6 for fp32 tensors
     int a_pitch, b_pitch;        // elements from one bf16 term of a row to the next
+    int b_chunks;                // B with its other dimension contiguous: its map counts that in chunks of 64, one load a stage
     // LSE and GRAD
     const void* target;          // [M]
     int target64;
@@ -515,19 +531,17 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                     const int pair = k / g.k_blocks, kk = (k - pair * g.k_blocks) * kHeadK;
                     head_pair(pair, g.pairs, ta, tb);
                     if constexpr (KIND == kHeadOut) {       // A is G, in blocks of 256 columns
-                        if constexpr (A_K) {
+                        if constexpr (A_K)
                             head::tma_load<CTAS>(sa, &map_a, ta * kHeadN + kk % kHeadN, row, kk / kHeadN, bar);
-                        } else {
-#pragma unroll
-                            for (int q = 0; q < kHeadM / 64; ++q)
-                                head::tma_load<CTAS>(sa + q * 8192, &map_a, ta * kHeadN + (row + q * 64) % kHeadN, kk,
-                                                     (row + q * 64) / kHeadN, bar);
-                        }
+                        else
+                            head::tma_load<CTAS>(sa, &map_a, 0, kk, (ta * kHeadN + row % kHeadN) / 64, row / kHeadN, bar);
                     } else {
                         head::tma_load<CTAS>(sa, &map_a, ta * g.a_pitch + kk, row, bar);
                     }
                     if constexpr (B_K) {
                         head::tma_load<CTAS>(sb, &map_b, tb * g.b_pitch + kk, column, bar);
+                    } else if (g.b_chunks) {
+                        head::tma_load<CTAS>(sb, &map_b, 0, kk, (tb * g.b_pitch + column) / 64, bar);
                     } else {
 #pragma unroll
                         for (int q = 0; q < Ring::kColumns / 64; ++q)

@@ -310,8 +310,28 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     return p;
 }
 
-// A matrix operand: `terms` bf16 terms a row, `pitch` elements apart.  With `blocks`, blocks of `columns` columns of all rows
-// after one another.
+// Tensor map of bf16 values; the box is 64 elements (128 bytes, swizzled) by box[1] by ...
+bool encode_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<void*> entry{nullptr};
+    void* fn = entry.load(std::memory_order_relaxed);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess || !fn)
+            return false;
+        entry.store(fn, std::memory_order_relaxed);
+    }
+    const cuuint32_t steps[4] = {1, 1, 1, 1};
+    return reinterpret_cast<Encode>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(base),
+                                        dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A matrix operand: `terms` bf16 terms a row, `pitch` elements apart.  With `blocks`, blocks of 256 columns (of each term) of
+// all rows after one another.
 struct Operand {
     const void* base;
     int64_t stride;     // elements from one row to the next
@@ -319,28 +339,27 @@ struct Operand {
     int terms, pitch;
     int blocks = 0;
 
-    // The tensor map; the box is 64 elements (128 bytes, swizzled) by `box_rows`.
-    bool map(CUtensorMap* m, unsigned box_rows) const {
-        using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                    const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                    CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-        static std::atomic<void*> entry{nullptr};
-        void* fn = entry.load(std::memory_order_relaxed);
-        if (!fn) {
-            cudaDriverEntryPointQueryResult found;
-            if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
-                found != cudaDriverEntryPointSuccess || !fn)
-                return false;
-            entry.store(fn, std::memory_order_relaxed);
-        }
-        const cuuint64_t wide = static_cast<cuuint64_t>(terms > 1 ? terms * static_cast<int64_t>(pitch) : columns);
-        const cuuint64_t dims[3] = {wide, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(blocks)};
+    cuuint64_t wide() const { return static_cast<cuuint64_t>(terms > 1 ? terms * static_cast<int64_t>(pitch) : columns); }
+    // Rows are read in whole chunks of 64 elements only where no chunk passes the row's end.
+    bool chunks() const { return wide() % 64 == 0; }
+
+    // K contiguous: `box_rows` rows of 64 elements of K.
+    bool map_k(CUtensorMap* m, unsigned box_rows) const {
+        const cuuint64_t dims[3] = {wide(), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(blocks)};
         const cuuint64_t strides[2] = {static_cast<cuuint64_t>(stride) * 2, static_cast<cuuint64_t>(stride) * 2 * rows};
-        const cuuint32_t box[3] = {kHeadK, box_rows, 1}, steps[3] = {1, 1, 1};
-        return reinterpret_cast<Encode>(fn)(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, blocks ? 3 : 2, const_cast<void*>(base), dims,
-                                            strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
-               CUDA_SUCCESS;
+        const cuuint32_t box[3] = {kHeadK, box_rows, 1};
+        return encode_map(m, base, blocks ? 3 : 2, dims, strides, box);
+    }
+    // The other dimension contiguous: 64 rows (of K) of `columns` elements, 64 at a time one after another in shared
+    // memory; where that can be one box, it is (a box for each 64 cost 5 % of the products' time).
+    bool map_mn(CUtensorMap* m, unsigned box_columns) const {
+        const cuuint64_t row_bytes = static_cast<cuuint64_t>(stride) * 2;
+        const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(rows), wide() / 64, static_cast<cuuint64_t>(blocks)};
+        const cuuint64_t strides[3] = {row_bytes, 128, row_bytes * rows};
+        const cuuint32_t box[4] = {64, kHeadK, box_columns / 64, 1};
+        if (chunks()) return encode_map(m, base, blocks ? 4 : 3, dims, strides, box);
+        const cuuint64_t flat[2] = {wide(), static_cast<cuuint64_t>(rows)};
+        return encode_map(m, base, 2, flat, strides, box);
     }
 };
 
@@ -370,7 +389,10 @@ template <int KIND, bool A_K, bool B_K, typename T>
 bns_status head_gemm(int kind, const Operand& a, const Operand& b, HeadGemm g, int K, cudaStream_t stream) {
     const int ctas = head_ctas(g.M);
     CUtensorMap ma, mb;
-    if (!a.map(&ma, A_K ? kHeadM : 64) || !b.map(&mb, B_K ? kHeadN / ctas : 64)) return BNS_ERR_CUDA;
+    if (!(A_K ? a.map_k(&ma, kHeadM) : a.map_mn(&ma, kHeadM))) return BNS_ERR_CUDA;
+    if (!(B_K ? b.map_k(&mb, static_cast<unsigned>(kHeadN / ctas)) : b.map_mn(&mb, static_cast<unsigned>(kHeadN / ctas))))
+        return BNS_ERR_CUDA;
+    g.b_chunks = !B_K && b.chunks();
     g.tiles_m = divide_up(g.M, kHeadM * ctas);
     g.tiles_n = divide_up(g.N, kHeadN);
     g.k_blocks = divide_up(K, kHeadK);
