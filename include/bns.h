@@ -411,7 +411,8 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
  * workspace (bf16 for bf16 tensors: half an ulp of the gradients' own type per term).
  * loss, lse: float[rows].  dx, dw: the type of x and w, dense.  x and w must be 16-byte aligned; bf16
  * rows whose stride or width is no multiple of 8 elements are copied piece by piece, and fp32 tensors are
- * split into three bf16 terms whose products are added up in fp32 (the result is that of an fp32 product).
+ * split into two fp16 terms (22 bits, kept down to 2^-28 of the tensor's largest value and falling off to
+ * 2^-49 of it) whose products are added up in fp32: the result is as near as that of an fp32 product.
  * rows <= 2^24, vocabulary <= 2^28, width <= 2^20.
  */
 typedef struct {

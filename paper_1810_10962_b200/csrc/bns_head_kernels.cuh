@@ -17,8 +17,10 @@
 // by TMA (64 elements of K, 128-byte swizzle), warp 1 of the first CTA issues tcgen05.mma, warps 4-11 read the
 // accumulator back, 128 columns of a row a thread; the accumulator is double buffered.  Operands are bf16; either may be
 // stored with K or with its other dimension contiguous (G^T, and W and x as the right-hand sides of the gradients),
-// so no tensor is transposed.  fp32 tensors are split into three bf16 terms (8 + 8 + 8 bits) and the six products
-// that matter in fp32 are added up, smallest first.
+// so no tensor is transposed.  fp32 tensors are split into two fp16 terms (11 + 11 bits): scaled by a power of two that
+// brings the tensor's largest value to 2^13, high = fp16(v), low = fp16((v - high) 2^11), so that the low term keeps its bits
+// down to 2^-38 of the largest value; the products high low and low high are added up first and scaled by 2^-11, then
+// high high (the fourth is below 2^-22 of the result).  Three bf16 terms need six products for the same accuracy.
 //
 // The tensor core truncates as it accumulates: after n steps of 16 a sum has lost some n 2^-25 of itself, always towards
 // zero.  Where the result is an fp32 number (the logits' statistics, everything of fp32 tensors) the sum is therefore
@@ -28,6 +30,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_fp16.h>
 
 #include "bns.h"
 #include "bns_async.cuh"
@@ -49,6 +52,8 @@ struct HeadRing {
     static constexpr unsigned kSmem = kStages * kStage + kStaging + 1024;
 };
 constexpr int kHeadRaster = 16;        // row tiles that are swept together, so that their operand stays in L2
+constexpr float kHeadLow = 2048.f;                       // what the low fp16 term is stored times
+constexpr float kHeadTop = 8192.f;                       // where an fp32 tensor's largest value is brought to, at the least
 constexpr float kHeadLog2e = 1.4426950408889634f, kHeadLn2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------------------------------ PTX wrappers
@@ -225,8 +230,8 @@ __device__ __forceinline__ int64_t load_index(const void* p, int64_t i, int is64
 struct HeadGemm {
     int M, N;                    // rows and columns of the product that exist
     int tiles_m, tiles_n, splits;
-    int k_blocks, pairs;         // stages of K per pair of terms; 1 pair, or 6 for fp32 tensors
-    int a_pitch, b_pitch;        // elements from one bf16 term of a row to the next
+    int k_blocks, pairs;         // stages of K per pair of terms; 1 pair, or 3 for fp32 tensors
+    int a_pitch, b_pitch;        // elements from one term of a row to the next
     int b_chunks;                // B with its other dimension contiguous: its map counts that in chunks of 64, one load a stage
     // LSE and GRAD
     const void* target;          // [M]
@@ -238,7 +243,8 @@ struct HeadGemm {
     unsigned* status;            // LSE: cleared here, set by the kernel that joins the partial sums
     const float *lse, *dloss;    // GRAD: [M]
     const float* unit;           // GRAD: G holds the gradient divided by this; OUT: multiplied in again
-    unsigned short* G;           // GRAD: [tiles_n][M][1 or 3 terms][256 columns]
+    const float *a_scale, *b_scale;   // fp32: what the terms of x (LSE, GRAD) and of B have been multiplied by
+    unsigned short* G;           // GRAD: [tiles_n][M][1 or 2 terms][256 columns]
     // OUT
     void* out;                   // the tensor's type
     int64_t out_stride;
@@ -249,11 +255,16 @@ struct HeadGemm {
 
 enum { kHeadLse = 0, kHeadGrad = 1, kHeadOut = 2 };
 
-// Which terms a pair multiplies, smallest products first (the single pair of bf16 tensors is the last one).
+// Which terms a pair multiplies: low high, high low, high high (the single pair of bf16 tensors is the last one).
 __device__ __forceinline__ void head_pair(int pair, int pairs, int& a, int& b) {
-    const int p = pair + 6 - pairs;
-    a = (0x201100 >> (4 * (5 - p))) & 15;
-    b = (0x021010 >> (4 * (5 - p))) & 15;
+    const int p = pair + 3 - pairs;
+    a = p == 0;
+    b = p == 1;
+}
+// Where a segment that begins at k ends: segments do not reach over pairs.
+__device__ __forceinline__ int head_segment_end(const HeadGemm& g, int k, int k1) {
+    const int pair_end = (k / g.k_blocks + 1) * g.k_blocks;
+    return min(min(k + kHeadSegment, pair_end), k1);
 }
 
 struct HeadTile {
@@ -276,10 +287,21 @@ struct HeadTile {
     }
 };
 
+// A value (scaled already) as two fp16 numbers.
+__device__ __forceinline__ void split_half(float v, unsigned short& high, unsigned short& low) {
+    const __half h = __float2half_rn(v);
+    high = __half_as_ushort(h);
+    low = __half_as_ushort(__float2half_rn((v - __half2float(h)) * kHeadLow));
+}
+__device__ __forceinline__ uint2 pack_halves(const unsigned short (&h)[4]) {
+    return make_uint2(h[0] | static_cast<unsigned>(h[1]) << 16, h[2] | static_cast<unsigned>(h[3]) << 16);
+}
+
 // What a thread of the epilogue does with its 128 columns of a row, 32 at a time.
 template <int KIND, typename T>
 struct HeadEpilogue {
     using S = typename T::storage;
+    static constexpr bool kFp32 = sizeof(S) == 4;
     const HeadGemm& g;
     const HeadTile& t;
     int row, column0, columns;   // first column, and how many of the 128 exist
@@ -287,6 +309,7 @@ struct HeadEpilogue {
     // LSE and GRAD
     int mine = -1;               // the target's place among the 128
     bool counts = false;
+    float unscale = 1.f, c;      // LSE and GRAD: logits = unscale accumulator; c = log2(e) unscale
     float m, s;                  // LSE
     float shift, factor, one;    // GRAD
     int half, lane;
@@ -309,21 +332,24 @@ struct HeadEpilogue {
             counts = y >= 0 && y < g.V;
             const int64_t place = y - g.first - column0;
             if (counts && place >= 0 && place < columns) mine = static_cast<int>(place);
+            if constexpr (kFp32) unscale = 1.f / *g.a_scale / *g.b_scale;      // powers of two
+            c = kHeadLog2e * unscale;
         }
         if constexpr (KIND == kHeadLse) {
             m = __int_as_float(0xff800000);
             s = 0.f;
         } else if constexpr (KIND == kHeadGrad) {
             const float lse = counts ? g.lse[row] : 0.f;
-            one = counts ? g.dloss[row] / *g.unit : 0.f;
+            one = counts ? g.dloss[row] / *g.unit * (kFp32 ? kHeadTop : 1.f) : 0.f;
             // lse log2(e) = shift + rest, log2(e) being the same fp32 number as in z log2(e), so that only the
             // difference z - lse feels its rounding; rest goes into the factor
             shift = lse * kHeadLog2e;
             factor = one * exp2_fast(-fmaf(lse, kHeadLog2e, -shift));
-            constexpr int kTerms = sizeof(S) == 4 ? 3 : 1;
+            constexpr int kTerms = kFp32 ? 2 : 1;
             G_at = g.G + (static_cast<int64_t>(t.n) * g.M + first) * (kTerms * kHeadN) + half * (kHeadN / 2) + 4 * (lane & 7);
         } else {
             factor = *g.unit;
+            if constexpr (kFp32) factor *= 1.f / *g.b_scale / kHeadTop;
             const int at = column0 + 4 * (lane & 7);
             if (g.sums) sums_at = g.sums + (t.split * static_cast<int64_t>(g.M) + first) * g.N + at;
             sums_step = 4 * static_cast<int64_t>(g.N);
@@ -336,54 +362,53 @@ struct HeadEpilogue {
         if constexpr (KIND == kHeadGrad) return min(kHeadN / 2, (max(columns, 0) + kHeadK - 1) / kHeadK * kHeadK);
         return columns;
     }
-    __device__ __forceinline__ void chunk(int c, float* f) {
+    __device__ __forceinline__ void chunk(int at, float* f) {
         if constexpr (KIND == kHeadLse) {
             const float inf = __int_as_float(0x7f800000);
-            if (columns - c < 32) {
+            if (columns - at < 32) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (c + j >= columns) f[j] = -inf;
+                    if (at + j >= columns) f[j] = -inf;
             }
             float top = f[0];
 #pragma unroll
             for (int j = 1; j < 32; ++j) top = fmaxf(top, f[j]);
-            top = fmaxf(top * kHeadLog2e, m);
+            top = fmaxf(top * c, m);
             const float ref = top == -inf ? 0.f : top;
             s *= exp2_fast(m - ref);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) s += exp2_fast(fmaf(f[j], kHeadLog2e, -ref));
+            for (int j = 0; j < 32; ++j) s += exp2_fast(fmaf(f[j], c, -ref));
             m = top;
-            if (mine >= c && mine < c + 32) {
+            if (mine >= at && mine < at + 32) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (mine == c + j) g.target_logit[row] = f[j];
+                    if (mine == at + j) g.target_logit[row] = f[j] * unscale;
             }
         } else if constexpr (KIND == kHeadGrad) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                f[j] = counts && c + j < columns ? exp2_fast(fmaf(f[j], kHeadLog2e, -shift)) * factor : 0.f;
-                if (mine == c + j) f[j] -= one;
+                f[j] = counts && at + j < columns ? exp2_fast(fmaf(f[j], c, -shift)) * factor : 0.f;
+                if (mine == at + j) f[j] -= one;
             }
-            constexpr int kTerms = sizeof(S) == 4 ? 3 : 1, kStep = 4 * kTerms * kHeadN;
-            unsigned short* to = G_at + c;
+            constexpr int kTerms = kFp32 ? 2 : 1, kStep = 4 * kTerms * kHeadN;
+            unsigned short* to = G_at + at;
             spread(f, [&](int i, float (&v)[4]) {
+                if constexpr (kFp32) {
+                    unsigned short high[4], low[4];
 #pragma unroll
-                for (int term = 0; term < kTerms; ++term) {
+                    for (int j = 0; j < 4; ++j) split_half(v[j], high[j], low[j]);
+                    *reinterpret_cast<uint2*>(to + i * kStep) = pack_halves(high);
+                    *reinterpret_cast<uint2*>(to + i * kStep + kHeadN) = pack_halves(low);
+                } else {
                     Vec<BF16, 4> o;
                     o.pack(v);
-                    o.store(to + i * kStep + term * kHeadN);
-                    if (term + 1 < kTerms) {
-                        float back[4];
-                        o.unpack(back);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) v[j] -= back[j];   // what the term leaves for the next
-                    }
+                    o.store(to + i * kStep);
                 }
             });
         } else {
-            const int left = columns - c - 4 * (lane & 7);
+            const int left = columns - at - 4 * (lane & 7);
             const bool whole = g.N % 4 == 0;     // rows of sums and of the output begin at whole vectors
-            S* to = out_at + c;
+            S* to = out_at + at;
             if (!g.sums && whole) {
                 spread(f, [&](int, float (&v)[4]) {
                     scale(v);
@@ -394,7 +419,7 @@ struct HeadEpilogue {
                 });
                 return;
             }
-            float* sums = sums_at + c;
+            float* sums = sums_at + at;
             spread(f, [&](int, float (&v)[4]) {
                 if (left > 0) {
                     scale(v);
@@ -477,7 +502,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     head_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const HeadGemm g) {
     using Ring = HeadRing<CTAS>;
     constexpr int kStages = Ring::kStages;
-    constexpr bool kSegments = KIND == kHeadLse || sizeof(typename T::storage) == 4;
+    constexpr bool kFp32 = sizeof(typename T::storage) == 4, kSegments = KIND == kHeadLse || kFp32;
     extern __shared__ unsigned char raw[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
     __shared__ unsigned tmem_base;
@@ -554,15 +579,15 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 ok = wait_bounded(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up);
             issued = it;
         } else if (warp == 1 && lane == 0 && rank == 0) {
-            constexpr unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_K ? 0u : 1u << 15) | (B_K ? 0u : 1u << 16) |
+            constexpr unsigned idesc = (1u << 4) | (kFp32 ? 0u : (1u << 7) | (1u << 10)) | (A_K ? 0u : 1u << 15) | (B_K ? 0u : 1u << 16) |
                                        ((kHeadN >> 3) << 17) | ((CTAS * kHeadM >> 4) << 24);
             int it = 0, n = 0;
             bool ok = true;
             for (int id = worker; ok && id < tiles; id += workers) {
                 const HeadTile t(g, id);
-                const int step = kSegments ? kHeadSegment : t.k1 - t.k0;
-                for (int k = t.k0; ok && k < t.k1; k += step, ++n) {
-                    const int buffer = n & 1, end = min(t.k1, k + step);
+                for (int k = t.k0, end; ok && k < t.k1; k = end, ++n) {
+                    const int buffer = n & 1;
+                    end = kSegments ? head_segment_end(g, k, t.k1) : t.k1;
                     if (n >= 2 && !(ok = wait_bounded(drained + 8 * buffer, (n / 2 - 1) & 1, &gave_up))) break;
                     head::fence_after();
                     const unsigned d = tmem + buffer * kHeadN;
@@ -609,14 +634,15 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 float acc[kHeadN / 2];
 #pragma unroll
                 for (int j = 0; j < kHeadN / 2; ++j) acc[j] = 0.f;
-                for (int k = t.k0; k < t.k1; k += kHeadSegment) {
+                for (int k = t.k0; k < t.k1; k = head_segment_end(g, k, t.k1)) {
                     if (!wait_ready()) break;
+                    const float weight = kFp32 && k < 2 * g.k_blocks ? 1.f / kHeadLow : 1.f;
 #pragma unroll
                     for (int c = 0; c < kHeadN / 2; c += 16) {
                         float f[16];
                         head::load16(lanes + (n & 1) * kHeadN + c, f);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[c + j] += f[j];
+                        for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(f[j], weight, acc[c + j]);
                     }
                     give_back();
                 }
@@ -687,43 +713,96 @@ __global__ void __launch_bounds__(1024) head_unit_kernel(const void* target, int
     }
 }
 
-// Rows into bf16 terms: the first is the value rounded, the next what that leaves, and so on; each term's row is padded
-// with zeros to `pitch` elements.  One term lays out bf16 rows whose stride TMA cannot take.  Eight columns a thread.
+// bf16 rows whose stride TMA cannot take, laid out with rows of `pitch` elements, padded with zeros.
+struct HeadCopy {
+    static constexpr int kTerms = 1;
+    using From = BF16;
+    __device__ __forceinline__ static void put(const float (&v)[8], float, unsigned short* to, int) {
+        Vec<BF16, 8> o;
+        o.pack(v);
+        o.store(to);
+    }
+};
+// fp32 rows as two fp16 terms, each padded with zeros to `pitch` elements.
+struct HeadSplit {
+    static constexpr int kTerms = 2;
+    using From = F32;
+    __device__ __forceinline__ static void put(const float (&v)[8], float scale, unsigned short* to, int pitch) {
+        unsigned short high[2][4], low[2][4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) split_half(v[j] * scale, high[j / 4][j % 4], low[j / 4][j % 4]);
+        const uint2 h0 = pack_halves(high[0]), h1 = pack_halves(high[1]), l0 = pack_halves(low[0]), l1 = pack_halves(low[1]);
+        *reinterpret_cast<uint4*>(to) = make_uint4(h0.x, h0.y, h1.x, h1.y);
+        *reinterpret_cast<uint4*>(to + pitch) = make_uint4(l0.x, l0.y, l1.x, l1.y);
+    }
+};
+
+// Eight columns of a row (zeros past its end), in 16-byte words where its stride allows it.
 template <typename T>
-__global__ void __launch_bounds__(256) head_terms_kernel(const void* src, int64_t stride, int rows, int D, int terms, int pitch,
-                                                         unsigned short* dst) {
-    using S = typename T::storage;
-    constexpr int kWord = 16 / sizeof(S);
+__device__ __forceinline__ void load_eight(const typename T::storage* row, int first, int D, bool words, float (&v)[8]) {
+    constexpr int kWord = 16 / sizeof(typename T::storage);
+    if (words && first + 8 <= D) {
+#pragma unroll
+        for (int j = 0; j < 8; j += kWord) {
+            Vec<T, kWord> x;
+            float f[kWord];
+            x.load(row + first + j);
+            x.unpack(f);
+#pragma unroll
+            for (int i = 0; i < kWord; ++i) v[j + i] = f[i];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = first + j < D ? to_float<T>(row[first + j]) : 0.f;
+    }
+}
+
+// The largest finite magnitude of a matrix, as the bits of a float, into *top (which starts at 0).
+__global__ void __launch_bounds__(256) head_top_kernel(const float* src, int64_t stride, int rows, int D, unsigned* top) {
     grid_dependency_wait();
     grid_dependency_launch();
+    const int first = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
+    unsigned most = 0;
+    if (first < D) {
+        for (int64_t row = blockIdx.y * 8 + (threadIdx.x >> 5); row < rows; row += gridDim.y * 8) {
+            float v[8];
+            load_eight<F32>(src + row * stride, first, D, stride % 4 == 0, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned bits = __float_as_uint(fabsf(v[j]));
+                if (bits < 0x7f800000u) most = max(most, bits);
+            }
+        }
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if ((threadIdx.x & 31) == 0 && most) atomicMax(top, most);
+}
+
+// The power of two that brings a tensor whose largest value has these bits to [2^13, 2^14).
+__device__ __forceinline__ float head_scale(unsigned top) {
+    const int exponent = top ? static_cast<int>(top >> 23) : 127;    // biased
+    return __uint_as_float(static_cast<unsigned>(min(254, 127 + 13 + 127 - exponent)) << 23);
+}
+
+// Eight columns a thread.  For fp32 the scale is made of *top and left in *scale.
+template <typename FORM>
+__global__ void __launch_bounds__(256) head_terms_kernel(const void* src, int64_t stride, int rows, int D, int pitch,
+                                                         unsigned short* dst, const unsigned* top, float* scale) {
+    using T = typename FORM::From;
+    grid_dependency_wait();
+    grid_dependency_launch();
+    float by = 1.f;
+    if constexpr (FORM::kTerms > 1) {
+        by = head_scale(*top);
+        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *scale = by;
+    }
     const int units = pitch / 8, unit = blockIdx.x * 32 + (threadIdx.x & 31);
     if (unit >= units) return;
+    const bool words = stride % (16 / static_cast<int>(sizeof(typename T::storage))) == 0;
     for (int64_t row = blockIdx.y * 8 + (threadIdx.x >> 5); row < rows; row += gridDim.y * 8) {
-        const S* from = static_cast<const S*>(src) + row * stride + unit * 8;
         float v[8];
-        if (unit * 8 + 8 <= D && stride % kWord == 0) {
-#pragma unroll
-            for (int j = 0; j < 8; j += kWord) {
-                Vec<T, kWord> x;
-                float f[kWord];
-                x.load(from + j);
-                x.unpack(f);
-#pragma unroll
-                for (int i = 0; i < kWord; ++i) v[j + i] = f[i];
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = unit * 8 + j < D ? to_float<T>(from[j]) : 0.f;
-        }
-        for (int t = 0; t < terms; ++t) {
-            Vec<BF16, 8> o;
-            float back[8];
-            o.pack(v);
-            o.store(dst + (row * terms + t) * pitch + unit * 8);
-            o.unpack(back);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] -= back[j];
-        }
+        load_eight<T>(static_cast<const typename T::storage*>(src) + row * stride, unit * 8, D, words, v);
+        FORM::put(v, by, dst + row * FORM::kTerms * pitch + unit * 8, pitch);
     }
 }
 

@@ -217,6 +217,13 @@ int rms_backward_blocks(int rows) { return std::min(rows, sm_count() * 32); }
 constexpr size_t kHeadPieceBytes = size_t{256} << 20;   // aimed at for G of a piece, and for a piece's operand in bf16 terms
 constexpr int kHeadPieceLeast = 4096;
 
+// What the kernels leave for one another besides arrays.
+struct HeadScalars {
+    float unit;                      // G is kept in units of this
+    float x_scale, w_scale;          // fp32: what the terms of x and of the piece of w have been multiplied by
+    unsigned x_top, w_top;           // their largest magnitudes
+};
+
 struct HeadProblem {
     int T, V, D, dtype;
     bool f32, copy_x, copy_w;       // operands laid out anew in the workspace
@@ -225,7 +232,7 @@ struct HeadProblem {
     int piece, pieces;              // columns of the vocabulary at a time
     int G_pitch;
     int splits;                     // of dx along the vocabulary
-    size_t off_unit, off_x, off_w, off_G, off_partial, off_logit, off_sums, total;
+    size_t off_scalars, off_x, off_w, off_G, off_partial, off_logit, off_sums, total;
 };
 
 bns_status check_head(const bns_head* sh) {
@@ -273,8 +280,8 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     p.f32 = sh->dtype == BNS_F32;
     p.copy_x = p.f32 || !tma_rows(sh->x_stride);
     p.copy_w = p.f32 || !tma_rows(sh->w_stride);
-    p.terms = p.f32 ? 3 : 1;
-    p.pairs = p.f32 ? 6 : 1;
+    p.terms = p.f32 ? 2 : 1;
+    p.pairs = p.f32 ? 3 : 1;
     p.pitch = divide_up(p.D, kHeadK) * kHeadK;
     size_t column = 0;              // workspace bytes per column of the vocabulary
     if (p.copy_w) column = static_cast<size_t>(p.terms) * p.pitch * 2;
@@ -296,10 +303,10 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
         return here;
     };
     const size_t T = p.T;
+    p.off_scalars = take(sizeof(HeadScalars));
     if (p.copy_x) p.off_x = take(T * p.terms * p.pitch * 2);
     if (p.copy_w) p.off_w = take(static_cast<size_t>(p.piece) * p.terms * p.pitch * 2);
     if (backward) {
-        p.off_unit = take(sizeof(float));
         p.off_G = take(T * p.terms * p.G_pitch * 2);
         if (p.splits > 1 || p.pieces > 1) p.off_sums = take(T * p.splits * p.D * 4);
     } else {
@@ -396,30 +403,48 @@ bns_status head_gemm(int kind, const Operand& a, const Operand& b, HeadGemm g, i
     g.tiles_m = divide_up(g.M, kHeadM * ctas);
     g.tiles_n = divide_up(g.N, kHeadN);
     g.k_blocks = divide_up(K, kHeadK);
-    g.pairs = a.terms > 1 ? 6 : 1;
+    g.pairs = a.terms > 1 ? 3 : 1;
     g.a_pitch = a.pitch;
     g.b_pitch = b.pitch;
     return ctas == 2 ? head_gemm_on<KIND, A_K, B_K, T, 2>(kind, ma, mb, g, stream)
                      : head_gemm_on<KIND, A_K, B_K, T, 1>(kind, ma, mb, g, stream);
 }
 
-void lay_out(int dtype, const void* src, int64_t stride, int rows, int D, int terms, int pitch, void* dst, cudaStream_t stream) {
-    const Shape grid{static_cast<unsigned>(divide_up(pitch / 8, 32)), 256, 1, static_cast<unsigned>(std::min(divide_up(rows, 8), 65535))};
-    BNS_LM_BY_TYPE(dtype, (launch(BNS_KERNEL_HEAD_VECTOR, head_terms_kernel<T>, grid, 0, stream, src, stride, rows, D, terms, pitch,
-                                  static_cast<unsigned short*>(dst))));
+// Rows laid out in the workspace: bf16 as they are, fp32 as two fp16 terms scaled by the largest value.
+bns_status lay_out(const HeadProblem& p, const void* src, int64_t stride, int rows, void* dst, unsigned* top, float* scale, cudaStream_t stream) {
+    const unsigned across = static_cast<unsigned>(divide_up(p.pitch / 8, 32)), down = static_cast<unsigned>(std::min(divide_up(rows, 8), 65535));
+    unsigned short* to = static_cast<unsigned short*>(dst);
+    if (!p.f32) {
+        launch(BNS_KERNEL_HEAD_VECTOR, head_terms_kernel<HeadCopy>, Shape{across, 256, 1, down}, 0, stream, src, stride, rows, p.D, p.pitch,
+               to, static_cast<const unsigned*>(nullptr), static_cast<float*>(nullptr));
+        return last_error();
+    }
+    if (cudaMemsetAsync(top, 0, sizeof(unsigned), stream) != cudaSuccess) return BNS_ERR_CUDA;
+    const unsigned few = std::max(1u, std::min(down, static_cast<unsigned>(sm_count()) * 8 / across));
+    launch(BNS_KERNEL_HEAD_VECTOR, head_top_kernel, Shape{across, 256, 1, few}, 0, stream, static_cast<const float*>(src), stride, rows,
+           p.D, top);
+    launch(BNS_KERNEL_HEAD_VECTOR, head_terms_kernel<HeadSplit>, Shape{across, 256, 1, down}, 0, stream, src, stride, rows, p.D, p.pitch,
+           to, static_cast<const unsigned*>(top), scale);
+    return last_error();
 }
 
-Operand rows_of_x(const HeadProblem& p, const bns_head* sh, const void* x, char* ws) {
-    if (p.copy_x) return {ws + p.off_x, static_cast<int64_t>(p.terms) * p.pitch, p.T, p.pitch, p.terms, p.pitch};
-    return {x, sh->x_stride, p.T, p.D, 1, 0};
+// x as an operand; a copy is laid out here.
+bns_status rows_of_x(const HeadProblem& p, const bns_head* sh, const void* x, char* ws, cudaStream_t stream, Operand& o) {
+    o = Operand{x, sh->x_stride, p.T, p.D, 1, 0};
+    if (!p.copy_x) return BNS_OK;
+    o = Operand{ws + p.off_x, static_cast<int64_t>(p.terms) * p.pitch, p.T, p.pitch, p.terms, p.pitch};
+    HeadScalars* s = reinterpret_cast<HeadScalars*>(ws + p.off_scalars);
+    return lay_out(p, x, sh->x_stride, p.T, ws + p.off_x, &s->x_top, &s->x_scale, stream);
 }
 
-// Rows [first, first + count) of w; copied ones are laid out here.
-Operand rows_of_w(const HeadProblem& p, const bns_head* sh, const void* w, int first, int count, char* ws, cudaStream_t stream) {
+// Rows [first, first + count) of w.
+bns_status rows_of_w(const HeadProblem& p, const bns_head* sh, const void* w, int first, int count, char* ws, cudaStream_t stream, Operand& o) {
     const char* from = static_cast<const char*>(w) + static_cast<int64_t>(first) * sh->w_stride * elem_bytes(p.dtype);
-    if (!p.copy_w) return {from, sh->w_stride, count, p.D, 1, 0};
-    lay_out(p.dtype, from, sh->w_stride, count, p.D, p.terms, p.pitch, ws + p.off_w, stream);
-    return {ws + p.off_w, static_cast<int64_t>(p.terms) * p.pitch, count, p.pitch, p.terms, p.pitch};
+    o = Operand{from, sh->w_stride, count, p.D, 1, 0};
+    if (!p.copy_w) return BNS_OK;
+    o = Operand{ws + p.off_w, static_cast<int64_t>(p.terms) * p.pitch, count, p.pitch, p.terms, p.pitch};
+    HeadScalars* s = reinterpret_cast<HeadScalars*>(ws + p.off_scalars);
+    return lay_out(p, from, sh->w_stride, count, ws + p.off_w, &s->w_top, &s->w_scale, stream);
 }
 
 // ------------------------------------------------------------------------------------ distillation
@@ -574,13 +599,16 @@ bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(workspace);
     if (p.T == 0) return cudaMemsetAsync(ws, 0, sizeof(uint32_t), stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
-    if (p.copy_x) lay_out(p.dtype, x, shape->x_stride, p.T, p.D, p.terms, p.pitch, ws + p.off_x, stream);
-    const Operand xs = rows_of_x(p, shape, x, ws);
+    Operand xs, rows;
+    st = rows_of_x(p, shape, x, ws, stream, xs);
+    if (st != BNS_OK) return st;
+    HeadScalars* scalars = reinterpret_cast<HeadScalars*>(ws + p.off_scalars);
     float2* partial = reinterpret_cast<float2*>(ws + p.off_partial);
     int tiles = 0;
     for (int first = 0; first < p.V; first += p.piece) {
         const int count = std::min(p.piece, p.V - first);
-        const Operand rows = rows_of_w(p, shape, w, first, count, ws, stream);
+        st = rows_of_w(p, shape, w, first, count, ws, stream, rows);
+        if (st != BNS_OK) return st;
         HeadGemm g{};
         g.M = p.T;
         g.N = count;
@@ -592,7 +620,9 @@ bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x
         g.partial = partial + static_cast<size_t>(tiles) * p.T;
         g.target_logit = reinterpret_cast<float*>(ws + p.off_logit);
         g.status = first == 0 ? reinterpret_cast<unsigned*>(ws) : nullptr;
-        st = head_gemm<kHeadLse, true, true, BF16>(BNS_KERNEL_HEAD_LOGITS, xs, rows, g, p.D, stream);
+        g.a_scale = &scalars->x_scale;
+        g.b_scale = &scalars->w_scale;
+        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadLse, true, true, T>(BNS_KERNEL_HEAD_LOGITS, xs, rows, g, p.D, stream)));
         if (st != BNS_OK) return st;
         tiles += 2 * divide_up(count, kHeadN);
     }
@@ -619,14 +649,17 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
     const size_t eb = elem_bytes(p.dtype);
     if (p.T == 0)
         return cudaMemsetAsync(dw, 0, eb * p.V * p.D, stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
-    if (p.copy_x) lay_out(p.dtype, x, shape->x_stride, p.T, p.D, p.terms, p.pitch, ws + p.off_x, stream);
-    const Operand xs = rows_of_x(p, shape, x, ws);
-    float* unit = reinterpret_cast<float*>(ws + p.off_unit);
+    Operand xs, rows;
+    st = rows_of_x(p, shape, x, ws, stream, xs);
+    if (st != BNS_OK) return st;
+    HeadScalars* scalars = reinterpret_cast<HeadScalars*>(ws + p.off_scalars);
+    float* unit = &scalars->unit;
     launch(BNS_KERNEL_HEAD_VECTOR, head_unit_kernel, Shape{1, 1024}, 0, stream, target, shape->target_is_int64, dloss, p.T, p.V, unit);
     float* sums = p.splits > 1 || p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sums) : nullptr;
     for (int first = 0; first < p.V; first += p.piece) {
         const int count = std::min(p.piece, p.V - first);
-        const Operand rows = rows_of_w(p, shape, w, first, count, ws, stream);
+        st = rows_of_w(p, shape, w, first, count, ws, stream, rows);
+        if (st != BNS_OK) return st;
         HeadGemm g{};
         g.M = p.T;
         g.N = count;
@@ -638,6 +671,8 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         g.lse = lse;
         g.dloss = dloss;
         g.unit = unit;
+        g.a_scale = &scalars->x_scale;
+        g.b_scale = &scalars->w_scale;
         g.G = reinterpret_cast<unsigned short*>(ws + p.off_G);
         BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadGrad, true, true, T>(BNS_KERNEL_HEAD_GRADIENT, xs, rows, g, p.D, stream)));
         if (st != BNS_OK) return st;
@@ -647,6 +682,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         o.N = p.D;
         o.splits = p.splits;
         o.unit = unit;
+        o.b_scale = &scalars->w_scale;
         o.out = dx;
         o.out_stride = p.D;
         o.sums = sums;
@@ -659,6 +695,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         q.N = p.D;
         q.splits = 1;
         q.unit = unit;
+        q.b_scale = &scalars->x_scale;
         q.out = static_cast<char*>(dw) + static_cast<size_t>(first) * p.D * eb;
         q.out_stride = p.D;
         BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, false, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, xs, q, p.T, stream)));
