@@ -242,7 +242,8 @@ struct HeadGemm {
     float* target_logit;         // LSE: [M]
     unsigned* status;            // LSE: cleared here, set by the kernel that joins the partial sums
     const float *lse, *dloss;    // GRAD: [M]
-    const float* unit;           // GRAD: G holds the gradient divided by this; OUT: multiplied in again
+    float* unit;                 // GRAD: G holds the gradient divided by this; OUT: multiplied in again
+    int find_unit;               // GRAD: every warp of the epilogue finds it itself, block 0 leaves it there
     const float *a_scale, *b_scale;   // fp32: what the terms of x (LSE, GRAD) and of B have been multiplied by
     unsigned short* G;           // GRAD: [tiles_n][M][1 or 2 terms][256 columns]
     // OUT
@@ -251,6 +252,11 @@ struct HeadGemm {
     float* sums;                 // [splits][M][N] fp32, or NULL: `out` is written directly
     int add;                     // add what `sums` holds
     int last;                    // with sums: write `out` (one split only)
+    // dW, after the last piece: an idle warp of each block adds up dx's parts
+    const float* join_sums;
+    void* join_out;
+    int join_parts;
+    int64_t join_total;          // elements of a part
 };
 
 enum { kHeadLse = 0, kHeadGrad = 1, kHeadOut = 2 };
@@ -287,6 +293,56 @@ struct HeadTile {
     }
 };
 
+// The largest |dloss| of the rows that count, over a warp's share of them: G is kept in units of it (1 if that is zero).
+// With one weight for all rows, as a mean has, the largest entry of a row of G is then p - 1 itself; its rounding to
+// bf16 does not carry that of the weight, which would be the same in every row and add up.
+__device__ __forceinline__ float head_unit(const void* target, int target64, const float* dloss, int rows, int V, int first, int step) {
+    float top = 0.f;
+#pragma unroll 4
+    for (int t = first; t < rows; t += step) {
+        const int64_t y = head::load_index(target, t, target64);
+        const float g = fabsf(dloss[t]);
+        if (y >= 0 && y < V && g < __int_as_float(0x7f800000)) top = fmaxf(top, g);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    return top;
+}
+
+// Adds up the parts of a product in their order and rounds once: vectors of V elements, lane `first` of `step`.
+template <typename T, int V>
+__device__ __forceinline__ void head_join_parts(const HeadGemm& g, int64_t first, int64_t step) {
+    constexpr int kBatch = 4;
+    const int64_t vectors = g.join_total / V;
+    for (int64_t i0 = first; i0 < vectors; i0 += step * kBatch) {
+        float v[kBatch][V] = {};
+#pragma unroll 4
+        for (int s = 0; s < g.join_parts; ++s) {
+            Vec<F32, V> x[kBatch];
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b)
+                if (i0 + b * step < vectors) x[b].load(g.join_sums + s * g.join_total + (i0 + b * step) * V);
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                if (i0 + b * step < vectors) {
+                    float f[V];
+                    x[b].unpack(f);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) v[b][j] += f[j];
+                }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            if (i0 + b * step < vectors) {
+                Vec<T, V> o;
+                o.pack(v[b]);
+                o.store(static_cast<typename T::storage*>(g.join_out) + (i0 + b * step) * V);
+            }
+        }
+    }
+}
+
 // A value (scaled already) as two fp16 numbers.
 __device__ __forceinline__ void split_half(float v, unsigned short& high, unsigned short& low) {
     const __half h = __float2half_rn(v);
@@ -321,7 +377,7 @@ struct HeadEpilogue {
     S* out_at = nullptr;
     int64_t sums_step = 0, out_step = 0;
 
-    __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_, float4* stage_)
+    __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_, float4* stage_, float unit)
         : g(g_), t(t_), row(row_), column0(t_.n * kHeadN + half_ * (kHeadN / 2)), in(row_ < g_.M), half(half_),
           lane(threadIdx.x & 31), stage(stage_) {
         const int64_t first = row - lane + (lane >> 3);
@@ -340,7 +396,7 @@ struct HeadEpilogue {
             s = 0.f;
         } else if constexpr (KIND == kHeadGrad) {
             const float lse = counts ? g.lse[row] : 0.f;
-            one = counts ? g.dloss[row] / *g.unit * (kFp32 ? kHeadTop : 1.f) : 0.f;
+            one = counts ? g.dloss[row] / unit * (kFp32 ? kHeadTop : 1.f) : 0.f;
             // lse log2(e) = shift + rest, log2(e) being the same fp32 number as in z log2(e), so that only the
             // difference z - lse feels its rounding; rest goes into the factor
             shift = lse * kHeadLog2e;
@@ -348,7 +404,7 @@ struct HeadEpilogue {
             constexpr int kTerms = kFp32 ? 2 : 1;
             G_at = g.G + (static_cast<int64_t>(t.n) * g.M + first) * (kTerms * kHeadN) + half * (kHeadN / 2) + 4 * (lane & 7);
         } else {
-            factor = *g.unit;
+            factor = unit;
             if constexpr (kFp32) factor *= 1.f / *g.b_scale / kHeadTop;
             const int at = column0 + 4 * (lane & 7);
             if (g.sums) sums_at = g.sums + (t.split * static_cast<int64_t>(g.M) + first) * g.N + at;
@@ -608,16 +664,33 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 }
             }
         }
+        if constexpr (KIND == kHeadOut && !A_K) {
+            if (warp == 3 && g.join_parts) {
+                const int64_t first = blockIdx.x * 32 + lane, step = gridDim.x * 32;
+                if (g.join_total % 4 == 0)       // a part begins at a 16-byte boundary
+                    head_join_parts<T, 4>(g, first, step);
+                else
+                    head_join_parts<T, 1>(g, first, step);
+            }
+        }
         __syncwarp();
     } else {
         const int slot = warp & 3, half = (warp - 4) >> 2;
         float4* stage = reinterpret_cast<float4*>(raw + (ring - head_raw) + kStages * Ring::kStage) + (warp - 4) * 256;
         if (KIND == kHeadLse && blockIdx.x == 0 && threadIdx.x == 128 && g.status) *g.status = 0;
+        float unit = 1.f;
+        if (KIND == kHeadGrad && g.find_unit) {
+            unit = head_unit(g.target, g.target64, g.dloss, g.M, g.V, lane, 32);
+            unit = unit > 0.f ? unit : 1.f;
+            if (blockIdx.x == 0 && threadIdx.x == 128) *g.unit = unit;
+        } else if (KIND != kHeadLse) {
+            unit = *g.unit;
+        }
         int n = 0;
         bool ok = true;
         for (int id = worker; ok && id < tiles; id += workers) {
             const HeadTile t(g, id);
-            HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half, stage);
+            HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half, stage, unit);
             const unsigned lanes = tmem + (static_cast<unsigned>(slot * 32) << 16) + half * (kHeadN / 2);
             auto wait_ready = [&]() {
                 ok = __all_sync(0xffffffffu, wait_bounded(ready + 8 * (n & 1), (n / 2) & 1, &gave_up));
@@ -687,29 +760,18 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
 }
 
 // ------------------------------------------------------------------------------------ around the products
-// The largest |dloss| of the rows that count (1 if that is zero): G is kept in units of it.  With one weight for all
-// rows, as a mean has, the largest entry of a row of G is then p - 1 itself; its rounding to bf16 does not carry that
-// of the weight, which would be the same in every row and add up.
 __global__ void __launch_bounds__(1024) head_unit_kernel(const void* target, int target64, const float* dloss, int rows, int V,
                                                          float* unit) {
     __shared__ float fold[32];
     grid_dependency_wait();
     grid_dependency_launch();
-    float top = 0.f;
-    for (int t = threadIdx.x; t < rows; t += 1024) {
-        const int64_t y = head::load_index(target, t, target64);
-        const float g = fabsf(dloss[t]);
-        if (y >= 0 && y < V && g < __int_as_float(0x7f800000)) top = fmaxf(top, g);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float top = head_unit(target, target64, dloss, rows, V, threadIdx.x, 1024);
     if ((threadIdx.x & 31) == 0) fold[threadIdx.x >> 5] = top;
     __syncthreads();
-    if (threadIdx.x < 32) {
-        top = fold[threadIdx.x];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (threadIdx.x == 0) *unit = top > 0.f ? top : 1.f;
+    if (threadIdx.x == 0) {
+        float all = 0.f;
+        for (int w = 0; w < 32; ++w) all = fmaxf(all, fold[w]);
+        *unit = all > 0.f ? all : 1.f;
     }
 }
 
@@ -844,48 +906,6 @@ __global__ void __launch_bounds__(1024) head_join_kernel(const float2* partial, 
     // the difference to the largest first: where the model is sure, lse and the target's logit are nearly equal
     loss[row] = y >= 0 && y < V ? (fmaf(-target_logit[row], kHeadLog2e, v.x) + rest) * kHeadLn2 : 0.f;
     if (y >= V) atomicOr(status, BNS_FLAG_BAD_TARGET);
-}
-
-// Adds up the parts of a product in a fixed order, and rounds once.  `total` elements a part, V at a time; GROUPS threads an
-// element each take every GROUPS-th part (many parts come with few elements: four threads shorten the chain of loads).
-template <typename T, int V, int GROUPS>
-__global__ void __launch_bounds__(256) head_sum_kernel(const float* sums, int parts, int64_t total, void* out) {
-    constexpr int kPer = 256 / GROUPS;
-    __shared__ float fold[GROUPS][kPer][V];
-    grid_dependency_wait();
-    grid_dependency_launch();
-    const int at = threadIdx.x % kPer, group = threadIdx.x / kPer;
-    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kPer * V; i0 < total; i0 += static_cast<int64_t>(gridDim.x) * kPer * V) {
-        const int64_t i = i0 + at * V;
-        float v[V] = {};
-        if (i < total) {
-#pragma unroll 10
-            for (int s = group; s < parts; s += GROUPS) {
-                Vec<F32, V> x;
-                float f[V];
-                x.load(sums + s * total + i);
-                x.unpack(f);
-#pragma unroll
-                for (int j = 0; j < V; ++j) v[j] += f[j];
-            }
-        }
-        if constexpr (GROUPS > 1) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) fold[group][at][j] = v[j];
-            __syncthreads();
-            if (group == 0) {
-                for (int q = 1; q < GROUPS; ++q)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) v[j] += fold[q][at][j];
-            }
-            __syncthreads();
-        }
-        if (group == 0 && i < total) {
-            Vec<T, V> o;
-            o.pack(v);
-            o.store(static_cast<typename T::storage*>(out) + i);
-        }
-    }
 }
 
 }  // namespace bns

@@ -386,7 +386,8 @@ bns_status head_gemm_on(int kind, const CUtensorMap& ma, const CUtensorMap& mb, 
     }
     const int64_t tiles = static_cast<int64_t>(g.tiles_m) * g.tiles_n * g.splits;
     if (tiles >= int64_t{1} << 30) return BNS_ERR_SHAPE;
-    launch(kind, kernel, Shape{static_cast<unsigned>(std::min<int64_t>(tiles, sm_count() / CTAS)) * CTAS, kHeadThreads, CTAS}, smem,
+    const int64_t workers = sm_count() / CTAS;
+    launch(kind, kernel, Shape{static_cast<unsigned>(g.join_parts ? workers : std::min(tiles, workers)) * CTAS, kHeadThreads, CTAS}, smem,
            stream, ma, mb, g);
     return last_error();
 }
@@ -654,7 +655,10 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
     if (st != BNS_OK) return st;
     HeadScalars* scalars = reinterpret_cast<HeadScalars*>(ws + p.off_scalars);
     float* unit = &scalars->unit;
-    launch(BNS_KERNEL_HEAD_VECTOR, head_unit_kernel, Shape{1, 1024}, 0, stream, target, shape->target_is_int64, dloss, p.T, p.V, unit);
+    // few rows: each warp finds the unit itself, under the first tile's copies; a launch costs some 3 us
+    const bool find_unit = p.T <= 1024;
+    if (!find_unit)
+        launch(BNS_KERNEL_HEAD_VECTOR, head_unit_kernel, Shape{1, 1024}, 0, stream, target, shape->target_is_int64, dloss, p.T, p.V, unit);
     float* sums = p.splits > 1 || p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sums) : nullptr;
     for (int first = 0; first < p.V; first += p.piece) {
         const int count = std::min(p.piece, p.V - first);
@@ -671,6 +675,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         g.lse = lse;
         g.dloss = dloss;
         g.unit = unit;
+        g.find_unit = find_unit;
         g.a_scale = &scalars->x_scale;
         g.b_scale = &scalars->w_scale;
         g.G = reinterpret_cast<unsigned short*>(ws + p.off_G);
@@ -695,23 +700,17 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         q.N = p.D;
         q.splits = 1;
         q.unit = unit;
+        if (p.splits > 1 && first + count == p.V) {
+            q.join_sums = sums;
+            q.join_out = dx;
+            q.join_parts = p.splits;
+            q.join_total = static_cast<int64_t>(p.T) * p.D;
+        }
         q.b_scale = &scalars->x_scale;
         q.out = static_cast<char*>(dw) + static_cast<size_t>(first) * p.D * eb;
         q.out_stride = p.D;
         BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, false, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, xs, q, p.T, stream)));
         if (st != BNS_OK) return st;
-    }
-    if (p.splits > 1) {
-        const int64_t total = static_cast<int64_t>(p.T) * p.D;
-        const int V = total % 4 ? 1 : 4;         // a part begins at a 16-byte boundary
-        const int groups = p.splits > 8 ? 4 : 1;
-        const Shape grid{static_cast<unsigned>(std::min<int64_t>(divide_up<int64_t>(total, 256 / groups * V), sm_count() * 16)), 256};
-        const float* parts = sums;
-        BNS_LM_BY_TYPE(p.dtype, {
-            auto kernel = V == 4 ? (groups == 4 ? head_sum_kernel<T, 4, 4> : head_sum_kernel<T, 4, 1>)
-                                 : (groups == 4 ? head_sum_kernel<T, 1, 4> : head_sum_kernel<T, 1, 1>);
-            launch(BNS_KERNEL_HEAD_VECTOR, kernel, grid, 0, stream, parts, p.splits, total, dx);
-        });
     }
     return last_error();
 }

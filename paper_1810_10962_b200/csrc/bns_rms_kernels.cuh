@@ -487,7 +487,9 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
     constexpr int NV = kRmsVectors<V, EPT>;
     __shared__ BlockExchange ex;
     const int B = blockDim.x;
-    const RowPhase<S, V, LOOSE> at(static_cast<const S*>(a.h) + blockIdx.x * a.h_stride, a.D);
+    // last row first: its h is what the forward kernel wrote last and may still be in L2 (1 % where it directly follows)
+    auto row_of = [&](int64_t step) { return a.rows - 1 - step; };
+    const RowPhase<S, V, LOOSE> at(static_cast<const S*>(a.h) + row_of(blockIdx.x) * a.h_stride, a.D);
     const int vectors = at.vectors;
     const bool aligned = !LOOSE && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     grid_dependency_wait();
@@ -515,8 +517,9 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
         next_rstd = a.rstd[row];
     };
     int turn = 0;
-    if (blockIdx.x < a.rows) fetch(blockIdx.x);
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    if (blockIdx.x < a.rows) fetch(row_of(blockIdx.x));
+    for (int64_t step = blockIdx.x; step < a.rows; step += gridDim.x, turn ^= 1) {
+        const int64_t row = row_of(step);
         const float rstd = next_rstd, extra_y = next_extra_y * extra_w, extra_xhat = next_extra_h * rstd;
         const S* dh = static_cast<const S*>(a.dh) + (a.dh ? row * a.dh_stride : 0);
         if (kAhead)
@@ -550,7 +553,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
             extra_dw = fmaf(next_extra_y, extra_xhat, extra_dw);
             sum = fmaf(extra_y, extra_xhat, sum);
         }
-        if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
+        if (step + gridDim.x < a.rows) fetch(row_of(step + gridDim.x));
         block_exchange<false>(sum, none, ex, turn);
         const float c = sum * a.inv_D;
         S* dx = static_cast<S*>(a.dx) + row * a.D;

@@ -234,7 +234,7 @@ def linear_cross_entropy_forward(x, w, target, workspace=None):
     are left out: their loss is 0.  The caller takes the mean, or whatever it wants, of the losses."""
     _, shape, at = _head_inputs(x, w, target)
     device, lib = x.device, _load()
-    loss, lse = _vector_of(x), _vector_of(x)
+    loss, lse = torch.empty_like(target, dtype=torch.float32), torch.empty_like(target, dtype=torch.float32)
     workspace = _scratch(workspace, lib.bns_linear_cross_entropy_workspace_bytes(shape, 0), device)
     _check(lib.bns_linear_cross_entropy_forward(shape, x.data_ptr(), w.data_ptr(), at, loss.data_ptr(),
                                                 lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(device)),
@@ -296,7 +296,7 @@ def topk_distillation_step(logits, teacher, index, dloss, temperature=1.0):
     the rows, say)."""
     fields, shape, at = _distillation_inputs(logits, teacher, index, temperature)
     device = logits.device
-    loss = _vector_of(logits)
+    loss = torch.empty_like(dloss) if dloss.shape == logits.shape[:-1] else _vector_of(logits)
     dlogits = _like(logits)
     _check(_load().bns_topk_distillation_step(shape, logits.data_ptr(), teacher.data_ptr(), at,
                                               _vector(dloss, fields.rows, "dloss", device), loss.data_ptr(),
