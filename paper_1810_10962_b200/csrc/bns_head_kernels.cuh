@@ -132,6 +132,24 @@ __device__ __forceinline__ void commit(unsigned bar) {
             "h"(static_cast<unsigned short>(3))
             : "memory");
 }
+// Boxes from shared to global memory, in groups that a thread waits for.
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, unsigned src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, unsigned src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y),
+                 "r"(z), "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// At most `LEFT` of the thread's groups have still to read their shared memory.
+template <int LEFT>
+__device__ __forceinline__ void wait_stores_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ void wait_stores() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 template <int CTAS>
@@ -245,10 +263,10 @@ struct HeadGemm {
     float* unit;                 // GRAD: G holds the gradient divided by this; OUT: multiplied in again
     int find_unit;               // GRAD: every warp of the epilogue finds it itself, block 0 leaves it there
     const float *a_scale, *b_scale;   // fp32: what the terms of x (LSE, GRAD) and of B have been multiplied by
-    unsigned short* G;           // GRAD: [tiles_n][M][1 or 2 terms][256 columns]
     // OUT
     void* out;                   // the tensor's type
     int64_t out_stride;
+    int out_boxes;               // OUT: rows of `out` are whole 16-byte words, so it is written by TMA
     float* sums;                 // [splits][M][N] fp32, or NULL: `out` is written directly
     int add;                     // add what `sums` holds
     int last;                    // with sums: write `out` (one split only)
@@ -370,16 +388,17 @@ struct HeadEpilogue {
     float shift, factor, one;    // GRAD
     int half, lane;
     float4* stage;               // the warp's 32 x 128 bytes
+    const CUtensorMap* map;      // of G, or of the output
+    int& turn;                   // of the two buffers
     // where the lane's four columns of the warp's row lane / 8 go, the step to four rows below, and rows that exist
     int rows_left;
-    unsigned short* G_at = nullptr;
     float* sums_at = nullptr;
     S* out_at = nullptr;
     int64_t sums_step = 0, out_step = 0;
 
-    __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_, float4* stage_, float unit)
+    __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_, float4* stage_, const CUtensorMap* map_, int& turn_, float unit)
         : g(g_), t(t_), row(row_), column0(t_.n * kHeadN + half_ * (kHeadN / 2)), in(row_ < g_.M), half(half_),
-          lane(threadIdx.x & 31), stage(stage_) {
+          lane(threadIdx.x & 31), stage(stage_), map(map_), turn(turn_) {
         const int64_t first = row - lane + (lane >> 3);
         rows_left = static_cast<int>(g.M - first);
         columns = min(kHeadN / 2, g.N - column0);
@@ -401,8 +420,6 @@ struct HeadEpilogue {
             // difference z - lse feels its rounding; rest goes into the factor
             shift = lse * kHeadLog2e;
             factor = one * exp2_fast(-fmaf(lse, kHeadLog2e, -shift));
-            constexpr int kTerms = kFp32 ? 2 : 1;
-            G_at = g.G + (static_cast<int64_t>(t.n) * g.M + first) * (kTerms * kHeadN) + half * (kHeadN / 2) + 4 * (lane & 7);
         } else {
             factor = unit;
             if constexpr (kFp32) factor *= 1.f / *g.b_scale / kHeadTop;
@@ -446,33 +463,39 @@ struct HeadEpilogue {
                 f[j] = counts && at + j < columns ? exp2_fast(fmaf(f[j], c, -shift)) * factor : 0.f;
                 if (mine == at + j) f[j] -= one;
             }
-            constexpr int kTerms = kFp32 ? 2 : 1, kStep = 4 * kTerms * kHeadN;
-            unsigned short* to = G_at + at;
-            spread(f, [&](int i, float (&v)[4]) {
-                if constexpr (kFp32) {
-                    unsigned short high[4], low[4];
+            if constexpr (kFp32) {
+                unsigned high[16], low[16];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) split_half(v[j], high[j], low[j]);
-                    *reinterpret_cast<uint2*>(to + i * kStep) = pack_halves(high);
-                    *reinterpret_cast<uint2*>(to + i * kStep + kHeadN) = pack_halves(low);
-                } else {
-                    Vec<BF16, 4> o;
-                    o.pack(v);
-                    o.store(to + i * kStep);
+                for (int j = 0; j < 16; ++j) {
+                    unsigned short h0, h1, l0, l1;
+                    split_half(f[2 * j], h0, l0);
+                    split_half(f[2 * j + 1], h1, l1);
+                    high[j] = h0 | static_cast<unsigned>(h1) << 16;
+                    low[j] = l0 | static_cast<unsigned>(l1) << 16;
                 }
-            });
+                send(high, half * (kHeadN / 2) + at, t.n);
+                send(low, kHeadN + half * (kHeadN / 2) + at, t.n);
+            } else {
+                unsigned w[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) w[j] = pack_pair(f[2 * j], f[2 * j + 1]);
+                send(w, half * (kHeadN / 2) + at, t.n);
+            }
         } else {
             const int left = columns - at - 4 * (lane & 7);
             const bool whole = g.N % 4 == 0;     // rows of sums and of the output begin at whole vectors
             S* to = out_at + at;
-            if (!g.sums && whole) {
-                spread(f, [&](int, float (&v)[4]) {
-                    scale(v);
-                    Vec<T, 4> o;
-                    o.pack(v);
-                    if (left > 0) o.store(to);
-                    to += out_step;
-                });
+            if (g.out_boxes) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) split_pair(mul2(make_pair(f[j], f[j + 1]), make_pair(factor, factor)), f[j], f[j + 1]);
+                if constexpr (kFp32) {
+                    send_floats(f, column0 + at);
+                } else {
+                    unsigned w[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) w[j] = pack_pair(f[2 * j], f[2 * j + 1]);
+                    send(w, column0 + at, -1);
+                }
                 return;
             }
             float* sums = sums_at + at;
@@ -496,6 +519,45 @@ struct HeadEpilogue {
                 to += out_step;
             });
         }
+    }
+    __device__ __forceinline__ static unsigned pack_pair(float lo, float hi) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const unsigned*>(&h);
+    }
+    // The warp's 32 rows x 32 columns of 16 bits, a row a lane, into shared memory (64-byte rows, 64-byte swizzle) and out
+    // by TMA, which drops rows and columns past the tensor's end.  Two buffers; z < 0: the map has two dimensions.
+    __device__ __forceinline__ void send(const unsigned (&w)[16], int x, int z) {
+        if (lane == 0) head::wait_stores_read<1>();
+        __syncwarp();
+        const unsigned buffer = smem_address(stage) + turn * 2048;
+        turn ^= 1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4)),
+                         "r"(w[4 * u]), "r"(w[4 * u + 1]), "r"(w[4 * u + 2]), "r"(w[4 * u + 3])
+                         : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0 && row < g.M) {
+            if (z < 0)
+                head::tma_store(map, buffer, x, row);
+            else
+                head::tma_store(map, buffer, x, row, z);
+        }
+    }
+    // The same for fp32: 128-byte rows, 128-byte swizzle, one buffer.
+    __device__ __forceinline__ void send_floats(const float* f, int x) {
+        if (lane == 0) head::wait_stores_read<0>();
+        __syncwarp();
+        const unsigned buffer = smem_address(stage);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + lane * 128 + ((u ^ (lane & 7)) << 4)), "f"(f[4 * u]),
+                         "f"(f[4 * u + 1]), "f"(f[4 * u + 2]), "f"(f[4 * u + 3])
+                         : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0 && row < g.M) head::tma_store(map, buffer, x, row);
     }
     __device__ __forceinline__ void scale(float (&v)[4]) const {
         const pair_t by = make_pair(factor, factor);
@@ -525,7 +587,7 @@ struct HeadEpilogue {
     }
     // Turns the warp's 32 rows x 32 columns, a row a lane, through shared memory into eight lanes a row: put(i, v) gets
     // columns 4 (lane % 8) .. + 3 of the warp's row 4 i + lane / 8, so that a store covers 64 or 128 contiguous bytes of a
-    // row (a row a lane writes half sectors).
+    // row.  For sums and for outputs that TMA cannot write.
     template <typename Put>
     __device__ __forceinline__ void spread(const float* f, Put&& put) const {
         __syncwarp();
@@ -555,7 +617,8 @@ struct HeadEpilogue {
 
 template <int KIND, bool A_K, bool B_K, typename T, int CTAS>
 __global__ void __launch_bounds__(kHeadThreads, 1)
-    head_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const HeadGemm g) {
+    head_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                     const __grid_constant__ CUtensorMap map_c, const HeadGemm g) {
     using Ring = HeadRing<CTAS>;
     constexpr int kStages = Ring::kStages;
     constexpr bool kFp32 = sizeof(typename T::storage) == 4, kSegments = KIND == kHeadLse || kFp32;
@@ -686,11 +749,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         } else if (KIND != kHeadLse) {
             unit = *g.unit;
         }
-        int n = 0;
+        int n = 0, turn = 0;
         bool ok = true;
         for (int id = worker; ok && id < tiles; id += workers) {
             const HeadTile t(g, id);
-            HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half, stage, unit);
+            HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half, stage, &map_c, turn, unit);
             const unsigned lanes = tmem + (static_cast<unsigned>(slot * 32) << 16) + half * (kHeadN / 2);
             auto wait_ready = [&]() {
                 ok = __all_sync(0xffffffffu, wait_bounded(ready + 8 * (n & 1), (n / 2) & 1, &gave_up));
@@ -737,6 +800,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 give_back();
             }
         }
+        if (KIND != kHeadLse && lane == 0) head::wait_stores();
     }
     __syncthreads();
     if (gave_up) {

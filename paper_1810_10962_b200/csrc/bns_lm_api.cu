@@ -317,8 +317,9 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     return p;
 }
 
-// Tensor map of bf16 values; the box is 64 elements (128 bytes, swizzled) by box[1] by ...
-bool encode_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+// Tensor map; operands are 16-bit values in boxes of 64 (128 bytes, swizzled) by box[1] by ...
+bool encode_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+                CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -332,8 +333,8 @@ bool encode_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* 
         entry.store(fn, std::memory_order_relaxed);
     }
     const cuuint32_t steps[4] = {1, 1, 1, 1};
-    return reinterpret_cast<Encode>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(base),
-                                        dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    return reinterpret_cast<Encode>(fn)(map, type, static_cast<cuuint32_t>(rank), const_cast<void*>(base), dims, strides, box, steps,
+                                        CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -368,10 +369,20 @@ struct Operand {
         const cuuint64_t flat[2] = {wide(), static_cast<cuuint64_t>(rows)};
         return encode_map(m, base, 2, flat, strides, box);
     }
+    // To be written by the epilogue: 32 x 32 values a box.
+    bool map_out(CUtensorMap* m, bool floats) const {
+        const cuuint64_t row_bytes = static_cast<cuuint64_t>(stride) * (floats ? 4 : 2);
+        const cuuint64_t dims[3] = {wide(), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(blocks)};
+        const cuuint64_t strides[2] = {row_bytes, row_bytes * rows};
+        const cuuint32_t box[3] = {32, 32, 1};
+        return encode_map(m, base, blocks ? 3 : 2, dims, strides, box,
+                          floats ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                          floats ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+    }
 };
 
 template <int KIND, bool A_K, bool B_K, typename T, int CTAS>
-bns_status head_gemm_on(int kind, const CUtensorMap& ma, const CUtensorMap& mb, const HeadGemm& g, cudaStream_t stream) {
+bns_status head_gemm_on(int kind, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const HeadGemm& g, cudaStream_t stream) {
     static std::atomic<bool> raised[kMaxDevices];
     int device = -1;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= kMaxDevices) return BNS_ERR_CUDA;
@@ -388,27 +399,33 @@ bns_status head_gemm_on(int kind, const CUtensorMap& ma, const CUtensorMap& mb, 
     if (tiles >= int64_t{1} << 30) return BNS_ERR_SHAPE;
     const int64_t workers = sm_count() / CTAS;
     launch(kind, kernel, Shape{static_cast<unsigned>(g.join_parts ? workers : std::min(tiles, workers)) * CTAS, kHeadThreads, CTAS}, smem,
-           stream, ma, mb, g);
+           stream, ma, mb, mc, g);
     return last_error();
 }
 
 // CTA pairs with 256 x 256 tiles; single CTAs where the product has no more rows than one of them holds.
 template <int KIND, bool A_K, bool B_K, typename T>
-bns_status head_gemm(int kind, const Operand& a, const Operand& b, HeadGemm g, int K, cudaStream_t stream) {
+bns_status head_gemm(int kind, const Operand& a, const Operand& b, const Operand& c, HeadGemm g, int K, cudaStream_t stream) {
     const int ctas = head_ctas(g.M);
-    CUtensorMap ma, mb;
+    CUtensorMap ma, mb, mc{};
     if (!(A_K ? a.map_k(&ma, kHeadM) : a.map_mn(&ma, kHeadM))) return BNS_ERR_CUDA;
     if (!(B_K ? b.map_k(&mb, static_cast<unsigned>(kHeadN / ctas)) : b.map_mn(&mb, static_cast<unsigned>(kHeadN / ctas))))
         return BNS_ERR_CUDA;
     g.b_chunks = !B_K && b.chunks();
+    if (KIND == kHeadGrad && !c.map_out(&mc, false)) return BNS_ERR_CUDA;
+    if (KIND == kHeadOut) {
+        constexpr bool floats = sizeof(typename T::storage) == 4;
+        g.out_boxes = !g.sums && c.stride % (floats ? 4 : 8) == 0;
+        if (g.out_boxes && !c.map_out(&mc, floats)) return BNS_ERR_CUDA;
+    }
     g.tiles_m = divide_up(g.M, kHeadM * ctas);
     g.tiles_n = divide_up(g.N, kHeadN);
     g.k_blocks = divide_up(K, kHeadK);
     g.pairs = a.terms > 1 ? 3 : 1;
     g.a_pitch = a.pitch;
     g.b_pitch = b.pitch;
-    return ctas == 2 ? head_gemm_on<KIND, A_K, B_K, T, 2>(kind, ma, mb, g, stream)
-                     : head_gemm_on<KIND, A_K, B_K, T, 1>(kind, ma, mb, g, stream);
+    return ctas == 2 ? head_gemm_on<KIND, A_K, B_K, T, 2>(kind, ma, mb, mc, g, stream)
+                     : head_gemm_on<KIND, A_K, B_K, T, 1>(kind, ma, mb, mc, g, stream);
 }
 
 // Rows laid out in the workspace: bf16 as they are, fp32 as two fp16 terms scaled by the largest value.
@@ -623,7 +640,7 @@ bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x
         g.status = first == 0 ? reinterpret_cast<unsigned*>(ws) : nullptr;
         g.a_scale = &scalars->x_scale;
         g.b_scale = &scalars->w_scale;
-        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadLse, true, true, T>(BNS_KERNEL_HEAD_LOGITS, xs, rows, g, p.D, stream)));
+        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadLse, true, true, T>(BNS_KERNEL_HEAD_LOGITS, xs, rows, Operand{}, g, p.D, stream)));
         if (st != BNS_OK) return st;
         tiles += 2 * divide_up(count, kHeadN);
     }
@@ -678,10 +695,9 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         g.find_unit = find_unit;
         g.a_scale = &scalars->x_scale;
         g.b_scale = &scalars->w_scale;
-        g.G = reinterpret_cast<unsigned short*>(ws + p.off_G);
-        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadGrad, true, true, T>(BNS_KERNEL_HEAD_GRADIENT, xs, rows, g, p.D, stream)));
+        const Operand G{ws + p.off_G, static_cast<int64_t>(p.terms) * kHeadN, p.T, kHeadN, p.terms, kHeadN, divide_up(count, kHeadN)};
+        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadGrad, true, true, T>(BNS_KERNEL_HEAD_GRADIENT, xs, rows, G, g, p.D, stream)));
         if (st != BNS_OK) return st;
-        const Operand G{g.G, static_cast<int64_t>(p.terms) * kHeadN, p.T, kHeadN, p.terms, kHeadN, divide_up(count, kHeadN)};
         HeadGemm o{};
         o.M = p.T;
         o.N = p.D;
@@ -693,7 +709,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         o.sums = sums;
         o.add = first > 0;
         o.last = p.splits == 1 && first + count == p.V;
-        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, true, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, rows, o, count, stream)));
+        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, true, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, rows, Operand{dx, p.D, p.T, p.D, 1, 0}, o, count, stream)));
         if (st != BNS_OK) return st;
         HeadGemm q{};
         q.M = count;
@@ -709,7 +725,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         q.b_scale = &scalars->x_scale;
         q.out = static_cast<char*>(dw) + static_cast<size_t>(first) * p.D * eb;
         q.out_stride = p.D;
-        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, false, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, xs, q, p.T, stream)));
+        BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadOut, false, false, T>(BNS_KERNEL_HEAD_PRODUCT, G, xs, Operand{q.out, p.D, count, p.D, 1, 0}, q, p.T, stream)));
         if (st != BNS_OK) return st;
     }
     return last_error();
