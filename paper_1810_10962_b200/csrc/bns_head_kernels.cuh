@@ -270,7 +270,7 @@ struct HeadGemm {
     float* sums;                 // [splits][M][N] fp32, or NULL: `out` is written directly
     int add;                     // add what `sums` holds
     int last;                    // with sums: write `out` (one split only)
-    // dW, after the last piece: an idle warp of each block adds up dx's parts
+    // dW, after the last piece: two idle warps of each block add up dx's parts
     const float* join_sums;
     void* join_out;
     int join_parts;
@@ -327,22 +327,26 @@ __device__ __forceinline__ float head_unit(const void* target, int target64, con
     return top;
 }
 
-// Adds up the parts of a product in their order and rounds once: vectors of V elements, lane `first` of `step`.
-template <typename T, int V>
-__device__ __forceinline__ void head_join_parts(const HeadGemm& g, int64_t first, int64_t step) {
-    constexpr int kBatch = 4;
-    const int64_t vectors = g.join_total / V;
-    for (int64_t i0 = first; i0 < vectors; i0 += step * kBatch) {
-        float v[kBatch][V] = {};
+// Adds up the parts of a product in a fixed order and rounds once: vectors of V elements, BATCH of them at a time.  LANES lanes
+// share a vector, each with every LANES-th part: many parts come with few elements, and one lane would wait for each
+// of them in turn.  Warp `warp` of `warps`.
+template <typename T, int V, int LANES, int BATCH>
+__device__ __forceinline__ void head_join_parts(const HeadGemm& g, int warp, int warps, int lane) {
+    constexpr int kPer = 32 / LANES;                         // vectors of a warp
+    const int64_t vectors = g.join_total / V, stride = static_cast<int64_t>(warps) * kPer;
+    const int mine = lane % LANES;
+    for (int64_t base = static_cast<int64_t>(warp) * kPer; base < vectors; base += stride * BATCH) {
+        const int64_t i0 = base + lane / LANES;
+        float v[BATCH][V] = {};
 #pragma unroll 4
-        for (int s = 0; s < g.join_parts; ++s) {
-            Vec<F32, V> x[kBatch];
+        for (int s = mine; s < g.join_parts; s += LANES) {
+            Vec<F32, V> x[BATCH];
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b)
-                if (i0 + b * step < vectors) x[b].load(g.join_sums + s * g.join_total + (i0 + b * step) * V);
+            for (int b = 0; b < BATCH; ++b)
+                if (i0 + b * stride < vectors) x[b].load(g.join_sums + s * g.join_total + (i0 + b * stride) * V);
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                if (i0 + b * step < vectors) {
+            for (int b = 0; b < BATCH; ++b) {
+                if (i0 + b * stride < vectors) {
                     float f[V];
                     x[b].unpack(f);
 #pragma unroll
@@ -350,12 +354,21 @@ __device__ __forceinline__ void head_join_parts(const HeadGemm& g, int64_t first
                 }
             }
         }
+        __syncwarp();
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            if (i0 + b * step < vectors) {
-                Vec<T, V> o;
-                o.pack(v[b]);
-                o.store(static_cast<typename T::storage*>(g.join_out) + (i0 + b * step) * V);
+        for (int o = LANES / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[b][j] += __shfl_xor_sync(0xffffffffu, v[b][j], o);
+        if (mine == 0) {
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                if (i0 + b * stride < vectors) {
+                    Vec<T, V> o;
+                    o.pack(v[b]);
+                    o.store(static_cast<typename T::storage*>(g.join_out) + (i0 + b * stride) * V);
+                }
             }
         }
     }
@@ -728,12 +741,20 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             }
         }
         if constexpr (KIND == kHeadOut && !A_K) {
-            if (warp == 3 && g.join_parts) {
-                const int64_t first = blockIdx.x * 32 + lane, step = gridDim.x * 32;
-                if (g.join_total % 4 == 0)       // a part begins at a 16-byte boundary
-                    head_join_parts<T, 4>(g, first, step);
-                else
-                    head_join_parts<T, 1>(g, first, step);
+            if (warp >= 2 && g.join_parts) {
+                const int at = blockIdx.x * 2 + warp - 2, of = gridDim.x * 2;
+                const bool whole = g.join_total % 4 == 0;       // a part begins at a 16-byte boundary
+                // eight lanes a vector where there are fewer vectors than two a lane (24 x 1024, 37 parts: dW's kernel 28 -> 18 us)
+                if (g.join_parts >= 8 && g.join_total < static_cast<int64_t>(of) * 32 * 2 * (whole ? 4 : 1)) {
+                    if (whole)
+                        head_join_parts<T, 4, 8, 1>(g, at, of, lane);
+                    else
+                        head_join_parts<T, 1, 8, 1>(g, at, of, lane);
+                } else if (whole) {
+                    head_join_parts<T, 4, 1, 4>(g, at, of, lane);
+                } else {
+                    head_join_parts<T, 1, 1, 4>(g, at, of, lane);
+                }
             }
         }
         __syncwarp();
