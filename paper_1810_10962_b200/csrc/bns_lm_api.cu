@@ -182,6 +182,7 @@ bns_status rms_forward(const bns_rows* sh, const void* x, int64_t x_stride, cons
         rule.bytes(y);
     else
         rule.tensor(y, sh->columns);
+    if (!aligned(weight, 16) && rule.kind == VectorRule::kAligned) rule.kind = VectorRule::kPhase;   // keeps its weights
     if (grouped && rule.kind == VectorRule::kPhase) rule.kind = VectorRule::kElements;   // groups begin at whole vectors
     const RmsPlan pl = plan_rms(sh->rows, sh->columns, sh->dtype, rule.kind, sh->dtype == BNS_F32);
     const RmsForward a{x, residual, weight, y, scales, h, rstd, sh->rows, x_stride, residual_stride, sh->columns, eps,
@@ -574,6 +575,7 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
     rule.tensor(h, h_stride);
     rule.tensor(dh, dh_stride);
     rule.tensor(dx, shape->columns);
+    if (!aligned(weight, 16) && rule.kind == VectorRule::kAligned) rule.kind = VectorRule::kPhase;
     const RmsPlan pl = plan_rms(shape->rows, shape->columns, shape->dtype, rule.kind, true);
     float* partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kHeaderBytes);
     const RmsBackward a{dy, h, dh, weight, rstd, dx, partial, shape->rows, dy_stride, h_stride, dh_stride, shape->columns,

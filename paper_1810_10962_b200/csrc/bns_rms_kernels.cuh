@@ -140,7 +140,7 @@ struct Quant {
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(top * lift));   // 1 ulp
         factor = a == 0.f ? 0.f : top < inf && a < inf ? 448.f * inverse : __int_as_float(0x7fffffff);
     }
-    __device__ __forceinline__ float scale() const { return a == 0.f ? 1.f : a / 448.f; }
+    __device__ __forceinline__ float scale() const { return a == 0.f ? 1.f : a * (1.f / 448.f); }
     template <int V>
     __device__ __forceinline__ void apply(float (&sw)[V]) const {
         if (lift != 1.f) multiply_by<V>(sw, lift);
@@ -178,24 +178,22 @@ struct RowPiece {
     }
 };
 
-// V weights; rows of weights are only as aligned as floats are.
-template <int V>
-__device__ __forceinline__ void load_weights(const float* weight, int at, bool aligned, float (&w)[V]) {
-    if constexpr (V >= 4) {
-        if (aligned) {
+// V weights, in 16-byte words where WORDS says that they begin at one.
+template <int V, bool WORDS>
+__device__ __forceinline__ void load_weights(const float* weight, int at, float (&w)[V]) {
+    if constexpr (WORDS && V >= 4) {
 #pragma unroll
-            for (int j = 0; j < V; j += 4) {
-                const float4 q = __ldg(reinterpret_cast<const float4*>(weight + at * V + j));
-                w[j] = q.x;
-                w[j + 1] = q.y;
-                w[j + 2] = q.z;
-                w[j + 3] = q.w;
-            }
-            return;
+        for (int j = 0; j < V; j += 4) {
+            const float4 q = __ldg(reinterpret_cast<const float4*>(weight + at * V + j));
+            w[j] = q.x;
+            w[j + 1] = q.y;
+            w[j + 2] = q.z;
+            w[j + 3] = q.w;
         }
-    }
+    } else {
 #pragma unroll
-    for (int j = 0; j < V; ++j) w[j] = __ldg(weight + at * V + j);
+        for (int j = 0; j < V; ++j) w[j] = __ldg(weight + at * V + j);
+    }
 }
 
 // Rows whose stride is no multiple of a vector begin at any phase.  The blocks of a launch are a multiple of V then, so
@@ -227,7 +225,6 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
     const int B = blockDim.x;
     const RowPhase<S, V, LOOSE> at(static_cast<const S*>(a.x) + blockIdx.x * a.x_stride, a.D);
     const int vectors = at.vectors;
-    const bool aligned = !LOOSE && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     grid_dependency_wait();
     grid_dependency_launch();
 
@@ -237,7 +234,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = threadIdx.x + i * B;
-            if (v < vectors) load_weights<V>(a.weight + at.head, v, false, kept[i]);
+            if (v < vectors) load_weights<V, false>(a.weight + at.head, v, kept[i]);
         }
         if (at.extra >= 0) extra_w = a.weight[at.extra];
     }
@@ -246,7 +243,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
 #pragma unroll
             for (int j = 0; j < V; ++j) w[j] = kept[i][j];
         } else {
-            load_weights<V>(a.weight, threadIdx.x + i * B, aligned, w);
+            load_weights<V, true>(a.weight, threadIdx.x + i * B, w);
         }
     };
     RowPiece<T, V, NV> vx, vr;
@@ -323,7 +320,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_kernel(const RmsFo
             __syncthreads();
         }
         block_exchange<kRow>(sum, top, ex, turn);
-        const float rstd = 1.f / sqrtf(fmaf(sum, a.inv_D, a.eps));
+        const float rstd = rsqrtf(fmaf(sum, a.inv_D, a.eps));   // 2 ulp
         if (threadIdx.x == 0) a.rstd[row] = rstd;
         if constexpr (!kRow && !kGroup) {
             S* y = static_cast<S*>(a.y) + row * a.D;
@@ -421,7 +418,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_forward_wide_kernel(const 
             }
         }
         block_exchange<kRow>(sum, top, ex, turn);
-        const float rstd = 1.f / sqrtf(fmaf(sum, a.inv_D, a.eps));
+        const float rstd = rsqrtf(fmaf(sum, a.inv_D, a.eps));   // 2 ulp
         if (threadIdx.x == 0) a.rstd[row] = rstd;
         if constexpr (kGroup) {
             // a warp per group, four columns a lane
@@ -491,7 +488,6 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
     auto row_of = [&](int64_t step) { return a.rows - 1 - step; };
     const RowPhase<S, V, LOOSE> at(static_cast<const S*>(a.h) + row_of(blockIdx.x) * a.h_stride, a.D);
     const int vectors = at.vectors;
-    const bool aligned = !LOOSE && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     grid_dependency_wait();
     grid_dependency_launch();
     float dw[NV][V], extra_dw = 0.f, extra_w = 0.f;
@@ -532,7 +528,7 @@ __global__ void __launch_bounds__(kRmsMaxThreads) rms_backward_kernel(const RmsB
             const int v = threadIdx.x + i * B;
             if (v < vectors) {
                 float w[V];
-                load_weights<V>(a.weight + at.head, v, aligned, w);
+                load_weights<V, !LOOSE>(a.weight + at.head, v, w);
                 vy.v[i].unpack(wdy[i]);
                 vh.v[i].unpack(xhat[i]);
                 multiply_by<V>(xhat[i], rstd);
