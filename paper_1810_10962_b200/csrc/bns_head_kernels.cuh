@@ -42,14 +42,19 @@ namespace bns {
 constexpr int kHeadM = 128, kHeadN = 256, kHeadK = 64;   // rows of a CTA, columns of a tile, K per stage
 constexpr int kHeadSegment = 8, kHeadSegmentHigh = 4, kHeadSegmentLow = 64;   // stages of K per segment
 constexpr int kHeadThreads = 384;
-constexpr unsigned kHeadStageA = kHeadM * kHeadK * 2;
 
-// Ring of a CTA that works alone (CTAS = 1) or as half of a pair (2): 192 KB either way.
-template <int CTAS>
+// Narrow tiles of the products with the logits, for few rows and few columns: 64 columns, and half of A's stage.
+constexpr int kHeadNarrow = 64, kHeadNarrowRows = 64;
+
+// Ring of a CTA that works alone (CTAS = 1) or as half of a pair (2) on tiles of N columns.
+template <int CTAS, int N>
 struct HeadRing {
-    static constexpr int kStages = CTAS == 2 ? 6 : 4;
-    static constexpr int kColumns = kHeadN / CTAS;       // of B in this CTA's stage
-    static constexpr unsigned kStageB = kColumns * kHeadK * 2, kStage = kHeadStageA + kStageB;
+    static constexpr bool kNarrow = N == kHeadNarrow;
+    static constexpr int kStages = kNarrow ? 10 : CTAS == 2 ? 6 : 4;
+    static constexpr int kRows = kNarrow ? kHeadNarrowRows : kHeadM;   // of A's stage; the products read 128 all the same, what
+                                                                       // lies there ends in rows that do not exist
+    static constexpr int kColumns = N / CTAS;            // of B in this CTA's stage
+    static constexpr unsigned kStageA = kRows * kHeadK * 2, kStageB = kColumns * kHeadK * 2, kStage = kStageA + kStageB;
     static constexpr unsigned kStaging = 8 * 32 * 128;   // 32 rows of 32 fp32 values for each warp of the epilogue
     static constexpr unsigned kSmem = kStages * kStage + kStaging + 1024;
 };
@@ -388,17 +393,18 @@ __device__ __forceinline__ uint2 pack_halves(const unsigned short (&h)[4]) {
     return make_uint2(h[0] | static_cast<unsigned>(h[1]) << 16, h[2] | static_cast<unsigned>(h[3]) << 16);
 }
 
-// What a thread of the epilogue does with its 128 columns of a row, 32 at a time.
-template <int KIND, typename T>
+// What a thread of the epilogue does with its half of a tile's columns of a row, 32 at a time.
+template <int KIND, typename T, int N>
 struct HeadEpilogue {
     using S = typename T::storage;
     static constexpr bool kFp32 = sizeof(S) == 4;
+    static constexpr int kHalf = N / 2;
     const HeadGemm& g;
     const HeadTile& t;
-    int row, column0, columns;   // first column, and how many of the 128 exist
+    int row, column0, columns;   // first column, and how many of the half exist
     bool in;
     // LSE and GRAD
-    int mine = -1;               // the target's place among the 128
+    int mine = -1;               // the target's place in the half
     bool counts = false;
     float unscale = 1.f, c;      // LSE and GRAD: logits = unscale accumulator; c = log2(e) unscale
     float m, s;                  // LSE
@@ -414,11 +420,11 @@ struct HeadEpilogue {
     int64_t sums_step = 0, out_step = 0;
 
     __device__ __forceinline__ HeadEpilogue(const HeadGemm& g_, const HeadTile& t_, int row_, int half_, float4* stage_, const CUtensorMap* map_, int& turn_, float unit)
-        : g(g_), t(t_), row(row_), column0(t_.n * kHeadN + half_ * (kHeadN / 2)), in(row_ < g_.M), half(half_),
+        : g(g_), t(t_), row(row_), column0(t_.n * N + half_ * kHalf), in(row_ < g_.M), half(half_),
           lane(threadIdx.x & 31), stage(stage_), map(map_), turn(turn_) {
         const int64_t first = row - lane + (lane >> 3);
         rows_left = static_cast<int>(g.M - first);
-        columns = min(kHeadN / 2, g.N - column0);
+        columns = min(kHalf, g.N - column0);
         if constexpr (KIND != kHeadOut) {
             const int64_t y = in ? head::load_index(g.target, row, g.target64) : -1;
             counts = y >= 0 && y < g.V;
@@ -449,7 +455,7 @@ struct HeadEpilogue {
     }
     // Columns that the accumulator has to be read for: G is written up to whole stages of K, zeros where nothing is.
     __device__ __forceinline__ int extent() const {
-        if constexpr (KIND == kHeadGrad) return min(kHeadN / 2, (max(columns, 0) + kHeadK - 1) / kHeadK * kHeadK);
+        if constexpr (KIND == kHeadGrad) return min(kHalf, (g.N + kHeadK - 1) / kHeadK * kHeadK - column0);
         return columns;
     }
     __device__ __forceinline__ void chunk(int at, float* f) {
@@ -490,13 +496,13 @@ struct HeadEpilogue {
                     high[j] = h0 | static_cast<unsigned>(h1) << 16;
                     low[j] = l0 | static_cast<unsigned>(l1) << 16;
                 }
-                send(high, half * (kHeadN / 2) + at, t.n);
-                send(low, kHeadN + half * (kHeadN / 2) + at, t.n);
+                send(high, column0 % kHeadN + at, column0 / kHeadN);
+                send(low, kHeadN + column0 % kHeadN + at, column0 / kHeadN);
             } else {
                 unsigned w[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) w[j] = pack_pair(f[2 * j], f[2 * j + 1]);
-                send(w, half * (kHeadN / 2) + at, t.n);
+                send(w, column0 % kHeadN + at, column0 / kHeadN);
             }
         } else {
             const int left = columns - at - 4 * (lane & 7);
@@ -632,11 +638,11 @@ struct HeadEpilogue {
     }
 };
 
-template <int KIND, bool A_K, bool B_K, typename T, int CTAS>
+template <int KIND, bool A_K, bool B_K, typename T, int CTAS, int N>
 __global__ void __launch_bounds__(kHeadThreads, 1)
     head_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                      const __grid_constant__ CUtensorMap map_c, const HeadGemm g) {
-    using Ring = HeadRing<CTAS>;
+    using Ring = HeadRing<CTAS, N>;
     constexpr int kStages = Ring::kStages;
     constexpr bool kFp32 = sizeof(typename T::storage) == 4, kSegments = KIND == kHeadLse || kFp32;
     extern __shared__ unsigned char raw[];
@@ -675,22 +681,30 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     grid_dependency_launch();
 
     const int tiles = g.tiles_m * g.tiles_n * g.splits;
-    int issued = 0;   // stages that thread 0 has asked TMA to fill
+    // The ring's place of this thread: stage, and parity of its barriers' current phase.  Neither loop divides: at some 500
+    // cycles a stage a few dozen of them in the loop that feeds the ring show.
+    int s = 0;
+    unsigned phase = 0;
+    auto advance = [&]() {
+        if (++s == kStages) {
+            s = 0;
+            phase ^= 1;
+        }
+    };
     if (warp < 4) {
         if (warp == 0 && lane == 0) {
-            int it = 0;
+            const unsigned full_first = head::in_first<CTAS>(full);
+            const int k_end = g.k_blocks * kHeadK;
             bool ok = true;
             for (int id = worker; ok && id < tiles; id += workers) {
                 const HeadTile t(g, id);
-                const int row = (t.m * CTAS + rank) * kHeadM, column = t.n * kHeadN + rank * Ring::kColumns;
-                for (int k = t.k0; k < t.k1; ++k, ++it) {
-                    const int s = it % kStages;
-                    if (it >= kStages && !(ok = wait_bounded(empty + 8 * s, (it / kStages - 1) & 1, &gave_up))) break;
-                    const unsigned bar = head::in_first<CTAS>(full + 8 * s), sa = ring + s * Ring::kStage, sb = sa + kHeadStageA;
+                const int row = (t.m * CTAS + rank) * kHeadM, column = t.n * N + rank * Ring::kColumns;
+                int pair = g.pairs > 1 ? t.k0 / g.k_blocks : 0, kk = (t.k0 - pair * g.k_blocks) * kHeadK, ta, tb;
+                head_pair(pair, g.pairs, ta, tb);
+                for (int k = t.k0; k < t.k1; ++k) {
+                    if (!(ok = wait_bounded(empty + 8 * s, phase ^ 1, &gave_up))) break;     // passes at once on the first round
+                    const unsigned bar = full_first + 8 * s, sa = ring + s * Ring::kStage, sb = sa + Ring::kStageA;
                     if (rank == 0) barrier_expect(full + 8 * s, CTAS * Ring::kStage);
-                    int ta, tb;
-                    const int pair = k / g.k_blocks, kk = (k - pair * g.k_blocks) * kHeadK;
-                    head_pair(pair, g.pairs, ta, tb);
                     if constexpr (KIND == kHeadOut) {       // A is G, in blocks of 256 columns
                         if constexpr (A_K)
                             head::tma_load<CTAS>(sa, &map_a, ta * kHeadN + kk % kHeadN, row, kk / kHeadN, bar);
@@ -708,16 +722,23 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                         for (int q = 0; q < Ring::kColumns / 64; ++q)
                             head::tma_load<CTAS>(sb + q * 8192, &map_b, tb * g.b_pitch + column + q * 64, kk, bar);
                     }
+                    advance();
+                    kk += kHeadK;
+                    if (kk == k_end) {
+                        kk = 0;
+                        head_pair(++pair, g.pairs, ta, tb);
+                    }
                 }
             }
             // the products have read every stage: nothing arrives here any more once the block ends
-            for (int i = max(0, it - kStages); ok && i < it; ++i)
-                ok = wait_bounded(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up);
-            issued = it;
+            for (int i = 0; ok && i < kStages; ++i) {
+                ok = wait_bounded(empty + 8 * s, phase ^ 1, &gave_up);
+                if (ok) advance();
+            }
         } else if (warp == 1 && lane == 0 && rank == 0) {
             constexpr unsigned idesc = (1u << 4) | (kFp32 ? 0u : (1u << 7) | (1u << 10)) | (A_K ? 0u : 1u << 15) | (B_K ? 0u : 1u << 16) |
-                                       ((kHeadN >> 3) << 17) | ((CTAS * kHeadM >> 4) << 24);
-            int it = 0, n = 0;
+                                       ((N >> 3) << 17) | ((CTAS * kHeadM >> 4) << 24);
+            int n = 0;
             bool ok = true;
             for (int id = worker; ok && id < tiles; id += workers) {
                 const HeadTile t(g, id);
@@ -726,18 +747,18 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                     end = kSegments ? head_segment_end<kFp32>(g, k, t.k1) : t.k1;
                     if (n >= 2 && !(ok = wait_bounded(drained + 8 * buffer, (n / 2 - 1) & 1, &gave_up))) break;
                     head::fence_after();
-                    const unsigned d = tmem + buffer * kHeadN;
-                    for (int kk = k; kk < end; ++kk, ++it) {
-                        const int s = it % kStages;
-                        if (!(ok = wait_bounded(full + 8 * s, (it / kStages) & 1, &gave_up))) break;
+                    const unsigned d = tmem + buffer * N;
+                    for (int kk = k; kk < end; ++kk) {
+                        if (!(ok = wait_bounded(full + 8 * s, phase, &gave_up))) break;
                         head::fence_after();
                         const unsigned sa = ring + s * Ring::kStage;
-                        const uint64_t da = head::descriptor<A_K>(sa), db = head::descriptor<B_K>(sa + kHeadStageA);
+                        const uint64_t da = head::descriptor<A_K>(sa), db = head::descriptor<B_K>(sa + Ring::kStageA);
 #pragma unroll
                         for (int q = 0; q < kHeadK / 16; ++q)
                             head::mma<CTAS>(d, da + q * head::descriptor_step<A_K>(), db + q * head::descriptor_step<B_K>(), idesc,
                                             kk > k || q > 0);
                         head::commit<CTAS>(empty + 8 * s);
+                        advance();
                     }
                     if (!ok) break;
                     head::commit<CTAS>(ready + 8 * buffer);
@@ -778,8 +799,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         bool ok = true;
         for (int id = worker; ok && id < tiles; id += workers) {
             const HeadTile t(g, id);
-            HeadEpilogue<KIND, T> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half, stage, &map_c, turn, unit);
-            const unsigned lanes = tmem + (static_cast<unsigned>(slot * 32) << 16) + half * (kHeadN / 2);
+            HeadEpilogue<KIND, T, N> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half, stage, &map_c, turn, unit);
+            const unsigned lanes = tmem + (static_cast<unsigned>(slot * 32) << 16) + half * (N / 2);
             auto wait_ready = [&]() {
                 ok = __all_sync(0xffffffffu, wait_bounded(ready + 8 * (n & 1), (n / 2) & 1, &gave_up));
                 head::fence_after();
@@ -792,16 +813,16 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 ++n;
             };
             if constexpr (kSegments) {
-                float acc[kHeadN / 2];
+                float acc[N / 2];
 #pragma unroll
-                for (int j = 0; j < kHeadN / 2; ++j) acc[j] = 0.f;
+                for (int j = 0; j < N / 2; ++j) acc[j] = 0.f;
                 for (int k = t.k0; k < t.k1; k = head_segment_end<kFp32>(g, k, t.k1)) {
                     if (!wait_ready()) break;
                     const float weight = kFp32 && k < 2 * g.k_blocks ? 1.f / kHeadLow : 1.f;
 #pragma unroll
-                    for (int c = 0; c < kHeadN / 2; c += 16) {
+                    for (int c = 0; c < N / 2; c += 16) {
                         float f[16];
-                        head::load16(lanes + (n & 1) * kHeadN + c, f);
+                        head::load16(lanes + (n & 1) * N + c, f);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(f[j], weight, acc[c + j]);
                     }
@@ -810,7 +831,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 if (!ok) break;
                 const int extent = e.extent();
 #pragma unroll
-                for (int c = 0; c < kHeadN / 2; c += 32)
+                for (int c = 0; c < N / 2; c += 32)
                     if (c < extent) e.chunk(c, acc + c);
                 e.finish();
             } else {
@@ -818,7 +839,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 const int extent = e.extent();
                 for (int c = 0; c < extent; c += 32) {
                     float f[32];
-                    head::load32(lanes + (n & 1) * kHeadN + c, f);
+                    head::load32(lanes + (n & 1) * N + c, f);
                     e.chunk(c, f);
                 }
                 e.finish();
@@ -831,8 +852,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     if (gave_up) {
         // a block that gave up leaves only when its copies have landed and its products have ended
         if (threadIdx.x == 0 && rank == 0)
-            for (int i = max(0, issued - kStages); i < issued; ++i)
-                for (unsigned n = 0; n < kPolls && !barrier_try(full + 8 * (i % kStages), (i / kStages) & 1); ++n) {
+            for (int q = 0; q < kStages; ++q)     // the last fill of stage q; one that was never filled passes
+                for (unsigned n = 0; n < kPolls && !barrier_try(full + 8 * q, q < s ? phase : phase ^ 1); ++n) {
                 }
         if (threadIdx.x == 32 && rank == 0) {
             head::commit<CTAS>(flush);

@@ -245,8 +245,13 @@ bns_status check_head(const bns_head* sh) {
     return BNS_OK;
 }
 
-// CTAs that work on a tile of a product with M rows.
+// CTAs that work on a tile of a product with M rows, and columns of a tile of the products with the logits.  Narrow tiles pay
+// while one round of them covers the vocabulary (5 x 2564 x 3160 forward: 32 -> 25 us); beyond that they read x too
+// often, and a product of 64 columns takes as long as one of 256 (24 x 32768 x 1024 forward: 24 -> 37 us).
 int head_ctas(int M) { return M <= kHeadM ? 1 : 2; }
+int head_columns(int rows, int vocabulary) {
+    return rows <= kHeadNarrowRows && vocabulary <= kHeadNarrow * sm_count() ? kHeadNarrow : kHeadN;
+}
 
 bool tma_rows(int64_t stride) { return stride % 8 == 0 && stride < int64_t{1} << 38; }
 
@@ -311,7 +316,7 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
         p.off_G = take(T * p.terms * p.G_pitch * 2);
         if (p.splits > 1 || p.pieces > 1) p.off_sums = take(T * p.splits * p.D * 4);
     } else {
-        p.off_partial = take(2 * T * (divide_up(p.V, kHeadN) + p.pieces) * sizeof(float2));
+        p.off_partial = take(2 * T * (divide_up(p.V, head_columns(p.T, p.V)) + p.pieces) * sizeof(float2));
         p.off_logit = take(T * 4);
     }
     p.total = at;
@@ -382,13 +387,13 @@ struct Operand {
     }
 };
 
-template <int KIND, bool A_K, bool B_K, typename T, int CTAS>
+template <int KIND, bool A_K, bool B_K, typename T, int CTAS, int N>
 bns_status head_gemm_on(int kind, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const HeadGemm& g, cudaStream_t stream) {
     static std::atomic<bool> raised[kMaxDevices];
     int device = -1;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= kMaxDevices) return BNS_ERR_CUDA;
-    auto kernel = head_gemm_kernel<KIND, A_K, B_K, T, CTAS>;
-    constexpr unsigned smem = HeadRing<CTAS>::kSmem;
+    auto kernel = head_gemm_kernel<KIND, A_K, B_K, T, CTAS, N>;
+    constexpr unsigned smem = HeadRing<CTAS, N>::kSmem;
     if (!raised[device].load(std::memory_order_relaxed)) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
             cudaGetLastError();
@@ -404,14 +409,15 @@ bns_status head_gemm_on(int kind, const CUtensorMap& ma, const CUtensorMap& mb, 
     return last_error();
 }
 
-// CTA pairs with 256 x 256 tiles; single CTAs where the product has no more rows than one of them holds.
+// CTA pairs with 256 x 256 tiles; single CTAs where the product has no more rows than one of them holds.  The products with
+// the logits may have narrow tiles.
 template <int KIND, bool A_K, bool B_K, typename T>
 bns_status head_gemm(int kind, const Operand& a, const Operand& b, const Operand& c, HeadGemm g, int K, cudaStream_t stream) {
-    const int ctas = head_ctas(g.M);
+    const int ctas = head_ctas(g.M), columns = KIND == kHeadOut ? kHeadN : head_columns(g.M, g.V);
+    const unsigned box_rows = columns == kHeadNarrow ? kHeadNarrowRows : kHeadM, box_columns = static_cast<unsigned>(columns / ctas);
     CUtensorMap ma, mb, mc{};
-    if (!(A_K ? a.map_k(&ma, kHeadM) : a.map_mn(&ma, kHeadM))) return BNS_ERR_CUDA;
-    if (!(B_K ? b.map_k(&mb, static_cast<unsigned>(kHeadN / ctas)) : b.map_mn(&mb, static_cast<unsigned>(kHeadN / ctas))))
-        return BNS_ERR_CUDA;
+    if (!(A_K ? a.map_k(&ma, box_rows) : a.map_mn(&ma, box_rows))) return BNS_ERR_CUDA;
+    if (!(B_K ? b.map_k(&mb, box_columns) : b.map_mn(&mb, box_columns))) return BNS_ERR_CUDA;
     g.b_chunks = !B_K && b.chunks();
     if (KIND == kHeadGrad && !c.map_out(&mc, false)) return BNS_ERR_CUDA;
     if (KIND == kHeadOut) {
@@ -420,13 +426,15 @@ bns_status head_gemm(int kind, const Operand& a, const Operand& b, const Operand
         if (g.out_boxes && !c.map_out(&mc, floats)) return BNS_ERR_CUDA;
     }
     g.tiles_m = divide_up(g.M, kHeadM * ctas);
-    g.tiles_n = divide_up(g.N, kHeadN);
+    g.tiles_n = divide_up(g.N, columns);
     g.k_blocks = divide_up(K, kHeadK);
     g.pairs = a.terms > 1 ? 3 : 1;
     g.a_pitch = a.pitch;
     g.b_pitch = b.pitch;
-    return ctas == 2 ? head_gemm_on<KIND, A_K, B_K, T, 2>(kind, ma, mb, mc, g, stream)
-                     : head_gemm_on<KIND, A_K, B_K, T, 1>(kind, ma, mb, mc, g, stream);
+    if constexpr (KIND != kHeadOut)
+        if (columns == kHeadNarrow) return head_gemm_on<KIND, A_K, B_K, T, 1, kHeadNarrow>(kind, ma, mb, mc, g, stream);
+    return ctas == 2 ? head_gemm_on<KIND, A_K, B_K, T, 2, kHeadN>(kind, ma, mb, mc, g, stream)
+                     : head_gemm_on<KIND, A_K, B_K, T, 1, kHeadN>(kind, ma, mb, mc, g, stream);
 }
 
 // Rows laid out in the workspace: bf16 as they are, fp32 as two fp16 terms scaled by the largest value.
@@ -644,7 +652,7 @@ bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x
         g.b_scale = &scalars->w_scale;
         BNS_LM_BY_TYPE(p.dtype, (st = head_gemm<kHeadLse, true, true, T>(BNS_KERNEL_HEAD_LOGITS, xs, rows, Operand{}, g, p.D, stream)));
         if (st != BNS_OK) return st;
-        tiles += 2 * divide_up(count, kHeadN);
+        tiles += 2 * divide_up(count, head_columns(p.T, p.V));
     }
     launch(BNS_KERNEL_HEAD_VECTOR, head_join_kernel, Shape{static_cast<unsigned>(divide_up(p.T, 32)), 1024}, 0, stream, partial, tiles, p.T,
            reinterpret_cast<const float*>(ws + p.off_logit), target, shape->target_is_int64, p.V, loss, lse,
