@@ -17,6 +17,7 @@
 // All exponentials are 2^x: with c = log2(e) / tau, exp(z / tau - max) = 2^(z c - max c) is one multiply-add.
 #pragma once
 
+#include <cfloat>
 #include <type_traits>
 
 #include "bns_async.cuh"
@@ -25,14 +26,19 @@ namespace bns {
 
 constexpr int kDistillMaxEntries = 1024;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kFar = 0x1p29f;       // beyond it the rounding of max c, 2^-24 of it, is too much for an exponent
+constexpr float kNear = 0x1p28f;      // beside a maximum within it, what lies below -kFar is 0
 
-// Maximum m of a set of values times c (rounded once: it is only the reference) and sum of 2^(value c - m).
+// Maximum m of a set of values times c (rounded once: it is only the reference) and sum of 2^(value c - m).  Values whose
+// maximum is beyond kFar (masks such as -1e10, or the type's lowest value) add nothing but the maximum: a row whose own
+// maximum is beyond kNear is done again, of differences.
 struct TopSum {
     float m, s;
 };
+__device__ __forceinline__ float reference(float m) { return fabsf(m) <= kFar ? m : __int_as_float(0x7f800000); }
 __device__ __forceinline__ TopSum top_of(float value, float c) {
     const float m = value * c;
-    return {m, m == __int_as_float(0xff800000) ? 0.f : exp2_fast(fmaf(value, c, -m))};
+    return {m, exp2_fast(fmaf(value, c, -reference(m)))};
 }
 // Joins two; a side without values (m = -inf, s = 0) changes nothing.  NaN travels in s.
 __device__ __forceinline__ TopSum join(TopSum a, TopSum b) {
@@ -146,6 +152,21 @@ __device__ __forceinline__ TopSum student_of(const Distill& a, float lse) {
     return {m, exp2_fast(static_cast<float>(exponent - m))};
 }
 
+// A value of all threads of the block, joined in warp order; `fold` is shared memory for a value of each warp.
+template <typename Join>
+__device__ __forceinline__ float block_of(float v, float* fold, Join&& join_two) {
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = join_two(v, __shfl_xor_sync(0xffffffffu, v, o));
+    __syncthreads();
+    if (lane == 0) fold[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = fold[0];
+    for (int w = 1; w < warps; ++w) v = join_two(v, fold[w]);
+    __syncthreads();
+    return v;
+}
+
 // Both pairs of all lanes joined: the maximum first, so that each sum is scaled once.
 __device__ __forceinline__ void warp_join(TopSum& a, TopSum& b) {
     float ma = a.m, mb = b.m;
@@ -166,6 +187,107 @@ __device__ __forceinline__ void warp_join(TopSum& a, TopSum& b) {
     }
 }
 
+// The teacher's probability at place i: the sum over all entries there, in the list's order.
+__device__ __forceinline__ float share_of(const int* place, const float* p, int K, int i) {
+    float share = 0.f;
+    for (int j = 0; j < K; j += 4) {
+        const int4 at = *reinterpret_cast<const int4*>(place + j);
+        const float4 pj = *reinterpret_cast<const float4*>(p + j);
+        share += at.x == i ? pj.x : 0.f;
+        share += at.y == i ? pj.y : 0.f;
+        share += at.z == i ? pj.z : 0.f;
+        share += at.w == i ? pj.w : 0.f;
+    }
+    return share;
+}
+
+// A row whose largest logit, or largest teacher's value, times c is beyond kNear (all of them masked with -1e10 or with the
+// type's lowest value, say): everything is taken of differences, which the fast form has no time for.  Runs after the fast
+// form has written what it made of the row, and replaces that: there nothing is kept in registers for later, and its
+// loops are left rolled (4096 x 131072: 419 us; 416 without it, 430 unrolled, 450 as a function that is called).  Every block looks at the whole row and writes its own columns.  A row of -inf alone
+// has no answer: it stays.
+template <typename T, bool LOSS, bool GRAD>
+__device__ __forceinline__ void distill_far_row(const Distill& a, const int* place, float* p, float* fold) {
+    using S = typename T::storage;
+    constexpr int V = 16 / sizeof(S);
+    int block, tid;      // read again, so that nothing derived from them is kept across the fast form's loops
+    asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(block));
+    asm volatile("mov.u32 %0, %%tid.x;" : "=r"(tid));
+    const int64_t row = block / a.parts;
+    const int part = block - static_cast<int>(row) * a.parts, threads = blockDim.x;
+    const S* z = static_cast<const S*>(a.z) + row * a.z_stride;
+    const float inf = __int_as_float(0x7f800000);
+    auto larger = [](float x, float y) { return fmaxf(x, y); };
+    auto plus = [](float x, float y) { return x + y; };
+    float base = 0.f, sum = 1.f;
+    if constexpr (LOSS) {
+        float top = -inf;
+#pragma unroll 1
+        for (int v = tid; v < a.V; v += threads) top = fmaxf(top, to_float<T>(z[v]));
+        base = block_of(top, fold, larger);
+        if (base == -inf) return;
+        float mine = 0.f;
+#pragma unroll 1
+        for (int v = tid; v < a.V; v += threads) mine += exp2_fast((to_float<T>(z[v]) - base) * a.c);
+        sum = block_of(mine, fold, plus);
+    } else {
+        base = a.lse_in[row] * a.tau;
+    }
+    auto entry = [&](int k) {
+        const int64_t e = row * a.K + k;
+        return a.teacher_bf16 ? to_float<BF16>(static_cast<const unsigned short*>(a.teacher)[e])
+                              : static_cast<const float*>(a.teacher)[e];
+    };
+    float most = -inf, total = 0.f;
+#pragma unroll 1
+    for (int k = tid; k < a.K; k += threads)
+        if (place[k] >= 0) most = fmaxf(most, entry(k));
+    most = block_of(most, fold, larger);
+    const bool any = most != -inf;
+#pragma unroll 1
+    for (int k = tid; k < a.K; k += threads)
+        if (place[k] >= 0 && any) total += exp2_fast((entry(k) - most) * a.c);
+    total = block_of(total, fold, plus);
+    float loss = 0.f;
+#pragma unroll 1
+    for (int k = tid; k < (a.K + 3) / 4 * 4; k += threads) {
+        float pk = 0.f;
+        if (k < a.K && place[k] >= 0 && any) {
+            const float v = (entry(k) - most) * a.c;
+            pk = exp2_fast(v) / total;
+            if (LOSS && pk != 0.f)
+                loss = fmaf(pk, (v + log2f(sum) - log2f(total)) * kLn2 + (base - to_float<T>(z[place[k]])) / a.tau, loss);
+        }
+        p[k] = pk;
+    }
+    if constexpr (LOSS) {
+        loss = block_of(loss, fold, plus);
+        if (tid == 0 && part == 0) {
+            a.loss[row] = a.tau * a.tau * loss;
+            if (a.lse) a.lse[row] = base / a.tau + log2f(sum) * kLn2;
+        }
+    }
+    if constexpr (GRAD) {
+        S* dz = static_cast<S*>(a.dz) + row * a.dz_stride;
+        const float g = a.dloss[row] * a.tau, factor = g / sum;
+        const int head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(S)));
+        const int vectors = (a.V - head) / V, begin = min(vectors, part * a.per), end = min(vectors, begin + a.per);
+        const int first = part == 0 ? 0 : head + begin * V, last = part == a.parts - 1 ? a.V : head + end * V;
+        auto q = [&](float v) {
+            const float e = (v - base) * a.c;
+            return exp2_fast(e > 0.f ? 0.f : e) * factor;      // above 0 only by the rounding of a given log-sum
+        };
+#pragma unroll 1
+        for (int v = first + tid; v < last; v += threads) dz[v] = from_float<T>(any ? q(to_float<T>(z[v])) : 0.f);
+        __syncthreads();
+#pragma unroll 1
+        for (int k = tid; k < a.K; k += threads) {
+            const int i = place[k];
+            if (i >= first && i < last && any) dz[i] = from_float<T>(q(to_float<T>(z[i])) - g * share_of(place, p, a.K, i));
+        }
+    }
+}
+
 // Part blockIdx % parts of row blockIdx / parts: `per` vectors, and the loose elements at either end of the row.
 template <typename T, typename WHAT, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const Distill a) {
@@ -177,6 +299,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
     __shared__ TopSum fold[2][kWarps];                  // teacher, student
     __shared__ TopSum of_part[kDistillParts];
     __shared__ float sums[kWarps];
+    __shared__ bool far;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float inf = __int_as_float(0x7f800000);
     grid_dependency_wait();
@@ -225,7 +348,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
             own_index[o] = -1;
             own_value[o] = -inf;
         } else {
-            teacher = join(teacher, top_of(own_value[o], a.c));
+            TopSum t = top_of(own_value[o], a.c);
+            if (own_value[o] != -inf) t.m = fmaxf(t.m, -FLT_MAX);      // the type's lowest value is not -inf
+            teacher = join(teacher, t);
         }
         own_z[o] = own_index[o] >= 0 ? to_float<T>(z[own_index[o]]) : 0.f;
         if (k < (a.K + 3) / 4 * 4) place[k] = static_cast<int>(own_index[o]);
@@ -240,7 +365,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
             for (int i = 0; i < kDistillDepth; ++i)
                 if (v0 + i * THREADS < end) top.add(x[i]);
             const float m = fmaxf(top.get() * a.c, st.m);
-            const float ref = m == -inf ? 0.f : m;
+            const float ref = reference(m);
             pair_t sum = make_pair(st.s * exp2_fast(st.m - ref), 0.f);
 #pragma unroll
             for (int i = 0; i < kDistillDepth; ++i)
@@ -270,21 +395,24 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
             st = of_part[0];
             for (int q = 1; q < a.parts; ++q) st = join(st, of_part[q]);
         }
-        if (tid == 0 && part == 0 && a.lse) a.lse[row] = (st.m + log2f(st.s)) * kLn2;
     } else {
         st = student_of(a, lse);
     }
     const bool any = teacher.s != 0.f;             // false: no entry, or all at -inf
 
-    // p_k, and the loss: log-sum of the student minus the teacher's, plus the difference of the logits
+    // the log-sum of a backward call tells -inf (nothing to do again) from far down
+    if (tid == 0) far = (!(fabsf(st.m) <= kNear) && (kLoss || lse != -inf)) || (fabsf(teacher.m) > kNear && teacher.m != -inf);
+    if (kLoss && tid == 0 && part == 0 && a.lse) a.lse[row] = (st.m + log2f(st.s)) * kLn2;
+
+    // p_k, and the loss of differences to the two maxima: log p_k - log q_k in units of ln 2
     float loss = 0.f;
-    const float between = kLoss ? ((st.m - teacher.m) + (log2f(st.s) - log2f(teacher.s))) * kLn2 : 0.f;
+    const float between = kLoss ? log2f(st.s) - log2f(teacher.s) : 0.f;
 #pragma unroll
     for (int o = 0; o < kDistillOwn; ++o) {
         const int k = tid + o * THREADS;
-        const float v = own_value[o];
-        const float pk = any && v != -inf ? exp2_fast(fmaf(v, a.c, -teacher.m)) / teacher.s : 0.f;
-        if (kLoss && pk != 0.f) loss = fmaf(pk, (v - own_z[o]) / a.tau + between, loss);
+        const float v = fmaf(own_value[o], a.c, -teacher.m);
+        const float pk = any && own_value[o] != -inf ? exp2_fast(v) / teacher.s : 0.f;
+        if (kLoss && pk != 0.f) loss = fmaf(pk, (v - fmaf(own_z[o], a.c, -st.m)) + between, loss);
         if (k < (a.K + 3) / 4 * 4) p[k] = pk;
     }
     if constexpr (kLoss) {
@@ -320,15 +448,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
         for (int o = 0; o < kDistillOwn; ++o) {
             const int i = static_cast<int>(own_index[o]);
             if (i < first || i >= last || !any) continue;
-            float share = 0.f;
-            for (int j = 0; j < a.K; j += 4) {
-                const int4 at = *reinterpret_cast<const int4*>(place + j);
-                const float4 pj = *reinterpret_cast<const float4*>(p + j);
-                share += at.x == i ? pj.x : 0.f;
-                share += at.y == i ? pj.y : 0.f;
-                share += at.z == i ? pj.z : 0.f;
-                share += at.w == i ? pj.w : 0.f;
-            }
+            const float share = share_of(place, p, a.K, i);
             dz[i] = from_float<T>(exp2_fast(fmaf(own_z[o], a.c, -shift)) * factor - g * share);
         }
     } else {
@@ -337,7 +457,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
     if (kLoss && tid == 0 && part == 0) {
         float sum = 0.f;
         for (int w = 0; w < kWarps; ++w) sum += sums[w];
-        a.loss[row] = a.tau * a.tau * sum;
+        a.loss[row] = a.tau * a.tau * kLn2 * sum;
+    }
+    if (far) {
+        __syncthreads();     // what this replaces is written
+        distill_far_row<T, kLoss, kGrad>(a, place, p, sums);
     }
 }
 

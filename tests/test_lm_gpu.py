@@ -383,7 +383,7 @@ def distill_want(z, a, index, dloss, tau):
     at = torch.where(there, index, torch.zeros_like(index)).long()
     terms = torch.where(p > 0, p * (torch.log(p) - zd.gather(1, at) + lse[:, None]), torch.zeros_like(p))
     loss, size = tau * tau * terms.sum(1), tau * tau * (p * (zd.gather(1, at).abs() + lse.abs()[:, None] + ad.nan_to_num(neginf=0).abs() + 1)).sum(1)
-    q = torch.exp(zd - lse[:, None]) * some[:, None]
+    q = torch.softmax(zd, 1) * some[:, None]      # not exp(z - lse): log V vanishes beside logits of 1e38 in 64 bits too
     share = torch.zeros_like(q).scatter_add_(1, at, p)
     scale = (dloss.double() * tau)[:, None]
     return loss, lse, (q - share) * scale, (q + share) * scale, size
@@ -448,6 +448,94 @@ def test_distillation_masked_vocabulary():
     assert bool(dz.isfinite().all()) and math.isclose(float(dz[1, 250]), -float(dloss[1]) / 6, rel_tol=1e-5)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [300, 5001])
+def test_distillation_logits_at_the_types_lowest_value(V, dtype):
+    """Masked with the lowest finite value: where some logits are not, they carry nothing; where all are, the student is
+    uniform."""
+    from paper_1810_10962_b200 import lm
+    z, a, index, dloss = distill_case(5, V, 6, dtype, 31)
+    lowest = torch.finfo(z.dtype).min
+    index = index.clamp(min=0)
+    a[:] = 0
+    z[1, V // 2:] = lowest
+    index[1] = index[1] % (V // 2)
+    z[3] = lowest
+    loss, lse, dz, size, terms = distill_want(z, a, index, dloss, 1.0)
+    got_loss, got_lse = lm.topk_distillation_forward(z, a, index, 1.0)
+    step_loss, step_dz = lm.topk_distillation_step(z, a, index, dloss, 1.0)
+    others = [0, 1, 2, 4]
+    assert torch.allclose(got_loss[others].double(), loss[others], rtol=1e-4, atol=1e-5)
+    assert torch.allclose(step_dz.double(), dz, rtol=2e-2 if dtype == "bf16" else 1e-4, atol=1e-7)
+    assert float(got_lse[3]) == lowest and torch.equal(step_loss, got_loss)
+    # six places of equal weight against a uniform student; the same place twice counts twice
+    assert math.isclose(float(got_loss[3]), math.log(V / 6), rel_tol=1e-4)
+    assert bool(lm.topk_distillation_backward(z, a, index, got_lse, dloss, 1.0).isfinite().all())
+
+
+@pytest.mark.parametrize("tau", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_distillation_teacher_at_the_types_lowest_value(dtype, tau):
+    """Entries at the lowest finite value carry nothing beside others, and are of equal weight where there are only such."""
+    from paper_1810_10962_b200 import lm
+    V, K = 1200, 5
+    g = gen(77)
+    z = randn(g, 4, V).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    a = randn(g, 4, K).to(z.dtype)
+    a[1, 2:] = torch.finfo(a.dtype).min
+    a[2] = torch.finfo(a.dtype).min
+    index = torch.stack([torch.randperm(V, generator=g, device=g.device)[:K] for _ in range(4)]).to(torch.int32).to(z.device)
+    dloss = torch.tensor([1.0, 2.0, -1.0, 0.5], device=z.device)
+    p = torch.softmax(a.double() / tau, -1)
+    log_q = torch.log_softmax(z.double() / tau, -1)
+    terms = torch.where(p > 0, p * (p.clamp(min=1e-300).log() - log_q.gather(1, index.long())), torch.zeros_like(p))
+    dz = log_q.exp().scatter_add(1, index.long(), -p) * (dloss.double() * tau)[:, None]
+    loss, lse = lm.topk_distillation_forward(z, a, index, tau)
+    step_loss, step_dz = lm.topk_distillation_step(z, a, index, dloss, tau)
+    # exponents of some 20 at most, in fp32: 20 x 2^-23 an operation, few of them in a row
+    assert torch.allclose(loss.double(), tau * tau * terms.sum(-1), rtol=2e-5, atol=2e-5 * tau * tau)
+    assert torch.equal(step_loss, loss)
+    for got in (step_dz, lm.topk_distillation_backward(z, a, index, lse, dloss, tau)):
+        assert torch.allclose(got.double(), dz, rtol=2.0 ** -8 if dtype == "bf16" else 5e-5, atol=2e-6 * tau)
+
+
+@pytest.mark.parametrize("tau", [0.7, 1.0])
+@pytest.mark.parametrize("mask", [-1e4, -1e9, -1e10, -3e20, -1e38, 1e10])
+def test_distillation_far_logits(mask, tau):
+    """Masks of other sizes, for stretches of a row, for most of it and for a whole row; likewise among the teacher's values.
+    As a positive number it is what the rest of the row vanishes beside."""
+    from paper_1810_10962_b200 import lm
+    V, K = 40000, 5
+    g = gen(78)
+    z, a = randn(g, 6, V), randn(g, 6, K)
+    z[1, 7000:23001] = mask
+    z[2, 3:V - 1] = mask
+    z[3] = mask
+    a[4, :3] = mask
+    a[5] = mask
+    index = torch.stack([torch.randperm(V, generator=g, device=g.device)[:K] for _ in range(6)]).to(torch.int32)
+    index[:, 0] = 5                # masked in rows 2 and 3
+    index[1:3, 1:] = torch.tensor([0, 1, 2, V - 1], device=index.device, dtype=torch.int32)
+    dloss = torch.tensor([1.0, 2.0, -1.0, 0.5, 1.0, 1.0], device=z.device)
+    p = torch.softmax(a.double() / tau, -1)
+    log_q = torch.log_softmax(z.double() / tau, -1)
+    terms = torch.where(p > 0, p * (p.clamp(min=1e-300).log() - log_q.gather(1, index.long())), torch.zeros_like(p))
+    want = tau * tau * terms.sum(-1)
+    dz = log_q.exp().scatter_add(1, index.long(), -p) * (dloss.double() * tau)[:, None]
+    loss, lse = lm.topk_distillation_forward(z, a, index, tau)
+    step_loss, step_dz = lm.topk_distillation_step(z, a, index, dloss, tau)
+    # losses: differences of logits and a log-sum of some 20, and of a mask where an entry is masked
+    assert torch.allclose(loss.double(), want, rtol=2e-5, atol=2e-5)
+    assert torch.equal(step_loss, loss)
+    assert torch.allclose(step_dz.double(), dz, rtol=1e-4, atol=2e-6)
+    assert torch.allclose(lse.double(), torch.logsumexp(z.double() / tau, -1), rtol=1e-6, atol=2e-5)
+    # the gradient from a log-sum in fp32 is as good as that number: the rows of usual size
+    usual = lse.abs() < 1e3
+    got = lm.topk_distillation_backward(z, a, index, lse, dloss, tau)
+    assert torch.allclose(got[usual].double(), dz[usual], rtol=1e-4, atol=2e-6)
+    assert bool(got.isfinite().all())
+
+
 def test_distillation_places_outside_the_vocabulary_are_no_entries():
     from paper_1810_10962_b200 import lm
     z, a, index, dloss = distill_case(3, 100, 8, "f32", 10, int64=True)
@@ -500,3 +588,57 @@ def test_example_learns():
     spec.loader.exec_module(module)
     first, last = module.main(["--steps", "1"]), module.main(["--steps", "40"])
     assert 6.0 < first < 8.0 and last < 0.5 * first       # log 1000 = 6.9 at the start
+
+
+# ----------------------------------------------------------------------------- more than 2^31 elements
+def test_norm_past_32_bit_offsets():
+    from paper_1810_10962_b200 import lm
+    T, D = 540_000, 4096                                     # 2.2e9 elements
+    x = torch.empty(T, D, dtype=torch.bfloat16, device="cuda")
+    x[-5:] = randn(gen(61), 5, D, dtype="bf16")
+    x[:-5] = 1
+    w = 1 + 0.3 * randn(gen(62), D)
+    y, _, rstd = lm.rms_norm_forward(x, None, w, EPS)
+    want = lm.rms_norm_forward(x[-5:].contiguous(), None, w, EPS)
+    assert torch.equal(y[-5:], want[0]) and torch.equal(rstd[-5:], want[2])
+    del y
+    q, scales, _, _ = lm.rms_norm_forward_fp8(x, None, w, EPS, group=128)
+    want_q = lm.rms_norm_forward_fp8(x[-5:].contiguous(), None, w, EPS, group=128)
+    assert torch.equal(q[-5:].float(), want_q[0].float()) and torch.equal(scales[-5:], want_q[1])
+    del q, scales
+    dx, _ = lm.rms_norm_backward(x, x, w, rstd)
+    assert torch.equal(dx[-5:], lm.rms_norm_backward(x[-5:].contiguous(), x[-5:].contiguous(), w, rstd[-5:].contiguous())[0])
+
+
+def test_distillation_past_32_bit_offsets():
+    from paper_1810_10962_b200 import lm
+    T, V, K = 17_000, 131072, 8                              # 2.2e9 elements
+    z = torch.zeros(T, V, dtype=torch.bfloat16, device="cuda")
+    tail, a, index, dloss = distill_case(5, V, K, "bf16", 63)
+    z[-5:] = tail
+    full = lambda t: torch.cat([t[:1].expand(T - 5, *t.shape[1:]), t]).contiguous()  # noqa: E731
+    loss, dz = lm.topk_distillation_step(z, full(a), full(index), full(dloss), 2.0)
+    want_loss, want_dz = lm.topk_distillation_step(tail, a, index, dloss, 2.0)
+    assert torch.allclose(loss[-5:], want_loss, rtol=1e-5, atol=1e-6)
+    assert torch.allclose(dz[-5:].float(), want_dz.float(), rtol=2 ** -7, atol=1e-9)
+
+
+def test_head_past_32_bit_offsets():
+    from paper_1810_10962_b200 import lm
+    T, V, D = 8, 1_100_000, 2048                             # 2.25e9 weights
+    w = torch.zeros(V, D, dtype=torch.bfloat16, device="cuda")
+    g = gen(64)
+    x = randn(g, T, D, dtype="bf16")
+    w[-300:] = (randn(g, 300, D) * 0.05).bfloat16()
+    target = torch.randint(V - 300, V, (T,), device="cuda", generator=g)
+    dloss = torch.rand(T, device="cuda", generator=g) + 0.5
+    loss, lse = lm.linear_cross_entropy_forward(x, w, target)
+    z = x.double() @ w[-300:].double().T
+    want = torch.logsumexp(torch.cat([z, torch.full((T, 1), math.log(V - 300), device="cuda", dtype=torch.float64)], 1), 1)
+    assert torch.allclose(lse.double(), want, rtol=1e-5)
+    at = (target - (V - 300))[:, None]
+    assert torch.allclose(loss.double(), want - z.gather(1, at)[:, 0], rtol=1e-5, atol=1e-5)
+    _, dw = lm.linear_cross_entropy_backward(x, w, target, lse, dloss)
+    G = torch.exp(z - want[:, None]) * dloss.double()[:, None]
+    G.scatter_add_(1, at, -dloss.double()[:, None])
+    assert_within(dw[-300:], G.T @ x.double(), 2.0 ** -7 * (G.abs().T @ x.double().abs()) + 1e-8, "dw")
