@@ -11,7 +11,7 @@ LIBRARY = os.path.join(HERE, "libbns.so")
 SOURCES = [os.path.join(CSRC, name) for name in ("bns_api.cu", "bns_lm_api.cu")]
 HEADERS = [os.path.join(CSRC, name) for name in (
     "bns_host.h", "bns_elements.cuh", "bns_async.cuh", "bns_kernels.cuh", "bns_nhwc_kernels.cuh", "bns_slab_kernels.cuh",
-    "bns_rms_kernels.cuh", "bns_head_kernels.cuh", "bns_distill_kernels.cuh")] + [os.path.join(ROOT, "include", "bns.h")]
+    "bns_rms_kernels.cuh", "bns_head_kernels.cuh", "bns_head_few_kernels.cuh", "bns_distill_kernels.cuh")] + [os.path.join(ROOT, "include", "bns.h")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

@@ -25,8 +25,10 @@
 // The tensor core truncates as it accumulates: after n steps of 16 a sum has lost some n 2^-25 of itself, always towards
 // zero.  Where the result is an fp32 number (the logits' statistics, everything of fp32 tensors) the sum is therefore
 // taken in segments of K, which the epilogue's threads add up in registers, rounding to nearest: 512 elements for bf16
-// (256 cost 9 % of the time, 307 -> 334 us at 2048 x 50257 x 2048, for half of an error of 3e-7), 256 for the high terms
-// of fp32 (at 512 the loss is 1e-6 off, at 256 4e-7), 4096 for products with a low term, which count 2^-11.
+// (256 cost 9 % of the time, 307 -> 334 us at 2048 x 50257 x 2048, for half of an error of 3e-7), 128 where a CTA works
+// alone (few rows, whose errors do not average out: at 4 x 3187 x 1120 the loss is 3e-7 off instead of 8e-7; 24 x 32768 x
+// 1024 takes 25 us either way, 128 x 50000 x 4096 96 instead of 90), 256 for the high terms of fp32 (at 512 the loss is
+// 1e-6 off, at 256 4e-7), 4096 for products with a low term, which count 2^-11.
 //
 // Every wait is bounded: one that runs out is counted, and the block ends without touching memory further.
 #pragma once
@@ -40,7 +42,7 @@
 namespace bns {
 
 constexpr int kHeadM = 128, kHeadN = 256, kHeadK = 64;   // rows of a CTA, columns of a tile, K per stage
-constexpr int kHeadSegment = 8, kHeadSegmentHigh = 4, kHeadSegmentLow = 64;   // stages of K per segment
+constexpr int kHeadSegment = 8, kHeadSegmentFew = 2, kHeadSegmentHigh = 4, kHeadSegmentLow = 64;   // stages of K per segment
 constexpr int kHeadThreads = 384;
 
 // Narrow tiles of the products with the logits, for few rows and few columns: 64 columns, and half of A's stage.
@@ -293,9 +295,9 @@ __device__ __forceinline__ void head_pair(int pair, int pairs, int& a, int& b) {
     b = p == 1;
 }
 // Where a segment that begins at k ends.  In fp32 those of the low terms end before the high ones begin.
-template <bool FP32>
+template <bool FP32, int CTAS>
 __device__ __forceinline__ int head_segment_end(const HeadGemm& g, int k, int k1) {
-    if constexpr (!FP32) return min(k + kHeadSegment, k1);
+    if constexpr (!FP32) return min(k + (CTAS == 1 ? kHeadSegmentFew : kHeadSegment), k1);
     const int low = 2 * g.k_blocks;
     return min(k < low ? min(k + kHeadSegmentLow, low) : k + kHeadSegmentHigh, k1);
 }
@@ -744,7 +746,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 const HeadTile t(g, id);
                 for (int k = t.k0, end; ok && k < t.k1; k = end, ++n) {
                     const int buffer = n & 1;
-                    end = kSegments ? head_segment_end<kFp32>(g, k, t.k1) : t.k1;
+                    end = kSegments ? head_segment_end<kFp32, CTAS>(g, k, t.k1) : t.k1;
                     if (n >= 2 && !(ok = wait_bounded(drained + 8 * buffer, (n / 2 - 1) & 1, &gave_up))) break;
                     head::fence_after();
                     const unsigned d = tmem + buffer * N;
@@ -816,7 +818,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 float acc[N / 2];
 #pragma unroll
                 for (int j = 0; j < N / 2; ++j) acc[j] = 0.f;
-                for (int k = t.k0; k < t.k1; k = head_segment_end<kFp32>(g, k, t.k1)) {
+                for (int k = t.k0; k < t.k1; k = head_segment_end<kFp32, CTAS>(g, k, t.k1)) {
                     if (!wait_ready()) break;
                     const float weight = kFp32 && k < 2 * g.k_blocks ? 1.f / kHeadLow : 1.f;
 #pragma unroll

@@ -5,6 +5,7 @@
 #include <atomic>
 
 #include "bns_distill_kernels.cuh"
+#include "bns_head_few_kernels.cuh"
 #include "bns_head_kernels.cuh"
 #include "bns_host.h"
 #include "bns_rms_kernels.cuh"
@@ -233,6 +234,9 @@ struct HeadProblem {
     int piece, pieces;              // columns of the vocabulary at a time
     int G_pitch;
     int splits;                     // of dx along the vocabulary
+    int few;                        // rows of the kernels for few rows, or 0; with them, of the products:
+    bool few_words;                 // W's rows are made of 16-byte words
+    int few_threads, few_groups, few_chunks, few_per;
     size_t off_scalars, off_x, off_w, off_G, off_partial, off_logit, off_sums, total;
 };
 
@@ -277,8 +281,21 @@ int split_head(const HeadProblem& p) {
     return best;
 }
 
+int few_pitch(int width, bool words) { return words ? width : divide_up(width, 32 * kFewLane) * 32 * kFewLane; }
+
+// Rows that the few rows' kernels are compiled for, or 0 where the tensor cores do the products: fp32 only (bf16 needs no new
+// layout for the tensor cores: 32768 x 1024 with one row 24 us forward, 64 on the fp32 pipes), while x fits shared memory.
+int few_rows(const bns_head* sh, bool words, bool backward) {
+    if (sh->dtype != BNS_F32 || sh->rows == 0 || sh->rows > (backward ? kFewRowsBackward : kFewRows)) return 0;
+    int rows = 1;
+    while (rows < sh->rows) rows *= 2;
+    return static_cast<size_t>(rows) * few_pitch(sh->width, words) * sizeof(float) <= kFewSharedMost ? rows : 0;
+}
+
 HeadProblem plan_head(const bns_head* sh, bool backward) {
     HeadProblem p{};
+    p.few_words = sh->width % kFewLane == 0 && sh->w_stride % kFewLane == 0;
+    p.few = few_rows(sh, p.few_words, backward);
     p.T = sh->rows;
     p.V = sh->vocabulary;
     p.D = sh->width;
@@ -292,6 +309,28 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     size_t column = 0;              // workspace bytes per column of the vocabulary
     if (p.copy_w) column = static_cast<size_t>(p.terms) * p.pitch * 2;
     if (backward) column = std::max(column, static_cast<size_t>(p.T) * p.terms * 2);
+    if (p.few) {
+        size_t at = kHeaderBytes;
+        auto take = [&](size_t bytes) {
+            const size_t here = at;
+            at = align_up(at + bytes);
+            return here;
+        };
+        p.few_threads = std::min(kFewProductThreads, divide_up(divide_up(p.D, kFewLane), 32) * 32);
+        p.few_groups = divide_up(p.D, p.few_threads * kFewLane);
+        const int blocks = sm_count() * 2 * (kFewProductThreads / p.few_threads);
+        p.few_per = std::max(8, divide_up(p.V, std::max(1, blocks / p.few_groups)));
+        p.few_chunks = divide_up(p.V, p.few_per);
+        if (backward) {
+            p.off_G = take(static_cast<size_t>(p.V) * p.few * 4);
+            p.off_sums = take(static_cast<size_t>(p.few_chunks) * p.T * p.D * 4);
+        } else {
+            p.off_partial = take(static_cast<size_t>(sm_count()) * p.T * sizeof(float2));
+            p.off_logit = take(static_cast<size_t>(p.T) * 4);
+        }
+        p.total = at;
+        return p;
+    }
     int64_t piece = p.V;
     if (column) piece = std::max<int64_t>(kHeadPieceLeast, static_cast<int64_t>(kHeadPieceBytes / column) / kHeadN * kHeadN);
     if (g_head_piece > 0 && (p.copy_w || backward)) piece = std::min<int64_t>(piece, g_head_piece);
@@ -475,6 +514,69 @@ bns_status rows_of_w(const HeadProblem& p, const bns_head* sh, const void* w, in
 }
 
 // ------------------------------------------------------------------------------------ distillation
+// The few rows' kernels: the logits' statistics, or the gradients.
+template <int ROWS, bool WORDS, bool GRAD>
+bns_status few_logits(const HeadFew& a, cudaStream_t stream) {
+    static std::atomic<bool> raised[kMaxDevices];
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= kMaxDevices) return BNS_ERR_CUDA;
+    auto kernel = head_few_logits_kernel<ROWS, WORDS, GRAD>;
+    if (!raised[device].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kFewSharedMost)) != cudaSuccess) {
+            cudaGetLastError();
+            return BNS_ERR_CUDA;
+        }
+        raised[device].store(true, std::memory_order_relaxed);
+    }
+    launch(GRAD ? BNS_KERNEL_HEAD_GRADIENT : BNS_KERNEL_HEAD_LOGITS, kernel,
+           Shape{static_cast<unsigned>(sm_count()), FewShape<ROWS>::kThreads}, static_cast<size_t>(ROWS) * a.pitch * sizeof(float), stream, a);
+    return last_error();
+}
+template <int ROWS, bool WORDS>
+bns_status few_head_of(const HeadProblem& p, HeadFew a, char* ws, bool backward, cudaStream_t stream) {
+    if (ROWS > kFewRowsBackward || !backward) {
+        a.partial = reinterpret_cast<float2*>(ws + p.off_partial);
+        a.target_logit = reinterpret_cast<float*>(ws + p.off_logit);
+        a.status = reinterpret_cast<unsigned*>(ws);
+        return few_logits<ROWS, WORDS, false>(a, stream);
+    }
+    if constexpr (ROWS <= kFewRowsBackward) {
+        a.G = reinterpret_cast<float*>(ws + p.off_G);
+        a.sums = reinterpret_cast<float*>(ws + p.off_sums);
+        a.chunks = p.few_chunks;
+        a.per = p.few_per;
+        a.groups = p.few_groups;
+        const bns_status st = few_logits<ROWS, WORDS, true>(a, stream);
+        if (st != BNS_OK) return st;
+        launch(BNS_KERNEL_HEAD_PRODUCT, head_few_products_kernel<ROWS, WORDS>,
+               Shape{static_cast<unsigned>(p.few_chunks * p.few_groups), static_cast<unsigned>(p.few_threads)}, 0, stream, a);
+        const int64_t elements = static_cast<int64_t>(p.T) * p.D;
+        launch(BNS_KERNEL_HEAD_VECTOR, head_few_join_kernel, Shape{static_cast<unsigned>(divide_up<int64_t>(elements, 32)), 256}, 0, stream, a);
+    }
+    return last_error();
+}
+template <bool WORDS>
+bns_status few_head_in(const HeadProblem& p, const HeadFew& a, char* ws, bool backward, cudaStream_t stream) {
+    switch (p.few) {
+        case 1: return few_head_of<1, WORDS>(p, a, ws, backward, stream);
+        case 2: return few_head_of<2, WORDS>(p, a, ws, backward, stream);
+        case 4: return few_head_of<4, WORDS>(p, a, ws, backward, stream);
+        case 8: return few_head_of<8, WORDS>(p, a, ws, backward, stream);
+        case 16: return few_head_of<16, WORDS>(p, a, ws, backward, stream);
+        default: return few_head_of<32, WORDS>(p, a, ws, backward, stream);
+    }
+}
+bns_status few_head(const HeadProblem& p, const bns_head* sh, HeadFew a, char* ws, bool backward, cudaStream_t stream) {
+    a.x_stride = sh->x_stride;
+    a.w_stride = sh->w_stride;
+    a.target64 = sh->target_is_int64;
+    a.T = p.T;
+    a.V = p.V;
+    a.D = p.D;
+    a.pitch = few_pitch(p.D, p.few_words);
+    return p.few_words ? few_head_in<true>(p, a, ws, backward, stream) : few_head_in<false>(p, a, ws, backward, stream);
+}
+
 bns_status check_distillation(const bns_distillation* sh) {
     if (!sh) return BNS_ERR_NULL;
     if (sh->rows < 0 || sh->vocabulary <= 0 || sh->vocabulary > 1 << 30 || sh->entries < 1 || sh->entries > kDistillMaxEntries ||
@@ -627,6 +729,18 @@ bns_status bns_linear_cross_entropy_forward(const bns_head* shape, const void* x
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(workspace);
     if (p.T == 0) return cudaMemsetAsync(ws, 0, sizeof(uint32_t), stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
+    if (p.few) {
+        HeadFew a{};
+        a.x = static_cast<const float*>(x);
+        a.w = static_cast<const float*>(w);
+        a.target = target;
+        st = few_head(p, shape, a, ws, false, stream);
+        if (st != BNS_OK) return st;
+        launch(BNS_KERNEL_HEAD_VECTOR, head_join_kernel, Shape{1, 1024}, 0, stream, reinterpret_cast<const float2*>(ws + p.off_partial),
+               sm_count(), p.T, reinterpret_cast<const float*>(ws + p.off_logit), target, shape->target_is_int64, p.V, loss, lse,
+               reinterpret_cast<unsigned*>(ws));
+        return last_error();
+    }
     Operand xs, rows;
     st = rows_of_x(p, shape, x, ws, stream, xs);
     if (st != BNS_OK) return st;
@@ -677,6 +791,17 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
     const size_t eb = elem_bytes(p.dtype);
     if (p.T == 0)
         return cudaMemsetAsync(dw, 0, eb * p.V * p.D, stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
+    if (p.few) {
+        HeadFew a{};
+        a.x = static_cast<const float*>(x);
+        a.w = static_cast<const float*>(w);
+        a.target = target;
+        a.lse = lse;
+        a.dloss = dloss;
+        a.dx = static_cast<float*>(dx);
+        a.dw = static_cast<float*>(dw);
+        return few_head(p, shape, a, ws, true, stream);
+    }
     Operand xs, rows;
     st = rows_of_x(p, shape, x, ws, stream, xs);
     if (st != BNS_OK) return st;

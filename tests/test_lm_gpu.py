@@ -290,6 +290,36 @@ def test_head_strided_rows(pad_x, pad_w, dtype):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 7, 8, 9, 16, 17, 32, 33])
+@pytest.mark.parametrize("V,D", [(1, 3), (7, 4), (1001, 130), (333, 1024), (6001, 36), (50, 1633), (35, 4100)])
+def test_head_few_rows_fp32(T, V, D):
+    check_head(*head_case(T, V, D, "f32", 300 + T + V, int64=T % 2 == 0), "f32")
+
+
+@pytest.mark.parametrize("pad_x,pad_w", [(4, 8), (3, 0), (0, 5)])
+@pytest.mark.parametrize("D", [88, 90])
+def test_head_few_rows_strided(D, pad_x, pad_w):
+    T, V = 6, 500
+    x, w, target, dloss = head_case(T, V, D, "f32", 56)
+    xs, ws = torch.full((T, D + pad_x), math.nan, device="cuda"), torch.full((V, D + pad_w), math.nan, device="cuda")
+    xs[:, :D], ws[:, :D] = x, w
+    check_head(xs[:, :D], ws[:, :D], target, dloss, "f32")
+
+
+def test_head_few_rows_left_out():
+    from paper_1810_10962_b200 import bns, lm
+    x, w, target, dloss = head_case(5, 300, 20, "f32", 79, left_out=0.0)
+    target[1], target[3] = -7, 300              # left out, the second as it is past the vocabulary
+    workspace = torch.empty(lm.linear_cross_entropy_workspace_bytes(x, w, target), dtype=torch.uint8, device="cuda")
+    loss, lse = lm.linear_cross_entropy_forward(x, w, target, workspace=workspace)
+    assert bns.workspace_status(workspace) == lm.FLAG_BAD_TARGET
+    assert bool((loss[[1, 3]] == 0).all()) and bool((loss[[0, 2, 4]] > 0).all())
+    dloss[1] = math.nan
+    lse[3] = math.nan
+    dx, dw = lm.linear_cross_entropy_backward(x, w, target, lse, dloss)
+    assert bool((dx[[1, 3]] == 0).all()) and bool((dx[[0, 2, 4]] != 0).any(1).all()) and bool(dw.isfinite().all())
+
+
 def test_head_rows_left_out():
     from paper_1810_10962_b200 import bns, lm
     x, w, target, dloss = head_case(40, 500, 64, "bf16", 77)
