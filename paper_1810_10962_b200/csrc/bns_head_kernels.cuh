@@ -60,7 +60,9 @@ struct HeadRing {
     static constexpr unsigned kStaging = 8 * 32 * 128;   // 32 rows of 32 fp32 values for each warp of the epilogue
     static constexpr unsigned kSmem = kStages * kStage + kStaging + 1024;
 };
-constexpr int kHeadRaster = 16;        // row tiles that are swept together, so that their operand stays in L2
+// Row tiles that are swept together, so that their operand stays in L2 (2048 x 50257 x 2048 forward 314 us, 326 with four, 314 with 64;
+// 4096 x 131072 x 4096 forward and backward 13.7 ms, 14.3 and 14.7).
+constexpr int kHeadRaster = 16;
 constexpr float kHeadLow = 2048.f;                       // what the low fp16 term is stored times
 constexpr float kHeadTop = 8192.f;                       // where an fp32 tensor's largest value is brought to, at the least
 constexpr float kHeadLog2e = 1.4426950408889634f, kHeadLn2 = 0.6931471805599453f;
