@@ -413,6 +413,8 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
  * rows whose stride or width is no multiple of 8 elements are copied piece by piece, and fp32 tensors are
  * split into two fp16 terms (22 bits, kept down to 2^-28 of the tensor's largest value and falling off to
  * 2^-49 of it) whose products are added up in fp32: the result is as near as that of an fp32 product.
+ * fp32 tensors with few rows (32 forward, 16 backward, x within 216 KB) are multiplied in fp32 as they are;
+ * G of all of the vocabulary is then in the workspace.  Logits: up to 10^9 in magnitude.
  * rows <= 2^24, vocabulary <= 2^28, width <= 2^20.
  */
 typedef struct {
