@@ -552,8 +552,11 @@ struct HeadEpilogue {
         return *reinterpret_cast<const unsigned*>(&h);
     }
     // The warp's 32 rows x 32 columns of 16 bits, a row a lane, into shared memory (64-byte rows, 64-byte swizzle) and out
-    // by TMA, which drops rows and columns past the tensor's end.  Two buffers; z < 0: the map has two dimensions.
+    // by TMA, which drops rows and columns past the tensor's end.  Two buffers; z < 0: the map has two dimensions.  A warp
+    // none of whose rows exist leaves both buffers alone: it would commit no group, and the wait for all groups but the last
+    // frees the other buffer only while every turn commits one.
     __device__ __forceinline__ void send(const unsigned (&w)[16], int x, int z) {
+        if (row - lane >= g.M) return;
         if (lane == 0) head::wait_stores_read<1>();
         __syncwarp();
         const unsigned buffer = smem_address(stage) + turn * 2048;
@@ -565,7 +568,7 @@ struct HeadEpilogue {
                          : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0 && row < g.M) {
+        if (lane == 0) {
             if (z < 0)
                 head::tma_store(map, buffer, x, row);
             else
@@ -574,6 +577,7 @@ struct HeadEpilogue {
     }
     // The same for fp32: 128-byte rows, 128-byte swizzle, one buffer.
     __device__ __forceinline__ void send_floats(const float* f, int x) {
+        if (row - lane >= g.M) return;
         if (lane == 0) head::wait_stores_read<0>();
         __syncwarp();
         const unsigned buffer = smem_address(stage);
@@ -584,7 +588,7 @@ struct HeadEpilogue {
                          : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0 && row < g.M) head::tma_store(map, buffer, x, row);
+        if (lane == 0) head::tma_store(map, buffer, x, row);
     }
     __device__ __forceinline__ void scale(float (&v)[4]) const {
         const pair_t by = make_pair(factor, factor);
