@@ -807,6 +807,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         bool ok = true;
         for (int id = worker; ok && id < tiles; id += workers) {
             const HeadTile t(g, id);
+            // The splits are made for a full piece of the vocabulary, whose parts have four stages at the least.  A last piece with
+            // fewer stages than splits leaves some without any: no product is made for those, and the sums have all of theirs
+            if (KIND == kHeadOut && t.k0 == t.k1) continue;
             HeadEpilogue<KIND, T, N> e(g, t, (t.m * CTAS + rank) * kHeadM + slot * 32 + lane, half, stage, &map_c, turn, unit);
             const unsigned lanes = tmem + (static_cast<unsigned>(slot * 32) << 16) + half * (N / 2);
             auto wait_ready = [&]() {

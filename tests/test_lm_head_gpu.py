@@ -57,28 +57,39 @@ def check(x, w, target, dloss, dtype, segment_z, segment_out):
             assert torch.equal(a, b), f"{what} differs from call to call"
     assert bns.wait_timeouts() == 0
 
-    xd, wd = x.double(), w.double()
-    counts = target >= 0
-    at = target.clamp(min=0)[:, None]
-    z = xd @ wd.T
-    tz = (xd.abs() @ wd.abs().T).mul_(chain(D, dtype, segment_z))
-    want_lse = torch.logsumexp(z, 1)
-    q = torch.exp(z - want_lse[:, None])
-    t_lse = (q * tz).sum(1) + 8 * U * (1 + want_lse.abs()) + U * (V / 64 / 16 + 64)       # sums of exponentials: by thread, strip, row
-    within(lse, want_lse, t_lse, "lse")
-    z_at = z.gather(1, at)[:, 0]
-    want_loss = torch.where(counts, want_lse - z_at, torch.zeros_like(z_at))
-    within(loss, want_loss, t_lse + tz.gather(1, at)[:, 0] + 8 * U * z_at.abs(), "loss")
-    g = (dloss.double() * counts)[:, None]
-    # of an exponential, relative: its logit, the log-sum, the exponent's rounding, 2^x to 2 ulp, the factor
-    tz.add_(t_lse[:, None] + 16 * U).add_((z - want_lse[:, None]).abs_().add_(want_lse.abs()[:, None]).mul_(4 * U))
-    G = q.mul_(g)
-    tG = tz.mul_(G)
-    G.scatter_add_(1, at, -g)
-    tG.add_(G.abs().mul_(STORE["bf16"] if dtype == "bf16" else 6 * U))
-    for A, tA, B, n, got, what in ((G, tG, wd, V, dx, "dx"), (G.T, tG.T, xd, T, dw, "dw")):
-        want, size, off = A @ B, A.abs() @ B.abs(), tA @ B.abs()
-        within(got, want, off * 1.01 + size * chain(n, dtype, segment_out) + STORE[dtype] * 1.01 * want.abs() + 1e-30, what)
+    wd = w.double()
+    # rows of dw add up over blocks of rows; 2^28 logits at a time
+    want_dw = torch.zeros(V, D, device="cuda", dtype=torch.float64)
+    off_dw, size_dw = torch.zeros_like(want_dw), torch.zeros_like(want_dw)
+    rows = max(1, 2 ** 28 // V)
+    for first in range(0, T, rows):
+        part = slice(first, min(T, first + rows))
+        xd = x[part].double()
+        counts = target[part] >= 0
+        at = target[part].clamp(min=0)[:, None]
+        z = xd @ wd.T
+        tz = (xd.abs() @ wd.abs().T).mul_(chain(D, dtype, segment_z))
+        want_lse = torch.logsumexp(z, 1)
+        q = torch.exp(z - want_lse[:, None])
+        t_lse = (q * tz).sum(1) + 8 * U * (1 + want_lse.abs()) + U * (V / 64 / 16 + 64)   # sums of exponentials: by thread, strip, row
+        within(lse[part], want_lse, t_lse, f"lse from row {first}")
+        z_at = z.gather(1, at)[:, 0]
+        want_loss = torch.where(counts, want_lse - z_at, torch.zeros_like(z_at))
+        within(loss[part], want_loss, t_lse + tz.gather(1, at)[:, 0] + 8 * U * z_at.abs(), f"loss from row {first}")
+        g = (dloss[part].double() * counts)[:, None]
+        # of an exponential, relative: its logit, the log-sum, the exponent's rounding, 2^x to 2 ulp, the factor
+        tz.add_(t_lse[:, None] + 16 * U).add_((z - want_lse[:, None]).abs_().add_(want_lse.abs()[:, None]).mul_(4 * U))
+        G = q.mul_(g)
+        tG = tz.mul_(G)
+        G.scatter_add_(1, at, -g)
+        tG.add_(G.abs().mul_(STORE["bf16"] if dtype == "bf16" else 6 * U))
+        want = G @ wd
+        tol = (tG @ wd.abs()) * 1.01 + (G.abs() @ wd.abs()) * chain(V, dtype, segment_out) + STORE[dtype] * 1.01 * want.abs() + 1e-30
+        within(dx[part], want, tol, f"dx from row {first}")
+        want_dw += G.T @ xd
+        off_dw += tG.T @ xd.abs()
+        size_dw += G.abs().T @ xd.abs()
+    within(dw, want_dw, off_dw * 1.01 + size_dw * chain(T, dtype, segment_out) + STORE[dtype] * 1.01 * want_dw.abs() + 1e-30, "dw")
 
 
 # Products that give a CTA pair several tiles, with a number of rows whose last tile has warps without any: rows of dw
@@ -88,3 +99,16 @@ def check(x, w, target, dloss, dtype, segment_z, segment_out):
 def test_many_tiles(T, V, D, dtype):
     segment_z = 256 if dtype == "f32" else max(D, 512)          # bf16 gradient: one sum over the width
     check(*case(T, V, D, dtype, T + V + D), dtype, segment_z, 256 if dtype == "f32" else 1 << 40)
+
+
+# Pieces of the vocabulary whose last one has fewer stages of K than dx's sum has parts: 4097 = 4 x 1024 + 1 in four parts, and
+# 61464 = 15 x 4096 + 24 in two without any setting.
+@pytest.mark.parametrize("T,V,D,piece", [(200, 4097, 64, 1024), (200, 2049, 64, 512), (41979, 61464, 64, 0)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_last_piece_shorter_than_the_parts(T, V, D, piece, dtype):
+    from paper_1810_10962_b200 import bns
+    try:
+        bns.set_tuning("head_piece", piece)
+        check(*case(T, V, D, dtype, T + V), dtype, 256 if dtype == "f32" else 512, 256 if dtype == "f32" else 1 << 40)
+    finally:
+        bns.set_tuning("head_piece", 0)
