@@ -302,6 +302,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
     __shared__ bool far;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float inf = __int_as_float(0x7f800000);
+    // Another block's shared memory may be written once that block runs: all of the cluster arrive here, and wait for one
+    // another after the row's pass, which hides it
+    if (kLoss && a.parts > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     grid_dependency_wait();
     grid_dependency_launch();
     const int64_t row = blockIdx.x / a.parts;
@@ -385,13 +388,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
     warp_join(teacher, st);
     if constexpr (kLoss) {
         if (a.parts > 1) {      // every block of the cluster gets every block's pair, and joins them in the same order
+            asm volatile("barrier.cluster.wait;" ::: "memory");      // all of them run
             if (tid < a.parts) {
                 unsigned to;
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_address(&of_part[part])), "r"(tid));
                 asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(st.m), "f"(st.s) : "memory");
             }
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
             st = of_part[0];
             for (int q = 1; q < a.parts; ++q) st = join(st, of_part[q]);
         }
