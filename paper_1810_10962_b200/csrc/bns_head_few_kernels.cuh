@@ -40,7 +40,7 @@ struct HeadFew {
     const void* target;
     const float* lse;      // gradient
     const float* dloss;
-    float2* partial;       // [blocks][T]
+    float2* partial;       // [blocks][T] maximum (base 2) and sum
     float* target_logit;
     unsigned* status;      // cleared here
     float* G;              // [V][ROWS]
@@ -169,8 +169,10 @@ __global__ void __launch_bounds__(FewShape<ROWS>::kThreads, 1) head_few_logits_k
                 const float q = exp2_fast((z[i] - lse[i]) * kHeadLog2e) - (v == y[i] ? 1.f : 0.f);
                 a.G[static_cast<int64_t>(v) * ROWS + t] = y[i] >= 0 && y[i] < a.V ? weight[i] * q : 0.f;
             } else {
-                const float m = fmaxf(st[i].x, z[i]), ref = m == -inf ? 0.f : m;
-                st[i] = make_float2(m, st[i].y * exp2_fast((st[i].x - ref) * kHeadLog2e) + exp2_fast((z[i] - ref) * kHeadLog2e));
+                // the reference is the rounded product z log2(e), the exponents are differences to just that number: its
+                // rounding, some 4e-4 at a logit of 3e4, is in the sum and so cancels when a target's logit is compared with it
+                const float m = fmaxf(st[i].x, z[i] * kHeadLog2e), ref = m == -inf ? 0.f : m;
+                st[i] = make_float2(m, st[i].y * exp2_fast(st[i].x - ref) + exp2_fast(fmaf(z[i], kHeadLog2e, -ref)));
                 if (v == y[i] && t < a.T) a.target_logit[t] = z[i];
             }
         }
@@ -188,9 +190,9 @@ __global__ void __launch_bounds__(FewShape<ROWS>::kThreads, 1) head_few_logits_k
             for (int w0 = 0; w0 < kWarps; ++w0)
                 for (int r = 0; r < R; ++r) {
                     const float2 p = fold[w0][r * ROWS + tid];
-                    s += p.y * exp2_fast((p.x - ref) * kHeadLog2e);
+                    s += p.y * exp2_fast(p.x - ref);
                 }
-            a.partial[static_cast<int64_t>(blockIdx.x) * a.T + tid] = make_float2(m * kHeadLog2e, s);
+            a.partial[static_cast<int64_t>(blockIdx.x) * a.T + tid] = make_float2(m, s);
         }
     }
 }

@@ -112,3 +112,28 @@ def test_last_piece_shorter_than_the_parts(T, V, D, piece, dtype):
         check(*case(T, V, D, dtype, T + V), dtype, 256 if dtype == "f32" else 512, 256 if dtype == "f32" else 1 << 40)
     finally:
         bns.set_tuning("head_piece", 0)
+
+
+# A row that is sure of its target has loss 0, and one that is sure of another place the difference of the two logits, at any
+# size of the logits.  A logit is one product with 1: exact, or in two fp16 terms right to 2^-22 = 4 u.  The exponents come from
+# multiply-adds against one rounded reference, so what is left of it is 2^x and log2 near 0: a few 2^-22.
+@pytest.mark.parametrize("logit", [17.3, 100.7, 1000.3, 29997.3, 3e8])
+@pytest.mark.parametrize("T,V,D", [(1, 5, 3), (4, 40000, 8), (7, 2000, 130), (32, 900, 64), (33, 900, 64), (200, 5000, 72)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_loss_of_sure_rows(T, V, D, logit, dtype):
+    from paper_1810_10962_b200 import lm
+    x, w = (torch.zeros(n, D, device="cuda", dtype=DTYPE[dtype]) for n in (T, V))
+    x[:, 0] = 1.0
+    w[:, 0] = -logit / 2
+    w[3, 0] = logit
+    w[1, 0] = logit / 4
+    target = torch.full((T,), 3, device="cuda")
+    target[::3] = 1
+    loss, lse = lm.linear_cross_entropy_forward(x, w, target)
+    z = w[:, 0].double()
+    want = torch.logsumexp(z, 0)
+    terms = 4 * U if dtype == "f32" else 0
+    assert bool(((lse.double() - want).abs() <= (4 * U + terms) * want.abs()).all())
+    off = (loss.double() - (want - z[target])).abs()
+    tol = 8 * 2.0 ** -22 + 8 * U * (want - z[target]).abs() + terms * torch.where(target == 3, 0.0, want.abs() + z[target].abs())
+    assert bool((off <= tol).all()), f"{float((off / tol).max()):.3g} times the bound, loss off by {float(off.max()):.3g}"
