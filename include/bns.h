@@ -403,8 +403,8 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
  * Linear head + softmax cross entropy, without keeping the logits.
  *   z = x w^T (x: rows x width, w: vocabulary x width)       lse_t = log sum_v exp z_tv
  *   loss_t = lse_t - z_{t, target_t}, and 0 where target_t is not in [0, vocabulary)
- * A negative target leaves its row out; one at or above the vocabulary's size does too, and sets
- * BNS_FLAG_BAD_TARGET in the workspace's status word (see bns_workspace_status).
+ * A negative target leaves its row out; one at or above the vocabulary's size does too, and is told by
+ * BNS_FLAG_BAD_TARGET in the workspace's status word (see bns_workspace_status), which either call writes.
  * Backward, with dloss float[rows] the gradient of each row's loss (rows that are left out: ignored):
  *   G_tv = dloss_t (exp(z_tv - lse_t) - [v = target_t])      dx = G w      dw = G^T x
  * The logits are computed again, one piece of the vocabulary at a time; G of a piece is held in the

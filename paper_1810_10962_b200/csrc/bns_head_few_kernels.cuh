@@ -42,7 +42,7 @@ struct HeadFew {
     const float* dloss;
     float2* partial;       // [blocks][T] maximum (base 2) and sum
     float* target_logit;
-    unsigned* status;      // cleared here
+    unsigned* status;      // cleared here, or (gradient) written
     float* G;              // [V][ROWS]
     float* sums;           // [chunks][T][D]
     float* dx;
@@ -104,6 +104,13 @@ __global__ void __launch_bounds__(FewShape<ROWS>::kThreads, 1) head_few_logits_k
             lse[i] = counts ? a.lse[t] : 0.f;
             weight[i] = counts ? a.dloss[t] : 0.f;
         }
+    }
+    if (GRAD && blockIdx.x == 0 && warp == 0) {       // a warp's lanes have all of the targets
+        bool past = false;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) past |= y[i] >= a.V;
+        past = __any_sync(0xffffffffu, past);
+        if (lane == 0) *a.status = past ? BNS_FLAG_BAD_TARGET : 0;
     }
     __syncthreads();
     const int step = gridDim.x * kWarps * R, chunks = (a.D + 32 * kFewLane - 1) / (32 * kFewLane);

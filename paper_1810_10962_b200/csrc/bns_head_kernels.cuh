@@ -272,7 +272,7 @@ struct HeadGemm {
     int V;
     float2* partial;             // LSE: [2 tiles_n][M] maximum (base 2) and sum of half a tile's columns
     float* target_logit;         // LSE: [M]
-    unsigned* status;            // LSE: cleared here, set by the kernel that joins the partial sums
+    unsigned* status;            // LSE: cleared here, set by the kernel that joins the partial sums; GRAD with find_unit: written
     const float *lse, *dloss;    // GRAD: [M]
     float* unit;                 // GRAD: G holds the gradient divided by this; OUT: multiplied in again
     int find_unit;               // GRAD: every warp of the epilogue finds it itself, block 0 leaves it there
@@ -329,15 +329,21 @@ struct HeadTile {
 
 // The largest |dloss| of the rows that count, over a warp's share of them: G is kept in units of it (1 if that is zero).
 // With one weight for all rows, as a mean has, the largest entry of a row of G is then p - 1 itself; its rounding to
-// bf16 does not carry that of the weight, which would be the same in every row and add up.
-__device__ __forceinline__ float head_unit(const void* target, int target64, const float* dloss, int rows, int V, int first, int step) {
+// bf16 does not carry that of the weight, which would be the same in every row and add up.  `flags` takes what the status word
+// says of the targets.
+__device__ __forceinline__ float head_unit(const void* target, int target64, const float* dloss, int rows, int V, int first, int step,
+                                           unsigned& flags) {
     float top = 0.f;
+    bool past = false;
 #pragma unroll 4
     for (int t = first; t < rows; t += step) {
         const int64_t y = head::load_index(target, t, target64);
         const float g = fabsf(dloss[t]);
         if (y >= 0 && y < V && g < __int_as_float(0x7f800000)) top = fmaxf(top, g);
+        past |= y >= V;
     }
+    __syncwarp();
+    flags = __any_sync(0xffffffffu, past) ? BNS_FLAG_BAD_TARGET : 0;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     return top;
@@ -800,9 +806,13 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         if (KIND == kHeadLse && blockIdx.x == 0 && threadIdx.x == 128 && g.status) *g.status = 0;
         float unit = 1.f;
         if (KIND == kHeadGrad && g.find_unit) {
-            unit = head_unit(g.target, g.target64, g.dloss, g.M, g.V, lane, 32);
+            unsigned flags;
+            unit = head_unit(g.target, g.target64, g.dloss, g.M, g.V, lane, 32, flags);
             unit = unit > 0.f ? unit : 1.f;
-            if (blockIdx.x == 0 && threadIdx.x == 128) *g.unit = unit;
+            if (blockIdx.x == 0 && threadIdx.x == 128) {
+                *g.unit = unit;
+                *g.status = flags;
+            }
         } else if (KIND != kHeadLse) {
             unit = *g.unit;
         }
@@ -885,14 +895,16 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
 
 // ------------------------------------------------------------------------------------ around the products
 __global__ void __launch_bounds__(1024) head_unit_kernel(const void* target, int target64, const float* dloss, int rows, int V,
-                                                         float* unit) {
+                                                         float* unit, unsigned* status) {
     __shared__ float fold[32];
     grid_dependency_wait();
     grid_dependency_launch();
-    const float top = head_unit(target, target64, dloss, rows, V, threadIdx.x, 1024);
+    unsigned flags;
+    const float top = head_unit(target, target64, dloss, rows, V, threadIdx.x, 1024, flags);
     if ((threadIdx.x & 31) == 0) fold[threadIdx.x >> 5] = top;
-    __syncthreads();
+    const bool past = __syncthreads_or(flags);
     if (threadIdx.x == 0) {
+        *status = past ? BNS_FLAG_BAD_TARGET : 0;
         float all = 0.f;
         for (int w = 0; w < 32; ++w) all = fmaxf(all, fold[w]);
         *unit = all > 0.f ? all : 1.f;

@@ -325,6 +325,10 @@ HeadProblem plan_head(const bns_head* sh, bool backward) {
     p.terms = p.f32 ? 2 : 1;
     p.pairs = p.f32 ? 3 : 1;
     p.pitch = divide_up(p.D, kHeadK) * kHeadK;
+    if (p.T == 0) {                 // the status word is all that is written
+        p.total = kHeaderBytes;
+        return p;
+    }
     size_t column = 0;              // workspace bytes per column of the vocabulary
     if (p.copy_w) column = static_cast<size_t>(p.terms) * p.pitch * 2;
     if (backward) column = std::max(column, static_cast<size_t>(p.T) * p.terms * 2);
@@ -553,10 +557,10 @@ bns_status few_logits(const HeadFew& a, cudaStream_t stream) {
 }
 template <int ROWS, bool WORDS>
 bns_status few_head_of(const HeadProblem& p, HeadFew a, char* ws, bool backward, cudaStream_t stream) {
+    a.status = reinterpret_cast<unsigned*>(ws);
     if (ROWS > kFewRowsBackward || !backward) {
         a.partial = reinterpret_cast<float2*>(ws + p.off_partial);
         a.target_logit = reinterpret_cast<float*>(ws + p.off_logit);
-        a.status = reinterpret_cast<unsigned*>(ws);
         return few_logits<ROWS, WORDS, false>(a, stream);
     }
     if constexpr (ROWS <= kFewRowsBackward) {
@@ -796,7 +800,10 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
     char* ws = static_cast<char*>(workspace);
     const size_t eb = elem_bytes(p.dtype);
     if (p.T == 0)
-        return cudaMemsetAsync(dw, 0, eb * p.V * p.D, stream) == cudaSuccess ? BNS_OK : BNS_ERR_CUDA;
+        return cudaMemsetAsync(ws, 0, sizeof(uint32_t), stream) == cudaSuccess &&
+                       cudaMemsetAsync(dw, 0, eb * p.V * p.D, stream) == cudaSuccess
+                   ? BNS_OK
+                   : BNS_ERR_CUDA;
     if (p.few) {
         HeadFew a{};
         a.x = static_cast<const float*>(x);
@@ -816,7 +823,8 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
     // few rows: each warp finds the unit itself, under the first tile's copies; a launch costs some 3 us
     const bool find_unit = p.T <= 1024;
     if (!find_unit)
-        launch(BNS_KERNEL_HEAD_VECTOR, head_unit_kernel, Shape{1, 1024}, 0, stream, target, shape->target_is_int64, dloss, p.T, p.V, unit);
+        launch(BNS_KERNEL_HEAD_VECTOR, head_unit_kernel, Shape{1, 1024}, 0, stream, target, shape->target_is_int64, dloss, p.T, p.V, unit,
+               reinterpret_cast<unsigned*>(ws));
     float* sums = p.splits > 1 || p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sums) : nullptr;
     for (int first = 0; first < p.V; first += p.piece) {
         const int count = std::min(p.piece, p.V - first);
@@ -834,6 +842,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
         g.dloss = dloss;
         g.unit = unit;
         g.find_unit = find_unit;
+        g.status = reinterpret_cast<unsigned*>(ws);
         g.a_scale = &scalars->x_scale;
         g.b_scale = &scalars->w_scale;
         const Operand G{ws + p.off_G, static_cast<int64_t>(p.terms) * kHeadN, p.T, kHeadN, p.terms, kHeadN, divide_up(count, kHeadN)};

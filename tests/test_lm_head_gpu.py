@@ -159,3 +159,26 @@ def test_gradient_of_sure_rows(T, V, D, dtype):
     tG = torch.zeros_like(G).scatter_(1, target[:, None], 6 * U * z.amax(1, keepdim=True) + 16 * U)
     for got, want, tol, what in ((dx, G @ w.double(), tG @ w.double().abs(), "dx"), (dw, G.T @ x.double(), tG.T @ x.double().abs(), "dw")):
         within(got, want, 1.02 * tol + 1e-12, what)
+
+
+# The four places where the gradient call looks at its targets: few fp32 rows, the products' own warps, a kernel before them (over
+# 1024 rows), and no rows at all.
+@pytest.mark.parametrize("T,dtype", [(5, "f32"), (16, "f32"), (17, "f32"), (40, "bf16"), (1024, "bf16"), (1025, "bf16"), (3000, "f32")])
+@pytest.mark.parametrize("int64", [True, False])
+def test_gradient_call_tells_of_bad_targets(T, dtype, int64):
+    from paper_1810_10962_b200 import bns, lm
+    V, D = 300, 64
+    x, w, target, dloss = case(T, V, D, dtype, 3)
+    target = target if int64 else target.int()
+    _, lse = lm.linear_cross_entropy_forward(x, w, target)
+    workspace = torch.full((lm.linear_cross_entropy_workspace_bytes(x, w, target, backward=True),), 0xAB, dtype=torch.uint8, device="cuda")
+    lm.linear_cross_entropy_backward(x, w, target, lse, dloss, workspace=workspace)
+    assert bns.workspace_status(workspace) == 0
+    for place in (0, T - 1, T // 2):
+        bad = target.clone()
+        bad[place] = V
+        dx, _ = lm.linear_cross_entropy_backward(x, w, bad, lse, dloss, workspace=workspace)
+        assert bns.workspace_status(workspace) == lm.FLAG_BAD_TARGET
+        assert bool((dx[place] == 0).all())
+    lm.linear_cross_entropy_backward(x[:0], w, target[:0], lse[:0], dloss[:0], workspace=workspace)
+    assert bns.workspace_status(workspace) == 0
