@@ -129,13 +129,14 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&f)[V]) {
 
 // What multiplies s w to give y / scale, from the largest |s w| of the group.  y = s rstd w, so rstd cancels in
 // y / scale = s w 448 / max|s w|: the 8-bit values carry no rounding of rstd or of the scale.  A group of zeros has
-// scale 1; infinities and NaN give NaN, as the formula does.  `lift` keeps 448 / max finite for groups below 2^-100.
+// scale 1; infinities and NaN give NaN, as the formula does.  `lift` keeps 448 / max finite for groups below 2^-100, and what
+// the reciprocal makes of those above 2^100 from the numbers that it takes for 0.
 struct Quant {
     float a, lift, factor;
     __device__ __forceinline__ Quant(float top, float rstd) {
         const float inf = __int_as_float(0x7f800000);
         a = top * rstd;
-        lift = top < 0x1p-100f ? 0x1p100f : 1.f;
+        lift = top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-100f : 1.f;
         float inverse;
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(top * lift));   // 1 ulp
         factor = a == 0.f ? 0.f : top < inf && a < inf ? 448.f * inverse : __int_as_float(0x7fffffff);
