@@ -440,7 +440,7 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
  *   dlogits_tv = dloss_t temperature (q_v - sum over k with index_k = v of p_k)
  * A row without entries (or whose entries are all -inf) has loss 0 and gradient 0.  _backward takes the
  * lse of _forward; _step gives loss and gradient in one launch where dloss is known beforehand.
- * 1 <= entries <= 1024.  Any alignment of the element type.
+ * 1 <= entries <= 1024, 10^-38 <= temperature <= 10^30.  Any alignment of the element type.
  */
 typedef struct {
     int rows, vocabulary, entries;

@@ -603,7 +603,7 @@ bns_status few_head(const HeadProblem& p, const bns_head* sh, HeadFew a, char* w
 bns_status check_distillation(const bns_distillation* sh) {
     if (!sh) return BNS_ERR_NULL;
     if (sh->rows < 0 || sh->vocabulary <= 0 || sh->vocabulary > 1 << 30 || sh->entries < 1 || sh->entries > kDistillMaxEntries ||
-        sh->stride < sh->vocabulary || !(sh->temperature > 0.f) || sh->temperature > 1e30f)
+        sh->stride < sh->vocabulary || !(sh->temperature >= 1e-38f) || sh->temperature > 1e30f)    // log2(e) / temperature is finite
         return BNS_ERR_SHAPE;
     if (!known(sh->dtype) || !known(sh->teacher_dtype)) return BNS_ERR_DTYPE;
     return BNS_OK;

@@ -98,6 +98,16 @@ def test_distillation_refusals(lib):
     assert lib.bns_topk_distillation_step(ctypes.byref(shape), P, P, P, None, P, P, 100, None) == -1
 
 
+def test_distillation_temperature_range(lib):
+    """Below some 4e-39 log2(e) / temperature is infinite, and every answer would be NaN."""
+    call = lambda temperature: lib.bns_topk_distillation_forward(  # noqa: E731
+        ctypes.byref(lm._Distillation(0, 100, 8, bns.F32, 100, bns.F32, 0, temperature)), P, P, P, P, P, None)
+    for temperature in (1e-45, 1e-40, 4e-39, 1.1e30):
+        assert call(temperature) == -2
+    for temperature in (1.1e-38, 1e-30, 1.0, 0.9e30):
+        assert call(temperature) == 0              # no rows: nothing is launched
+
+
 def test_binding_refuses_what_is_not_a_cuda_tensor():
     x, w = torch.zeros(4, 64), torch.ones(64)
     with pytest.raises(TypeError):
