@@ -29,9 +29,10 @@ def case(T, V, D, dtype, seed):
     return x, w, target, torch.rand(T, device="cuda", generator=g) + 0.5
 
 
-def chain(n, dtype, segment):
-    """What a sum of n terms may be off by, as a part of the sum of the terms' magnitudes."""
-    inside = 2 * U * (min(n, segment) / 16 + 2) + U * (n / segment + 70)     # 70: parts of a split sum, pieces
+def chain(n, dtype, segment, parts=0):
+    """What a sum of n terms may be off by, as a part of the sum of the terms' magnitudes.  `parts`: additions of a split sum's
+    parts, and of pieces of the vocabulary."""
+    inside = 2 * U * (min(n, segment) / 16 + 2) + U * (n / segment + 2 + parts)
     if dtype == "bf16":
         return inside
     return inside + 12 * U + 2 * 2.0 ** -11 * 2 * U * (min(n, 4096) / 16 + 2)
@@ -84,12 +85,12 @@ def check(x, w, target, dloss, dtype, segment_z, segment_out):
         G.scatter_add_(1, at, -g)
         tG.add_(G.abs().mul_(STORE["bf16"] if dtype == "bf16" else 6 * U))
         want = G @ wd
-        tol = (tG @ wd.abs()) * 1.01 + (G.abs() @ wd.abs()) * chain(V, dtype, segment_out) + STORE[dtype] * 1.01 * want.abs() + 1e-30
+        tol = (tG @ wd.abs()) * 1.01 + (G.abs() @ wd.abs()) * chain(V, dtype, segment_out, 70) + STORE[dtype] * 1.01 * want.abs() + 1e-30
         within(dx[part], want, tol, f"dx from row {first}")
         want_dw += G.T @ xd
         off_dw += tG.T @ xd.abs()
         size_dw += G.abs().T @ xd.abs()
-    within(dw, want_dw, off_dw * 1.01 + size_dw * chain(T, dtype, segment_out) + STORE[dtype] * 1.01 * want_dw.abs() + 1e-30, "dw")
+    within(dw, want_dw, off_dw * 1.01 + size_dw * chain(T, dtype, segment_out, 70) + STORE[dtype] * 1.01 * want_dw.abs() + 1e-30, "dw")
 
 
 # Products that give a CTA pair several tiles, with a number of rows whose last tile has warps without any: rows of dw
@@ -98,6 +99,12 @@ def check(x, w, target, dloss, dtype, segment_z, segment_out):
                                          (4000, 20000, 64, "f32"), (700, 30000, 512, "f32")])
 def test_many_tiles(T, V, D, dtype):
     check(*case(T, V, D, dtype, T + V + D), dtype, 256 if dtype == "f32" else 512, 256 if dtype == "f32" else 1 << 40)
+
+
+# fp32 sums that are long enough for a lost product of terms, or for segments that are too long, to pass the bound.
+@pytest.mark.parametrize("T,V,D", [(300, 3001, 4100), (1021, 8003, 1000), (140, 20000, 2048)])
+def test_long_fp32_sums(T, V, D):
+    check(*case(T, V, D, "f32", T + V + D), "f32", 256, 256)
 
 
 # Pieces of the vocabulary whose last one has fewer stages of K than dx's sum has parts: 4097 = 4 x 1024 + 1 in four parts, and

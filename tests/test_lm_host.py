@@ -120,6 +120,33 @@ def test_binding_refuses_what_is_not_a_cuda_tensor():
         lm.topk_distillation_forward(x, torch.zeros(4, 2), torch.zeros(4, 2, dtype=torch.int32))
 
 
+@pytest.mark.parametrize("D", [512, 1000, 4100])
+def test_bound_of_fp32_products_sees_a_lost_term(D):
+    """The bound that the GPU tests hold fp32 logits to, on sums made here: of all three products of terms they stay
+    within it, without one of them nearly every row passes it."""
+    from test_lm_head_gpu import chain
+    g = torch.Generator().manual_seed(D)
+    T, V = 40, 300
+    x, w = torch.randn(T, D, generator=g), torch.randn(V, D, generator=g) * (2 / D ** 0.5)
+
+    def terms(t):
+        t = (t * 2.0 ** (13 - float(t.abs().max().log2().floor()))).float()
+        high = t.half()
+        return t.double(), high.double(), ((t - high.float()) * 2048).half().double() / 2048
+
+    (xs, xh, xl), (ws, wh, wl) = terms(x), terms(w)
+    scale = float((x.double() @ w.double().T).abs().max() / (xs @ ws.T).abs().max())
+    target = torch.randint(0, V, (T, 1), generator=g)
+    loss = lambda z: torch.logsumexp(z, 1) - z.gather(1, target)[:, 0]  # noqa: E731
+    z = xs @ ws.T * scale
+    tz = (xs.abs() @ ws.abs().T) * scale * chain(D, "f32", 256)
+    bound = (torch.softmax(z, 1) * tz).sum(1) + tz.gather(1, target)[:, 0]
+    off = lambda *products: ((loss(sum(products) * scale) - loss(z)).abs() / bound)  # noqa: E731
+    assert float(off(xh @ wh.T, xh @ wl.T, xl @ wh.T).max()) < 1
+    for lost in ((xh @ wh.T, xl @ wh.T), (xh @ wh.T, xh @ wl.T)):
+        assert float(off(*lost).max()) > 1
+
+
 @pytest.mark.gpu
 def test_binding_refuses_tensors_that_do_not_fit():
     c = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
