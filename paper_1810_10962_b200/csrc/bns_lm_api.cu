@@ -630,9 +630,11 @@ bns_status distill(const bns_distillation* sh, Distill a, cudaStream_t stream) {
     // short rows take small blocks (8192 x 1000 bf16: 38 us against 100)
     const bool small = vectors <= kDistillSmall * 8 && a.K <= kDistillSmall * kDistillOwn && rows > 2 * sm_count();
     // A row that is read twice should still be in L2 the second time: long ones go over two blocks, so that half as many
-    // are in flight (131072 bf16 values: 456 -> 416 us per 4096 rows; 50257, 100 KB: 184 us with one, 246 with two).
+    // are in flight.  Per 4096 rows with one block / two: bf16 50257 (98 KB) 179 / 248 us, 100277 (196 KB) 328 / 370, 112000
+    // (219 KB) 376 / 385, 128256 (250 KB) 451 / 422, 200064 733 / 673; fp32 50257 (196 KB) 316 / 354, 65536
+    // (256 KB) 458 / 401.
     const size_t row_bytes = static_cast<size_t>(a.V) * eb;
-    a.parts = __is_same(WHAT, DistillStep) && row_bytes > (size_t{192} << 10) ? 2 : 1;
+    a.parts = __is_same(WHAT, DistillStep) && row_bytes > (size_t{224} << 10) ? 2 : 1;
     // few rows are spread over the SMs
     while (a.parts < kDistillParts && rows * (a.parts + 1) <= 2 * sm_count() && vectors > a.parts * kDistillThreads) ++a.parts;
     a.per = divide_up(vectors, a.parts);
