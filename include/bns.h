@@ -380,7 +380,8 @@ bns_status bns_rms_norm_forward(const bns_rows* shape, const void* x, int64_t x_
  * The same with y in 8 bits (e4m3: 4 bits of exponent, 3 of fraction, largest value 448) and scales:
  *   a = max |y| over a group of columns     scale = a / 448, 1 where a = 0     q = e4m3(y / scale)
  * group = 0: one scale per row, scales is float[rows]; group = 128: one per 128 columns (the last group
- * may be shorter), scales is float[rows][ceil(columns / 128)].  q is a dense byte matrix.
+ * may be shorter), scales is float[rows][ceil(columns / 128)].  q is a dense byte matrix.  s weight has to be within
+ * fp32's range, as it is quantised before rstd is known.
  */
 bns_status bns_rms_norm_forward_quantized(const bns_rows* shape, const void* x, int64_t x_stride,
                                           const void* residual, int64_t residual_stride, const float* weight,
@@ -408,11 +409,14 @@ bns_status bns_rms_norm_backward(const bns_rows* shape, const void* dy, int64_t 
  * Backward, with dloss float[rows] the gradient of each row's loss (rows that are left out: ignored):
  *   G_tv = dloss_t (exp(z_tv - lse_t) - [v = target_t])      dx = G w      dw = G^T x
  * The logits are computed again, one piece of the vocabulary at a time; G of a piece is held in the
- * workspace (bf16 for bf16 tensors: half an ulp of the gradients' own type per term).
+ * workspace (bf16 for bf16 tensors: half an ulp of the gradients' own type per term).  A row that is left out has a G
+ * of zeros, which its x is multiplied with: infinities or NaN there reach dw.
  * loss, lse: float[rows].  dx, dw: the type of x and w, dense.  x and w must be 16-byte aligned; bf16
- * rows whose stride or width is no multiple of 8 elements are copied piece by piece, and fp32 tensors are
+ * rows whose stride is no multiple of 8 elements are copied piece by piece, and fp32 tensors are
  * split into two fp16 terms (22 bits, kept down to 2^-28 of the tensor's largest value and falling off to
- * 2^-49 of it) whose products are added up in fp32: the result is as near as that of an fp32 product.
+ * 2^-49 of it) whose products are added up in fp32: the result is as near as that of an fp32 product.  G
+ * of fp32 tensors is held the same way; its scale is the largest |dloss| of the rows that count, so that entries below
+ * 2^-27 of that, of rows whose dloss is far smaller than another's, keep fewer than 22 bits.
  * fp32 tensors with few rows (32 forward, 16 backward, x within 216 KB) are multiplied in fp32 as they are;
  * G of all of the vocabulary is then in the workspace.  Logits: up to 10^9 in magnitude.
  * rows <= 2^24, vocabulary <= 2^28, width <= 2^20.

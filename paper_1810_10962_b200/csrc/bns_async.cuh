@@ -23,33 +23,21 @@ __device__ __forceinline__ void barrier_init(unsigned bar, unsigned arrivals) {
 __device__ __forceinline__ void barrier_expect(unsigned bar, unsigned bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// CLUSTER: what other blocks of the cluster wrote before they arrived is seen after the wait.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool barrier_try(unsigned bar, unsigned parity) {
     unsigned done;
-    if constexpr (CLUSTER)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
     return done != 0;
 }
 // False once this wait, or another one of the block, has run out.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait_bounded(unsigned bar, unsigned parity, volatile int* gave_up) {
     for (unsigned i = 0; i < kPolls; ++i) {
-        if (barrier_try<CLUSTER>(bar, parity)) return true;
+        if (barrier_try(bar, parity)) return true;
         if ((i & 255) == 255 && *gave_up) return false;
     }
     *gave_up = 1;

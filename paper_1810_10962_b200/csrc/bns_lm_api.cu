@@ -406,7 +406,7 @@ bool encode_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* 
                                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// A matrix operand: `terms` bf16 terms a row, `pitch` elements apart.  With `blocks`, blocks of 256 columns (of each term) of
+// A matrix operand: rows of `terms` terms (one of bf16, or two of fp16), `pitch` elements apart.  With `blocks`, blocks of 256 columns (of each term) of
 // all rows after one another.
 struct Operand {
     const void* base;
@@ -536,7 +536,6 @@ bns_status rows_of_w(const HeadProblem& p, const bns_head* sh, const void* w, in
     return lay_out(p, from, sh->w_stride, count, ws + p.off_w, &s->w_top, &s->w_scale, stream);
 }
 
-// ------------------------------------------------------------------------------------ distillation
 // The few rows' kernels: the logits' statistics, or the gradients.
 template <int ROWS, bool WORDS, bool GRAD>
 bns_status few_logits(const HeadFew& a, cudaStream_t stream) {
@@ -600,6 +599,7 @@ bns_status few_head(const HeadProblem& p, const bns_head* sh, HeadFew a, char* w
     return p.few_words ? few_head_in<true>(p, a, ws, backward, stream) : few_head_in<false>(p, a, ws, backward, stream);
 }
 
+// ------------------------------------------------------------------------------------ distillation
 bns_status check_distillation(const bns_distillation* sh) {
     if (!sh) return BNS_ERR_NULL;
     if (sh->rows < 0 || sh->vocabulary <= 0 || sh->vocabulary > 1 << 30 || sh->entries < 1 || sh->entries > kDistillMaxEntries ||
