@@ -10,6 +10,9 @@
 //         (with whole rows of G instead, whose 64 KB strides put each row of a box of G^T in another page, the product
 //         G^T x ran at two thirds of the tensor cores' cycles instead of four fifths)
 //   OUT   dx and dW tiles -> the gradient in the tensor's type, or fp32 partial sums
+// bf16 tensors have a G of bf16: both operands of a product have one type, and a second term for the rest would double the time of dx
+// and dW.  It costs bits: dx and dW are 0.0019 of their norm from 64 bits at 4096 x 131072 x 4096, where their own rounding alone
+// makes 0.0017; 0.0020 at 24 rows.
 //
 // A CTA pair (two SMs) owns a 256 x 256 tile: each CTA keeps 128 rows of it in its tensor memory and half of either
 // operand's stage in its shared memory, so that a stage's bytes per product are half of what two single CTAs would
