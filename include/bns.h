@@ -351,10 +351,11 @@ bns_status bns_workspace_status(const void* workspace, uint32_t* flags, void* cu
 int bns_slab_plan(const bns_shape* shape, const bns_sampling* sampling, int backward, int32_t* plan);
 bns_status bns_wait_timeouts(uint32_t* count, void* cuda_stream);
 
-/* ==== operators at the end of a language model's step =============================================
+/* ==== operators of a language model's step ========================================================
  *
  * Residual add + root-mean-square norm, linear head + softmax cross entropy, distillation from a
- * teacher's top logits.  The conventions at the top of this file hold, except for what is said here:
+ * teacher's top logits, log probabilities of given tokens, norm + rotation of queries' and keys' heads,
+ * the norm over all gradients and clipping.  The conventions at the top of this file hold, except for what is said here:
  * the large tensors are matrices whose rows are dense and may lie apart (strides in elements, at least
  * the row's length); outputs of the caller's type are dense unless a stride is passed for them.
  * rows = 0 is allowed: nothing is read, gradients of weights are set to zero, row pointers may be NULL.
@@ -463,6 +464,92 @@ bns_status bns_topk_distillation_step(const bns_distillation* shape, const void*
                                       const void* index, const float* dloss, float* loss, void* dlogits,
                                       int64_t dlogits_stride, void* cuda_stream);
 
+/*
+ * Log probabilities of given tokens, with the distribution's entropy and its top alternatives.
+ *   q = softmax of logits / temperature     logprob_t = log q_{t, token_t}     entropy_t = - sum_v q_tv log q_tv
+ *   top_index[t][k]: the entries places with the largest logits, the lowest place first among equals
+ *   top_logprob[t][k] = log q there         lse_t = log sum_v exp(logits_tv / temperature)
+ * A token outside [0, vocabulary) is none: its logprob is 0.  Logits of -inf are masked places: probability 0, log
+ * probability -inf, nothing added to the entropy.  A row of -inf alone has lse and log probabilities of -inf, entropy 0
+ * and gradient 0; one with NaN or +inf has NaN.  NaN is never among the alternatives: places without a value get index -1.
+ * Backward, with dlogprob and dentropy (may be NULL: entropy is then not read) the gradients of each row's outputs:
+ *   dlogits_tv = (dlogprob_t ([v = token_t] - q_tv) - dentropy_t q_tv (log q_tv + entropy_t)) / temperature
+ * logprob, entropy (may be NULL in _forward), lse: float[rows]; top_logprob float[rows][entries], top_index
+ * int32_t[rows][entries].  0 <= entries <= 64, entries <= vocabulary, 10^-6 <= temperature <= 10^6; entries = 0: no
+ * alternatives.  |dentropy / temperature| up to 10^12.  Any alignment of the element type.
+ */
+typedef struct {
+    int rows, vocabulary, entries;
+    int dtype;                  /* bns_dtype of logits and dlogits    */
+    int64_t stride;             /* elements from one row of logits to the next */
+    int token_is_int64;         /* 0: token is int32_t[rows]          */
+    float temperature;
+} bns_token_log_probs;
+bns_status bns_token_log_probs_forward(const bns_token_log_probs* shape, const void* logits, const void* token,
+                                       float* logprob, float* entropy, float* lse, float* top_logprob,
+                                       int32_t* top_index, void* cuda_stream);
+bns_status bns_token_log_probs_backward(const bns_token_log_probs* shape, const void* logits, const void* token,
+                                        const float* lse, const float* entropy, const float* dlogprob,
+                                        const float* dentropy, void* dlogits, int64_t dlogits_stride,
+                                        void* cuda_stream);
+
+/*
+ * Root-mean-square norm of every head of queries and keys, with the rotation by position in the same pass.
+ *   rstd = 1 / sqrt(mean(x^2) + eps) over a head     n = x rstd     y = R_p (n weight)
+ * R_p turns the first `rotary` elements of a head pair by pair, with the angles in row p = position of the tables
+ * cos, sin: float[positions][rotary / 2]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin),  pair i is (i, rotary / 2 + i), or (2 i, 2 i + 1) where interleaved
+ * q and k are [batch][length][heads][head_dim] with dense heads and any strides (views of a packed projection, heads
+ * before positions); outputs and their gradients are dense in that order.  Weights are float[head_dim], the same for all
+ * heads of q, or of k.  k_heads may be 0: then everything of k may be NULL.  position is [batch][length]; one outside
+ * [0, positions) is padding: its outputs and gradients are zeros, whatever is there.
+ * Backward, with d = R_p^T dy:   dx = rstd (weight d - n mean(weight d n))     dweight = sum over positions, heads of d n
+ * from the inputs of the forward call; rstd is found again.  Sums are taken in fp32 in a fixed order.
+ * head_dim <= 1024, 2 <= rotary <= head_dim, even.  Any alignment of the element type; 16-byte vectors are used where pointers,
+ * strides, rotary / 2 and the rest of a head allow them.  batch * length = 0 is allowed (weights' gradients become zero).
+ */
+typedef struct {
+    int batch, length, q_heads, k_heads, head_dim, rotary;
+    int dtype;                  /* bns_dtype of q, k, outputs, gradients */
+    int64_t q_strides[3];       /* elements from one batch, position, head to the next */
+    int64_t k_strides[3];
+    int positions;              /* rows of the tables                 */
+    int position_is_int64;      /* 0: position is int32_t             */
+    int interleaved;
+    float eps;
+} bns_head_norm;
+bns_status bns_head_norm_rotary_forward(const bns_head_norm* shape, const void* q, const void* k, const float* q_weight,
+                                        const float* k_weight, const float* cos, const float* sin, const void* position,
+                                        void* q_out, void* k_out, void* cuda_stream);
+size_t bns_head_norm_rotary_workspace_bytes(const bns_head_norm* shape);
+bns_status bns_head_norm_rotary_backward(const bns_head_norm* shape, const void* dq_out, const void* dk_out, const void* q,
+                                         const void* k, const float* q_weight, const float* k_weight, const float* cos,
+                                         const float* sin, const void* position, void* dq, void* dk, float* dq_weight,
+                                         float* dk_weight, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Global norm over many gradients, and clipping by it.
+ *   norm = sqrt(sum over all elements of all tensors of g^2)
+ *   factor = 1 where norm <= max_norm, else max_norm / norm        out = g factor, rounded once
+ * Squares of the whole range of fp32 are added without overflow or loss.  Infinities and NaN follow the formula: a norm of
+ * inf makes finite gradients 0 and infinite ones NaN, a norm of NaN makes all NaN.  A tensor may be clipped in place
+ * (out[i] = data[i]); apart from that outputs overlap neither each other nor a gradient.
+ * The arrays are HOST memory, read during the call; tensors are dense, any alignment of their element type.
+ * norm: float on the device.  max_norm >= 0.
+ */
+typedef struct {
+    int count;
+    const void* const* data;    /* device pointers                    */
+    void* const* out;           /* not read by bns_gradient_norm      */
+    const int64_t* elements;
+    const int* dtype;           /* bns_dtype of each tensor and its output */
+} bns_gradients;
+size_t bns_gradient_norm_workspace_bytes(const bns_gradients* list);
+bns_status bns_gradient_norm(const bns_gradients* list, float* norm, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream);
+bns_status bns_clip_gradients(const bns_gradients* list, float max_norm, float* norm, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream);
+
 const char* bns_status_string(bns_status status);
 
 /* ---- measurement hooks (process-wide, not thread-safe; off by default) ---------------------- */
@@ -488,7 +575,10 @@ typedef enum {
     BNS_KERNEL_HEAD_PRODUCT = 18,  /* head: dx and dw                                                  */
     BNS_KERNEL_HEAD_VECTOR = 19,   /* head: joining of partial results, copies of operands             */
     BNS_KERNEL_DISTILL = 20,       /* distillation: loss, gradient                                     */
-    BNS_KERNEL_KINDS = 21
+    BNS_KERNEL_LOGP = 21,          /* log probabilities of tokens: forward, gradient                   */
+    BNS_KERNEL_HEAD_NORM = 22,     /* norm + rotation of queries' and keys' heads                      */
+    BNS_KERNEL_CLIP = 23,          /* norm over many gradients, clipping                               */
+    BNS_KERNEL_KINDS = 24
 } bns_kernel_kind;
 
 /* Number of kernels this library has launched in this process since load (or since reset). */

@@ -23,11 +23,12 @@ RULE_FULL, RULE_BATCH, RULE_FEATURE, RULE_VIRTUAL = 0, 1, 2, 3
 OFF_SHARED, OFF_PER_SAMPLE, OFF_PER_MAP = 0, 1, 2
 FLAG_BAD_OFFSET = 1
 
-KERNEL_KINDS = 21
+KERNEL_KINDS = 24
 (KERNEL_COL_MOMENTS, KERNEL_PATCH_MOMENTS, KERNEL_FINALIZE_STATS, KERNEL_NORMALIZE, KERNEL_BWD_REDUCE,
  KERNEL_FINALIZE_BWD, KERNEL_COL_FIXUP, KERNEL_PATCH_FIXUP, KERNEL_MASK, KERNEL_DIRECT_MOMENTS,
  KERNEL_DIRECT_FIXUP, KERNEL_VECTOR, KERNEL_SLAB_FORWARD, KERNEL_SLAB_BACKWARD, KERNEL_RMS_FORWARD, KERNEL_RMS_BACKWARD,
- KERNEL_HEAD_LOGITS, KERNEL_HEAD_GRADIENT, KERNEL_HEAD_PRODUCT, KERNEL_HEAD_VECTOR, KERNEL_DISTILL) = range(KERNEL_KINDS)
+ KERNEL_HEAD_LOGITS, KERNEL_HEAD_GRADIENT, KERNEL_HEAD_PRODUCT, KERNEL_HEAD_VECTOR, KERNEL_DISTILL, KERNEL_LOGP,
+ KERNEL_HEAD_NORM, KERNEL_CLIP) = range(KERNEL_KINDS)
 
 EXPORTS = [
     "bns_workspace_bytes", "bns_forward", "bns_forward_static", "bns_static_workspace_bytes", "bns_backward", "bns_full_bn", "bns_host_arena_bytes",
@@ -44,6 +45,9 @@ EXPORTS = [
     "bns_rms_norm_forward", "bns_rms_norm_forward_quantized", "bns_rms_norm_workspace_bytes", "bns_rms_norm_backward",
     "bns_linear_cross_entropy_workspace_bytes", "bns_linear_cross_entropy_forward", "bns_linear_cross_entropy_backward",
     "bns_topk_distillation_forward", "bns_topk_distillation_backward", "bns_topk_distillation_step",
+    "bns_token_log_probs_forward", "bns_token_log_probs_backward",
+    "bns_head_norm_rotary_forward", "bns_head_norm_rotary_workspace_bytes", "bns_head_norm_rotary_backward",
+    "bns_gradient_norm_workspace_bytes", "bns_gradient_norm", "bns_clip_gradients",
 ]
 
 

@@ -8,10 +8,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIBRARY = os.path.join(HERE, "libbns.so")
-SOURCES = [os.path.join(CSRC, name) for name in ("bns_api.cu", "bns_lm_api.cu")]
+SOURCES = [os.path.join(CSRC, name) for name in ("bns_api.cu", "bns_lm_api.cu", "bns_lm_step_api.cu")]
 HEADERS = [os.path.join(CSRC, name) for name in (
-    "bns_host.h", "bns_elements.cuh", "bns_async.cuh", "bns_kernels.cuh", "bns_nhwc_kernels.cuh", "bns_slab_kernels.cuh",
-    "bns_rms_kernels.cuh", "bns_head_kernels.cuh", "bns_head_few_kernels.cuh", "bns_distill_kernels.cuh")] + [os.path.join(ROOT, "include", "bns.h")]
+    "bns_host.h", "bns_lm_host.h", "bns_elements.cuh", "bns_async.cuh", "bns_logits.cuh", "bns_kernels.cuh", "bns_nhwc_kernels.cuh", "bns_slab_kernels.cuh",
+    "bns_rms_kernels.cuh", "bns_head_kernels.cuh", "bns_head_few_kernels.cuh", "bns_distill_kernels.cuh", "bns_logp_kernels.cuh",
+    "bns_rotary_kernels.cuh", "bns_clip_kernels.cuh")] + [os.path.join(ROOT, "include", "bns.h")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

@@ -1688,6 +1688,9 @@ const char* bns_kernel_name(int kernel_kind) {
     case BNS_KERNEL_HEAD_PRODUCT: return "head_gemm_kernel (gradients)";
     case BNS_KERNEL_HEAD_VECTOR: return "head: joining and layout kernels";
     case BNS_KERNEL_DISTILL: return "distill_kernel";
+    case BNS_KERNEL_LOGP: return "token log probabilities";
+    case BNS_KERNEL_HEAD_NORM: return "heads' norm + rotation";
+    case BNS_KERNEL_CLIP: return "gradient norm and clipping";
     }
     return "unknown";
 }

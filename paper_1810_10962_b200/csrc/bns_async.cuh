@@ -1,4 +1,4 @@
-// Barriers in shared memory with bounded waits, and 2^x: what the language-model kernels share.
+// Barriers in shared memory with bounded waits.
 #pragma once
 
 #include "bns_elements.cuh"
@@ -10,13 +10,6 @@ constexpr unsigned kPolls = 1u << 22;   // attempts before a wait gives up
 // Bounded waits that ran out since the library was loaded.
 __device__ unsigned g_lm_timeouts;
 
-__device__ __forceinline__ float exp2_fast(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));   // 2 ulp, 2^-126 and below give 0
-    return r;
-}
-
-__device__ __forceinline__ unsigned smem_address(const void* p) { return static_cast<unsigned>(__cvta_generic_to_shared(p)); }
 __device__ __forceinline__ void barrier_init(unsigned bar, unsigned arrivals) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(arrivals) : "memory");
 }

@@ -1,0 +1,239 @@
+// Global norm over many gradients, and clipping by it.
+//
+//   norm = sqrt(sum over all elements of all tensors of g^2);  factor = 1 where norm <= max_norm, else max_norm / norm
+//   out = g factor
+//
+// Bound by HBM: the norm reads every element once, clipping reads it again (what fits of it out of L2, hence back to front)
+// and writes it.  The list travels in the kernels' arguments, so nothing is copied to the device and a captured graph holds
+// all it needs.  All tensors are taken as one line of 16-byte vectors which the blocks share evenly, whatever the tensors'
+// sizes; elements outside whole vectors go with a place of their own in front of each tensor's vectors.
+//
+// Squares are added in fp32 over a batch of vectors, batches and everything above in 64 bits.  A batch whose sum leaves the
+// range in which fp32 squares are exact enough is done again in 64 bits.
+#pragma once
+
+#include "bns_elements.cuh"
+
+namespace bns {
+
+constexpr int kClipThreads = 256;
+constexpr int kClipDepth = 8;            // vectors in flight per thread
+constexpr int kClipBlocks = 4;           // of a launch, per SM
+
+struct ClipEntry {
+    const void* in;
+    void* out;
+    int64_t elements;                    // times two, plus one for bf16
+    int64_t first;                       // place in the line
+};
+template <int N>
+struct ClipList {
+    ClipEntry entry[N];
+    int64_t places;                      // of the line
+    int count;
+};
+
+// Where a tensor's whole vectors begin and how many there are.
+template <typename T>
+struct ClipSpan {
+    int head;
+    int64_t vectors, n;
+    __device__ __forceinline__ ClipSpan(const void* p, int64_t elements) : n(elements) {
+        constexpr int V = 16 / sizeof(typename T::storage);
+        const int to_word = static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / static_cast<int>(sizeof(typename T::storage));
+        head = n < to_word ? static_cast<int>(n) : to_word;
+        vectors = (n - head) / V;
+    }
+    // thread t's element outside whole vectors, or -1: at most 2 V - 2 of them
+    __device__ __forceinline__ int64_t loose(int t) const {
+        constexpr int V = 16 / sizeof(typename T::storage);
+        const int64_t tail = head + vectors * V;
+        return t < head ? t : t >= 16 && t < 32 && tail + t - 16 < n ? tail + t - 16 : -1;
+    }
+};
+
+// Calls visit(entry, [begin, end) of its places) for the block's share of the line.
+template <int N, typename Visit>
+__device__ __forceinline__ void walk_line(const ClipList<N>& list, int block, int blocks, Visit&& visit) {
+    const int64_t begin = list.places / blocks * block + min(static_cast<int64_t>(block), list.places % blocks);
+    const int64_t end = begin + list.places / blocks + (block < list.places % blocks);
+    if (begin >= end) return;
+    int low = 0, high = list.count - 1;              // the last entry that begins at or before `begin`
+    while (low < high) {
+        const int middle = (low + high + 1) / 2;
+        if (list.entry[middle].first <= begin)
+            low = middle;
+        else
+            high = middle - 1;
+    }
+    for (int e = low; e < list.count && list.entry[e].first < end; ++e) {
+        const int64_t first = list.entry[e].first, last = e + 1 < list.count ? list.entry[e + 1].first : list.places;
+        visit(list.entry[e], (begin > first ? begin : first) - first, (end < last ? end : last) - first);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ double squares_of(const void* data, int64_t elements, int64_t from, int64_t to) {
+    using S = typename T::storage;
+    constexpr int V = 16 / sizeof(S);
+    const S* p = static_cast<const S*>(data);
+    const ClipSpan<T> span(data, elements);
+    double total = 0.;
+    if (from == 0) {
+        const int64_t i = span.loose(threadIdx.x);
+        if (i >= 0) {
+            const double f = to_float<T>(p[i]);
+            total = f * f;
+        }
+    }
+    const uint4* body = reinterpret_cast<const uint4*>(p + span.head);
+    const int64_t end = to - 1;
+    for (int64_t v0 = (from > 0 ? from - 1 : 0) + threadIdx.x; v0 < end; v0 += kClipThreads * kClipDepth) {
+        Vec<T, V> x[kClipDepth];
+#pragma unroll
+        for (int i = 0; i < kClipDepth; ++i) {
+            x[i].raw = make_uint4(0, 0, 0, 0);
+            if (v0 + i * kClipThreads < end) x[i].raw = body[v0 + i * kClipThreads];
+        }
+        pair_t sum[2] = {};
+#pragma unroll
+        for (int i = 0; i < kClipDepth; ++i)
+#pragma unroll
+            for (int q = 0; q < V / 2; ++q) {
+                const pair_t f = vec_pair<T, V>(x[i], q);
+                sum[q & 1] = fma2(f, f, sum[q & 1]);
+            }
+        float lo, hi;
+        split_pair(add2(sum[0], sum[1]), lo, hi);
+        const float s = lo + hi;
+        if (s > 0x1p-80f && s < 0x1p120f) {          // squares below 2^-126 are not whole, but then they do not count
+            total += s;
+            continue;
+        }
+        unsigned bits = 0;
+#pragma unroll
+        for (int i = 0; i < kClipDepth; ++i) bits |= x[i].raw.x | x[i].raw.y | x[i].raw.z | x[i].raw.w;
+        if (bits & (sizeof(S) == 2 ? 0x7fff7fffu : 0x7fffffffu)) {      // not all zeros
+#pragma unroll 1
+            for (int i = 0; i < kClipDepth; ++i) {
+                const int64_t v = v0 + i * kClipThreads;
+                if (v >= end) break;
+                const S* f = reinterpret_cast<const S*>(body + v);
+#pragma unroll 1
+                for (int j = 0; j < V; ++j) {
+                    const double d = to_float<T>(f[j]);
+                    total += d * d;
+                }
+            }
+        }
+    }
+    return total;
+}
+
+// The sum over the block's threads, for thread 0.
+__device__ __forceinline__ double block_sum(double v, double* fold) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) fold[threadIdx.x >> 5] = v;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        v = threadIdx.x < kClipThreads / 32 ? fold[threadIdx.x] : 0.;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    }
+    return v;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads) clip_squares_kernel(const __grid_constant__ ClipList<N> list, double* partial) {
+    __shared__ double fold[kClipThreads / 32];
+    grid_dependency_wait();
+    grid_dependency_launch();
+    double total = 0.;
+    walk_line(list, blockIdx.x, gridDim.x, [&](const ClipEntry& e, int64_t from, int64_t to) {
+        if (e.elements & 1)
+            total += squares_of<BF16>(e.in, e.elements >> 1, from, to);
+        else
+            total += squares_of<F32>(e.in, e.elements >> 1, from, to);
+    });
+    total = block_sum(total, fold);
+    if (threadIdx.x == 0) partial[blockIdx.x] = total;
+}
+
+// The norm from the blocks' sums, in the same order by every block that asks; all its threads get the sum.
+__device__ __forceinline__ double sum_partials(const double* partial, int count, double* fold) {
+    double v = 0.;
+    for (int i = threadIdx.x; i < count; i += kClipThreads) v += partial[i];
+    v = block_sum(v, fold);
+    __syncthreads();
+    if (threadIdx.x == 0) fold[0] = v;
+    __syncthreads();
+    return fold[0];
+}
+
+__global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const double* partial, int count, float* norm) {
+    __shared__ double fold[kClipThreads / 32];
+    grid_dependency_wait();
+    grid_dependency_launch();
+    const double sum = sum_partials(partial, count, fold);
+    if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(sum));
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_span(const void* data, void* out, int64_t elements, int64_t from, int64_t to, float factor) {
+    using S = typename T::storage;
+    constexpr int V = 16 / sizeof(S);
+    const S* p = static_cast<const S*>(data);
+    S* o = static_cast<S*>(out);
+    const ClipSpan<T> span(data, elements);
+    if (from == 0) {
+        const int64_t i = span.loose(threadIdx.x);
+        if (i >= 0) o[i] = from_float<T>(to_float<T>(p[i]) * factor);
+    }
+    const uint4* body = reinterpret_cast<const uint4*>(p + span.head);
+    S* to_body = o + span.head;
+    const bool words = (reinterpret_cast<uintptr_t>(to_body) & 15) == 0;
+    const pair_t by = make_pair(factor, factor);
+    const int64_t end = to - 1;
+    for (int64_t v0 = (from > 0 ? from - 1 : 0) + threadIdx.x; v0 < end; v0 += kClipThreads * kClipDepth) {
+        Vec<T, V> x[kClipDepth];
+#pragma unroll
+        for (int i = 0; i < kClipDepth; ++i)
+            if (v0 + i * kClipThreads < end) x[i].raw = body[v0 + i * kClipThreads];
+#pragma unroll
+        for (int i = 0; i < kClipDepth; ++i) {
+            const int64_t v = v0 + i * kClipThreads;
+            if (v >= end) continue;
+#pragma unroll
+            for (int q = 0; q < V / 2; ++q) set_vec_pair<T, V>(x[i], q, mul2(vec_pair<T, V>(x[i], q), by));
+            if (words) {
+                __stcs(reinterpret_cast<uint4*>(to_body + v * V), x[i].raw);
+            } else {
+                const S* f = reinterpret_cast<const S*>(&x[i].raw);
+#pragma unroll
+                for (int j = 0; j < V; ++j) to_body[v * V + j] = f[j];
+            }
+        }
+    }
+}
+
+// Every block finds the norm itself.  The last block walks the line's front: what the norm read last is still in L2.
+template <int N>
+__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_constant__ ClipList<N> list, const double* partial, int count, float max_norm, float* norm) {
+    __shared__ double fold[kClipThreads / 32];
+    grid_dependency_wait();
+    grid_dependency_launch();
+    const double exact = sqrt(sum_partials(partial, count, fold));
+    const float rounded = static_cast<float>(exact);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = rounded;
+    const float factor = rounded <= max_norm ? 1.f : static_cast<float>(max_norm / exact);
+    walk_line(list, gridDim.x - 1 - blockIdx.x, gridDim.x, [&](const ClipEntry& e, int64_t from, int64_t to) {
+        if (factor == 1.f && e.in == e.out) return;
+        if (e.elements & 1)
+            scale_span<BF16>(e.in, e.out, e.elements >> 1, from, to, factor);
+        else
+            scale_span<F32>(e.in, e.out, e.elements >> 1, from, to, factor);
+    });
+}
+
+}  // namespace bns

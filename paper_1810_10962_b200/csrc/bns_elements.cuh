@@ -1,5 +1,5 @@
 // What every kernel file of the library uses: programmatic dependent launch, element types, vectors of
-// up to 16 bytes, packed fp32 pairs.
+// up to 16 bytes, packed fp32 pairs, 2^x.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -151,5 +151,13 @@ __device__ __forceinline__ void set_vec_pair(Vec<T, V>& v, int q, pair_t p) {
         f[2 * q + 1] = hi;
     }
 }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));   // 2 ulp, 2^-126 and below give 0
+    return r;
+}
+
+__device__ __forceinline__ unsigned smem_address(const void* p) { return static_cast<unsigned>(__cvta_generic_to_shared(p)); }
 
 }  // namespace bns

@@ -1,0 +1,556 @@
+// Log probabilities of given tokens with the distribution's entropy and its top alternatives, and the logits' gradient.
+//
+//   q = softmax of z / tau;  logp = log q_token;  H = - sum_v q_v log q_v;  alternatives: the K largest (z_v, lowest v first)
+//   dz_v = (dlogp ([v = token] - q_v) - dH q_v (log q_v + H)) / tau
+//
+// Bound by HBM: forward reads the logits once, backward reads them and writes the gradient.  With c = log2(e) / tau and a
+// reference m, the largest z c so far, a pass keeps  s = sum 2^(z c - m)  and  t = sum 2^(z c - m) (z c - m);  then
+//   log2 q_v = z_v c - m - log2 s      H = ln 2 (log2 s - t / s)
+// t is a sum of terms of one sign, and a change of the reference by d scales both by 2^d after t has got d s.
+//
+// Alternatives without a second pass: a thread keeps the largest value of each of its segments (up to eight) beside the
+// sums, which the running maximum needs anyway.  K threads' largest values bound the K-th largest of the row from below,
+// so only segments that reach that bound are read again (K of 512 threads x segments, a few per cent of the row, out of L2);
+// what reaches it, some K values, is ordered by comparing all with all.
+#pragma once
+
+#include "bns_logits.cuh"
+
+namespace bns {
+
+constexpr int kLogpThreads = 512, kLogpSmall = 128;     // of a block; the second for short rows
+constexpr int kLogpParts = 8;                           // most blocks a row is split over
+constexpr int kLogpDepth = 8;                           // vectors in flight per thread
+constexpr int kLogpMaxTop = 64;
+constexpr int kLogpSegments = 8;                        // of a thread
+constexpr int kLogpFound = 1024;                        // values that reach the bound, before the slow way is taken
+constexpr float kLogpFloor = -0x1p60f;                  // stands in for anything lower: 2^(floor c - m) = 0, and 0 times it is 0
+static_assert(kLogpParts * kLogpMaxTop <= kLogpFound);
+
+struct LogProbs {
+    const void* z;
+    const void* token;
+    const float *lse_in, *entropy_in, *dlogp, *dentropy;   // backward; dentropy may be NULL
+    float *logp, *entropy, *lse, *top;
+    int* index;
+    void* dz;
+    int64_t z_stride, dz_stride, rows;
+    int V, K, token64;
+    float tau, c;
+    int parts, per;       // blocks of a row, vectors of each
+};
+
+// Largest log-sum that the gradient takes q from: its rounding, 2^-24 of it, is off by 2^-16 in q then, or for bf16 by 2^-12.
+template <typename T>
+constexpr float kLogpKept = sizeof(typename T::storage) == 2 ? 0x1p12f : 0x1p8f;
+
+// m, s and t of a set of values; m = -inf: none that counts.
+struct Stats {
+    float m, s, t;
+};
+// 2^d and d for a side whose reference moves up by -d; no reference yet: nothing to scale.
+__device__ __forceinline__ void move_reference(Stats& a, float m) {
+    const float d = a.m == m ? 0.f : fmaxf(a.m - m, -0x1p30f), f = exp2_fast(d);
+    a.t = f * fmaf(d, a.s, a.t);
+    a.s *= f;
+    a.m = m;
+}
+__device__ __forceinline__ void join_stats(Stats& a, Stats b) {
+    const float m = fmaxf(a.m, b.m);
+    move_reference(a, m);
+    move_reference(b, m);
+    a.s += b.s;
+    a.t += b.t;
+}
+
+// Whole numbers in the order of the values, both zeros alike; 0 is below -inf.
+__device__ __forceinline__ unsigned order_key(float v) {
+    const unsigned u = __float_as_uint(v + 0.f);
+    return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float of_key(unsigned k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
+
+// Not below the floor; NaN stays.
+template <typename T>
+__device__ __forceinline__ void raise_to_floor(uint4& raw) {
+    if constexpr (sizeof(typename T::storage) == 2) {
+        __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(&raw);
+        const __nv_bfloat162 floor = __float2bfloat162_rn(kLogpFloor);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = __hmax2_nan(w[q], floor);
+    } else {
+        float* f = reinterpret_cast<float*>(&raw);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) asm("max.NaN.f32 %0, %0, %1;" : "+f"(f[q]) : "f"(kLogpFloor));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void add_stats(uint4 raw, pair_t c, pair_t minus_ref, pair_t& sum, pair_t& weighted) {
+    constexpr int V = 16 / sizeof(typename T::storage);
+    raise_to_floor<T>(raw);
+    Vec<T, V> x;
+    x.raw = raw;
+#pragma unroll
+    for (int q = 0; q < V / 2; ++q) {
+        const pair_t u = fma2(vec_pair<T, V>(x, q), c, minus_ref);
+        float lo, hi;
+        split_pair(u, lo, hi);
+        const pair_t e = make_pair(exp2_fast(lo), exp2_fast(hi));
+        sum = add2(sum, e);
+        weighted = fma2(e, u, weighted);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ bool any_nan(const uint4& raw) {
+    constexpr int V = 16 / sizeof(typename T::storage);
+    Vec<T, V> x;
+    x.raw = raw;
+    bool nan = false;
+#pragma unroll
+    for (int j = 0; j < V; ++j) nan |= x.get(j) != x.get(j);
+    return nan;
+}
+
+// What a row's values are turned into log q with.
+struct LogQ {
+    float tau, c, m, log_s, base, lse;
+    bool far;            // of differences to the largest value
+    __device__ __forceinline__ float operator()(float v) const {
+        if (far) return (v - base) / tau - log_s * kLn2;
+        if (v < 0.f && !(v * c >= -kFar)) return v / tau - lse;     // a mask beside ordinary values: v c may leave fp32's range
+        return (fmaf(v, c, -m) - log_s) * kLn2;
+    }
+};
+
+// Values found and their places, the K first of them in order.
+struct Found {
+    unsigned key[kLogpFound];
+    int at[kLogpFound];
+    int count;
+};
+
+// Ranks `count` values by (value, lowest place first); put(rank, key, place) gets those below K.
+template <typename Put>
+__device__ __forceinline__ void rank_found(const unsigned* key, const int* at, int count, int K, Put&& put) {
+    for (int i = threadIdx.x; i < count; i += blockDim.x) {
+        const unsigned mine = key[i];
+        const int place = at[i];
+        int rank = 0;
+        for (int j = 0; j < count; ++j) rank += key[j] > mine || (key[j] == mine && at[j] < place);
+        if (rank < K) put(rank, mine, place);
+    }
+}
+
+// The slow way, for rows where more values reach the bound than there is room for: equal logits all over a row, most of
+// the vocabulary masked with one value, or the top ones next to one another.  [first, last) are the part's places.
+// Leaves at most kLogpFound values, the K largest among them, the same set in every run.
+template <typename T>
+__device__ __noinline__ void find_slowly(const typename T::storage* z, int first, int last, unsigned bound, int K, Found& found, int* fold) {
+    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
+    auto key_at = [&](int v) {
+        const float x = to_float<T>(z[v]);
+        return x == x ? order_key(x) : 0u;
+    };
+    auto above = [&](unsigned limit) {     // how many values lie above it
+        __syncthreads();
+        if (tid == 0) found.count = 0;
+        __syncthreads();
+        int n = 0;
+        for (int v = first + tid; v < last; v += threads) n += key_at(v) > limit;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+        if (lane == 0 && n) atomicAdd(&found.count, n);
+        __syncthreads();
+        return found.count;
+    };
+    int more = above(bound);
+    if (more >= K && more > kLogpFound) {  // the K-th largest itself: the largest key that K values reach
+        unsigned low = bound + 1, high = 0xffffffffu;
+        while (low < high) {
+            const unsigned middle = high - (high - low) / 2;
+            if (above(middle - 1) >= K)
+                low = middle;
+            else
+                high = middle - 1;
+        }
+        bound = low;
+        more = above(bound);               // fewer than K
+    }
+    __syncthreads();
+    if (tid == 0) found.count = 0;
+    __syncthreads();
+    for (int v = first + tid; v < last; v += threads) {
+        const unsigned k = key_at(v);
+        if (k > bound) {
+            const int to = atomicAdd(&found.count, 1);
+            found.key[to] = k;
+            found.at[to] = v;
+        }
+    }
+    // of those at the bound the first ones, place by place
+    int have = more;
+    for (int v0 = first; v0 < last && have < K; v0 += threads) {
+        const int v = v0 + tid;
+        const bool here = bound != 0 && v < last && key_at(v) == bound;
+        const unsigned votes = __ballot_sync(0xffffffffu, here);
+        __syncthreads();
+        if (lane == 0) fold[warp] = __popc(votes);
+        __syncthreads();
+        int before = have + __popc(votes & ((1u << lane) - 1)), all = 0;
+        for (int w = 0; w < warps; ++w) {
+            before += w < warp ? fold[w] : 0;
+            all += fold[w];
+        }
+        if (here && before < K) {
+            found.key[before] = bound;
+            found.at[before] = v;
+        }
+        have = min(K, have + all);
+    }
+    __syncthreads();
+    if (tid == 0) found.count = max(have, more);
+    __syncthreads();
+}
+
+// Part blockIdx % parts of row blockIdx / parts: `per` vectors, and the loose elements at either end of the row.
+template <typename T, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(const LogProbs a) {
+    using S = typename T::storage;
+    constexpr int V = 16 / sizeof(S), kWarps = THREADS / 32;
+    __shared__ Stats fold[kWarps];
+    __shared__ Stats of_part[kLogpParts];
+    __shared__ float sums[kWarps];
+    __shared__ float segment[TOP ? kLogpSegments : 1][TOP ? THREADS : 1];
+    __shared__ Found found;                           // unused without TOP
+    __shared__ unsigned merged_key[TOP ? kLogpParts * kLogpMaxTop : 1];
+    __shared__ int merged_at[TOP ? kLogpParts * kLogpMaxTop : 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const float inf = __int_as_float(0x7f800000);
+    // Another block's shared memory may be written once that block runs: all of the cluster arrive here, and wait for one
+    // another after the row's pass, which hides it
+    if (a.parts > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+    grid_dependency_wait();
+    grid_dependency_launch();
+    const int64_t row = blockIdx.x / a.parts;
+    const int part = blockIdx.x - static_cast<int>(row) * a.parts;
+    const S* z = static_cast<const S*>(a.z) + row * a.z_stride;
+    int64_t token = -1;
+    if (tid == 0 && part == 0) token = a.token64 ? static_cast<const long long*>(a.token)[row] : static_cast<const int*>(a.token)[row];
+    const int head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(S)));
+    const int vectors = (a.V - head) / V, tail = head + vectors * V;
+    const int begin = min(vectors, part * a.per), end = min(vectors, begin + a.per);
+    // elements outside whole vectors: those before them belong to the first part, those after them to the last
+    const int loose = part == 0 && tid < head ? tid : part == a.parts - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
+    const float loose_z = loose >= 0 ? to_float<T>(z[loose]) : -inf;
+    const uint4* body = reinterpret_cast<const uint4*>(z + head);
+    uint4 x[kLogpDepth];
+    auto fetch = [&](int v0) {
+#pragma unroll
+        for (int i = 0; i < kLogpDepth; ++i)
+            if (v0 + i * THREADS < end) x[i] = body[v0 + i * THREADS];
+    };
+    fetch(begin + tid);
+    float token_z = 0.f;
+    const bool given = token >= 0 && token < a.V;
+    if (given) token_z = to_float<T>(z[token]);
+
+    Stats st{-inf, 0.f, 0.f};
+    if (loose >= 0) {
+        const float m = loose_z * a.c;
+        if (fabsf(m) <= kFar)
+            st = Stats{m, exp2_fast(fmaf(loose_z, a.c, -m)), 0.f};
+        else
+            st = Stats{m == m ? m : -inf, m == m ? 0.f : m, 0.f};
+    }
+    // batches of a segment, so that there are kLogpSegments at the most
+    constexpr int kBatch = THREADS * kLogpDepth;
+    const int batches = (a.per + kBatch - 1) / kBatch, group = (batches + kLogpSegments - 1) / kLogpSegments;
+    float mine = loose_z == loose_z ? loose_z : -inf;   // the thread's largest
+    float of_segment = -inf;
+    int batch = 0;
+    for (int v0 = begin + tid; v0 < end; v0 += kBatch) {
+        if (v0 != begin + tid) fetch(v0);
+        TopOf<T> top;
+#pragma unroll
+        for (int i = 0; i < kLogpDepth; ++i)
+            if (v0 + i * THREADS < end) top.add(x[i]);
+        const float largest = top.get();
+        const float m = fmaxf(largest * a.c, st.m);
+        if (fabsf(m) <= kFar) {
+            move_reference(st, m);
+            pair_t sum = make_pair(st.s, 0.f), weighted = make_pair(st.t, 0.f);
+#pragma unroll
+            for (int i = 0; i < kLogpDepth; ++i)
+                if (v0 + i * THREADS < end) add_stats<T>(x[i], twice(a.c), twice(-m), sum, weighted);
+            st.s = both(sum);
+            st.t = both(weighted);
+        } else {                                       // nothing here counts beside an ordinary maximum, but NaN does
+            bool nan = false;
+#pragma unroll
+            for (int i = 0; i < kLogpDepth; ++i)
+                if (v0 + i * THREADS < end) nan |= any_nan<T>(x[i]);
+            st = Stats{m, nan ? __int_as_float(0x7fffffff) : st.s, 0.f};
+        }
+        if constexpr (TOP) {
+            of_segment = fmaxf(of_segment, largest);
+            mine = fmaxf(mine, largest);
+            if (++batch % group == 0 || v0 + kBatch >= end) {
+                segment[(batch - 1) / group][tid] = of_segment;
+                of_segment = -inf;
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const Stats other{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.t, o)};
+        join_stats(st, other);
+    }
+    if (lane == 0) fold[warp] = st;
+    __syncthreads();
+    st = fold[0];
+    for (int w = 1; w < kWarps; ++w) join_stats(st, fold[w]);
+    if (a.parts > 1) {      // every block of the cluster gets every block's sums, and joins them in the same order
+        asm volatile("barrier.cluster.wait;" ::: "memory");      // all of them run
+        if (tid < a.parts) {
+            unsigned to;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_address(&of_part[part])), "r"(tid));
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(st.m) : "memory");
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4), "f"(st.s) : "memory");
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 8), "f"(st.t) : "memory");
+        }
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        st = of_part[0];
+        for (int p = 1; p < a.parts; ++p) join_stats(st, of_part[p]);
+    }
+
+    const float log_s = log2f(st.s);
+    float lse = (st.m + log_s) * kLn2, entropy = (log_s - st.t / st.s) * kLn2;
+    LogQ log_q{a.tau, a.c, st.m, log_s, 0.f, lse, false};
+    if (!(fabsf(st.m) <= kNear)) {
+        // The largest value times c is too large for the fast form (a row masked with -1e10 or the type's lowest value
+        // throughout, say): everything of differences.  Every block looks at the whole row.
+        auto larger = [](float p, float q) { return fmaxf(p, q); };
+        auto plus = [](float p, float q) { return p + q; };
+        float top = -inf, s = 0.f, t = 0.f;
+#pragma unroll 1
+        for (int v = tid; v < a.V; v += THREADS) top = fmaxf(top, to_float<T>(z[v]));
+        top = block_of(top, sums, larger);
+        if (top != -inf || st.s != st.s) {
+#pragma unroll 1
+            for (int v = tid; v < a.V; v += THREADS) {
+                const float d = (to_float<T>(z[v]) - top) * a.c, e = exp2_fast(d);
+                s += e;
+                if (e != 0.f) t = fmaf(e, d, t);
+            }
+            s = block_of(s, sums, plus);
+            t = block_of(t, sums, plus);
+            log_q = LogQ{a.tau, a.c, 0.f, log2f(s), top, 0.f, true};
+            lse = top / a.tau + log_q.log_s * kLn2;
+            entropy = (log_q.log_s - t / s) * kLn2;
+        } else {                                       // nothing is left of the row
+            log_q = LogQ{1.f, 1.f, 0.f, 0.f, 0.f, 0.f, false};   // -inf of all that is there
+            lse = -inf;
+            entropy = 0.f;
+        }
+    }
+    if (tid == 0 && part == 0) {
+        a.logp[row] = given ? log_q(token_z) : 0.f;
+        a.lse[row] = lse;
+        if (a.entropy) a.entropy[row] = entropy;
+    }
+
+    if constexpr (TOP) {
+        // the largest bound that K threads' values reach, or a little lower; keys of bf16 values differ in their upper half
+        const bool has = loose >= 0 || begin + tid < end;
+        const unsigned own_key = has ? order_key(mine) : 0u;
+        unsigned bound = 0;
+        constexpr int kLowest = sizeof(S) == 2 ? 16 : 0;
+        int enough = a.K + a.K / 4 + 4;
+#pragma unroll 1
+        for (int bit = 31; bit >= kLowest; --bit) {
+            const unsigned candidate = bound | (1u << bit);
+            const int reach = __syncthreads_count(own_key >= candidate);
+            if (reach >= a.K) bound = candidate;
+            if (reach >= a.K && reach <= enough) break;
+        }
+        if (tid == 0) found.count = 0;
+        __syncthreads();
+        auto look = [&](float v, int at) {
+            const unsigned k = order_key(v);
+            if (v == v && k >= bound) {
+                const int to = atomicAdd(&found.count, 1);
+                if (to < kLogpFound) {
+                    found.key[to] = k;
+                    found.at[to] = at;
+                }
+            }
+        };
+        if (own_key >= bound && has) {
+            if (loose >= 0) look(loose_z, loose);
+#pragma unroll 1
+            for (int v0 = begin + tid, b = 0; v0 < end; v0 += kBatch, ++b) {
+                if (order_key(segment[b / group][tid]) < bound) continue;
+#pragma unroll 1
+                for (int i = 0; i < kLogpDepth; ++i) {
+                    const int v = v0 + i * THREADS;
+                    if (v >= end) break;
+                    Vec<T, V> y;
+                    y.raw = body[v];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) look(y.get(j), head + v * V + j);
+                }
+            }
+        }
+        __syncthreads();
+        const int first = part == 0 ? 0 : head + begin * V, last = part == a.parts - 1 ? a.V : head + end * V;
+        if (found.count > kLogpFound) {
+            // the bound itself: the K-th largest of the threads' values
+            unsigned exact = 0;
+#pragma unroll 1
+            for (int bit = 31; bit >= kLowest; --bit)
+                if (__syncthreads_count(own_key >= (exact | (1u << bit))) >= a.K) exact |= 1u << bit;
+            if (kLowest && exact && !(exact >> 31)) exact |= 0xffffu;      // of values below zero the lower half is ones
+            find_slowly<T>(z, first, last, exact, a.K, found, reinterpret_cast<int*>(sums));
+        }
+        const int count = found.count;
+        auto write = [&](int rank, unsigned key, int at) {
+            a.top[row * a.K + rank] = log_q(of_key(key));
+            a.index[row * a.K + rank] = at;
+        };
+        auto nothing = [&](int rank) {
+            a.top[row * a.K + rank] = -inf;
+            a.index[row * a.K + rank] = -1;
+        };
+        if (a.parts == 1) {
+            rank_found(found.key, found.at, count, a.K, write);
+            for (int k = count + tid; k < a.K; k += THREADS) nothing(k);
+        } else {
+            // every part's K first go to the first block, which orders them; places without a value have key 0
+            auto send = [&](int rank, unsigned key, int at) {
+                unsigned to_key, to_at;
+                const int slot = part * a.K + rank;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to_key) : "r"(smem_address(&merged_key[slot])), "r"(0));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to_at) : "r"(smem_address(&merged_at[slot])), "r"(0));
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to_key), "r"(key) : "memory");
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to_at), "r"(at) : "memory");
+            };
+            rank_found(found.key, found.at, count, a.K, send);
+            for (int k = count + tid; k < a.K; k += THREADS) send(k, 0u, 0x7fffffff - k - part * a.K);
+            asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+            if (part == 0)
+                rank_found(merged_key, merged_at, a.parts * a.K, a.K, [&](int rank, unsigned key, int at) {
+                    if (key)
+                        write(rank, key, at);
+                    else
+                        nothing(rank);
+                });
+        }
+    }
+}
+
+// The gradient: q_v = 2^(z_v c - m) / rest from the forward call's log-sum, so every element by itself:
+//   dz_v = 2^u (k0 + k1 u) with u = z_v c - m,  and dlogp / tau more at the token.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(const LogProbs a) {
+    using S = typename T::storage;
+    constexpr int V = 16 / sizeof(S);
+    __shared__ float fold[THREADS / 32];
+    const int tid = threadIdx.x;
+    const float inf = __int_as_float(0x7f800000);
+    grid_dependency_wait();
+    grid_dependency_launch();
+    // last row first: what the forward call read last may still be in L2
+    const int64_t block = blockIdx.x / a.parts, row = a.rows - 1 - block;
+    const int part = blockIdx.x - static_cast<int>(block) * a.parts;
+    const S* z = static_cast<const S*>(a.z) + row * a.z_stride;
+    S* dz = static_cast<S*>(a.dz) + row * a.dz_stride;
+    const int head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(S)));
+    const int vectors = (a.V - head) / V, tail = head + vectors * V;
+    const int begin = min(vectors, part * a.per), end = min(vectors, begin + a.per);
+    const int loose = part == 0 && tid < head ? tid : part == a.parts - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
+    const float loose_z = loose >= 0 ? to_float<T>(z[loose]) : 0.f;
+    const uint4* body = reinterpret_cast<const uint4*>(z + head);
+    uint4 x[kLogpDepth];
+    auto fetch = [&](int v0) {
+#pragma unroll
+        for (int i = 0; i < kLogpDepth; ++i)
+            if (v0 + i * THREADS < end) x[i] = body[v0 + i * THREADS];
+    };
+    fetch(begin + tid);
+    const int64_t given = a.token64 ? static_cast<const long long*>(a.token)[row] : static_cast<const int*>(a.token)[row];
+    const int token = given >= 0 && given < a.V ? static_cast<int>(given) : -1;
+    const float g = token >= 0 ? a.dlogp[row] / a.tau : 0.f, h = a.dentropy ? a.dentropy[row] / a.tau : 0.f;
+    const float lse = a.lse_in[row], entropy = a.dentropy ? a.entropy_in[row] : 0.f;
+    // lse tau c = m + rest with the same c as in z c, so that only z - lse tau feels its rounding
+    const double exponent = static_cast<double>(lse) * a.tau * a.c;
+    const float m = static_cast<float>(exponent), rest = static_cast<float>(exponent - m);
+    // log q = ln 2 (u - rest)
+    const float scale = exp2_fast(-rest), k0 = -(g + h * (entropy - rest * kLn2)) * scale, k1 = -h * kLn2 * scale;
+    const bool empty = lse == -inf, far = !empty && !(fabsf(lse) <= kLogpKept<T>);
+    float base = 0.f, log_s = 0.f;
+    if (far) {                       // the log-sum's rounding is too much for q: both parts of it once more, of differences
+        auto larger = [](float p, float q) { return fmaxf(p, q); };
+        auto plus = [](float p, float q) { return p + q; };
+        float s = 0.f;
+        base = -inf;
+#pragma unroll 1
+        for (int v = tid; v < a.V; v += THREADS) base = fmaxf(base, to_float<T>(z[v]));
+        base = block_of(base, fold, larger);
+#pragma unroll 1
+        for (int v = tid; v < a.V; v += THREADS) s += exp2_fast((to_float<T>(z[v]) - base) * a.c);
+        log_s = log2f(block_of(s, fold, plus));
+    }
+    auto value = [&](float v) {
+        if (empty) return 0.f;
+        const float u = far ? (v - base) * a.c - log_s : fmaf(v < kLogpFloor ? kLogpFloor : v, a.c, -m), e = exp2_fast(u);
+        return far ? e == 0.f ? 0.f : -e * (g + h * fmaf(u, kLn2, entropy)) : e * fmaf(k1, u, k0);
+    };
+    // the token's element has its thread add what is due there
+    auto at_token = [&](float v) { return empty ? 0.f : value(v) + g; };
+    const bool in_body = token >= head + begin * V && token < head + end * V;
+    const bool mine = in_body && ((token - head) / V - begin) % THREADS == tid;
+    const float token_z = mine ? to_float<T>(z[token]) : 0.f;
+    if (loose >= 0) dz[loose] = from_float<T>(loose == token ? at_token(loose_z) : value(loose_z));
+    const bool words = ((reinterpret_cast<uintptr_t>(dz) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
+    for (int v0 = begin + tid; v0 < end; v0 += THREADS * kLogpDepth) {
+        if (v0 != begin + tid) fetch(v0);
+#pragma unroll
+        for (int i = 0; i < kLogpDepth; ++i) {
+            const int v = v0 + i * THREADS;
+            if (v >= end) continue;
+            Vec<T, V> o;
+            if (!far && !empty) {
+                raise_to_floor<T>(x[i]);
+                Vec<T, V> y;
+                y.raw = x[i];
+#pragma unroll
+                for (int q = 0; q < V / 2; ++q) {
+                    const pair_t u = fma2(vec_pair<T, V>(y, q), twice(a.c), twice(-m));
+                    float lo, hi;
+                    split_pair(u, lo, hi);
+                    set_vec_pair<T, V>(o, q, mul2(make_pair(exp2_fast(lo), exp2_fast(hi)), fma2(u, twice(k1), twice(k0))));
+                }
+            } else {
+                Vec<T, V> y;
+                y.raw = x[i];
+#pragma unroll
+                for (int j = 0; j < V; ++j) o.set(j, value(y.get(j)));
+            }
+            S* to = dz + head + static_cast<int64_t>(v) * V;
+            if (words) {
+                __stcs(reinterpret_cast<uint4*>(to), o.raw);
+            } else {
+                const S* f = reinterpret_cast<const S*>(&o.raw);
+#pragma unroll
+                for (int j = 0; j < V; ++j) to[j] = f[j];
+            }
+        }
+    }
+    if (mine) dz[token] = from_float<T>(at_token(token_z));
+}
+
+}  // namespace bns

@@ -1,10 +1,11 @@
-"""Operators at the end of a language model's step: residual add + root-mean-square norm, linear head + softmax
-cross entropy, distillation from a teacher's top logits.
+"""Operators of a language model's step: residual add + root-mean-square norm, linear head + softmax cross entropy,
+distillation from a teacher's top logits, log probabilities of given tokens, norm + rotation of queries' and keys' heads,
+the norm over all gradients and clipping by it.
 
 Argument marshalling for the entry points of ``include/bns.h``, in the manner of ``bns.py``: tensors are CUDA
 tensors, work goes to the current CUDA stream, nothing falls back.  Row tensors are [..., columns] with dense rows;
 leading dimensions are taken together, so a tensor is either contiguous or two-dimensional with a row stride.
-Outputs are new dense tensors.  ``bns.BnsError`` carries the status of a refused call, ``TypeError`` stands for a tensor
+Outputs are new dense tensors, but for clipped gradients.  ``bns.BnsError`` carries the status of a refused call, ``TypeError`` stands for a tensor
 of the wrong kind.
 """
 from __future__ import annotations
@@ -40,6 +41,22 @@ class _Distillation(ctypes.Structure):
                 ("temperature", ctypes.c_float)]
 
 
+class _LogProbs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("vocabulary", ctypes.c_int), ("entries", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("stride", ctypes.c_int64), ("token_is_int64", ctypes.c_int), ("temperature", ctypes.c_float)]
+
+
+class _HeadNorm(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("batch", "length", "q_heads", "k_heads", "head_dim", "rotary", "dtype")] + [
+        (name, ctypes.c_int64) for name in ("q_batch", "q_position", "q_head", "k_batch", "k_position", "k_head")] + [
+        ("positions", ctypes.c_int), ("position_is_int64", ctypes.c_int), ("interleaved", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class _Gradients(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int), ("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("elements", ctypes.c_void_p),
+                ("dtype", ctypes.c_void_p)]
+
+
 @lru_cache(maxsize=4096)
 def _shape(kind, *fields):
     """(structure, reference to it) for these values; the library only reads it."""
@@ -55,7 +72,8 @@ def _load():
     if _lib is None:
         lib = _bns.load()
         vp, sz, fl, i64, it = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float, ctypes.c_int64, ctypes.c_int
-        rows, head, dist = (ctypes.POINTER(s) for s in (_Rows, _Head, _Distillation))
+        rows, head, dist, logp, turn, grads = (ctypes.POINTER(s) for s in (_Rows, _Head, _Distillation, _LogProbs, _HeadNorm,
+                                                                           _Gradients))
         for name, result, arguments in (
                 ("bns_rms_norm_forward", it, [rows, vp, i64, vp, i64, vp, fl, vp, vp, vp, vp]),
                 ("bns_rms_norm_forward_quantized", it, [rows, vp, i64, vp, i64, vp, fl, it, vp, vp, vp, vp, vp]),
@@ -66,7 +84,15 @@ def _load():
                 ("bns_linear_cross_entropy_backward", it, [head, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
                 ("bns_topk_distillation_forward", it, [dist, vp, vp, vp, vp, vp, vp]),
                 ("bns_topk_distillation_backward", it, [dist, vp, vp, vp, vp, vp, vp, i64, vp]),
-                ("bns_topk_distillation_step", it, [dist, vp, vp, vp, vp, vp, vp, i64, vp])):
+                ("bns_topk_distillation_step", it, [dist, vp, vp, vp, vp, vp, vp, i64, vp]),
+                ("bns_token_log_probs_forward", it, [logp, *[vp] * 8]),
+                ("bns_token_log_probs_backward", it, [logp, *[vp] * 7, i64, vp]),
+                ("bns_head_norm_rotary_forward", it, [turn, *[vp] * 10]),
+                ("bns_head_norm_rotary_workspace_bytes", sz, [turn]),
+                ("bns_head_norm_rotary_backward", it, [turn, *[vp] * 14, sz, vp]),
+                ("bns_gradient_norm_workspace_bytes", sz, [grads]),
+                ("bns_gradient_norm", it, [grads, vp, vp, sz, vp]),
+                ("bns_clip_gradients", it, [grads, fl, vp, vp, sz, vp])):
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = result, arguments
         _lib = lib
@@ -303,3 +329,218 @@ def topk_distillation_step(logits, teacher, index, dloss, temperature=1.0):
                                               dlogits.data_ptr(), fields.vocabulary, _stream(device)),
            "bns_topk_distillation_step")
     return loss, dlogits
+
+
+# ----------------------------------------------------------------------------- log probabilities of given tokens
+def _log_probs_inputs(logits, token, temperature, entries=0):
+    rows, vocabulary, stride = _matrix(logits, "logits")
+    at, wide = _indices(token, logits.shape[:-1], "token", logits.device)
+    return (*_shape(_LogProbs, rows, vocabulary, entries, _code(logits), stride, wide, float(temperature)), at)
+
+
+def token_log_probs_forward(logits, token, temperature=1.0):
+    """bns_token_log_probs_forward without alternatives: returns (logprob, entropy, lse), float32 per row: the log probability
+    of ``token`` under softmax(logits / temperature), 0 where it is negative, and the distribution's entropy."""
+    _, shape, at = _log_probs_inputs(logits, token, temperature)
+    logprob, entropy, lse = _vector_of(logits), _vector_of(logits), _vector_of(logits)
+    _check(_load().bns_token_log_probs_forward(shape, logits.data_ptr(), at, logprob.data_ptr(), entropy.data_ptr(),
+                                               lse.data_ptr(), None, None, _stream(logits.device)),
+           "bns_token_log_probs_forward")
+    return logprob, entropy, lse
+
+
+def token_log_probs_forward_top(logits, token, entries, temperature=1.0):
+    """bns_token_log_probs_forward with alternatives: returns (logprob, entropy, lse, top_logprob, top_index); the last two
+    are [..., entries], float32 and int32, the largest logit first and the lowest place first among equals.  1 to 64
+    entries."""
+    if entries < 1:
+        raise ValueError("entries must be at least 1")
+    _, shape, at = _log_probs_inputs(logits, token, temperature, int(entries))
+    logprob, entropy, lse = _vector_of(logits), _vector_of(logits), _vector_of(logits)
+    top = logits.new_empty((*logits.shape[:-1], entries), dtype=torch.float32)
+    index = logits.new_empty((*logits.shape[:-1], entries), dtype=torch.int32)
+    _check(_load().bns_token_log_probs_forward(shape, logits.data_ptr(), at, logprob.data_ptr(), entropy.data_ptr(),
+                                               lse.data_ptr(), top.data_ptr(), index.data_ptr(), _stream(logits.device)),
+           "bns_token_log_probs_forward")
+    return logprob, entropy, lse, top, index
+
+
+def token_log_probs_backward(logits, token, lse, entropy, dlogprob, dentropy=None, temperature=1.0):
+    """bns_token_log_probs_backward: the gradient of the logits; lse and entropy are what the forward call returned,
+    dlogprob and dentropy the gradients of every row's outputs.  Without dentropy the entropy may be None."""
+    fields, shape, at = _log_probs_inputs(logits, token, temperature)
+    device, rows = logits.device, fields.rows
+    entropy_at = dentropy_at = None
+    if dentropy is not None:
+        entropy_at, dentropy_at = _vector(entropy, rows, "entropy", device), _vector(dentropy, rows, "dentropy", device)
+    dlogits = _like(logits)
+    _check(_load().bns_token_log_probs_backward(shape, logits.data_ptr(), at, _vector(lse, rows, "lse", device), entropy_at,
+                                                _vector(dlogprob, rows, "dlogprob", device), dentropy_at, dlogits.data_ptr(),
+                                                fields.vocabulary, _stream(device)), "bns_token_log_probs_backward")
+    return dlogits
+
+
+# ----------------------------------------------------------------------------- norm + rotation of heads
+def _heads(t, name: str, like=None):
+    """(batch, length, heads, head_dim, strides) of [length, heads, head_dim] or [batch, length, heads, head_dim]."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA tensor (this library has no CPU path)")
+    n = t.dim()
+    if n not in (3, 4):
+        raise TypeError(f"{name}: expected [length, heads, head_dim] or [batch, length, heads, head_dim]")
+    if like is not None and (t.shape[:-2] != like.shape[:-2] or t.shape[-1] != like.shape[-1] or t.dtype != like.dtype
+                             or t.device != like.device):
+        raise TypeError(f"{name} must match q in positions, head_dim, dtype and device")
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise TypeError(f"{name}: heads must be dense")
+    if n == 3:
+        return 1, *t.shape, (0, *t.stride()[:2])
+    return *t.shape, t.stride()[:3]
+
+
+def _head_norm_inputs(q, k, q_weight, k_weight, cos, sin, position, eps, interleaved):
+    batch, length, heads, dim, strides = _heads(q, "q")
+    device, k_heads, k_strides, k_at, k_weight_at = q.device, 0, (0, 0, 0), None, None
+    if k is not None:
+        _, _, k_heads, _, k_strides = _heads(k, "k", q)
+        k_at, k_weight_at = k.data_ptr(), _vector(k_weight, dim, "k_weight", device)
+    if (not isinstance(cos, torch.Tensor) or cos.dim() != 2 or cos.dtype != torch.float32 or cos.device != device
+            or not cos.is_contiguous()):
+        raise TypeError(f"cos must be a contiguous float32 tensor [positions, rotary / 2] on {device}")
+    at, wide = _indices(position, q.shape[:-2], "position", device)
+    shape = _shape(_HeadNorm, batch, length, heads, k_heads, dim, 2 * cos.shape[1], _code(q), *strides, *k_strides, cos.shape[0],
+                   wide, 1 if interleaved else 0, float(eps))[1]
+    return shape, (q.data_ptr(), k_at, _vector(q_weight, dim, "q_weight", device), k_weight_at, cos.data_ptr(),
+                   _vector(sin, cos.numel(), "sin", device), at)
+
+
+def head_norm_rotary_forward(q, k, q_weight, k_weight, cos, sin, position, eps, interleaved=False):
+    """bns_head_norm_rotary_forward: returns (q_out, k_out).  q and k are [length, heads, head_dim] or [batch, length, heads,
+    head_dim], their heads dense, anything else strided (views of a packed projection); k and k_weight may be None.  cos
+    and sin are float32 [positions, rotary / 2], position int32 or int64 in the shape of q's leading dimensions; a negative
+    one is padding, whose outputs are zeros."""
+    shape, arguments = _head_norm_inputs(q, k, q_weight, k_weight, cos, sin, position, eps, interleaved)
+    q_out = q.new_empty(q.shape)
+    k_out = None if k is None else k.new_empty(k.shape)
+    _check(_load().bns_head_norm_rotary_forward(shape, *arguments, q_out.data_ptr(), None if k is None else k_out.data_ptr(),
+                                                _stream(q.device)), "bns_head_norm_rotary_forward")
+    return q_out, k_out
+
+
+def head_norm_rotary_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, position, eps, interleaved=False,
+                              workspace=None):
+    """bns_head_norm_rotary_backward: returns (dq, dk, dq_weight, dk_weight) from the contiguous gradients of the outputs and
+    the inputs of the forward call."""
+    shape, arguments = _head_norm_inputs(q, k, q_weight, k_weight, cos, sin, position, eps, interleaved)
+    device, lib = q.device, _load()
+    for d, t, name in ((dq_out, q, "dq_out"), (dk_out, k, "dk_out")):
+        if t is not None and (not isinstance(d, torch.Tensor) or d.shape != t.shape or d.dtype != t.dtype or d.device != device
+                              or not d.is_contiguous()):
+            raise TypeError(f"{name} must be contiguous and match its input in shape, dtype and device")
+    dq, dq_weight = q.new_empty(q.shape), torch.empty_like(q_weight)
+    dk = dk_weight = dk_at = dk_out_at = dk_weight_at = None
+    if k is not None:
+        dk, dk_weight = k.new_empty(k.shape), torch.empty_like(k_weight)
+        dk_at, dk_out_at, dk_weight_at = dk.data_ptr(), dk_out.data_ptr(), dk_weight.data_ptr()
+    workspace = _scratch(workspace, lib.bns_head_norm_rotary_workspace_bytes(shape), device)
+    _check(lib.bns_head_norm_rotary_backward(shape, dq_out.data_ptr(), dk_out_at, *arguments, dq.data_ptr(), dk_at,
+                                             dq_weight.data_ptr(), dk_weight_at, workspace.data_ptr(), workspace.nbytes,
+                                             _stream(device)), "bns_head_norm_rotary_backward")
+    return dq, dk, dq_weight, dk_weight
+
+
+# ----------------------------------------------------------------------------- norm over many gradients, clipping
+def _dense(t) -> bool:
+    """Whether the tensor's elements fill its span of memory, in any order of the dimensions."""
+    if t.is_contiguous():
+        return True
+    expected = 1
+    for stride, size in sorted(zip(t.stride(), t.shape)):
+        if size != 1:
+            if stride != expected:
+                return False
+            expected *= size
+    return True
+
+
+class GradientList:
+    """Gradients whose norm is taken together, checked and laid out once for many steps.
+
+    ``gradients``: dense tensors, float32 or bfloat16, in any mixture; ``out``: where clipped gradients go, tensors of the
+    same shapes, types and strides, or None to clip in place.  The list keeps the tensors; their memory has to stay where it
+    is."""
+
+    def __init__(self, gradients, out=None):
+        gradients = list(gradients)
+        out = gradients if out is None else list(out)
+        if len(out) != len(gradients):
+            raise TypeError("out must have a tensor for each gradient")
+        spans = []
+        for i, (g, o) in enumerate(zip(gradients, out)):
+            if not isinstance(g, torch.Tensor) or not g.is_cuda:
+                raise TypeError(f"gradient {i}: expected a CUDA tensor (this library has no CPU path)")
+            if g.device != gradients[0].device or not _dense(g):
+                raise TypeError(f"gradient {i} must be dense and on the device of the first one")
+            if o is not g and (not isinstance(o, torch.Tensor) or o.shape != g.shape or o.dtype != g.dtype
+                               or o.device != g.device or o.stride() != g.stride()):
+                raise TypeError(f"out {i} must match its gradient in shape, strides, dtype and device")
+            _code(g)
+            if g.numel():
+                start, to = g.data_ptr(), o.data_ptr()
+                if start != to:
+                    spans.append((start, start + g.nbytes, False))
+                spans.append((to, to + o.nbytes, True))
+        self._overlap = False           # of an output with another one or a gradient: clipping would depend on the order
+        read = written = 0
+        for start, end, is_out in sorted(spans):
+            self._overlap |= start < (max(read, written) if is_out else written)
+            if is_out:
+                written = max(written, end)
+            else:
+                read = max(read, end)
+        n = len(gradients)
+        self.gradients, self.out = gradients, out
+        self._arrays = ((ctypes.c_void_p * n)(*(g.data_ptr() for g in gradients)),
+                        (ctypes.c_void_p * n)(*(o.data_ptr() for o in out)),
+                        (ctypes.c_int64 * n)(*(g.numel() for g in gradients)),
+                        (ctypes.c_int * n)(*(_code(g) for g in gradients)))
+        self._list = _Gradients(n, *(ctypes.addressof(a) for a in self._arrays))
+        self._reference = ctypes.byref(self._list)
+        self._device = gradients[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        self._need = _load().bns_gradient_norm_workspace_bytes(self._reference)
+
+    def norm(self, workspace=None):
+        """bns_gradient_norm: the norm over all elements of all gradients, a float32 scalar on the device."""
+        stream = _stream(self._device)
+        workspace = _scratch(workspace, self._need, self._device)
+        norm = torch.empty((), dtype=torch.float32, device=self._device)
+        _check(_load().bns_gradient_norm(self._reference, norm.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream),
+               "bns_gradient_norm")
+        return norm
+
+    def clip(self, max_norm, workspace=None):
+        """bns_clip_gradients: writes the gradients, scaled down to ``max_norm`` where their norm is larger, to ``out``, and
+        returns the norm that they had."""
+        if self._overlap:
+            raise TypeError("outputs overlap one another or another gradient")
+        stream = _stream(self._device)
+        workspace = _scratch(workspace, self._need, self._device)
+        norm = torch.empty((), dtype=torch.float32, device=self._device)
+        _check(_load().bns_clip_gradients(self._reference, float(max_norm), norm.data_ptr(), workspace.data_ptr(),
+                                          workspace.nbytes, stream), "bns_clip_gradients")
+        return norm
+
+
+def gradient_norm(gradients):
+    """The norm over all elements of the gradients (tensors, or a GradientList)."""
+    return (gradients if isinstance(gradients, GradientList) else GradientList(gradients)).norm()
+
+
+def clip_gradients(gradients, max_norm, out=None):
+    """Clips the gradients (tensors, or a GradientList, which has its own ``out``) by their common norm, in place where
+    ``out`` is None; returns the norm that they had."""
+    if isinstance(gradients, GradientList):
+        if out is not None:
+            raise TypeError("a GradientList has its own out")
+        return gradients.clip(max_norm)
+    return GradientList(gradients, out).clip(max_norm)
