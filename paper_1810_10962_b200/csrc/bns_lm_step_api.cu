@@ -276,19 +276,32 @@ bns_status bns_token_log_probs_forward(const bns_token_log_probs* shape, const v
     a.top = top_logprob;
     a.index = top_index;
     const int vectors = std::max(1, a.V / (16 / eb));
-    const bool small = vectors <= kLogpSmall * kLogpDepth && a.rows > 2 * sm_count();
+    const int64_t rows = a.rows, sms = sm_count();
+    // Threads of a block, with 1024 an SM.  Small blocks let more rows' ends lie under other rows' streams: bf16, 20
+    // alternatives, 128 / 256 / 512 threads: 4096 x 32768 67 / 75 / 106 us, 2047 x 50257 53 / 57 / 72, 1024 x 131072 65 / 59 / 65;
+    // without alternatives 2047 x 50257 39 / 40 / 47.  More than 32 alternatives want more threads' maxima: 2047 x 50257
+    // with 64 72 / 68 / 82, unless a row has no more than some vectors for each thread (8192 x 4096 82 / 101).  Two to three rows
+    // an SM are too few blocks of 256: 300 x 131072 30 / 33 / 26.
+    const int threads = (vectors <= 1024 && rows > 2 * sms) || (vectors <= 8192 && rows > 8 * sms && a.K <= 32) ? kLogpSmall
+                        : rows > 2 * sms && rows <= 3 * sms ? kLogpLarge
+                                                            : kLogpThreads;
+    // Few rows are spread over the SMs, less thinly with alternatives, whose lists are joined (64 x 50257 fp32, 20: 8.7 us over
+    // four blocks, 12.3 over eight; 16 x 32768 bf16 6.6 with eight vectors a thread, 8.3 with two).
+    const int blocks = a.K ? 2 : 4, vectors_each = a.K ? 8 : 2;
     a.parts = 1;
-    // few rows are spread over the SMs
-    while (a.parts < kLogpParts && a.rows * (a.parts + 1) <= 2 * sm_count() && vectors > a.parts * kLogpThreads) ++a.parts;
+    while (a.parts < kLogpParts && rows * (a.parts + 1) <= blocks * sms && vectors > a.parts * threads * vectors_each) ++a.parts;
     a.per = divide_up(vectors, a.parts);
-    if (a.rows * a.parts >= int64_t{1} << 31) return BNS_ERR_SHAPE;
-    const unsigned parts = static_cast<unsigned>(a.parts), grid = static_cast<unsigned>(a.rows) * parts;
+    if (rows * a.parts >= int64_t{1} << 31) return BNS_ERR_SHAPE;
+    const unsigned parts = static_cast<unsigned>(a.parts), grid = static_cast<unsigned>(rows) * parts;
+    const Shape launch_shape{grid, static_cast<unsigned>(threads), parts};
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     BNS_LM_BY_TYPE(shape->dtype, {
-        if (small)
-            (logp_forward<T, kLogpSmall>(a, Shape{grid, kLogpSmall, parts}, stream));
+        if (threads == kLogpSmall)
+            (logp_forward<T, kLogpSmall>(a, launch_shape, stream));
+        else if (threads == kLogpLarge)
+            (logp_forward<T, kLogpLarge>(a, launch_shape, stream));
         else
-            (logp_forward<T, kLogpThreads>(a, Shape{grid, kLogpThreads, parts}, stream));
+            (logp_forward<T, kLogpThreads>(a, launch_shape, stream));
     });
     return last_error();
 }

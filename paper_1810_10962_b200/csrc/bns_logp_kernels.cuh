@@ -18,12 +18,14 @@
 
 namespace bns {
 
-constexpr int kLogpThreads = 512, kLogpSmall = 128;     // of a block; the second for short rows
+constexpr int kLogpThreads = 256, kLogpSmall = 128, kLogpLarge = 512;     // of a block
 constexpr int kLogpParts = 8;                           // most blocks a row is split over
 constexpr int kLogpDepth = 8;                           // vectors in flight per thread
 constexpr int kLogpMaxTop = 64;
 constexpr int kLogpSegments = 8;                        // of a thread
 constexpr int kLogpFound = 1024;                        // values that reach the bound, before the slow way is taken
+constexpr int kLogpQueue = 512;                         // segments that reach it, likewise
+constexpr int kLogpLooks = 4;                           // vectors of queued segments in flight per thread
 constexpr float kLogpFloor = -0x1p60f;                  // stands in for anything lower: 2^(floor c - m) = 0, and 0 times it is 0
 static_assert(kLogpParts * kLogpMaxTop <= kLogpFound);
 
@@ -55,12 +57,17 @@ __device__ __forceinline__ void move_reference(Stats& a, float m) {
     a.s *= f;
     a.m = m;
 }
-__device__ __forceinline__ void join_stats(Stats& a, Stats b) {
-    const float m = fmaxf(a.m, b.m);
+// All lanes' sums joined: the maximum first, so that each is scaled once.
+__device__ __forceinline__ void warp_join(Stats& a) {
+    float m = a.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     move_reference(a, m);
-    move_reference(b, m);
-    a.s += b.s;
-    a.t += b.t;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+        a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
+    }
 }
 
 // Whole numbers in the order of the values, both zeros alike; 0 is below -inf.
@@ -124,22 +131,26 @@ struct LogQ {
     }
 };
 
-// Values found and their places, the K first of them in order.
+// A value and its place as one number: the larger value, then the lower place, is the larger number.
+using ranked_t = unsigned long long;
+__device__ __forceinline__ ranked_t ranked(unsigned key, int at) { return static_cast<ranked_t>(key) << 32 | (0xffffffffu - static_cast<unsigned>(at)); }
+__device__ __forceinline__ unsigned key_of(ranked_t r) { return static_cast<unsigned>(r >> 32); }
+__device__ __forceinline__ int place_of(ranked_t r) { return static_cast<int>(0xffffffffu - static_cast<unsigned>(r)); }
+
 struct Found {
-    unsigned key[kLogpFound];
-    int at[kLogpFound];
+    ranked_t value[kLogpFound];
     int count;
 };
 
-// Ranks `count` values by (value, lowest place first); put(rank, key, place) gets those below K.
+// put(rank, value) gets the K largest of `count` different numbers.
 template <typename Put>
-__device__ __forceinline__ void rank_found(const unsigned* key, const int* at, int count, int K, Put&& put) {
+__device__ __forceinline__ void rank_found(const ranked_t* value, int count, int K, Put&& put) {
     for (int i = threadIdx.x; i < count; i += blockDim.x) {
-        const unsigned mine = key[i];
-        const int place = at[i];
+        const ranked_t mine = value[i];
         int rank = 0;
-        for (int j = 0; j < count; ++j) rank += key[j] > mine || (key[j] == mine && at[j] < place);
-        if (rank < K) put(rank, mine, place);
+#pragma unroll 8
+        for (int j = 0; j < count; ++j) rank += value[j] > mine;
+        if (rank < K) put(rank, mine);
     }
 }
 
@@ -185,8 +196,7 @@ __device__ __noinline__ void find_slowly(const typename T::storage* z, int first
         const unsigned k = key_at(v);
         if (k > bound) {
             const int to = atomicAdd(&found.count, 1);
-            found.key[to] = k;
-            found.at[to] = v;
+            found.value[to] = ranked(k, v);
         }
     }
     // of those at the bound the first ones, place by place
@@ -203,10 +213,7 @@ __device__ __noinline__ void find_slowly(const typename T::storage* z, int first
             before += w < warp ? fold[w] : 0;
             all += fold[w];
         }
-        if (here && before < K) {
-            found.key[before] = bound;
-            found.at[before] = v;
-        }
+        if (here && before < K) found.value[before] = ranked(bound, v);
         have = min(K, have + all);
     }
     __syncthreads();
@@ -224,8 +231,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
     __shared__ float sums[kWarps];
     __shared__ float segment[TOP ? kLogpSegments : 1][TOP ? THREADS : 1];
     __shared__ Found found;                           // unused without TOP
-    __shared__ unsigned merged_key[TOP ? kLogpParts * kLogpMaxTop : 1];
-    __shared__ int merged_at[TOP ? kLogpParts * kLogpMaxTop : 1];
+    __shared__ unsigned key_range[2][kWarps];
+    __shared__ int queue[TOP ? kLogpQueue : 1], queued;
+    __shared__ ranked_t merged[TOP ? kLogpParts * kLogpMaxTop : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float inf = __int_as_float(0x7f800000);
     // Another block's shared memory may be written once that block runs: all of the cluster arrive here, and wait for one
@@ -302,15 +310,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
             }
         }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const Stats other{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.t, o)};
-        join_stats(st, other);
-    }
+    warp_join(st);
     if (lane == 0) fold[warp] = st;
     __syncthreads();
-    st = fold[0];
-    for (int w = 1; w < kWarps; ++w) join_stats(st, fold[w]);
+    st = lane < kWarps ? fold[lane] : Stats{-inf, 0.f, 0.f};
+    warp_join(st);
     if (a.parts > 1) {      // every block of the cluster gets every block's sums, and joins them in the same order
         asm volatile("barrier.cluster.wait;" ::: "memory");      // all of them run
         if (tid < a.parts) {
@@ -322,8 +326,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
         }
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        st = of_part[0];
-        for (int p = 1; p < a.parts; ++p) join_stats(st, of_part[p]);
+        st = lane < a.parts ? of_part[lane] : Stats{-inf, 0.f, 0.f};
+        warp_join(st);
     }
 
     const float log_s = log2f(st.s);
@@ -363,88 +367,105 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
     }
 
     if constexpr (TOP) {
-        // the largest bound that K threads' values reach, or a little lower; keys of bf16 values differ in their upper half
+        // The largest bound that K threads' values reach, or a little lower, bit by bit below what all values have in common;
+        // keys of bf16 values differ in their upper half.
         const bool has = loose >= 0 || begin + tid < end;
         const unsigned own_key = has ? order_key(mine) : 0u;
-        unsigned bound = 0;
         constexpr int kLowest = sizeof(S) == 2 ? 16 : 0;
-        int enough = a.K + a.K / 4 + 4;
+        const unsigned warp_most = __reduce_max_sync(0xffffffffu, own_key), warp_least = __reduce_min_sync(0xffffffffu, own_key);
+        if (lane == 0) key_range[0][warp] = warp_most, key_range[1][warp] = warp_least;
+        if (tid == 0) found.count = queued = 0;
+        __syncthreads();
+        const unsigned most = __reduce_max_sync(0xffffffffu, key_range[0][lane % kWarps]);
+        const unsigned least = __reduce_min_sync(0xffffffffu, key_range[1][lane % kWarps]);
+        const int highest = 31 - __clz(most ^ least);          // -1: all the same
+        const unsigned common = highest == 31 ? 0u : most & ~((2u << (highest & 31)) - 1u);
+        unsigned bound = highest < 0 ? most : common;
+        const int enough = a.K + a.K / 4 + 4;
 #pragma unroll 1
-        for (int bit = 31; bit >= kLowest; --bit) {
+        for (int bit = highest; bit >= kLowest; --bit) {
             const unsigned candidate = bound | (1u << bit);
             const int reach = __syncthreads_count(own_key >= candidate);
             if (reach >= a.K) bound = candidate;
             if (reach >= a.K && reach <= enough) break;
         }
-        if (tid == 0) found.count = 0;
-        __syncthreads();
         auto look = [&](float v, int at) {
             const unsigned k = order_key(v);
             if (v == v && k >= bound) {
                 const int to = atomicAdd(&found.count, 1);
-                if (to < kLogpFound) {
-                    found.key[to] = k;
-                    found.at[to] = at;
-                }
+                if (to < kLogpFound) found.value[to] = ranked(k, at);
             }
         };
-        if (own_key >= bound && has) {
+        // segments that reach the bound are queued, and all threads share their vectors
+        if (has && own_key >= bound) {
             if (loose >= 0) look(loose_z, loose);
-#pragma unroll 1
-            for (int v0 = begin + tid, b = 0; v0 < end; v0 += kBatch, ++b) {
-                if (order_key(segment[b / group][tid]) < bound) continue;
-#pragma unroll 1
-                for (int i = 0; i < kLogpDepth; ++i) {
-                    const int v = v0 + i * THREADS;
-                    if (v >= end) break;
-                    Vec<T, V> y;
-                    y.raw = body[v];
-#pragma unroll
-                    for (int j = 0; j < V; ++j) look(y.get(j), head + v * V + j);
+            for (int g = 0; begin + tid + g * group * kBatch < end; ++g)
+                if (order_key(segment[g][tid]) >= bound) {
+                    const int to = atomicAdd(&queued, 1);
+                    if (to < kLogpQueue) queue[to] = tid + g * group * kBatch;
                 }
+        }
+        __syncthreads();
+        const int deep = min(kLogpDepth, (end - begin + THREADS - 1) / THREADS), per_segment = deep * group;
+        const int looks = min(queued, kLogpQueue) * per_segment;
+        for (int w0 = tid; w0 < looks; w0 += THREADS * kLogpLooks) {
+            int at[kLogpLooks];
+#pragma unroll
+            for (int i = 0; i < kLogpLooks; ++i) {
+                const int w = w0 + i * THREADS, s = w / per_segment;
+                at[i] = w < looks ? begin + queue[s] + (w - s * per_segment) * THREADS : end;
+                if (at[i] < end) x[i] = body[at[i]];
+            }
+#pragma unroll
+            for (int i = 0; i < kLogpLooks; ++i) {
+                if (at[i] >= end) continue;
+                Vec<T, V> y;
+                y.raw = x[i];
+                TopOf<T> top;
+                top.add(y.raw);
+                if (order_key(top.get()) < bound) continue;
+#pragma unroll
+                for (int j = 0; j < V; ++j) look(y.get(j), head + at[i] * V + j);
             }
         }
         __syncthreads();
         const int first = part == 0 ? 0 : head + begin * V, last = part == a.parts - 1 ? a.V : head + end * V;
-        if (found.count > kLogpFound) {
+        if (found.count > kLogpFound || queued > kLogpQueue) {
             // the bound itself: the K-th largest of the threads' values
-            unsigned exact = 0;
+            unsigned exact = highest < 0 ? most : common;
 #pragma unroll 1
-            for (int bit = 31; bit >= kLowest; --bit)
+            for (int bit = highest; bit >= kLowest; --bit)
                 if (__syncthreads_count(own_key >= (exact | (1u << bit))) >= a.K) exact |= 1u << bit;
             if (kLowest && exact && !(exact >> 31)) exact |= 0xffffu;      // of values below zero the lower half is ones
             find_slowly<T>(z, first, last, exact, a.K, found, reinterpret_cast<int*>(sums));
         }
         const int count = found.count;
-        auto write = [&](int rank, unsigned key, int at) {
-            a.top[row * a.K + rank] = log_q(of_key(key));
-            a.index[row * a.K + rank] = at;
+        auto write = [&](int rank, ranked_t value) {
+            a.top[row * a.K + rank] = log_q(of_key(key_of(value)));
+            a.index[row * a.K + rank] = place_of(value);
         };
         auto nothing = [&](int rank) {
             a.top[row * a.K + rank] = -inf;
             a.index[row * a.K + rank] = -1;
         };
         if (a.parts == 1) {
-            rank_found(found.key, found.at, count, a.K, write);
+            rank_found(found.value, count, a.K, write);
             for (int k = count + tid; k < a.K; k += THREADS) nothing(k);
         } else {
-            // every part's K first go to the first block, which orders them; places without a value have key 0
-            auto send = [&](int rank, unsigned key, int at) {
-                unsigned to_key, to_at;
-                const int slot = part * a.K + rank;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to_key) : "r"(smem_address(&merged_key[slot])), "r"(0));
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to_at) : "r"(smem_address(&merged_at[slot])), "r"(0));
-                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to_key), "r"(key) : "memory");
-                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to_at), "r"(at) : "memory");
+            // every part's K first go to the first block, which orders them; what is not there has key 0
+            auto send = [&](int rank, ranked_t value) {
+                unsigned to;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_address(&merged[part * a.K + rank])), "r"(0));
+                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(value) : "memory");
             };
-            rank_found(found.key, found.at, count, a.K, send);
-            for (int k = count + tid; k < a.K; k += THREADS) send(k, 0u, 0x7fffffff - k - part * a.K);
+            rank_found(found.value, count, a.K, send);
+            for (int k = count + tid; k < a.K; k += THREADS) send(k, ranked(0u, k + part * a.K));
             asm volatile("barrier.cluster.arrive.release;" ::: "memory");
             asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
             if (part == 0)
-                rank_found(merged_key, merged_at, a.parts * a.K, a.K, [&](int rank, unsigned key, int at) {
-                    if (key)
-                        write(rank, key, at);
+                rank_found(merged, a.parts * a.K, a.K, [&](int rank, ranked_t value) {
+                    if (key_of(value))
+                        write(rank, value);
                     else
                         nothing(rank);
                 });
