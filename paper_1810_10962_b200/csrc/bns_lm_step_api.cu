@@ -87,7 +87,7 @@ HeadPlan plan_heads(const bns_head_norm* sh, const HeadNorm& a) {
     return pl;
 }
 
-HeadNorm head_norm_of(const bns_head_norm* sh, const float* cos, const float* sin, const void* position) {
+HeadNorm problem_of(const bns_head_norm* sh, const float* cos, const float* sin, const void* position) {
     HeadNorm a{};
     a.cos = cos;
     a.sin = sin;
@@ -115,52 +115,77 @@ HeadNorm head_norm_of(const bns_head_norm* sh, const float* cos, const float* si
     return a;
 }
 
-// Blocks of the gradient kernel at the most, each of which leaves a row of sums.
-int head_norm_blocks(const bns_head_norm* sh) { return std::max(sh->q_heads + sh->k_heads, sm_count() * 8); }
+// Blocks of the gradient kernel at the most, each of which leaves a row of sums: what fits the SMs, or one for each chunk of heads.
+constexpr int kHeadBlocks = 4;
+int head_norm_blocks(const bns_head_norm* sh) { return sh->q_heads + sh->k_heads + sm_count() * kHeadBlocks; }
 
-constexpr int kHeadsForward = 4, kHeadsBackward = 2;    // of a lane group, in flight
+// Rounds over the heads that a warp makes at one position.  Many amortise the angles and weights that it fetches first (8192
+// positions of 32 + 8 heads of 128 bf16, forward, up to 4 / 8 / 16 rounds: 35 / 31 / 31 us); few spread a small batch over the SMs
+// (512 positions, aiming at 24 / 32 / 48 warps an SM: 4.2 / 3.9 / 5.2 us).
+constexpr int kHeadWarps = 32, kHeadRounds = 16;
+int head_rounds(const HeadNorm& a, int heads, int slots) {
+    const int64_t all = a.tokens * (divide_up(a.q.heads, slots) + divide_up(a.k.heads, slots));
+    const int64_t rounds = std::min<int64_t>(divide_up<int64_t>(all, kHeadWarps * sm_count()), kHeadRounds);
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(rounds, divide_up(heads, slots))));
+}
 
 // Blocks of a gradient launch that leave sums of the queries' and of the keys' weight.
 struct HeadBlocks {
     int q, k;
 };
 
-template <typename T, int V, bool BACKWARD>
+template <typename T, int V, bool BACKWARD, bool INTERLEAVED>
 HeadBlocks head_norm_of_vectors(HeadNorm a, const HeadPlan& pl, cudaStream_t stream) {
-    constexpr int kWide = 1024 / (64 * V), kHeads = BACKWARD ? kHeadsBackward : kHeadsForward;
-    const int per_chunk = 32 / pl.lanes * (pl.wide ? 1 : kHeads);
-    a.q.chunks = divide_up(a.q.heads, per_chunk);
-    a.k.chunks = divide_up(a.k.heads, per_chunk);
-    const unsigned chunks = static_cast<unsigned>(a.q.chunks + a.k.chunks);
-    unsigned blocks = static_cast<unsigned>(divide_up<int64_t>(a.tokens, kRotaryWarps));
-    if (BACKWARD) blocks = std::min(blocks, std::max(1u, static_cast<unsigned>(sm_count()) * 8 / chunks));
-    const Shape shape{blocks, kRotaryWarps * 32, 1, chunks};
+    // heads in flight: two, but one where the gradient's registers hold no more (bf16 58 us against 60, fp32 93 against 89)
+    constexpr int kWide = 1024 / (64 * V), kDepth = BACKWARD && V == 8 ? 1 : 2;
+    const int slots = 32 / pl.lanes;
+    for (HeadRows* r : {&a.q, &a.k}) {
+        r->rounds = head_rounds(a, r->heads, slots);
+        r->chunks = divide_up(divide_up(r->heads, slots), r->rounds);
+    }
+    const int64_t blocks = divide_up<int64_t>(a.tokens, kRotaryWarps);
+    Shape shape{static_cast<unsigned>(blocks), kRotaryWarps * 32, 1, static_cast<unsigned>(a.q.chunks + a.k.chunks)};
+    if (BACKWARD) {
+        const int all = a.q.rounds * a.q.chunks + a.k.rounds * a.k.chunks;
+        for (HeadRows* r : {&a.q, &a.k})
+            r->blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(blocks, static_cast<int64_t>(sm_count()) * kHeadBlocks * r->rounds / all)));
+        shape = Shape{static_cast<unsigned>(a.q.chunks * a.q.blocks + a.k.chunks * a.k.blocks), kRotaryWarps * 32};
+    }
     if constexpr (BACKWARD) {
         const size_t smem = static_cast<size_t>(kRotaryWarps) * a.D * sizeof(float);
         if (pl.wide)
-            launch(BNS_KERNEL_HEAD_NORM, head_norm_backward_kernel<T, V, kWide, 1>, shape, smem, stream, a, pl.lanes, pl.words);
+            launch(BNS_KERNEL_HEAD_NORM, head_norm_backward_kernel<T, V, kWide, 1, INTERLEAVED>, shape, smem, stream, a, pl.lanes, pl.words);
         else
-            launch(BNS_KERNEL_HEAD_NORM, head_norm_backward_kernel<T, V, 1, kHeads>, shape, smem, stream, a, pl.lanes, pl.words);
+            launch(BNS_KERNEL_HEAD_NORM, head_norm_backward_kernel<T, V, 1, kDepth, INTERLEAVED>, shape, smem, stream, a, pl.lanes, pl.words);
     } else {
         if (pl.wide)
-            launch(BNS_KERNEL_HEAD_NORM, head_norm_forward_kernel<T, V, kWide, 1>, shape, 0, stream, a, pl.lanes, pl.words);
+            launch(BNS_KERNEL_HEAD_NORM, head_norm_forward_kernel<T, V, kWide, 1, INTERLEAVED>, shape, 0, stream, a, pl.lanes, pl.words);
         else
-            launch(BNS_KERNEL_HEAD_NORM, head_norm_forward_kernel<T, V, 1, kHeads>, shape, 0, stream, a, pl.lanes, pl.words);
+            launch(BNS_KERNEL_HEAD_NORM, head_norm_forward_kernel<T, V, 1, kDepth, INTERLEAVED>, shape, 0, stream, a, pl.lanes, pl.words);
     }
-    return HeadBlocks{static_cast<int>(blocks) * a.q.chunks, static_cast<int>(blocks) * a.k.chunks};
+    return HeadBlocks{a.q.chunks * a.q.blocks, a.k.chunks * a.k.blocks};
+}
+
+template <typename T, int V, bool BACKWARD>
+HeadBlocks head_norm_of(const HeadNorm& a, const HeadPlan& pl, cudaStream_t stream) {
+    // a vector of one element holds a pair either way
+    if constexpr (V > 1) {
+        if (!a.interleaved) return head_norm_of_vectors<T, V, BACKWARD, false>(a, pl, stream);
+    }
+    return head_norm_of_vectors<T, V, BACKWARD, true>(a, pl, stream);
 }
 
 template <bool BACKWARD>
 HeadBlocks head_norm(const HeadNorm& a, const HeadPlan& pl, int dtype, cudaStream_t stream) {
     if (dtype == BNS_F32) {
-        if (pl.V == 4) return head_norm_of_vectors<F32, 4, BACKWARD>(a, pl, stream);
-        if (pl.V == 2) return head_norm_of_vectors<F32, 2, BACKWARD>(a, pl, stream);
-        return head_norm_of_vectors<F32, 1, BACKWARD>(a, pl, stream);
+        if (pl.V == 4) return head_norm_of<F32, 4, BACKWARD>(a, pl, stream);
+        if (pl.V == 2) return head_norm_of<F32, 2, BACKWARD>(a, pl, stream);
+        return head_norm_of<F32, 1, BACKWARD>(a, pl, stream);
     }
-    if (pl.V == 8) return head_norm_of_vectors<BF16, 8, BACKWARD>(a, pl, stream);
-    if (pl.V == 4) return head_norm_of_vectors<BF16, 4, BACKWARD>(a, pl, stream);
-    if (pl.V == 2) return head_norm_of_vectors<BF16, 2, BACKWARD>(a, pl, stream);
-    return head_norm_of_vectors<BF16, 1, BACKWARD>(a, pl, stream);
+    if (pl.V == 8) return head_norm_of<BF16, 8, BACKWARD>(a, pl, stream);
+    if (pl.V == 4) return head_norm_of<BF16, 4, BACKWARD>(a, pl, stream);
+    if (pl.V == 2) return head_norm_of<BF16, 2, BACKWARD>(a, pl, stream);
+    return head_norm_of<BF16, 1, BACKWARD>(a, pl, stream);
 }
 
 // ------------------------------------------------------------------------------------ gradients
@@ -355,7 +380,7 @@ bns_status bns_head_norm_rotary_forward(const bns_head_norm* shape, const void* 
     if (!aligned(q, eb) || !aligned(q_out, eb) || !aligned(q_weight, 4) || !aligned(cos, 4) || !aligned(sin, 4) ||
         !aligned(position, shape->position_is_int64 ? 8 : 4) || (keys && (!aligned(k, eb) || !aligned(k_out, eb) || !aligned(k_weight, 4))))
         return BNS_ERR_ALIGN;
-    HeadNorm a = head_norm_of(shape, cos, sin, position);
+    HeadNorm a = problem_of(shape, cos, sin, position);
     a.q.x = q;
     a.q.weight = q_weight;
     a.q.y = q_out;
@@ -394,7 +419,7 @@ bns_status bns_head_norm_rotary_backward(const bns_head_norm* shape, const void*
         (keys && (!aligned(dk_out, eb) || !aligned(k, eb) || !aligned(dk, eb) || !aligned(k_weight, 4))))
         return BNS_ERR_ALIGN;
     if (!workspace_fits(workspace, workspace_bytes, bns_head_norm_rotary_workspace_bytes(shape))) return BNS_ERR_WORKSPACE;
-    HeadNorm a = head_norm_of(shape, cos, sin, position);
+    HeadNorm a = problem_of(shape, cos, sin, position);
     a.q.x = q;
     a.q.dy = dq_out;
     a.q.weight = q_weight;
