@@ -5,8 +5,8 @@
 //
 // Bound by HBM: the norm reads every element once, clipping reads it again (what fits of it out of L2, hence back to front)
 // and writes it.  The list travels in the kernels' arguments, so nothing is copied to the device and a captured graph holds
-// all it needs.  All tensors are taken as one line of 16-byte vectors which the blocks share evenly, whatever the tensors'
-// sizes; elements outside whole vectors go with a place of their own in front of each tensor's vectors.
+// all it needs.  All tensors are taken as one line of 16-byte vectors, whatever their sizes, which the blocks take chunk by
+// chunk; elements outside whole vectors go with a place of their own in front of each tensor's vectors.
 //
 // Squares are added in fp32 over a batch of vectors, batches and everything above in 64 bits.  A batch whose sum leaves the
 // range in which fp32 squares are exact enough is done again in 64 bits.
@@ -17,20 +17,16 @@
 namespace bns {
 
 constexpr int kClipThreads = 256;
-constexpr int kClipDepth = 8;            // vectors in flight per thread
-constexpr int kClipBlocks = 4;           // of a launch, per SM
+constexpr int kClipDepth = 8;             // vectors in flight per thread
+constexpr int kClipBlocks = 3;           // per SM: 80 registers, which clipping needs (four an SM: 3.8 TB/s in fp32 for 6.2)
 
-struct ClipEntry {
-    const void* in;
-    void* out;
-    int64_t elements;                    // times two, plus one for bf16
-    int64_t first;                       // place in the line
-};
 template <int N>
 struct ClipList {
-    ClipEntry entry[N];
-    int64_t places;                      // of the line
-    int count;
+    int64_t first[N + 1];                // places in the line, and its length
+    const void* in[N];
+    void* out[N];
+    int64_t elements[N];                 // times two, plus one for bf16
+    int count, chunk;                    // tensors; places that a block takes at a time
 };
 
 // Where a tensor's whole vectors begin and how many there are.
@@ -52,25 +48,27 @@ struct ClipSpan {
     }
 };
 
-// Calls visit(entry, [begin, end) of its places) for the block's share of the line.
+// Calls visit(tensor, from, to: its places) for the tensors of chunk c of the line.
 template <int N, typename Visit>
-__device__ __forceinline__ void walk_line(const ClipList<N>& list, int block, int blocks, Visit&& visit) {
-    const int64_t begin = list.places / blocks * block + min(static_cast<int64_t>(block), list.places % blocks);
-    const int64_t end = begin + list.places / blocks + (block < list.places % blocks);
-    if (begin >= end) return;
-    int low = 0, high = list.count - 1;              // the last entry that begins at or before `begin`
-    while (low < high) {
-        const int middle = (low + high + 1) / 2;
-        if (list.entry[middle].first <= begin)
+__device__ __forceinline__ void visit_chunk(const ClipList<N>& list, int64_t c, Visit&& visit) {
+    const int64_t begin = c * list.chunk, end = min(begin + list.chunk, list.first[list.count]);
+    int low = 0, high = list.count;                      // the last tensor that begins at or before `begin` is in [low, high)
+    while (high - low > 1) {
+        const int middle = (low + high) / 2;
+        if (list.first[middle] <= begin)
             low = middle;
         else
-            high = middle - 1;
+            high = middle;
     }
-    for (int e = low; e < list.count && list.entry[e].first < end; ++e) {
-        const int64_t first = list.entry[e].first, last = e + 1 < list.count ? list.entry[e + 1].first : list.places;
-        visit(list.entry[e], (begin > first ? begin : first) - first, (end < last ? end : last) - first);
+    int64_t first = list.first[low];
+    for (int e = low; e < list.count && first < end; ++e) {
+        const int64_t last = list.first[e + 1];
+        visit(e, max(begin, first) - first, min(end, last) - first);
+        first = last;
     }
 }
+template <int N>
+__host__ __device__ __forceinline__ int64_t chunks_of(const ClipList<N>& list) { return (list.first[list.count] + list.chunk - 1) / list.chunk; }
 
 template <typename T>
 __device__ __forceinline__ double squares_of(const void* data, int64_t elements, int64_t from, int64_t to) {
@@ -86,14 +84,15 @@ __device__ __forceinline__ double squares_of(const void* data, int64_t elements,
             total = f * f;
         }
     }
-    const uint4* body = reinterpret_cast<const uint4*>(p + span.head);
-    const int64_t end = to - 1;
-    for (int64_t v0 = (from > 0 ? from - 1 : 0) + threadIdx.x; v0 < end; v0 += kClipThreads * kClipDepth) {
+    const int64_t begin = from > 0 ? from - 1 : 0;
+    const uint4* body = reinterpret_cast<const uint4*>(p + span.head) + begin;
+    const int count = static_cast<int>(to - 1 - begin);
+    for (int v0 = threadIdx.x; v0 < count; v0 += kClipThreads * kClipDepth) {
         Vec<T, V> x[kClipDepth];
 #pragma unroll
         for (int i = 0; i < kClipDepth; ++i) {
             x[i].raw = make_uint4(0, 0, 0, 0);
-            if (v0 + i * kClipThreads < end) x[i].raw = body[v0 + i * kClipThreads];
+            if (v0 + i * kClipThreads < count) x[i].raw = body[v0 + i * kClipThreads];
         }
         pair_t sum[2] = {};
 #pragma unroll
@@ -116,8 +115,8 @@ __device__ __forceinline__ double squares_of(const void* data, int64_t elements,
         if (bits & (sizeof(S) == 2 ? 0x7fff7fffu : 0x7fffffffu)) {      // not all zeros
 #pragma unroll 1
             for (int i = 0; i < kClipDepth; ++i) {
-                const int64_t v = v0 + i * kClipThreads;
-                if (v >= end) break;
+                const int v = v0 + i * kClipThreads;
+                if (v >= count) break;
                 const S* f = reinterpret_cast<const S*>(body + v);
 #pragma unroll 1
                 for (int j = 0; j < V; ++j) {
@@ -145,17 +144,20 @@ __device__ __forceinline__ double block_sum(double v, double* fold) {
 }
 
 template <int N>
-__global__ void __launch_bounds__(kClipThreads) clip_squares_kernel(const __grid_constant__ ClipList<N> list, double* partial) {
+__global__ void __launch_bounds__(kClipThreads, kClipBlocks) clip_squares_kernel(const __grid_constant__ ClipList<N> list, double* partial) {
     __shared__ double fold[kClipThreads / 32];
     grid_dependency_wait();
     grid_dependency_launch();
     double total = 0.;
-    walk_line(list, blockIdx.x, gridDim.x, [&](const ClipEntry& e, int64_t from, int64_t to) {
-        if (e.elements & 1)
-            total += squares_of<BF16>(e.in, e.elements >> 1, from, to);
-        else
-            total += squares_of<F32>(e.in, e.elements >> 1, from, to);
-    });
+    const int64_t chunks = chunks_of(list);
+    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x)
+        visit_chunk(list, c, [&](int e, int64_t from, int64_t to) {
+            const int64_t elements = list.elements[e];
+            if (elements & 1)
+                total += squares_of<BF16>(list.in[e], elements >> 1, from, to);
+            else
+                total += squares_of<F32>(list.in[e], elements >> 1, from, to);
+        });
     total = block_sum(total, fold);
     if (threadIdx.x == 0) partial[blockIdx.x] = total;
 }
@@ -190,36 +192,41 @@ __device__ __forceinline__ void scale_span(const void* data, void* out, int64_t 
         const int64_t i = span.loose(threadIdx.x);
         if (i >= 0) o[i] = from_float<T>(to_float<T>(p[i]) * factor);
     }
-    const uint4* body = reinterpret_cast<const uint4*>(p + span.head);
-    S* to_body = o + span.head;
-    const bool words = (reinterpret_cast<uintptr_t>(to_body) & 15) == 0;
+    const int64_t begin = from > 0 ? from - 1 : 0;
+    const uint4* body = reinterpret_cast<const uint4*>(p + span.head) + begin;
+    S* to_body = o + span.head + begin * V;
+    const int count = static_cast<int>(to - 1 - begin);
+    if (reinterpret_cast<uintptr_t>(to_body) & 15) {       // at another phase than the gradient: element by element
+        for (int v = threadIdx.x; v < count; v += kClipThreads) {
+            Vec<T, V> x;
+            x.raw = body[v];
+#pragma unroll
+            for (int j = 0; j < V; ++j) to_body[static_cast<int64_t>(v) * V + j] = from_float<T>(x.get(j) * factor);
+        }
+        return;
+    }
     const pair_t by = make_pair(factor, factor);
-    const int64_t end = to - 1;
-    for (int64_t v0 = (from > 0 ? from - 1 : 0) + threadIdx.x; v0 < end; v0 += kClipThreads * kClipDepth) {
+    for (int v0 = threadIdx.x; v0 < count; v0 += kClipThreads * kClipDepth) {
         Vec<T, V> x[kClipDepth];
 #pragma unroll
         for (int i = 0; i < kClipDepth; ++i)
-            if (v0 + i * kClipThreads < end) x[i].raw = body[v0 + i * kClipThreads];
+            if (v0 + i * kClipThreads < count) x[i].raw = body[v0 + i * kClipThreads];
 #pragma unroll
         for (int i = 0; i < kClipDepth; ++i) {
-            const int64_t v = v0 + i * kClipThreads;
-            if (v >= end) continue;
+            if (v0 + i * kClipThreads >= count) continue;
+            Vec<T, V> y;
 #pragma unroll
-            for (int q = 0; q < V / 2; ++q) set_vec_pair<T, V>(x[i], q, mul2(vec_pair<T, V>(x[i], q), by));
-            if (words) {
-                __stcs(reinterpret_cast<uint4*>(to_body + v * V), x[i].raw);
-            } else {
-                const S* f = reinterpret_cast<const S*>(&x[i].raw);
-#pragma unroll
-                for (int j = 0; j < V; ++j) to_body[v * V + j] = f[j];
-            }
+            for (int q = 0; q < V / 2; ++q) set_vec_pair<T, V>(y, q, mul2(vec_pair<T, V>(x[i], q), by));
+            __stcs(reinterpret_cast<uint4*>(to_body) + v0 + i * kClipThreads, y.raw);
         }
     }
 }
 
-// Every block finds the norm itself.  The last block walks the line's front: what the norm read last is still in L2.
+// A block takes one chunk: blocks that walk down several drift apart, and reads and writes then go all over the memory (3.7 GB
+// of bf16: 4.8 TB/s read + written for 6.5).  Every block finds the norm itself.  The line is taken back to front, since what
+// the norm read last may still be in L2.
 template <int N>
-__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_constant__ ClipList<N> list, const double* partial, int count, float max_norm, float* norm) {
+__global__ void __launch_bounds__(kClipThreads, kClipBlocks) clip_scale_kernel(const __grid_constant__ ClipList<N> list, const double* partial, int count, float max_norm, float* norm) {
     __shared__ double fold[kClipThreads / 32];
     grid_dependency_wait();
     grid_dependency_launch();
@@ -227,12 +234,15 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
     const float rounded = static_cast<float>(exact);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = rounded;
     const float factor = rounded <= max_norm ? 1.f : static_cast<float>(max_norm / exact);
-    walk_line(list, gridDim.x - 1 - blockIdx.x, gridDim.x, [&](const ClipEntry& e, int64_t from, int64_t to) {
-        if (factor == 1.f && e.in == e.out) return;
-        if (e.elements & 1)
-            scale_span<BF16>(e.in, e.out, e.elements >> 1, from, to, factor);
+    visit_chunk(list, gridDim.x - 1 - blockIdx.x, [&](int e, int64_t from, int64_t to) {
+        const void* in = list.in[e];
+        void* out = list.out[e];
+        if (factor == 1.f && in == out) return;
+        const int64_t elements = list.elements[e];
+        if (elements & 1)
+            scale_span<BF16>(in, out, elements >> 1, from, to, factor);
         else
-            scale_span<F32>(e.in, e.out, e.elements >> 1, from, to, factor);
+            scale_span<F32>(in, out, elements >> 1, from, to, factor);
     });
 }
 

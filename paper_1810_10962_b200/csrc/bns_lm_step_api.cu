@@ -216,23 +216,31 @@ int clip_launches(const bns_gradients* list) { return std::max(1, divide_up(list
 template <int N>
 int fill_list(const bns_gradients* list, int begin, bool out, ClipList<N>& to) {
     to.count = 0;
-    to.places = 0;
+    int64_t places = 0;
     int i = begin;
     for (; i < list->count && to.count < N; ++i) {
         if (list->elements[i] == 0) continue;
         const size_t eb = elem_bytes(list->dtype[i]);
         const int64_t n = list->elements[i];
         const int64_t head = std::min<int64_t>(n, static_cast<int64_t>((16 - reinterpret_cast<uintptr_t>(list->data[i]) % 16) % 16 / eb));
-        to.entry[to.count++] = ClipEntry{list->data[i], out ? list->out[i] : nullptr, 2 * n + (list->dtype[i] == BNS_BF16), to.places};
-        to.places += 1 + (n - head) / static_cast<int64_t>(16 / eb);
+        const int k = to.count++;
+        to.first[k] = places;
+        to.in[k] = list->data[i];
+        to.out[k] = out ? list->out[i] : nullptr;
+        to.elements[k] = 2 * n + (list->dtype[i] == BNS_BF16);
+        places += 1 + (n - head) / static_cast<int64_t>(16 / eb);
     }
+    to.first[to.count] = places;
     return i;
 }
 
-// A block for every two vectors a thread, up to what the SMs hold.
-unsigned clip_grid(int64_t places) {
-    return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(clip_blocks(), divide_up<int64_t>(places, 2 * kClipThreads))));
+// Places of a chunk: up to `most`, and such that what the SMs hold of blocks takes the line in whole rounds.
+template <int N>
+void share_out(ClipList<N>& list, int64_t most) {
+    const int64_t each = divide_up<int64_t>(list.first[list.count], clip_blocks()), rounds = std::max<int64_t>(1, divide_up(each, most));
+    list.chunk = static_cast<int>(std::max<int64_t>(1, divide_up(divide_up(each, rounds), int64_t{kClipThreads}))) * kClipThreads;
 }
+constexpr int64_t kSquaresChunk = 8192, kScaleChunk = 4096;    // 128 KB (3.7 GB: 534 us; shares in one piece 578) and 64 KB (6.5 TB/s; 128 KB 6.3)
 
 struct ClipWork {
     double* partial;
@@ -249,21 +257,26 @@ void clip_lists(const bns_gradients* list, const ClipWork& w, cudaStream_t strea
     for (int begin = 0; begin < list->count || begin == 0;) {
         last = begin;
         begin = std::max(1, fill_list(list, begin, w.out, here));
-        const unsigned grid = clip_grid(here.places);
-        launch(BNS_KERNEL_CLIP, clip_squares_kernel<N>, Shape{grid, kClipThreads}, 0, stream, here, w.partial + count);
-        count += static_cast<int>(grid);
+        share_out(here, kSquaresChunk);
+        const int grid = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(clip_blocks(), chunks_of(here))));
+        launch(BNS_KERNEL_CLIP, clip_squares_kernel<N>, Shape{static_cast<unsigned>(grid), kClipThreads}, 0, stream, here, w.partial + count);
+        count += grid;
     }
+    const double* partial = w.partial;
     if (!w.out) {
-        launch(BNS_KERNEL_CLIP, clip_norm_kernel, Shape{1, kClipThreads}, 0, stream, static_cast<const double*>(w.partial), count, w.norm);
+        launch(BNS_KERNEL_CLIP, clip_norm_kernel, Shape{1, kClipThreads}, 0, stream, partial, count, w.norm);
         return;
     }
     // the last list first, which is already at hand: its tensors may still be in L2
-    launch(BNS_KERNEL_CLIP, clip_scale_kernel<N>, Shape{clip_grid(here.places), kClipThreads}, 0, stream, here,
-           static_cast<const double*>(w.partial), count, w.max_norm, w.norm);
+    auto scale = [&](float* norm) {
+        share_out(here, kScaleChunk);
+        launch(BNS_KERNEL_CLIP, clip_scale_kernel<N>, Shape{static_cast<unsigned>(std::max<int64_t>(1, chunks_of(here))), kClipThreads}, 0, stream,
+               here, partial, count, w.max_norm, norm);
+    };
+    scale(w.norm);
     for (int begin = 0; begin < last;) {
         begin = fill_list(list, begin, true, here);
-        launch(BNS_KERNEL_CLIP, clip_scale_kernel<N>, Shape{clip_grid(here.places), kClipThreads}, 0, stream, here,
-               static_cast<const double*>(w.partial), count, w.max_norm, static_cast<float*>(nullptr));
+        scale(nullptr);
     }
 }
 

@@ -515,13 +515,16 @@ class GradientList:
         self._list = _Gradients(n, *(ctypes.addressof(a) for a in self._arrays))
         self._reference = ctypes.byref(self._list)
         self._device = gradients[0].device if n else torch.device("cuda", torch.cuda.current_device())
-        self._need = _load().bns_gradient_norm_workspace_bytes(self._reference)
+        need = _load().bns_gradient_norm_workspace_bytes(self._reference)
+        # new tensors are made like these: half the time of torch.empty
+        self._scratch = torch.empty(need, dtype=torch.uint8, device=self._device)
+        self._norm = torch.empty((), dtype=torch.float32, device=self._device)
 
     def norm(self, workspace=None):
         """bns_gradient_norm: the norm over all elements of all gradients, a float32 scalar on the device."""
         stream = _stream(self._device)
-        workspace = _scratch(workspace, self._need, self._device)
-        norm = torch.empty((), dtype=torch.float32, device=self._device)
+        workspace = torch.empty_like(self._scratch) if workspace is None else _scratch(workspace, 0, self._device)
+        norm = torch.empty_like(self._norm)
         _check(_load().bns_gradient_norm(self._reference, norm.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream),
                "bns_gradient_norm")
         return norm
@@ -532,8 +535,8 @@ class GradientList:
         if self._overlap:
             raise TypeError("outputs overlap one another or another gradient")
         stream = _stream(self._device)
-        workspace = _scratch(workspace, self._need, self._device)
-        norm = torch.empty((), dtype=torch.float32, device=self._device)
+        workspace = torch.empty_like(self._scratch) if workspace is None else _scratch(workspace, 0, self._device)
+        norm = torch.empty_like(self._norm)
         _check(_load().bns_clip_gradients(self._reference, float(max_norm), norm.data_ptr(), workspace.data_ptr(),
                                           workspace.nbytes, stream), "bns_clip_gradients")
         return norm
