@@ -221,6 +221,40 @@ __device__ __noinline__ void find_slowly(const typename T::storage* z, int first
     __syncthreads();
 }
 
+// Largest value of a row and sums over it of 2^d and 2^d d, d = (value - largest) c, by one block; for rows that the fast
+// forms have no exponent for.  A row of -inf alone has sums of 0.
+template <typename T>
+__device__ __noinline__ void sums_of_differences(const typename T::storage* z, int V, float c, float* fold, float& top, float& s, float& t) {
+    using S = typename T::storage;
+    constexpr int kVec = 16 / sizeof(S);
+    auto larger = [](float p, float q) { return fmaxf(p, q); };
+    auto plus = [](float p, float q) { return p + q; };
+    const int head = min(V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(S)));
+    const int vectors = (V - head) / kVec, tail = head + vectors * kVec, tid = threadIdx.x, threads = blockDim.x;
+    const uint4* body = reinterpret_cast<const uint4*>(z + head);
+    const int loose = tid < head ? tid : tid >= 32 && tid - 32 < V - tail ? tail + tid - 32 : -1;
+    TopOf<T> mine;
+#pragma unroll 4
+    for (int v = tid; v < vectors; v += threads) mine.add(body[v]);
+    top = block_of(fmaxf(mine.get(), loose >= 0 ? to_float<T>(z[loose]) : -__builtin_huge_valf()), fold, larger);
+    s = t = 0.f;
+    auto add = [&](float value) {
+        const float d = (value - top) * c, e = exp2_fast(d);
+        s += e;
+        if (e != 0.f) t = fmaf(e, d, t);
+    };
+    if (loose >= 0) add(to_float<T>(z[loose]));
+#pragma unroll 2
+    for (int v = tid; v < vectors; v += threads) {
+        Vec<T, kVec> x;
+        x.raw = body[v];
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) add(x.get(j));
+    }
+    s = block_of(s, fold, plus);
+    t = block_of(t, fold, plus);
+}
+
 // Part blockIdx % parts of row blockIdx / parts: `per` vectors, and the loose elements at either end of the row.
 template <typename T, bool TOP, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(const LogProbs a) {
@@ -336,21 +370,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
     if (!(fabsf(st.m) <= kNear)) {
         // The largest value times c is too large for the fast form (a row masked with -1e10 or the type's lowest value
         // throughout, say): everything of differences.  Every block looks at the whole row.
-        auto larger = [](float p, float q) { return fmaxf(p, q); };
-        auto plus = [](float p, float q) { return p + q; };
-        float top = -inf, s = 0.f, t = 0.f;
-#pragma unroll 1
-        for (int v = tid; v < a.V; v += THREADS) top = fmaxf(top, to_float<T>(z[v]));
-        top = block_of(top, sums, larger);
+        float top, s, t;
+        sums_of_differences<T>(z, a.V, a.c, sums, top, s, t);
         if (top != -inf || st.s != st.s) {
-#pragma unroll 1
-            for (int v = tid; v < a.V; v += THREADS) {
-                const float d = (to_float<T>(z[v]) - top) * a.c, e = exp2_fast(d);
-                s += e;
-                if (e != 0.f) t = fmaf(e, d, t);
-            }
-            s = block_of(s, sums, plus);
-            t = block_of(t, sums, plus);
             log_q = LogQ{a.tau, a.c, 0.f, log2f(s), top, 0.f, true};
             lse = top / a.tau + log_q.log_s * kLn2;
             entropy = (log_q.log_s - t / s) * kLn2;
@@ -514,16 +536,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(
     const bool empty = lse == -inf, far = !empty && !(fabsf(lse) <= kLogpKept<T>);
     float base = 0.f, log_s = 0.f;
     if (far) {                       // the log-sum's rounding is too much for q: both parts of it once more, of differences
-        auto larger = [](float p, float q) { return fmaxf(p, q); };
-        auto plus = [](float p, float q) { return p + q; };
-        float s = 0.f;
-        base = -inf;
-#pragma unroll 1
-        for (int v = tid; v < a.V; v += THREADS) base = fmaxf(base, to_float<T>(z[v]));
-        base = block_of(base, fold, larger);
-#pragma unroll 1
-        for (int v = tid; v < a.V; v += THREADS) s += exp2_fast((to_float<T>(z[v]) - base) * a.c);
-        log_s = log2f(block_of(s, fold, plus));
+        float s, t;
+        sums_of_differences<T>(z, a.V, a.c, fold, base, s, t);
+        log_s = log2f(s);
     }
     auto value = [&](float v) {
         if (empty) return 0.f;

@@ -416,9 +416,9 @@ def _head_norm_inputs(q, k, q_weight, k_weight, cos, sin, position, eps, interle
         raise TypeError("cos must be [positions, rotary / 2]")
     positions, half = cos.shape
     at, wide = _indices(position, q.shape[:-2], "position", device)
-    shape = _shape(_HeadNorm, batch, length, heads, k_heads, dim, 2 * half, _code(q), *strides, *k_strides, positions, wide,
-                   1 if interleaved else 0, float(eps))[1]
-    return shape, (q.data_ptr(), k_at, _vector(q_weight, dim, "q_weight", device), k_weight_at,
+    fields, shape = _shape(_HeadNorm, batch, length, heads, k_heads, dim, 2 * half, _code(q), *strides, *k_strides, positions,
+                           wide, 1 if interleaved else 0, float(eps))
+    return fields, shape, (q.data_ptr(), k_at, _vector(q_weight, dim, "q_weight", device), k_weight_at,
                    _vector(cos, positions * half, "cos", device), _vector(sin, positions * half, "sin", device), at)
 
 
@@ -427,7 +427,7 @@ def head_norm_rotary_forward(q, k, q_weight, k_weight, cos, sin, position, eps, 
     head_dim], their heads dense, anything else strided (views of a packed projection); k and k_weight may be None.  cos
     and sin are float32 [positions, rotary / 2], position int32 or int64 in the shape of q's leading dimensions; a negative
     one is padding, whose outputs are zeros."""
-    shape, arguments = _head_norm_inputs(q, k, q_weight, k_weight, cos, sin, position, eps, interleaved)
+    _, shape, arguments = _head_norm_inputs(q, k, q_weight, k_weight, cos, sin, position, eps, interleaved)
     q_out = _dense_like(q)
     k_out = None if k is None else _dense_like(k)
     _check(_load().bns_head_norm_rotary_forward(shape, *arguments, q_out.data_ptr(), None if k is None else k_out.data_ptr(),
@@ -435,22 +435,29 @@ def head_norm_rotary_forward(q, k, q_weight, k_weight, cos, sin, position, eps, 
     return q_out, k_out
 
 
+def _match(d, t, name: str) -> None:
+    if (not isinstance(d, torch.Tensor) or d.shape != t.shape or d.dtype != t.dtype or d.device != t.device
+            or not d.is_contiguous()):
+        raise TypeError(f"{name} must be contiguous and match its input in shape, dtype and device")
+
+
 def head_norm_rotary_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, position, eps, interleaved=False,
                               workspace=None):
     """bns_head_norm_rotary_backward: returns (dq, dk, dq_weight, dk_weight) from the contiguous gradients of the outputs and
     the inputs of the forward call."""
-    shape, arguments = _head_norm_inputs(q, k, q_weight, k_weight, cos, sin, position, eps, interleaved)
+    fields, shape, arguments = _head_norm_inputs(q, k, q_weight, k_weight, cos, sin, position, eps, interleaved)
     device, lib = q.device, _load()
-    for d, t, name in ((dq_out, q, "dq_out"), (dk_out, k, "dk_out")):
-        if t is not None and (not isinstance(d, torch.Tensor) or d.shape != t.shape or d.dtype != t.dtype or d.device != device
-                              or not d.is_contiguous()):
-            raise TypeError(f"{name} must be contiguous and match its input in shape, dtype and device")
+    _match(dq_out, q, "dq_out")
     dq, dq_weight = _dense_like(q), torch.empty_like(q_weight)
     dk = dk_weight = dk_at = dk_out_at = dk_weight_at = None
     if k is not None:
+        _match(dk_out, k, "dk_out")
         dk, dk_weight = _dense_like(k), torch.empty_like(k_weight)
         dk_at, dk_out_at, dk_weight_at = dk.data_ptr(), dk_out.data_ptr(), dk_weight.data_ptr()
-    workspace = _scratch(workspace, lib.bns_head_norm_rotary_workspace_bytes(shape), device)
+    need = getattr(fields, "workspace_bytes", None)
+    if need is None:
+        need = fields.workspace_bytes = lib.bns_head_norm_rotary_workspace_bytes(shape)
+    workspace = _scratch(workspace, need, device)
     _check(lib.bns_head_norm_rotary_backward(shape, dq_out.data_ptr(), dk_out_at, *arguments, dq.data_ptr(), dk_at,
                                              dq_weight.data_ptr(), dk_weight_at, workspace.data_ptr(), workspace.nbytes,
                                              _stream(device)), "bns_head_norm_rotary_backward")
