@@ -39,7 +39,7 @@ LogProbs log_probs_of(const bns_token_log_probs* sh, const void* logits, const v
 template <typename T, int THREADS>
 void logp_forward(const LogProbs& a, Shape shape, cudaStream_t stream) {
     if (a.K)
-        launch(BNS_KERNEL_LOGP, logp_forward_kernel<T, true, THREADS>, shape, 0, stream, a);
+        launch(BNS_KERNEL_LOGP, logp_forward_kernel<T, true, THREADS>, shape, sizeof(TopShared<THREADS>), stream, a);
     else
         launch(BNS_KERNEL_LOGP, logp_forward_kernel<T, false, THREADS>, shape, 0, stream, a);
 }

@@ -154,56 +154,56 @@ __device__ __forceinline__ void rank_found(const ranked_t* value, int count, int
     }
 }
 
-// The slow way, for rows where more values reach the bound than there is room for: equal logits all over a row, most of
-// the vocabulary masked with one value, or the top ones next to one another.  [first, last) are the part's places.
-// Leaves at most kLogpFound values, the K largest among them, the same set in every run.
+// Whole numbers of the values, NaN below all of them.
 template <typename T>
-__device__ __noinline__ void find_slowly(const typename T::storage* z, int first, int last, unsigned bound, int K, Found& found, int* fold) {
-    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
-    auto key_at = [&](int v) {
-        const float x = to_float<T>(z[v]);
-        return x == x ? order_key(x) : 0u;
-    };
-    auto above = [&](unsigned limit) {     // how many values lie above it
+__device__ __forceinline__ unsigned key_at(const typename T::storage* z, int v) {
+    const float x = to_float<T>(z[v]);
+    return x == x ? order_key(x) : 0u;
+}
+
+// The K-th largest number of the places [first, last) itself, for parts where more than kLogpFound values lie above `bound`, K
+// of them or more: by halving, a walk over the part each time.  `found` gets the fewer than K numbers above it.
+template <typename T>
+__device__ __noinline__ unsigned find_bound(const typename T::storage* z, int first, int last, unsigned bound, int K, Found& found) {
+    const int tid = threadIdx.x, threads = blockDim.x;
+    auto reached = [&](unsigned key) {      // how many values reach it
         __syncthreads();
         if (tid == 0) found.count = 0;
         __syncthreads();
         int n = 0;
-        for (int v = first + tid; v < last; v += threads) n += key_at(v) > limit;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        if (lane == 0 && n) atomicAdd(&found.count, n);
+        for (int v = first + tid; v < last; v += threads) n += key_at<T>(z, v) >= key;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if ((tid & 31) == 0 && n) atomicAdd(&found.count, n);
         __syncthreads();
         return found.count;
     };
-    int more = above(bound);
-    if (more >= K && more > kLogpFound) {  // the K-th largest itself: the largest key that K values reach
-        unsigned low = bound + 1, high = 0xffffffffu;
-        while (low < high) {
-            const unsigned middle = high - (high - low) / 2;
-            if (above(middle - 1) >= K)
-                low = middle;
-            else
-                high = middle - 1;
-        }
-        bound = low;
-        more = above(bound);               // fewer than K
+    unsigned low = bound + 1, high = 0xffffffffu;
+    while (low < high) {
+        const unsigned middle = high - (high - low) / 2;
+        if (reached(middle) >= K)
+            low = middle;
+        else
+            high = middle - 1;
     }
     __syncthreads();
     if (tid == 0) found.count = 0;
     __syncthreads();
     for (int v = first + tid; v < last; v += threads) {
-        const unsigned k = key_at(v);
-        if (k > bound) {
-            const int to = atomicAdd(&found.count, 1);
-            found.value[to] = ranked(k, v);
-        }
+        const unsigned k = key_at<T>(z, v);
+        if (k > low) found.value[atomicAdd(&found.count, 1)] = ranked(k, v);
     }
-    // of those at the bound the first ones, place by place
-    int have = more;
+    __syncthreads();
+    return low;
+}
+
+// Adds to `found`, up to K, the first places of [first, last) whose value is at the bound.
+template <typename T>
+__device__ __noinline__ void find_equals(const typename T::storage* z, int first, int last, unsigned bound, int K, Found& found, int* fold) {
+    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
+    int have = found.count;
     for (int v0 = first; v0 < last && have < K; v0 += threads) {
         const int v = v0 + tid;
-        const bool here = bound != 0 && v < last && key_at(v) == bound;
+        const bool here = v < last && key_at<T>(z, v) == bound;
         const unsigned votes = __ballot_sync(0xffffffffu, here);
         __syncthreads();
         if (lane == 0) fold[warp] = __popc(votes);
@@ -217,7 +217,7 @@ __device__ __noinline__ void find_slowly(const typename T::storage* z, int first
         have = min(K, have + all);
     }
     __syncthreads();
-    if (tid == 0) found.count = max(have, more);
+    if (tid == 0) found.count = have;
     __syncthreads();
 }
 
@@ -255,19 +255,188 @@ __device__ __noinline__ void sums_of_differences(const typename T::storage* z, i
     t = block_of(t, fold, plus);
 }
 
+// What a block has in shared memory for the alternatives.
+template <int THREADS>
+struct TopShared {
+    float segment[kLogpSegments][THREADS];                  // each thread's largest values
+    Found found;
+    ranked_t merged[kLogpParts * kLogpMaxTop];              // first block: every part's first ones
+    unsigned key_range[2][THREADS / 32];
+    int queue[kLogpQueue], queued;
+    int fold[THREADS / 32];
+};
+template <int THREADS>
+__device__ __forceinline__ TopShared<THREADS>& top_shared() {
+    extern __shared__ __align__(16) char dynamic[];
+    return *reinterpret_cast<TopShared<THREADS>*>(dynamic);
+}
+
+// A row's place in memory: elements in front of whole vectors, the part's vectors, the thread's element outside them or -1.  Those
+// before the vectors belong to the first part, those after them to the last.
+template <typename T>
+struct RowPart {
+    int head, begin, end, loose;
+    __device__ __forceinline__ RowPart(const void* z, const LogProbs& a, int part) {
+        using S = typename T::storage;
+        constexpr int V = 16 / sizeof(S);
+        const int tid = threadIdx.x;
+        head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(S)));
+        const int vectors = (a.V - head) / V;
+        const int tail = head + vectors * V;
+        begin = min(vectors, part * a.per);
+        end = min(vectors, begin + a.per);
+        loose = part == 0 && tid < head ? tid : part == a.parts - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
+    }
+};
+// Batches of vectors that make up a segment, so that a thread has kLogpSegments at the most.
+template <int THREADS>
+__device__ __forceinline__ int segment_batches(const LogProbs& a) {
+    constexpr int kBatch = THREADS * kLogpDepth;
+    return ((a.per + kBatch - 1) / kBatch + kLogpSegments - 1) / kLogpSegments;
+}
+
+// The K largest values of a row and their places.  `loose_z` and `mine` are the thread's element outside vectors and its largest
+// one; everything else is found again, so that the pass over the row has its registers.
+template <typename T, int THREADS>
+__device__ __forceinline__ void alternatives(const LogProbs& a, int64_t row, int part, float loose_z, float mine, LogQ log_q) {
+    using S = typename T::storage;
+    constexpr int V = 16 / sizeof(S), kWarps = THREADS / 32, kBatch = THREADS * kLogpDepth;
+    TopShared<THREADS>& sh = top_shared<THREADS>();
+    Found& found = sh.found;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const float inf = __int_as_float(0x7f800000);
+    const S* z = static_cast<const S*>(a.z) + row * a.z_stride;
+    const RowPart<T> at_row(z, a, part);
+    const int head = at_row.head, begin = at_row.begin, end = at_row.end, loose = at_row.loose, group = segment_batches<THREADS>(a);
+    const uint4* body = reinterpret_cast<const uint4*>(z + head);
+    // The largest bound that K threads' values reach, or a little lower, bit by bit below what all values have in common;
+    // keys of bf16 values differ in their upper half.
+    const bool has = loose >= 0 || begin + tid < end;
+    const unsigned own_key = has ? order_key(mine) : 0u;
+    constexpr int kLowest = sizeof(S) == 2 ? 16 : 0;
+    const unsigned warp_most = __reduce_max_sync(0xffffffffu, own_key), warp_least = __reduce_min_sync(0xffffffffu, own_key);
+    if (lane == 0) sh.key_range[0][warp] = warp_most, sh.key_range[1][warp] = warp_least;
+    if (tid == 0) found.count = sh.queued = 0;
+    __syncthreads();
+    const unsigned most = __reduce_max_sync(0xffffffffu, sh.key_range[0][lane % kWarps]);
+    const unsigned least = __reduce_min_sync(0xffffffffu, sh.key_range[1][lane % kWarps]);
+    const int highest = 31 - __clz(most ^ least);          // -1: all the same
+    const unsigned common = highest == 31 ? 0u : most & ~((2u << (highest & 31)) - 1u);
+    unsigned bound = highest < 0 ? most : common;
+    const int enough = a.K + a.K / 4 + 4;
+#pragma unroll 1
+    for (int bit = highest; bit >= kLowest; --bit) {
+        const unsigned candidate = bound | (1u << bit);
+        const int reach = __syncthreads_count(own_key >= candidate);
+        if (reach >= a.K) bound = candidate;
+        if (reach >= a.K && reach <= enough) break;
+    }
+    const int first = part == 0 ? 0 : head + begin * V, last = part == a.parts - 1 ? a.V : head + end * V;
+    const int deep = min(kLogpDepth, (end - begin + THREADS - 1) / THREADS), per_segment = deep * group;
+    auto look = [&](float v, int at) {
+        const unsigned k = order_key(v);
+        if (v == v && k >= bound) {
+            const int to = atomicAdd(&found.count, 1);
+            if (to < kLogpFound) found.value[to] = ranked(k, at);
+        }
+    };
+    // Once as a rule.  Where there is no room for all that reach the bound (equal logits all over a row, a vocabulary masked
+    // with one value but for a few places) the exact bound is taken, values above it are looked for in the same way, and
+    // those at it place by place.
+#pragma unroll 1
+    for (bool exactly = false;; exactly = true) {
+        // segments that reach the bound are queued, and all threads share their vectors
+        if (has && own_key >= bound) {
+            if (loose >= 0) look(loose_z, loose);
+            for (int g = 0; begin + tid + g * group * kBatch < end; ++g)
+                if (order_key(sh.segment[g][tid]) >= bound) {
+                    const int to = atomicAdd(&sh.queued, 1);
+                    if (to < kLogpQueue) sh.queue[to] = tid + g * group * kBatch;
+                }
+        }
+        __syncthreads();
+        const int looks = sh.queued > kLogpQueue ? 0 : sh.queued * per_segment;
+        for (int w0 = tid; w0 < looks; w0 += THREADS * kLogpLooks) {
+            int at[kLogpLooks];
+            uint4 x[kLogpLooks];
+#pragma unroll
+            for (int i = 0; i < kLogpLooks; ++i) {
+                const int w = w0 + i * THREADS, s = w / per_segment;
+                at[i] = w < looks ? begin + sh.queue[s] + (w - s * per_segment) * THREADS : end;
+                if (at[i] < end) x[i] = body[at[i]];
+            }
+#pragma unroll
+            for (int i = 0; i < kLogpLooks; ++i) {
+                if (at[i] >= end) continue;
+                Vec<T, V> y;
+                y.raw = x[i];
+                TopOf<T> top;
+                top.add(y.raw);
+                if (order_key(top.get()) < bound) continue;
+#pragma unroll
+                for (int j = 0; j < V; ++j) look(y.get(j), head + at[i] * V + j);
+            }
+        }
+        __syncthreads();
+        const bool room = found.count <= kLogpFound && sh.queued <= kLogpQueue;
+        if (room && !exactly) break;
+        if (exactly) {
+            --bound;             // what lies above it has been looked for
+            if (!room) bound = find_bound<T>(z, first, last, bound, a.K, found);
+            if (bound && found.count < a.K) find_equals<T>(z, first, last, bound, a.K, found, sh.fold);
+            break;
+        }
+        bound = highest < 0 ? most : common;
+#pragma unroll 1
+        for (int bit = highest; bit >= kLowest; --bit)
+            if (__syncthreads_count(own_key >= (bound | (1u << bit))) >= a.K) bound |= 1u << bit;
+        if (kLowest && bound && !(bound >> 31)) bound |= 0xffffu;      // of values below zero the lower half is ones
+        ++bound;
+        __syncthreads();
+        if (tid == 0) found.count = sh.queued = 0;
+        __syncthreads();
+    }
+    const int count = found.count;
+    auto write = [&](int rank, ranked_t value) {
+        a.top[row * a.K + rank] = log_q(of_key(key_of(value)));
+        a.index[row * a.K + rank] = place_of(value);
+    };
+    auto nothing = [&](int rank) {
+        a.top[row * a.K + rank] = -inf;
+        a.index[row * a.K + rank] = -1;
+    };
+    if (a.parts == 1) {
+        rank_found(found.value, count, a.K, write);
+        for (int k = count + tid; k < a.K; k += THREADS) nothing(k);
+    } else {
+        // every part's K first go to the first block, which orders them; what is not there has key 0
+        auto send = [&](int rank, ranked_t value) {
+            unsigned to;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_address(&sh.merged[part * a.K + rank])), "r"(0));
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(value) : "memory");
+        };
+        rank_found(found.value, count, a.K, send);
+        for (int k = count + tid; k < a.K; k += THREADS) send(k, ranked(0u, k + part * a.K));
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        if (part == 0)
+            rank_found(sh.merged, a.parts * a.K, a.K, [&](int rank, ranked_t value) {
+                if (key_of(value))
+                    write(rank, value);
+                else
+                    nothing(rank);
+            });
+    }
+}
+
 // Part blockIdx % parts of row blockIdx / parts: `per` vectors, and the loose elements at either end of the row.
 template <typename T, bool TOP, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(const LogProbs a) {
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(const __grid_constant__ LogProbs a) {
     using S = typename T::storage;
-    constexpr int V = 16 / sizeof(S), kWarps = THREADS / 32;
+    constexpr int kWarps = THREADS / 32;
     __shared__ Stats fold[kWarps];
     __shared__ Stats of_part[kLogpParts];
     __shared__ float sums[kWarps];
-    __shared__ float segment[TOP ? kLogpSegments : 1][TOP ? THREADS : 1];
-    __shared__ Found found;                           // unused without TOP
-    __shared__ unsigned key_range[2][kWarps];
-    __shared__ int queue[TOP ? kLogpQueue : 1], queued;
-    __shared__ ranked_t merged[TOP ? kLogpParts * kLogpMaxTop : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float inf = __int_as_float(0x7f800000);
     // Another block's shared memory may be written once that block runs: all of the cluster arrive here, and wait for one
@@ -280,11 +449,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
     const S* z = static_cast<const S*>(a.z) + row * a.z_stride;
     int64_t token = -1;
     if (tid == 0 && part == 0) token = a.token64 ? static_cast<const long long*>(a.token)[row] : static_cast<const int*>(a.token)[row];
-    const int head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(S)));
-    const int vectors = (a.V - head) / V, tail = head + vectors * V;
-    const int begin = min(vectors, part * a.per), end = min(vectors, begin + a.per);
-    // elements outside whole vectors: those before them belong to the first part, those after them to the last
-    const int loose = part == 0 && tid < head ? tid : part == a.parts - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
+    const RowPart<T> at_row(z, a, part);
+    const int head = at_row.head, begin = at_row.begin, end = at_row.end, loose = at_row.loose;
     const float loose_z = loose >= 0 ? to_float<T>(z[loose]) : -inf;
     const uint4* body = reinterpret_cast<const uint4*>(z + head);
     uint4 x[kLogpDepth];
@@ -306,9 +472,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
         else
             st = Stats{m == m ? m : -inf, m == m ? 0.f : m, 0.f};
     }
-    // batches of a segment, so that there are kLogpSegments at the most
     constexpr int kBatch = THREADS * kLogpDepth;
-    const int batches = (a.per + kBatch - 1) / kBatch, group = (batches + kLogpSegments - 1) / kLogpSegments;
+    const int group = segment_batches<THREADS>(a);
     float mine = loose_z == loose_z ? loose_z : -inf;   // the thread's largest
     float of_segment = -inf;
     int batch = 0;
@@ -339,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
             of_segment = fmaxf(of_segment, largest);
             mine = fmaxf(mine, largest);
             if (++batch % group == 0 || v0 + kBatch >= end) {
-                segment[(batch - 1) / group][tid] = of_segment;
+                top_shared<THREADS>().segment[(batch - 1) / group][tid] = of_segment;
                 of_segment = -inf;
             }
         }
@@ -388,111 +553,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
         if (a.entropy) a.entropy[row] = entropy;
     }
 
-    if constexpr (TOP) {
-        // The largest bound that K threads' values reach, or a little lower, bit by bit below what all values have in common;
-        // keys of bf16 values differ in their upper half.
-        const bool has = loose >= 0 || begin + tid < end;
-        const unsigned own_key = has ? order_key(mine) : 0u;
-        constexpr int kLowest = sizeof(S) == 2 ? 16 : 0;
-        const unsigned warp_most = __reduce_max_sync(0xffffffffu, own_key), warp_least = __reduce_min_sync(0xffffffffu, own_key);
-        if (lane == 0) key_range[0][warp] = warp_most, key_range[1][warp] = warp_least;
-        if (tid == 0) found.count = queued = 0;
-        __syncthreads();
-        const unsigned most = __reduce_max_sync(0xffffffffu, key_range[0][lane % kWarps]);
-        const unsigned least = __reduce_min_sync(0xffffffffu, key_range[1][lane % kWarps]);
-        const int highest = 31 - __clz(most ^ least);          // -1: all the same
-        const unsigned common = highest == 31 ? 0u : most & ~((2u << (highest & 31)) - 1u);
-        unsigned bound = highest < 0 ? most : common;
-        const int enough = a.K + a.K / 4 + 4;
-#pragma unroll 1
-        for (int bit = highest; bit >= kLowest; --bit) {
-            const unsigned candidate = bound | (1u << bit);
-            const int reach = __syncthreads_count(own_key >= candidate);
-            if (reach >= a.K) bound = candidate;
-            if (reach >= a.K && reach <= enough) break;
-        }
-        auto look = [&](float v, int at) {
-            const unsigned k = order_key(v);
-            if (v == v && k >= bound) {
-                const int to = atomicAdd(&found.count, 1);
-                if (to < kLogpFound) found.value[to] = ranked(k, at);
-            }
-        };
-        // segments that reach the bound are queued, and all threads share their vectors
-        if (has && own_key >= bound) {
-            if (loose >= 0) look(loose_z, loose);
-            for (int g = 0; begin + tid + g * group * kBatch < end; ++g)
-                if (order_key(segment[g][tid]) >= bound) {
-                    const int to = atomicAdd(&queued, 1);
-                    if (to < kLogpQueue) queue[to] = tid + g * group * kBatch;
-                }
-        }
-        __syncthreads();
-        const int deep = min(kLogpDepth, (end - begin + THREADS - 1) / THREADS), per_segment = deep * group;
-        const int looks = min(queued, kLogpQueue) * per_segment;
-        for (int w0 = tid; w0 < looks; w0 += THREADS * kLogpLooks) {
-            int at[kLogpLooks];
-#pragma unroll
-            for (int i = 0; i < kLogpLooks; ++i) {
-                const int w = w0 + i * THREADS, s = w / per_segment;
-                at[i] = w < looks ? begin + queue[s] + (w - s * per_segment) * THREADS : end;
-                if (at[i] < end) x[i] = body[at[i]];
-            }
-#pragma unroll
-            for (int i = 0; i < kLogpLooks; ++i) {
-                if (at[i] >= end) continue;
-                Vec<T, V> y;
-                y.raw = x[i];
-                TopOf<T> top;
-                top.add(y.raw);
-                if (order_key(top.get()) < bound) continue;
-#pragma unroll
-                for (int j = 0; j < V; ++j) look(y.get(j), head + at[i] * V + j);
-            }
-        }
-        __syncthreads();
-        const int first = part == 0 ? 0 : head + begin * V, last = part == a.parts - 1 ? a.V : head + end * V;
-        if (found.count > kLogpFound || queued > kLogpQueue) {
-            // the bound itself: the K-th largest of the threads' values
-            unsigned exact = highest < 0 ? most : common;
-#pragma unroll 1
-            for (int bit = highest; bit >= kLowest; --bit)
-                if (__syncthreads_count(own_key >= (exact | (1u << bit))) >= a.K) exact |= 1u << bit;
-            if (kLowest && exact && !(exact >> 31)) exact |= 0xffffu;      // of values below zero the lower half is ones
-            find_slowly<T>(z, first, last, exact, a.K, found, reinterpret_cast<int*>(sums));
-        }
-        const int count = found.count;
-        auto write = [&](int rank, ranked_t value) {
-            a.top[row * a.K + rank] = log_q(of_key(key_of(value)));
-            a.index[row * a.K + rank] = place_of(value);
-        };
-        auto nothing = [&](int rank) {
-            a.top[row * a.K + rank] = -inf;
-            a.index[row * a.K + rank] = -1;
-        };
-        if (a.parts == 1) {
-            rank_found(found.value, count, a.K, write);
-            for (int k = count + tid; k < a.K; k += THREADS) nothing(k);
-        } else {
-            // every part's K first go to the first block, which orders them; what is not there has key 0
-            auto send = [&](int rank, ranked_t value) {
-                unsigned to;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_address(&merged[part * a.K + rank])), "r"(0));
-                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(value) : "memory");
-            };
-            rank_found(found.value, count, a.K, send);
-            for (int k = count + tid; k < a.K; k += THREADS) send(k, ranked(0u, k + part * a.K));
-            asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-            asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-            if (part == 0)
-                rank_found(merged, a.parts * a.K, a.K, [&](int rank, ranked_t value) {
-                    if (key_of(value))
-                        write(rank, value);
-                    else
-                        nothing(rank);
-                });
-        }
-    }
+    if constexpr (TOP) alternatives<T, THREADS>(a, row, part, loose_z, mine, log_q);
 }
 
 // The gradient: q_v = 2^(z_v c - m) / rest from the forward call's log-sum, so every element by itself:
@@ -511,10 +572,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(
     const int part = blockIdx.x - static_cast<int>(block) * a.parts;
     const S* z = static_cast<const S*>(a.z) + row * a.z_stride;
     S* dz = static_cast<S*>(a.dz) + row * a.dz_stride;
-    const int head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(S)));
-    const int vectors = (a.V - head) / V, tail = head + vectors * V;
-    const int begin = min(vectors, part * a.per), end = min(vectors, begin + a.per);
-    const int loose = part == 0 && tid < head ? tid : part == a.parts - 1 && tid >= 32 && tid - 32 < a.V - tail ? tail + tid - 32 : -1;
+    const RowPart<T> at_row(z, a, part);
+    const int head = at_row.head, begin = at_row.begin, end = at_row.end, loose = at_row.loose;
     const float loose_z = loose >= 0 ? to_float<T>(z[loose]) : 0.f;
     const uint4* body = reinterpret_cast<const uint4*>(z + head);
     uint4 x[kLogpDepth];
