@@ -592,12 +592,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(
     const float m = static_cast<float>(exponent), rest = static_cast<float>(exponent - m);
     // log q = ln 2 (u - rest)
     const float scale = exp2_fast(-rest), k0 = -(g + h * (entropy - rest * kLn2)) * scale, k1 = -h * kLn2 * scale;
-    const bool empty = lse == -inf, far = !empty && !(fabsf(lse) <= kLogpKept<T>);
+    const bool far = !(fabsf(lse) <= kLogpKept<T>);
+    bool empty = false;
     float base = 0.f, log_s = 0.f;
     if (far) {                       // the log-sum's rounding is too much for q: both parts of it once more, of differences
         float s, t;
         sums_of_differences<T>(z, a.V, a.c, fold, base, s, t);
         log_s = log2f(s);
+        empty = lse == -inf && base == -inf;       // a log-sum of -inf may also be one that has left fp32's range
     }
     auto value = [&](float v) {
         if (empty) return 0.f;
@@ -618,7 +620,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(
             const int v = v0 + i * THREADS;
             if (v >= end) continue;
             Vec<T, V> o;
-            if (!far && !empty) {
+            if (!far) {
                 raise_to_floor<T>(x[i]);
                 Vec<T, V> y;
                 y.raw = x[i];

@@ -152,6 +152,24 @@ def test_masked_vocabulary(T, V, dtype):
     check(z.masked_fill(~keep, torch.finfo(dtype).min), token, dlogp, dentropy, 0.5, 20)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_at_the_types_lowest_value(dtype):
+    """At a temperature below 1 the log-sum leaves fp32's range; the probabilities are all the same, and so is the gradient."""
+    from paper_1810_10962_b200 import lm
+    z = torch.full((2, 4000), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+    token, one = torch.tensor([7, -1], device="cuda"), torch.ones(2, device="cuda")
+    logp, entropy, lse, top, index = lm.token_log_probs_forward_top(z, token, 3, 0.5)
+    log = math.log(4000)
+    assert abs(float(logp[0]) + log) < 1e-5 and logp[1] == 0 and bool(((entropy - log).abs() < 1e-5).all())
+    assert index.tolist() == [[0, 1, 2]] * 2 and bool(((top + log).abs() < 1e-5).all())
+    dz = lm.token_log_probs_backward(z, token, lse, entropy, one, one, 0.5)
+    want = torch.full((2, 4000), -1 / 4000 / 0.5, device="cuda", dtype=torch.float64)
+    want[0, 7] += 2
+    want[1] = 0
+    # log q + H is zero but for the rounding of both, some 2e-6
+    assert bool(((dz.double() - want).abs() <= STORE[dtype] * want.abs() + 4e-6 / 4000).all())
+
+
 def test_rows_of_which_nothing_is_left():
     from paper_1810_10962_b200 import lm
     z, token, dlogp, dentropy = case(5, 3000, torch.float32, 13, none=0)
