@@ -332,7 +332,7 @@ __device__ __forceinline__ void alternatives(const LogProbs& a, int64_t row, int
         if (reach >= a.K && reach <= enough) break;
     }
     const int first = part == 0 ? 0 : head + begin * V, last = part == a.parts - 1 ? a.V : head + end * V;
-    const int deep = min(kLogpDepth, (end - begin + THREADS - 1) / THREADS), per_segment = deep * group;
+    const int deep = max(1, min(kLogpDepth, (end - begin + THREADS - 1) / THREADS)), per_segment = deep * group, shift = 32 - __clz(per_segment - 1);
     auto look = [&](float v, int at) {
         const unsigned k = order_key(v);
         if (v == v && k >= bound) {
@@ -355,14 +355,14 @@ __device__ __forceinline__ void alternatives(const LogProbs& a, int64_t row, int
                 }
         }
         __syncthreads();
-        const int looks = sh.queued > kLogpQueue ? 0 : sh.queued * per_segment;
+        const int looks = sh.queued > kLogpQueue ? 0 : sh.queued << shift;
         for (int w0 = tid; w0 < looks; w0 += THREADS * kLogpLooks) {
             int at[kLogpLooks];
             uint4 x[kLogpLooks];
 #pragma unroll
             for (int i = 0; i < kLogpLooks; ++i) {
-                const int w = w0 + i * THREADS, s = w / per_segment;
-                at[i] = w < looks ? begin + sh.queue[s] + (w - s * per_segment) * THREADS : end;
+                const int w = w0 + i * THREADS, k = w & ((1 << shift) - 1);
+                at[i] = w < looks && k < per_segment ? begin + sh.queue[w >> shift] + k * THREADS : end;
                 if (at[i] < end) x[i] = body[at[i]];
             }
 #pragma unroll
@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
     const int group = segment_batches<THREADS>(a);
     float mine = loose_z == loose_z ? loose_z : -inf;   // the thread's largest
     float of_segment = -inf;
-    int batch = 0;
+    int segments = 0, left = group;
     for (int v0 = begin + tid; v0 < end; v0 += kBatch) {
         if (v0 != begin + tid) fetch(v0);
         TopOf<T> top;
@@ -503,9 +503,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
         if constexpr (TOP) {
             of_segment = fmaxf(of_segment, largest);
             mine = fmaxf(mine, largest);
-            if (++batch % group == 0 || v0 + kBatch >= end) {
-                top_shared<THREADS>().segment[(batch - 1) / group][tid] = of_segment;
+            if (--left == 0 || v0 + kBatch >= end) {
+                top_shared<THREADS>().segment[segments++][tid] = of_segment;
                 of_segment = -inf;
+                left = group;
             }
         }
     }
