@@ -86,7 +86,7 @@ def check(z, token, dlogp, dentropy, tau, K):
         best = logq.gather(1, at)
         within(top, best, 2 * ue[:, None] + torch.where(best < -1e9, -4 * U * best, 0.0), "alternatives")
     for got in results:
-        within(got[0], logp, 2 * ue, "logprob")
+        within(got[0], logp, 2 * ue + torch.where(logp < -1e9, -4 * U * logp, 0.0), "logprob")
         within(got[1], entropy, 2 * ue * (1 + r), "entropy")      # log s and t / s, each of a size up to r
         within(got[2], lse, 2 * ue, "lse")
     if dlogp is not None:
@@ -94,7 +94,10 @@ def check(z, token, dlogp, dentropy, tau, K):
         want, size = gradient_of(z, token, dlogp, dentropy, tau)
         assert dz.dtype == z.dtype and dz.shape == z.shape
         # the log-sum's and the entropy's own allowances come in once more
-        within(dz, want, 8 * ue[:, None] * (1 + r[:, None]) * size + STORE[z.dtype] * want.abs() + 1e-37, "dlogits")
+        # and 2^x below 2^-126 is 0: a probability that small is lost with all that multiplies it
+        spread = torch.where(logq == -math.inf, 0.0, logq.abs()) + entropy[:, None] + 1
+        lost = 2.0 ** -126 * (dlogp.abs()[:, None] + (0 if dentropy is None else dentropy.abs()[:, None]) * spread) / tau
+        within(dz, want, 8 * ue[:, None] * (1 + r[:, None]) * size + STORE[z.dtype] * want.abs() + 2 * lost, "dlogits")
 
 
 # one to eight blocks a row, short rows in small blocks, rows shorter than a vector, odd lengths
@@ -133,6 +136,11 @@ def test_strided_rows_and_odd_addresses(pad, offset, dtype):
 
 def test_leading_dimensions():
     from paper_1810_10962_b200 import lm
+    row, place = torch.randn(700, device="cuda", generator=gen(9)), torch.tensor(5, device="cuda")
+    one = lm.token_log_probs_forward_top(row, place, 2)
+    assert one[0].shape == () and one[3].shape == (2,)
+    assert all(torch.equal(a, b[0]) for a, b in zip(one, lm.token_log_probs_forward_top(row[None], place[None], 2)))
+    assert lm.token_log_probs_backward(row, place, one[2], one[1], one[0], one[1]).shape == (700,)
     z, token, _, _ = case(6, 500, torch.float32, 8)
     flat = lm.token_log_probs_forward_top(z, token, 4)
     for got, want in zip(lm.token_log_probs_forward_top(z.view(2, 3, 500), token.view(2, 3), 4), flat):
