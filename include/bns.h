@@ -476,7 +476,8 @@ bns_status bns_topk_distillation_step(const bns_distillation* shape, const void*
  *   dlogits_tv = (dlogprob_t ([v = token_t] - q_tv) - dentropy_t q_tv (log q_tv + entropy_t)) / temperature
  * logprob, entropy (may be NULL in _forward), lse: float[rows]; top_logprob float[rows][entries], top_index
  * int32_t[rows][entries].  0 <= entries <= 64, entries <= vocabulary, 10^-6 <= temperature <= 10^6; entries = 0: no
- * alternatives.  |dentropy / temperature| up to 10^12.  Any alignment of the element type.
+ * alternatives.  |dentropy / temperature| up to 10^12; probabilities below 2^-126 count as 0 in the gradient.  Any
+ * alignment of the element type.
  */
 typedef struct {
     int rows, vocabulary, entries;

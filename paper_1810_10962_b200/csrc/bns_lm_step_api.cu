@@ -216,6 +216,7 @@ int clip_launches(const bns_gradients* list) { return std::max(1, divide_up(list
 template <int N>
 int fill_list(const bns_gradients* list, int begin, bool out, ClipList<N>& to) {
     to.count = 0;
+    to.in_place = 1;
     int64_t places = 0;
     int i = begin;
     for (; i < list->count && to.count < N; ++i) {
@@ -227,6 +228,7 @@ int fill_list(const bns_gradients* list, int begin, bool out, ClipList<N>& to) {
         to.first[k] = places;
         to.in[k] = list->data[i];
         to.out[k] = out ? list->out[i] : nullptr;
+        to.in_place &= to.out[k] == to.in[k];
         to.elements[k] = 2 * n + (list->dtype[i] == BNS_BF16);
         places += 1 + (n - head) / static_cast<int64_t>(16 / eb);
     }
@@ -243,7 +245,7 @@ void share_out(ClipList<N>& list, int64_t most) {
 constexpr int64_t kSquaresChunk = 8192, kScaleChunk = 4096;    // 128 KB (3.7 GB: 534 us; shares in one piece 578) and 64 KB (6.5 TB/s; 128 KB 6.3)
 
 struct ClipWork {
-    double* partial;
+    double *total, *partial;
     float max_norm;
     float* norm;
     bool out;
@@ -263,9 +265,18 @@ void clip_lists(const bns_gradients* list, const ClipWork& w, cudaStream_t strea
         count += grid;
     }
     const double* partial = w.partial;
+    auto total = [&] { launch(BNS_KERNEL_CLIP, clip_norm_kernel, Shape{1, kClipThreads}, 0, stream, partial, count, w.total, w.norm); };
     if (!w.out) {
-        launch(BNS_KERNEL_CLIP, clip_norm_kernel, Shape{1, kClipThreads}, 0, stream, partial, count, w.norm);
+        total();
         return;
+    }
+    // Many blocks to scale: the sums are added up once, by a launch of its own.  3.7 GB in place and
+    // below the limit: 597 us, with every block adding up and looking for its tensor 698.
+    const bool many = list->count > kClipMost || divide_up<int64_t>(here.first[here.count], kScaleChunk) > 8 * clip_blocks();
+    if (many) {
+        total();
+        partial = w.total;
+        count = 1;
     }
     // the last list first, which is already at hand: its tensors may still be in L2
     auto scale = [&](float* norm) {
@@ -284,6 +295,7 @@ bns_status clip(const bns_gradients* list, ClipWork w, void* workspace, size_t w
     if (!w.norm) return BNS_ERR_NULL;
     if (!aligned(w.norm, 4)) return BNS_ERR_ALIGN;
     if (!workspace_fits(workspace, workspace_bytes, bns_gradient_norm_workspace_bytes(list))) return BNS_ERR_WORKSPACE;
+    w.total = static_cast<double*>(workspace);
     w.partial = reinterpret_cast<double*>(static_cast<char*>(workspace) + kHeaderBytes);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (list->count <= kClipFew)
@@ -456,7 +468,7 @@ size_t bns_gradient_norm_workspace_bytes(const bns_gradients* list) {
 bns_status bns_gradient_norm(const bns_gradients* list, float* norm, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     const bns_status st = check_gradients(list, false);
     if (st != BNS_OK) return st;
-    return clip(list, ClipWork{nullptr, 0.f, norm, false}, workspace, workspace_bytes, cuda_stream);
+    return clip(list, ClipWork{nullptr, nullptr, 0.f, norm, false}, workspace, workspace_bytes, cuda_stream);
 }
 
 bns_status bns_clip_gradients(const bns_gradients* list, float max_norm, float* norm, void* workspace, size_t workspace_bytes,
@@ -464,7 +476,7 @@ bns_status bns_clip_gradients(const bns_gradients* list, float max_norm, float* 
     const bns_status st = check_gradients(list, true);
     if (st != BNS_OK) return st;
     if (!(max_norm >= 0.f)) return BNS_ERR_SHAPE;
-    return clip(list, ClipWork{nullptr, max_norm, norm, true}, workspace, workspace_bytes, cuda_stream);
+    return clip(list, ClipWork{nullptr, nullptr, max_norm, norm, true}, workspace, workspace_bytes, cuda_stream);
 }
 
 }  // extern "C"
