@@ -4,9 +4,10 @@
 //   out = g factor
 //
 // Bound by HBM: the norm reads every element once, clipping reads it again (what fits of it out of L2, hence back to front)
-// and writes it (3.7 GB of bf16: the norm 0.53 ms, 7.0 TB/s; clipping 1.69 ms in all).  The list travels in the kernels' arguments, so nothing is copied to the device and a captured graph holds
-// all it needs.  All tensors are taken as one line of 16-byte vectors, whatever their sizes, which the blocks take chunk by
-// chunk; elements outside whole vectors go with a place of their own in front of each tensor's vectors.
+// and writes it (3.7 GB of bf16: the norm 0.53 ms, 7.0 TB/s; clipping 1.69 ms in all).  The list travels in the kernels'
+// arguments, so nothing is copied to the device and a captured graph holds all it needs.  All tensors are taken as one line
+// of 16-byte vectors, whatever their sizes, which the blocks take chunk by chunk; elements outside whole vectors go with a
+// place of their own in front of each tensor's vectors.
 //
 // Squares are added in fp32 over a batch of vectors, batches and everything above in 64 bits.  A batch whose sum leaves the
 // range in which fp32 squares are exact enough is done again in 64 bits.
@@ -17,7 +18,7 @@
 namespace bns {
 
 constexpr int kClipThreads = 256;
-constexpr int kClipDepth = 8;             // vectors in flight per thread
+constexpr int kClipDepth = 8;            // vectors in flight per thread
 constexpr int kClipBlocks = 3;           // per SM: 80 registers, which clipping needs (four an SM: 3.8 TB/s in fp32 for 6.2)
 
 template <int N>
