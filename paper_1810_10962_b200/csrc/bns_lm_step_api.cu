@@ -78,10 +78,21 @@ HeadPlan plan_heads(const bns_head_norm* sh, const HeadNorm& a) {
                         !in_vectors(sh, sh->q_strides, sh->q_heads, a.q.x, a.q.dy, a.q.y, pl.V) ||
                         (sh->k_heads && !in_vectors(sh, sh->k_strides, sh->k_heads, a.k.x, a.k.dy, a.k.y, pl.V))))
         pl.V /= 2;
-    const int units = sh->rotary / 2 / pl.V + divide_up(sh->head_dim - sh->rotary, 2 * pl.V);
-    pl.lanes = 1;
-    while (pl.lanes < 32 && pl.lanes < units) pl.lanes *= 2;
-    pl.wide = units > 32;
+    auto share = [&] {
+        const int units = sh->rotary / 2 / pl.V + divide_up(sh->head_dim - sh->rotary, 2 * pl.V);
+        pl.lanes = 1;
+        while (pl.lanes < 32 && pl.lanes < units) pl.lanes *= 2;
+        pl.wide = units > 32;
+    };
+    share();
+    // A warp with little to do at a position waits for angles and weights: half as large vectors make these half as many for a
+    // lane.  16384 positions, bf16, vectors of 16 / 8 bytes: 4 + 1 heads of 64 forward 20 / 16 us, gradient 25 / 20; 16 + 4 of 64 24 / 22
+    // and 38 / 49; 8 + 8 of 128 30 / 31 and 45 / 51.
+    const int rounds = divide_up(sh->q_heads, 32 / pl.lanes);
+    if (pl.V == 8 && (a.q.dy ? rounds == 1 && pl.lanes <= 4 : rounds * pl.lanes <= 8)) {
+        pl.V = 4;
+        share();
+    }
     pl.words = (aligned(a.cos, 16) && aligned(a.sin, 16) && sh->rotary / 2 % 4 == 0 ? 1 : 0) |
                (aligned(a.q.weight, 16) && aligned(a.k.weight, 16) ? 2 : 0);
     return pl;
