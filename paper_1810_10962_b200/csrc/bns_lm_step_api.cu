@@ -147,7 +147,7 @@ struct HeadBlocks {
 
 template <typename T, int V, bool BACKWARD, bool INTERLEAVED>
 HeadBlocks head_norm_of_vectors(HeadNorm a, const HeadPlan& pl, cudaStream_t stream) {
-    // heads in flight: two, but one where the gradient's registers hold no more (bf16 58 us against 60, fp32 93 against 89)
+    // rounds in flight: two, but one where the gradient's registers hold no more (one / two: bf16 58 / 60 us, fp32 93 / 89)
     constexpr int kWide = 1024 / (64 * V), kDepth = BACKWARD && V == 8 ? 1 : 2;
     const int slots = 32 / pl.lanes;
     for (HeadRows* r : {&a.q, &a.k}) {

@@ -225,7 +225,7 @@ __device__ __noinline__ void find_equals(const typename T::storage* z, int first
 }
 
 // Largest value of a row and sums over it of 2^d and 2^d d, d = (value - largest) c, by one block; for rows that the fast
-// forms have no exponent for.  A row of -inf alone has sums of 0.
+// forms have no exponent for.  A row of -inf alone has a largest value of -inf, and NaN for sums.
 template <typename T>
 __device__ __noinline__ void sums_of_differences(const typename T::storage* z, int V, float c, float* fold, float& top, float& s, float& t) {
     using S = typename T::storage;

@@ -271,6 +271,28 @@ def test_tokens_outside_the_vocabulary_are_none():
     assert bool((dz == 0).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_calls_of_the_c_interface(dtype):
+    """Without an entropy, and a gradient whose rows lie apart: what is between them stays."""
+    import ctypes
+    from paper_1810_10962_b200 import bns, lm
+    T, V, pad = 5, 4003, 13
+    z, token, dlogp, _ = case(T, V, dtype, 25)
+    want = lm.token_log_probs_forward(z, token)
+    want_dz = lm.token_log_probs_backward(z, token, want[2], None, dlogp)
+    shape = lm._LogProbs(T, V, 0, lm._CODES[dtype], V, 1, 1.0)
+    logp, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    room = torch.full((T * (V + pad) + 1,), 7.0, dtype=dtype, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lm._load().bns_token_log_probs_forward(ctypes.byref(shape), z.data_ptr(), token.data_ptr(), logp.data_ptr(), None, lse.data_ptr(),
+                                                  None, None, stream) == bns.OK
+    dz = room[1:].view(T, V + pad)
+    assert lm._load().bns_token_log_probs_backward(ctypes.byref(shape), z.data_ptr(), token.data_ptr(), lse.data_ptr(), None, dlogp.data_ptr(),
+                                                   None, dz.data_ptr(), V + pad, stream) == bns.OK
+    assert torch.equal(logp, want[0]) and torch.equal(lse, want[2]) and torch.equal(dz[:, :V], want_dz)
+    assert bool((dz[:, V:] == 7).all()) and room[0] == 7
+
+
 def test_same_bits_every_time_and_no_rows():
     from paper_1810_10962_b200 import lm
     z, token, dlogp, dentropy = case(40, 50257, torch.bfloat16, 29)
