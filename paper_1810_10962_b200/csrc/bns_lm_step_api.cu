@@ -128,16 +128,49 @@ HeadNorm problem_of(const bns_head_norm* sh, const float* cos, const float* sin,
 
 // Blocks of the gradient kernel at the most, each of which leaves a row of sums: what fits the SMs, or one for each chunk of heads.
 constexpr int kHeadBlocks = 4;
+constexpr double kHeadPosition = 1.5;    // (none / 1 / 2 / 5: 16384 positions of 16 + 4 heads of 80 bf16 62 / 50 / 50 / 52 us)
 int head_norm_blocks(const bns_head_norm* sh) { return sh->q_heads + sh->k_heads + sm_count() * kHeadBlocks; }
 
-// Rounds over the heads that a warp makes at one position.  Many amortise the angles and weights that it fetches first (8192
-// positions of 32 + 8 heads of 128 bf16, forward, up to 4 / 8 / 16 rounds: 35 / 31 / 31 us); few spread a small batch over the SMs
-// (512 positions, aiming at 24 / 32 / 48 warps an SM: 4.2 / 3.9 / 5.2 us).
+// Rounds over the heads that a warp makes at one position, and the chunks that this makes, as even as they come out.
+void share_heads(HeadRows& r, int slots, int most) {
+    const int all = divide_up(r.heads, slots);
+    r.chunks = divide_up(all, most);
+    r.rounds = r.chunks ? divide_up(all, r.chunks) : 1;
+}
+
+// Forward: many rounds amortise the angles and weights that a warp fetches first (8192 positions of 32 + 8 heads of 128 bf16, up
+// to 4 / 8 / 16 rounds: 35 / 31 / 31 us); few spread a small batch over the SMs (512 positions, aiming at 24 / 32 / 48 warps
+// an SM: 4.2 / 3.9 / 5.2 us).
 constexpr int kHeadWarps = 32, kHeadRounds = 16;
-int head_rounds(const HeadNorm& a, int heads, int slots) {
+void plan_forward(HeadNorm& a, int slots) {
     const int64_t all = a.tokens * (divide_up(a.q.heads, slots) + divide_up(a.k.heads, slots));
-    const int64_t rounds = std::min<int64_t>(divide_up<int64_t>(all, kHeadWarps * sm_count()), kHeadRounds);
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(rounds, divide_up(heads, slots))));
+    const int most = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(divide_up<int64_t>(all, kHeadWarps * sm_count()), kHeadRounds)));
+    share_heads(a.q, slots, most);
+    share_heads(a.k, slots, most);
+}
+
+// Gradient: blocks stay, and each chunk has some of them, in proportion to the time of a position: its rounds and what else a
+// position takes, some kHeadPosition rounds.  The number of rounds is the one with which the last warp is done first.
+void plan_backward(HeadNorm& a, int slots) {
+    const int64_t tokens = divide_up<int64_t>(a.tokens, kRotaryWarps);
+    HeadNorm best = a;
+    double least = 1e300;
+    for (int most = kHeadRounds; most >= 1; --most) {
+        share_heads(a.q, slots, most);
+        share_heads(a.k, slots, most);
+        const double all = a.q.chunks * (a.q.rounds + kHeadPosition) + a.k.chunks * (a.k.rounds + kHeadPosition);
+        double cost = 0;
+        for (HeadRows* r : {&a.q, &a.k}) {
+            if (!r->chunks) continue;
+            r->blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(tokens, static_cast<int64_t>(sm_count() * kHeadBlocks * (r->rounds + kHeadPosition) / all))));
+            cost = std::max(cost, static_cast<double>(divide_up<int64_t>(tokens, r->blocks)) * (r->rounds + kHeadPosition));
+        }
+        if (cost < least) {
+            least = cost;
+            best = a;
+        }
+    }
+    a = best;
 }
 
 // Blocks of a gradient launch that leave sums of the queries' and of the keys' weight.
@@ -150,17 +183,14 @@ HeadBlocks head_norm_of_vectors(HeadNorm a, const HeadPlan& pl, cudaStream_t str
     // rounds in flight: two, but one where the gradient's registers hold no more (one / two: bf16 58 / 60 us, fp32 93 / 89)
     constexpr int kWide = 1024 / (64 * V), kDepth = BACKWARD && V == 8 ? 1 : 2;
     const int slots = 32 / pl.lanes;
-    for (HeadRows* r : {&a.q, &a.k}) {
-        r->rounds = head_rounds(a, r->heads, slots);
-        r->chunks = divide_up(divide_up(r->heads, slots), r->rounds);
-    }
-    const int64_t blocks = divide_up<int64_t>(a.tokens, kRotaryWarps);
-    Shape shape{static_cast<unsigned>(blocks), kRotaryWarps * 32, 1, static_cast<unsigned>(a.q.chunks + a.k.chunks)};
+    Shape shape{0, kRotaryWarps * 32};
     if (BACKWARD) {
-        const int all = a.q.rounds * a.q.chunks + a.k.rounds * a.k.chunks;
-        for (HeadRows* r : {&a.q, &a.k})
-            r->blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(blocks, static_cast<int64_t>(sm_count()) * kHeadBlocks * r->rounds / all)));
-        shape = Shape{static_cast<unsigned>(a.q.chunks * a.q.blocks + a.k.chunks * a.k.blocks), kRotaryWarps * 32};
+        plan_backward(a, slots);
+        shape.grid = static_cast<unsigned>(a.q.chunks * a.q.blocks + a.k.chunks * a.k.blocks);
+    } else {
+        plan_forward(a, slots);
+        shape.grid = static_cast<unsigned>(divide_up<int64_t>(a.tokens, kRotaryWarps));
+        shape.grid_y = static_cast<unsigned>(a.q.chunks + a.k.chunks);
     }
     if constexpr (BACKWARD) {
         const size_t smem = static_cast<size_t>(kRotaryWarps) * a.D * sizeof(float);

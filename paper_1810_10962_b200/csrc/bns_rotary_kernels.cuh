@@ -12,9 +12,10 @@
 // takes both sums in one exchange.
 //
 // 8192 positions of 32 + 8 heads of 128 bf16: forward 30 us (5.6 TB/s; four heads a warp without rounds, scalar arithmetic and
-// factors 45), gradient 58 us (4.4 TB/s).  The gradient is held back by its registers: angles, weights, the weight's sums and
-// two heads' elements leave 16 warps an SM.  Smaller vectors (63 us), the sums in shared memory (58) and copies ahead through
-// shared memory (54, but 145 instead of 114 where neighbours are paired and 107 instead of 89 in fp32) did not pay.
+// factors 45), gradient 54 us (4.7 TB/s).  The gradient is held back by its registers: angles, weights, the weight's sums and
+// two heads' elements leave 16 warps an SM.  Of what was tried against that, each against 58 us at the time, smaller vectors
+// (63), the sums in shared memory (58) and copies ahead through shared memory (54, but 145 instead of 114 where neighbours are
+// paired and 107 instead of 89 in fp32) did not pay.
 #pragma once
 
 #include "bns_elements.cuh"
