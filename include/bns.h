@@ -502,8 +502,8 @@ bns_status bns_token_log_probs_backward(const bns_token_log_probs* shape, const 
  *   (a, b) -> (a cos - b sin, b cos + a sin),  pair i is (i, rotary / 2 + i), or (2 i, 2 i + 1) where interleaved
  * q and k are [batch][length][heads][head_dim] with dense heads and any strides (views of a packed projection, heads
  * before positions); outputs and their gradients are dense in that order.  Weights are float[head_dim], the same for all
- * heads of q, or of k.  k_heads may be 0: then everything of k may be NULL.  position is [batch][length]; one outside
- * [0, positions) is padding: its outputs and gradients are zeros, whatever is there.
+ * heads of q, or of k.  k_heads may be 0: then everything of k may be NULL (dk_weight, if not, becomes zero).  position is
+ * [batch][length]; one outside [0, positions) is padding: its outputs and gradients are zeros, whatever is there.
  * Backward, with d = R_p^T dy:   dx = rstd (weight d - n mean(weight d n))     dweight = sum over positions, heads of d n
  * from the inputs of the forward call; rstd is found again.  Sums are taken in fp32 in a fixed order.
  * head_dim <= 1024, 2 <= rotary <= head_dim, even.  Any alignment of the element type; 16-byte vectors are used where pointers,

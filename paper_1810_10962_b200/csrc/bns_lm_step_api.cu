@@ -471,13 +471,9 @@ bns_status bns_head_norm_rotary_backward(const bns_head_norm* shape, const void*
     const bool keys = shape->k_heads > 0;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (!dq_weight || (keys && !dk_weight)) return BNS_ERR_NULL;
-    if (!aligned(dq_weight, 4) || (keys && !aligned(dk_weight, 4))) return BNS_ERR_ALIGN;
-    if (shape->batch == 0 || shape->length == 0) {
-        const size_t bytes = sizeof(float) * shape->head_dim;
-        return cudaMemsetAsync(dq_weight, 0, bytes, stream) == cudaSuccess && (!keys || cudaMemsetAsync(dk_weight, 0, bytes, stream) == cudaSuccess)
-                   ? BNS_OK
-                   : BNS_ERR_CUDA;
-    }
+    if (!aligned(dq_weight, 4) || !aligned(dk_weight, 4)) return BNS_ERR_ALIGN;
+    auto clear = [&](float* weight) { return cudaMemsetAsync(weight, 0, sizeof(float) * shape->head_dim, stream) == cudaSuccess; };
+    if (shape->batch == 0 || shape->length == 0) return clear(dq_weight) && (!dk_weight || clear(dk_weight)) ? BNS_OK : BNS_ERR_CUDA;
     if (!dq_out || !q || !q_weight || !cos || !sin || !position || !dq || (keys && (!dk_out || !k || !k_weight || !dk))) return BNS_ERR_NULL;
     const size_t eb = elem_bytes(shape->dtype);
     if (!aligned(dq_out, eb) || !aligned(q, eb) || !aligned(dq, eb) || !aligned(q_weight, 4) || !aligned(cos, 4) || !aligned(sin, 4) ||
@@ -485,6 +481,7 @@ bns_status bns_head_norm_rotary_backward(const bns_head_norm* shape, const void*
         (keys && (!aligned(dk_out, eb) || !aligned(k, eb) || !aligned(dk, eb) || !aligned(k_weight, 4))))
         return BNS_ERR_ALIGN;
     if (!workspace_fits(workspace, workspace_bytes, bns_head_norm_rotary_workspace_bytes(shape))) return BNS_ERR_WORKSPACE;
+    if (!keys && dk_weight && !clear(dk_weight)) return BNS_ERR_CUDA;
     HeadNorm a = problem_of(shape, cos, sin, position);
     a.q.x = q;
     a.q.dy = dq_out;

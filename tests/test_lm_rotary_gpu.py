@@ -151,6 +151,17 @@ def test_queries_alone_and_three_dimensions():
     within(dqw, reference(q, qw, cos, sin, position, grads[0], False)[0][2], 200 * U * reference(q, qw, cos, sin, position, grads[0], False)[1][2], "dq_weight")
 
 
+def test_keys_without_heads():
+    from paper_1810_10962_b200 import lm
+    q, k, qw, kw, cos, sin, position, grads = case(2, 5, 3, 1, 64, 64, torch.bfloat16, 14)
+    none = k[:, :, :0]
+    torch.full((64,), 7.0, device="cuda")                    # what a new tensor would find
+    outs = lm.head_norm_rotary_forward(q, none, qw, kw, cos, sin, position, EPS)
+    assert outs[1].shape == (2, 5, 0, 64) and torch.equal(outs[0], lm.head_norm_rotary_forward(q, None, qw, None, cos, sin, position, EPS)[0])
+    got = lm.head_norm_rotary_backward(grads[0], outs[1], q, none, qw, kw, cos, sin, position, EPS)
+    assert bool((got[3] == 0).all()) and torch.equal(got[0], lm.head_norm_rotary_backward(grads[0], None, q, None, qw, None, cos, sin, position, EPS)[0])
+
+
 def test_heads_of_zeros_and_of_large_values():
     q, k, qw, kw, cos, sin, position, grads = case(1, 4, 2, 2, 64, 64, torch.float32, 15)
     q[0, 0] = 0
