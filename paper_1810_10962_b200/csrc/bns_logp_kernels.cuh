@@ -470,10 +470,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
     Stats st{-inf, 0.f, 0.f};
     if (loose >= 0) {
         const float m = loose_z * a.c;
-        if (fabsf(m) <= kFar)
-            st = Stats{m, exp2_fast(fmaf(loose_z, a.c, -m)), 0.f};
-        else
+        if (fabsf(m) <= kFar) {
+            const float u = fmaf(loose_z, a.c, -m), e = exp2_fast(u);      // what rounding m has left
+            st = Stats{m, e, e * u};
+        } else {
             st = Stats{m == m ? m : -inf, m == m ? 0.f : m, 0.f};
+        }
     }
     constexpr int kBatch = THREADS * kLogpDepth;
     const int group = segment_batches<THREADS>(a);

@@ -1,0 +1,78 @@
+"""Entropy of token log probabilities with a bound from the kernels' own roundings, whatever a row's common part is.
+
+u = 2^-24 is fp32's rounding, L = log q, d = the distance to the largest logit over the temperature.  Exponents are
+z c - m by one multiply-add, with c rounded once and m, the rounded reference, which is off its logit by rho = u |z| log2(e) / tau
+at the most:
+* a term 2^(z c - m) of either sum is good to 4 u (2^x, two ulp), the exponent's rounding u (d + rho), and as much again where the reference moves;
+* a thread adds up V / 256 terms in a row at the most, some 20 joins follow: es = u (4 + 2 E[d] + 2 rho + V / 256 + 20) for the
+  sum s, and as much relative to E[d] + rho for the weighted sum t;
+* log2 s - t / s: two ulp of the first, which is H + rho at the most, a division, a difference and a product;
+* c's own rounding is a temperature off by u, which moves the entropy by u Var L."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+STORE = {torch.float32: U, torch.bfloat16: 2.0 ** -8}
+TYPES = [torch.bfloat16, torch.float32]
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+class Exact:
+    """A row's values in 64 bits, differences to the largest logit first, and the allowances above."""
+
+    def __init__(self, z, tau):
+        tau = float(torch.tensor(tau, dtype=torch.float32))
+        zd = z.double()
+        most = zd.amax(1, keepdim=True)
+        d = (most - zd) / tau
+        logs = torch.logsumexp(-d, 1, keepdim=True)
+        self.lse = (most / tau + logs)[:, 0]
+        self.logq = -d - logs
+        self.q = self.logq.exp()
+        weighted = lambda x: torch.where(self.q > 0, self.q * x, 0.0).sum(1)  # noqa: E731
+        self.entropy = -weighted(self.logq)
+        self.rho = U * zd.abs().masked_fill(zd.isinf(), 0.0).amax(1) * 1.4427 / tau
+        distance = weighted(d) + self.rho
+        self.of_sum = U * (24 + 2 * distance + z.shape[1] / 256)
+        self.of_entropy = self.of_sum * (1 + 2 * distance) + U * (8 * distance + 4 * (self.entropy + self.rho) + weighted(self.logq.square()))
+
+
+def within(got, want, tol, what):
+    off = (got.double() - want).abs()
+    bad = ~(off <= tol)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst {float((off / tol).nan_to_num(math.inf).max()):.3g} times the bound"
+
+
+# --------------------------------------------------------------------------------------------- entropy
+@pytest.mark.parametrize("top", [0.0, 10.0, 1e3, -1e4, 1e5, 1e6, 1e7, -1e8, 1.5e8])
+@pytest.mark.parametrize("V", [5, 37])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_entropy_wherever_the_largest_logit_lies(dtype, V, top):
+    """Each place of a row in turn, inside 16-byte vectors and outside, by itself far above the others and a little above."""
+    from paper_1810_10962_b200 import lm
+    below = (torch.arange(V, device="cuda") % 4).float()
+    for others in (below - abs(top), top - 1 - below / 2):
+        z = others.repeat(V, 1).fill_diagonal_(top).to(dtype)
+        token = torch.zeros(V, dtype=torch.int64, device="cuda")
+        want = Exact(z, 1.0)
+        for got in (lm.token_log_probs_forward(z, token)[1], lm.token_log_probs_forward_top(z, token, 3)[1]):
+            within(got, want.entropy, want.of_entropy, "entropy")
+
+
+@pytest.mark.parametrize("tau", [1.0, 0.7])
+@pytest.mark.parametrize("shift", [0.0, 300.0, -5000.0, 1e5, 1e7])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(40, 1003), (3, 9001), (2, 50257)])
+def test_entropy_of_rows_with_a_common_part(T, V, dtype, shift, tau):
+    from paper_1810_10962_b200 import lm
+    z = (torch.randn(T, V, device="cuda", generator=gen(3 + V)) * 2 + shift).to(dtype)
+    want = Exact(z, tau)
+    entropy = lm.token_log_probs_forward(z, torch.zeros(T, dtype=torch.int64, device="cuda"), tau)[1]
+    within(entropy, want.entropy, want.of_entropy, "entropy")
