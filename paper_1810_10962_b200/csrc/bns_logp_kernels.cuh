@@ -29,6 +29,7 @@ constexpr int kLogpSegments = 8;                        // of a thread
 constexpr int kLogpFound = 1024;                        // values that reach the bound, before the slow way is taken
 constexpr int kLogpQueue = 512;                         // segments that reach it, likewise
 constexpr int kLogpLooks = 4;                           // vectors of queued segments in flight per thread
+constexpr double kLn2Exact = 0.693147180559945309;
 constexpr float kLogpFloor = -0x1p60f;                  // stands in for anything lower: 2^(floor c - m) = 0, and 0 times it is 0
 static_assert(kLogpParts * kLogpMaxTop <= kLogpFound);
 
@@ -45,7 +46,8 @@ struct LogProbs {
     int parts, per;       // blocks of a row, vectors of each
 };
 
-// Largest log-sum that the gradient takes q from: its rounding, 2^-24 of it, is off by 2^-16 in q then, or for bf16 by 2^-12.
+// Largest log-sum that the gradient takes q from.  It is rounded once, so q is off by half its step: 2^-17 just below 256 in fp32, 2^-13
+// below 4096 for bf16 (2^-21 at ordinary log-sums of 8 to 16), beside the sum's own error.
 template <typename T>
 constexpr float kLogpKept = sizeof(typename T::storage) == 2 ? 0x1p12f : 0x1p8f;
 
@@ -536,7 +538,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
     }
 
     const float log_s = log2f(st.s);
-    float lse = (st.m + log_s) * kLn2, entropy = (log_s - st.t / st.s) * kLn2;
+    float lse = static_cast<float>((static_cast<double>(st.m) + log_s) * kLn2Exact), entropy = (log_s - st.t / st.s) * kLn2;
     LogQ log_q{a.tau, a.c, st.m, log_s, 0.f, lse, false};
     if (!(fabsf(st.m) <= kNear)) {
         // The largest value times c is too large for the fast form (a row masked with -1e10 or the type's lowest value
@@ -593,8 +595,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(
     const int token = given >= 0 && given < a.V ? static_cast<int>(given) : -1;
     const float g = token >= 0 ? a.dlogp[row] / a.tau : 0.f, h = a.dentropy ? a.dentropy[row] / a.tau : 0.f;
     const float lse = a.lse_in[row], entropy = a.dentropy ? a.entropy_in[row] : 0.f;
-    // lse tau c = m + rest with the same c as in z c, so that only z - lse tau feels its rounding
-    const double exponent = static_cast<double>(lse) * a.tau * a.c;
+    // The forward call's m + log2 s again, which was found with the same rounded c as z c here: times log2(e) itself, since with tau c in its
+    // place c's rounding would move every q of the row by up to 2^-24 lse.
+    const double exponent = static_cast<double>(lse) * (1. / kLn2Exact);
     const float m = static_cast<float>(exponent), rest = static_cast<float>(exponent - m);
     // log q = ln 2 (u - rest)
     const float scale = exp2_fast(-rest), k0 = -(g + h * (entropy - rest * kLn2)) * scale, k1 = -h * kLn2 * scale;

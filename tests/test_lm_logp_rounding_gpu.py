@@ -76,3 +76,21 @@ def test_entropy_of_rows_with_a_common_part(T, V, dtype, shift, tau):
     want = Exact(z, tau)
     entropy = lm.token_log_probs_forward(z, torch.zeros(T, dtype=torch.int64, device="cuda"), tau)[1]
     within(entropy, want.entropy, want.of_entropy, "entropy")
+
+
+# --------------------------------------------------------------------------------------------- the gradient's probabilities
+@pytest.mark.parametrize("tau", [0.05, 0.7, 1.0, 1.2, 1.3, 1.7])
+def test_probabilities_of_the_gradient_add_up(tau):
+    """With a gradient of -1 for one token's log probability the row of dlogits adds up to (sum of q - 1) / tau.  q comes from the
+    log-sum, which is rounded once (u |lse|); 2^x, the exponent and the store take their roundings in either call."""
+    from paper_1810_10962_b200 import lm
+    T, V = 4096, 100
+    g = gen(7)
+    z = (torch.randn(T, V, device="cuda", generator=g) * 2 + 100 + 145 * torch.rand(T, 1, device="cuda", generator=g)) * tau
+    token = z.argmin(1)
+    want = Exact(z, tau)
+    _, entropy, lse = lm.token_log_probs_forward(z, token, tau)
+    assert float(lse.min()) > 64 and float(lse.max()) < 256
+    dz = lm.token_log_probs_backward(z, token, lse, entropy, torch.full((T,), -1.0, device="cuda"), None, tau)
+    distance = want.entropy - want.logq.amax(1)          # no less than E[d]
+    within(dz.double().sum(1) * tau, torch.zeros_like(want.lse), want.of_sum + U * (want.lse.abs() + 12 + 2 * distance), "sum of q - 1")
