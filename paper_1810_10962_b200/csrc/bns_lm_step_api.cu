@@ -423,6 +423,8 @@ bns_status bns_token_log_probs_backward(const bns_token_log_probs* shape, const 
     while (a.rows * (a.parts + 1) <= 2 * sm_count() && vectors > a.parts * threads) ++a.parts;
     a.per = divide_up(vectors, a.parts);
     if (a.rows * a.parts >= int64_t{1} << 31) return BNS_ERR_SHAPE;
+    a.walkers = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(a.parts, sm_count() * (1024 / threads) / a.rows)));
+    a.walk = divide_up(vectors, a.walkers);
     const unsigned grid = static_cast<unsigned>(a.rows * a.parts);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     BNS_LM_BY_TYPE(shape->dtype, {

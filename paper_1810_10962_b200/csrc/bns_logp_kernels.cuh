@@ -44,6 +44,7 @@ struct LogProbs {
     int V, K, token64;
     float tau, c;
     int parts, per;       // blocks of a row, vectors of each
+    int walkers, walk;    // backward: the same where each block walks over all of its row
 };
 
 // Largest log-sum that the gradient takes q from.  It is rounded once, so q is off by half its step: 2^-17 just below 256 in fp32, 2^-13
@@ -564,6 +565,56 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_forward_kernel(c
     if constexpr (TOP) alternatives<T, THREADS>(a, row, part, loose_z, mine, log_q);
 }
 
+// Gradients of the elements outside vectors and of the vectors [begin, end) of a row whose log-sum's rounding is too much for q: largest value and
+// sum once more, of differences.
+template <typename T>
+__device__ __noinline__ void gradient_of_differences(const LogProbs& a, const typename T::storage* z, typename T::storage* dz, int head, int begin, int end,
+                                                     int loose, int token, float g, float h, float entropy, float lse, float* fold) {
+    using S = typename T::storage;
+    constexpr int V = 16 / sizeof(S);
+    float base, s, t;
+    sums_of_differences<T>(z, a.V, a.c, fold, base, s, t);
+    const float log_s = log2f(s);
+    const bool empty = lse == -__builtin_huge_valf() && base == lse;       // a log-sum of -inf may also be one that has left fp32's range
+    auto value = [&](float v) {
+        if (empty) return 0.f;
+        const float u = (v - base) * a.c - log_s, e = exp2_fast(u);
+        return e == 0.f ? 0.f : -e * (g + h * fmaf(u, kLn2, entropy));
+    };
+    auto at_token = [&](float v) { return empty ? 0.f : value(v) + g; };
+    const uint4* body = reinterpret_cast<const uint4*>(z + head);
+    const int threads = blockDim.x;
+    const bool in_body = token >= head + begin * V && token < head + end * V;
+    const bool mine = in_body && ((token - head) / V - begin) % threads == threadIdx.x;
+    const float token_z = mine ? to_float<T>(z[token]) : 0.f;
+    if (loose >= 0) dz[loose] = from_float<T>(loose == token ? at_token(to_float<T>(z[loose])) : value(to_float<T>(z[loose])));
+    const bool words = ((reinterpret_cast<uintptr_t>(dz) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
+    for (int v0 = begin + threadIdx.x; v0 < end; v0 += threads * kLogpDepth) {
+        uint4 x[kLogpDepth];
+#pragma unroll
+        for (int i = 0; i < kLogpDepth; ++i)
+            if (v0 + i * threads < end) x[i] = body[v0 + i * threads];
+#pragma unroll
+        for (int i = 0; i < kLogpDepth; ++i) {
+            const int v = v0 + i * threads;
+            if (v >= end) continue;
+            Vec<T, V> y, o;
+            y.raw = x[i];
+#pragma unroll
+            for (int j = 0; j < V; ++j) o.set(j, value(y.get(j)));
+            S* to = dz + head + static_cast<int64_t>(v) * V;
+            if (words) {
+                __stcs(reinterpret_cast<uint4*>(to), o.raw);
+            } else {
+                const S* f = reinterpret_cast<const S*>(&o.raw);
+#pragma unroll
+                for (int j = 0; j < V; ++j) to[j] = f[j];
+            }
+        }
+    }
+    if (mine) dz[token] = from_float<T>(at_token(token_z));
+}
+
 // The gradient: q_v = 2^(z_v c - m) / rest from the forward call's log-sum, so every element by itself:
 //   dz_v = 2^u (k0 + k1 u) with u = z_v c - m,  and dlogp / tau more at the token.
 template <typename T, int THREADS>
@@ -572,7 +623,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(
     constexpr int V = 16 / sizeof(S);
     __shared__ float fold[THREADS / 32];
     const int tid = threadIdx.x;
-    const float inf = __int_as_float(0x7f800000);
     grid_dependency_wait();
     grid_dependency_launch();
     // last row first: what the forward call read last may still be in L2
@@ -601,22 +651,24 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(
     const float m = static_cast<float>(exponent), rest = static_cast<float>(exponent - m);
     // log q = ln 2 (u - rest)
     const float scale = exp2_fast(-rest), k0 = -(g + h * (entropy - rest * kLn2)) * scale, k1 = -h * kLn2 * scale;
-    const bool far = !(fabsf(lse) <= kLogpKept<T>);
-    bool empty = false;
-    float base = 0.f, log_s = 0.f;
-    if (far) {                       // the log-sum's rounding is too much for q: both parts of it once more, of differences
-        float s, t;
-        sums_of_differences<T>(z, a.V, a.c, fold, base, s, t);
-        log_s = log2f(s);
-        empty = lse == -inf && base == -inf;       // a log-sum of -inf may also be one that has left fp32's range
+    if (!(fabsf(lse) <= kLogpKept<T>)) {
+        // Each block walks over all of the row for the sum, so only as many of them work on it as run at the same time
+        // (2048 x 131072 fp32, all rows like this: eight 3.37 ms, one 0.93; rows within kLogpKept 0.32).
+        if (part < a.walkers) {
+            LogProbs walk = a;
+            walk.parts = a.walkers;
+            walk.per = a.walk;
+            const RowPart<T> share(z, walk, part);
+            gradient_of_differences<T>(a, z, dz, head, share.begin, share.end, share.loose, token, g, h, entropy, lse, fold);
+        }
+        return;
     }
     auto value = [&](float v) {
-        if (empty) return 0.f;
-        const float u = far ? (v - base) * a.c - log_s : fmaf(v < kLogpFloor ? kLogpFloor : v, a.c, -m), e = exp2_fast(u);
-        return far ? e == 0.f ? 0.f : -e * (g + h * fmaf(u, kLn2, entropy)) : e * fmaf(k1, u, k0);
+        const float u = fmaf(v < kLogpFloor ? kLogpFloor : v, a.c, -m);
+        return exp2_fast(u) * fmaf(k1, u, k0);
     };
     // the token's element has its thread add what is due there
-    auto at_token = [&](float v) { return empty ? 0.f : value(v) + g; };
+    auto at_token = [&](float v) { return value(v) + g; };
     const bool in_body = token >= head + begin * V && token < head + end * V;
     const bool mine = in_body && ((token - head) / V - begin) % THREADS == tid;
     const float token_z = mine ? to_float<T>(z[token]) : 0.f;
@@ -629,22 +681,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_backward_kernel(
             const int v = v0 + i * THREADS;
             if (v >= end) continue;
             Vec<T, V> o;
-            if (!far) {
-                raise_to_floor<T>(x[i]);
-                Vec<T, V> y;
-                y.raw = x[i];
+            raise_to_floor<T>(x[i]);
+            Vec<T, V> y;
+            y.raw = x[i];
 #pragma unroll
-                for (int q = 0; q < V / 2; ++q) {
-                    const pair_t u = fma2(vec_pair<T, V>(y, q), twice(a.c), twice(-m));
-                    float lo, hi;
-                    split_pair(u, lo, hi);
-                    set_vec_pair<T, V>(o, q, mul2(make_pair(exp2_fast(lo), exp2_fast(hi)), fma2(u, twice(k1), twice(k0))));
-                }
-            } else {
-                Vec<T, V> y;
-                y.raw = x[i];
-#pragma unroll
-                for (int j = 0; j < V; ++j) o.set(j, value(y.get(j)));
+            for (int q = 0; q < V / 2; ++q) {
+                const pair_t u = fma2(vec_pair<T, V>(y, q), twice(a.c), twice(-m));
+                float lo, hi;
+                split_pair(u, lo, hi);
+                set_vec_pair<T, V>(o, q, mul2(make_pair(exp2_fast(lo), exp2_fast(hi)), fma2(u, twice(k1), twice(k0))));
             }
             S* to = dz + head + static_cast<int64_t>(v) * V;
             if (words) {

@@ -94,3 +94,70 @@ def test_probabilities_of_the_gradient_add_up(tau):
     dz = lm.token_log_probs_backward(z, token, lse, entropy, torch.full((T,), -1.0, device="cuda"), None, tau)
     distance = want.entropy - want.logq.amax(1)          # no less than E[d]
     within(dz.double().sum(1) * tau, torch.zeros_like(want.lse), want.of_sum + U * (want.lse.abs() + 12 + 2 * distance), "sum of q - 1")
+
+
+KEPT = {torch.float32: 2.0 ** 8, torch.bfloat16: 2.0 ** 12}
+
+
+def check_gradient(z, tau, seed, with_entropy=True):
+    """The gradient in 64 bits.  q is off by the log-sum's errors, 2^x, and roundings of the exponent's size; beyond KEPT the sum is found again
+    and the log-sum's rounding does not come in.  What multiplies q has the size of its terms and the entropy's error."""
+    from paper_1810_10962_b200 import lm
+    T, V = z.shape
+    g = gen(seed)
+    token = torch.randint(0, V, (T,), device="cuda", generator=g)
+    token[::3] = z[::3].argmax(1)
+    token[1::7] = -100
+    dlogp, dentropy = torch.randn(T, device="cuda", generator=g), torch.randn(T, device="cuda", generator=g)
+    logp, entropy, lse = lm.token_log_probs_forward(z, token, tau)
+    got = lm.token_log_probs_backward(z, token, lse, entropy if with_entropy else None, dlogp, dentropy if with_entropy else None, tau)
+    want, tau = Exact(z, tau), float(torch.tensor(tau, dtype=torch.float32))
+    given = token >= 0
+    one = torch.zeros(T, V, dtype=torch.bool, device="cuda")
+    one[given, token[given]] = True
+    a, b = (dlogp.double() * given)[:, None], dentropy.double()[:, None] * with_entropy
+    L, H, q = torch.where(want.q > 0, want.logq, 0.0), want.entropy[:, None], want.q
+    exact = (a * (one.double() - q) - b * q * (L + H)) / tau
+    distance = want.entropy - want.logq.amax(1) + want.rho
+    rounded = torch.where(want.lse.abs() < KEPT[z.dtype], want.lse.abs(), 0.0)
+    of_q = (want.of_sum + U * (8 + 4 * distance + rounded))[:, None] + U * (4 * L.abs() + (L + H).abs())
+    a, b = a.abs(), b.abs()
+    size = a * (one.double() + q) + b * q * (L.abs() + H + 1)
+    bound = (q * of_q * (a + b * (L + H).abs()) + b * q * (of_q + want.of_entropy[:, None]) + 6 * U * size) / tau
+    lost = 2.0 ** -126 * (a + b * (want.logq.nan_to_num(0.0, 0.0, 0.0).abs() + H + 1)) / tau      # 2^x below 2^-126 is 0
+    within(got, exact, bound + STORE[z.dtype] * exact.abs() + 2 * lost, "dlogits")
+
+
+def normal_rows(T, V, seed, spread=2.0):
+    return torch.randn(T, V, device="cuda", generator=gen(seed)) * spread
+
+
+# a row's blocks all at once, and more of them than run at a time; rows at any phase, their tails in the first block or in another one
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(2, 131075), (300, 131075), (700, 70001), (650, 131072), (5, 300), (3, 9001)])
+def test_gradient_of_rows_whose_sum_is_found_again(T, V, dtype):
+    """Every other row has a log-sum beyond KEPT, in either direction."""
+    z = normal_rows(T, V, 11 + V)
+    z[::2] += KEPT[dtype] * 1.5
+    z[::4] -= KEPT[dtype] * 3.5
+    check_gradient(z.to(dtype), 1.0, 13)
+
+
+def test_gradient_of_rows_whose_sum_is_found_again_takes_its_share_of_time():
+    """Three passes over a row that is read once as a rule, whatever its length: not one for each of its blocks."""
+    from paper_1810_10962_b200 import lm
+    T, V = 600, 131072
+    z, token, one = normal_rows(T, V, 15), torch.zeros(T, dtype=torch.int64, device="cuda"), torch.ones(T, device="cuda")
+    times = []
+    for shift in (0.0, 400.0):
+        lse = lm.token_log_probs_forward(z + shift, token)[2]
+        moved, best = z + shift, math.inf
+        for _ in range(6):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            lm.token_log_probs_backward(moved, token, lse, None, one)
+            end.record()
+            end.synchronize()
+            best = min(best, start.elapsed_time(end))
+        times.append(best)
+    assert times[1] < 6 * times[0], times
