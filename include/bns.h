@@ -531,9 +531,11 @@ bns_status bns_head_norm_rotary_backward(const bns_head_norm* shape, const void*
 /*
  * Global norm over many gradients, and clipping by it.
  *   norm = sqrt(sum over all elements of all tensors of g^2)
- *   factor = 1 where norm <= max_norm, else max_norm / norm        out = g factor, rounded once
- * Squares of the whole range of fp32 are added without overflow or loss.  Infinities and NaN follow the formula: a norm of
- * inf makes finite gradients 0 and infinite ones NaN, a norm of NaN makes all NaN.  A tensor may be clipped in place
+ *   factor = 1 where norm <= max_norm, else max_norm / norm        out = g factor
+ * Squares of the whole range of fp32 are added without overflow or loss.  norm is rounded to fp32 (inf beyond it), the factor
+ * is taken from the unrounded norm and rounded to fp32 (kept in 64 bits where it is below 2^-126), each product is rounded once.
+ * Infinities and NaN follow the formula: an infinite gradient makes finite ones 0 and infinite ones NaN unless max_norm is inf,
+ * NaN makes all NaN; finite gradients whose norm is beyond fp32 are clipped by it all the same.  A tensor may be clipped in place
  * (out[i] = data[i]); apart from that outputs overlap neither each other nor a gradient.
  * The arrays are HOST memory, read during the call; tensors are dense, any alignment of their element type.
  * norm: float on the device.  max_norm >= 0.

@@ -229,6 +229,28 @@ __device__ __forceinline__ void scale_span(const void* data, void* out, int64_t 
     }
 }
 
+// The block's chunk with a factor that fp32 has no normal number for, in 64 bits.
+template <typename T>
+__device__ __forceinline__ void scale_span_exactly(const void* data, void* out, int64_t elements, int64_t from, int64_t to, double factor) {
+    constexpr int V = 16 / sizeof(typename T::storage);
+    const typename T::storage* p = static_cast<const typename T::storage*>(data);
+    typename T::storage* o = static_cast<typename T::storage*>(out);
+    const ClipSpan<T> span(data, elements);
+    auto scale = [&](int64_t i) { o[i] = from_float<T>(static_cast<float>(to_float<T>(p[i]) * factor)); };
+    if (from == 0 && span.loose(threadIdx.x) >= 0) scale(span.loose(threadIdx.x));
+    const int64_t begin = span.head + (from > 0 ? from - 1 : 0) * V, end = span.head + (to - 1) * V;
+    for (int64_t i = begin + threadIdx.x; i < end; i += kClipThreads) scale(i);
+}
+template <int N>
+__device__ __noinline__ void scale_exactly(const ClipList<N>& list, double factor) {
+    visit_chunk(list, gridDim.x - 1 - blockIdx.x, [&](int e, int64_t from, int64_t to) {
+        if (list.elements[e] & 1)
+            scale_span_exactly<BF16>(list.in[e], list.out[e], list.elements[e] >> 1, from, to, factor);
+        else
+            scale_span_exactly<F32>(list.in[e], list.out[e], list.elements[e] >> 1, from, to, factor);
+    });
+}
+
 // A block takes one chunk: blocks that walk down several drift apart, and reads and writes then go all over the memory (3.7 GB
 // of bf16: 4.8 TB/s read + written for 6.5).  Every block finds the norm itself from the blocks' sums, or from their total where
 // there are many blocks.  The line is taken back to front, since what the norm read last may still be in L2.
@@ -240,8 +262,14 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocks) clip_scale_kernel(c
     const double exact = sqrt(sum_partials(partial, count, fold));
     const float rounded = static_cast<float>(exact);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = rounded;
-    const float factor = rounded <= max_norm ? 1.f : static_cast<float>(max_norm / exact);
+    const double quotient = max_norm / exact;
+    const float factor = rounded <= max_norm ? 1.f : static_cast<float>(quotient);
+    const bool small = factor < 0x1p-126f && quotient > 0.;
     if (factor == 1.f && list.in_place) return;
+    if (small) {
+        scale_exactly(list, quotient);
+        return;
+    }
     visit_chunk(list, gridDim.x - 1 - blockIdx.x, [&](int e, int64_t from, int64_t to) {
         const void* in = list.in[e];
         void* out = list.out[e];
