@@ -1,4 +1,4 @@
-"""Entropy of token log probabilities with a bound from the kernels' own roundings, whatever a row's common part is.
+"""Token log probabilities with bounds from the kernels' own roundings, whatever a row's common part is.
 
 u = 2^-24 is fp32's rounding, L = log q, d = the distance to the largest logit over the temperature.  Exponents are
 z c - m by one multiply-add, with c rounded once and m, the rounded reference, which is off its logit by rho = u |z| log2(e) / tau
@@ -38,7 +38,7 @@ class Exact:
         self.q = self.logq.exp()
         weighted = lambda x: torch.where(self.q > 0, self.q * x, 0.0).sum(1)  # noqa: E731
         self.entropy = -weighted(self.logq)
-        self.rho = U * zd.abs().masked_fill(zd.isinf(), 0.0).amax(1) * 1.4427 / tau
+        self.rho = U * torch.where(d < 300, zd.abs(), 0.0).amax(1) * 1.4427 / tau       # of what counts
         distance = weighted(d) + self.rho
         self.of_sum = U * (24 + 2 * distance + z.shape[1] / 256)
         self.of_entropy = self.of_sum * (1 + 2 * distance) + U * (8 * distance + 4 * (self.entropy + self.rho) + weighted(self.logq.square()))
@@ -161,3 +161,67 @@ def test_gradient_of_rows_whose_sum_is_found_again_takes_its_share_of_time():
             best = min(best, start.elapsed_time(end))
         times.append(best)
     assert times[1] < 6 * times[0], times
+
+
+# --------------------------------------------------------------------------------------------- all outputs
+def check_forward(z, tau, K):
+    """log q is (z c - m) - log2 s times ln 2: roundings of the size of both, the sum's error, and c's own rounding, which moves it by
+    u |L + H|; the log-sum is rounded once, and c's rounding moves it by u |z| / tau."""
+    from paper_1810_10962_b200 import lm
+    T, V = z.shape
+    token = torch.randint(0, V, (T,), device="cuda", generator=gen(V))
+    token[::3] = z[::3].argmax(1)
+    want = Exact(z, tau)
+    distance = want.entropy - want.logq.amax(1) + want.rho
+    of_log = lambda L: (want.of_sum + 4 * U * distance)[:, None] + U * (6 * L.abs() + (L + want.entropy[:, None]).abs())  # noqa: E731
+    given = want.logq.gather(1, token[:, None])
+    of_lse = want.of_sum + U * (want.lse.abs() + 4 * distance + 1) + want.rho
+    *first, top, index = lm.token_log_probs_forward_top(z, token, K, tau)
+    at = torch.sort(z.float(), dim=1, descending=True, stable=True).indices[:, :K]
+    assert torch.equal(index.long(), at)
+    within(top, want.logq.gather(1, at), of_log(want.logq.gather(1, at)), "alternatives")
+    for got in (first, lm.token_log_probs_forward(z, token, tau)):
+        within(got[0], given[:, 0], of_log(given)[:, 0], "logprob")
+        within(got[1], want.entropy, want.of_entropy, "entropy")
+        within(got[2], want.lse, of_lse, "lse")
+
+
+# one to eight blocks a row, each number of threads, short rows and rows without a vector, odd lengths
+@pytest.mark.parametrize("tau", [1.0, 0.6])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V,K", [(1, 1, 1), (3, 7, 5), (4, 100, 64), (400, 1003, 7), (700, 130, 64), (3, 4099, 33), (37, 50257, 10), (140, 32768, 1),
+                                   (320, 20001, 20), (310, 65537, 3), (1, 131072, 20), (2, 300001, 64), (1300, 9001, 5)])
+def test_ordinary_rows(T, V, K, dtype, tau):
+    z = normal_rows(T, V, 17 + T + V)
+    z[:, V // 2] += 4
+    check_forward(z.to(dtype), tau, K)
+    check_gradient(z.to(dtype), tau, 19)
+    check_gradient(z.to(dtype), tau, 19, with_entropy=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shift", [-3000.0, 300.0, 3700.0, 5000.0, 1e5, 3e6])
+def test_a_common_part_costs_the_gradient_nothing(shift, dtype):
+    """At a temperature of 16.  A log-sum's own rounding, 2^-12 for a shift of 1e5 and 2^-7 for one of 3e6, would be twenty times the bound and more."""
+    z = (normal_rows(5, 9001, 23, 32.0) + shift).to(dtype)
+    check_forward(z, 16.0, 4)
+    check_gradient(z, 16.0, 29)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tau", [0.01, 0.1, 30.0])
+def test_sharp_and_flat_distributions(tau, dtype):
+    z = normal_rows(40, 9001, 31).to(dtype)
+    check_forward(z, tau, 9)
+    check_gradient(z, tau, 37)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("mask", [-math.inf, -1e30, -1e9])
+def test_masked_places_beside_ordinary_ones(mask, dtype):
+    from paper_1810_10962_b200 import lm
+    z = normal_rows(30, 9001, 41)
+    z[torch.rand(30, 9001, device="cuda", generator=gen(43)) < 0.9] = mask
+    check_gradient(z.to(dtype), 0.7, 47)
+    want, got = Exact(z.to(dtype), 0.7), lm.token_log_probs_forward(z.to(dtype), z.argmax(1), 0.7)
+    within(got[1], want.entropy, want.of_entropy, "entropy")
