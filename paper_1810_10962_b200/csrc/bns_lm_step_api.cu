@@ -371,11 +371,17 @@ bns_status bns_token_log_probs_forward(const bns_token_log_probs* shape, const v
     // Threads of a block, with 1024 an SM.  Small blocks let more rows' ends lie under other rows' streams: bf16, 20
     // alternatives, 128 / 256 / 512 threads: 4096 x 32768 67 / 75 / 106 us, 2047 x 50257 53 / 57 / 72, 1024 x 131072 65 / 59 / 65;
     // without alternatives 2047 x 50257 39 / 40 / 47.  More than 32 alternatives want more threads' maxima: 2047 x 50257
-    // with 64 72 / 68 / 82, unless a row has no more than some vectors for each thread (8192 x 4096 82 / 101).  Two to three rows
-    // an SM are too few blocks of 256: 300 x 131072 30 / 33 / 26.
+    // with 64 72 / 68 / 82, unless a row has no more than some vectors for each thread (8192 x 4096 82 / 101).
+    // Two to three long rows an SM are an uneven number of blocks of 256 threads, and large blocks have them done sooner.  256 / 512 threads, 370 rows, bf16
+    // without alternatives: 20011 7.1 / 6.9, 32768 8.4 / 7.9, 50257 12.0 / 10.5, 131072 27.4 / 21.9, 262144 52 / 42; with 20: 40000 14.6 / 15.8, 50257
+    // 16.9 / 17.1, 65536 18.7 / 18.1, 131072 33.3 / 29.1, 262144 59 / 52 (444 rows, three an SM: 131072 24.1 / 24.2 and 32.6 / 31.6).  fp32 gains where the
+    // rows lie in L2: without alternatives 20000 7.1 / 7.6, 32768 9.4 / 8.9, 50001 14.1 / 12.8, 65536 17.6 / 15.7, but 80000 22.7 / 25.4; with 20
+    // 32768 14.3 / 15.3, 50001 20.2 / 20.5, 65536 24.2 / 23.8, 131072 42 / 46.
+    const bool uneven = rows > 2 * sms && rows < 3 * sms;
+    const bool large = uneven && a.V >= (a.K ? 65536 : 32768) && (eb == 2 || rows * a.V * eb <= 96 << 20);
     const int threads = (vectors <= 1024 && rows > 2 * sms) || (vectors <= 8192 && rows > 8 * sms && a.K <= 32) ? kLogpSmall
-                        : rows > 2 * sms && rows <= 3 * sms ? kLogpLarge
-                                                            : kLogpThreads;
+                        : large                                                                                ? kLogpLarge
+                                                                                                                : kLogpThreads;
     // Few rows are spread over the SMs, less thinly with alternatives, whose lists are joined (64 x 50257 fp32, 20: 8.7 us over
     // four blocks, 12.3 over eight; 16 x 32768 bf16 6.6 with eight vectors a thread, 8.3 with two).
     const int blocks = a.K ? 2 : 4, vectors_each = a.K ? 8 : 2;

@@ -225,3 +225,11 @@ def test_masked_places_beside_ordinary_ones(mask, dtype):
     check_gradient(z.to(dtype), 0.7, 47)
     want, got = Exact(z.to(dtype), 0.7), lm.token_log_probs_forward(z.to(dtype), z.argmax(1), 0.7)
     within(got[1], want.entropy, want.of_entropy, "entropy")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [296, 297, 443, 444])
+@pytest.mark.parametrize("V,K", [(32767, 3), (32768, 1), (65535, 20), (65536, 64), (98305, 2)])
+def test_where_the_number_of_threads_changes(T, V, K, dtype):
+    z = normal_rows(T, V, 53 + T + V).to(dtype)
+    check_forward(z, 1.0, K)
