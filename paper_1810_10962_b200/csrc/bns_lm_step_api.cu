@@ -85,11 +85,17 @@ HeadPlan plan_heads(const bns_head_norm* sh, const HeadNorm& a) {
         pl.wide = units > 32;
     };
     share();
-    // A warp with little to do at a position waits for angles and weights: half as large vectors make these half as many for a
-    // lane.  16384 positions, bf16, vectors of 16 / 8 bytes: 4 + 1 heads of 64 forward 20 / 16 us, gradient 25 / 20; 16 + 4 of 64 24 / 22
-    // and 38 / 49; 8 + 8 of 128 30 / 31 and 45 / 51.
-    const int rounds = divide_up(sh->q_heads, 32 / pl.lanes);
-    if (pl.V == 8 && (a.q.dy ? rounds == 1 && pl.lanes <= 4 : rounds * pl.lanes <= 8)) {
+    // A warp with little to do at a position waits for angles and weights: half as large vectors make these half as many for a lane.  With more heads
+    // than a few rounds of a warp, queries' and keys' together, or for the gradient more than one round of the smaller vectors each, that only holds
+    // while there is no more than two 16-byte vectors for each thread that the SMs hold.  16384 positions (65536 in parentheses), bf16, vectors of
+    // 16 / 8 bytes, forward: 4 + 1 heads of 64 20.0 / 16.1 us (76 / 61), 16 + 4 of 64 24.5 / 22.9 (96 / 92), 8 + 8 of 64 21.6 / 20.6 (85 / 80), 4 + 1 of 128 22.2 / 18.6
+    // (84 / 72), but 32 + 32 of 32 28.3 / 30.3 (112 / 119) and 16 + 16 of 64 28.9 / 30.9 (115 / 123); 1024 positions of the last two 4.7 / 3.9 and 4.8 / 3.9.
+    // Gradient: 4 + 1 of 64 24.8 / 19.9 (84 / 70), 8 + 8 of 32 25.1 / 19.3 (85 / 71), but 8 + 8 of 64 26.8 / 28.7 (92 / 105) and 16 + 16 of 32 26.6 / 27.6
+    // (90 / 101); 1024 positions of the last two 7.0 / 5.9 and 7.5 / 6.1.
+    const int slots = 32 / pl.lanes, rounds = divide_up(sh->q_heads, slots), all_rounds = rounds + divide_up(sh->k_heads, slots);
+    const bool spare = a.tokens * (sh->q_heads + sh->k_heads) * sh->head_dim <= int64_t{sm_count()} * 2048 * 16;
+    const bool one_each = 2 * std::max(sh->q_heads, sh->k_heads) <= slots;
+    if (pl.V == 8 && (a.q.dy ? rounds == 1 && pl.lanes <= 4 && (one_each || spare) : rounds * pl.lanes <= 8 && (all_rounds <= 3 || spare))) {
         pl.V = 4;
         share();
     }
