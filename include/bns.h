@@ -505,7 +505,8 @@ bns_status bns_token_log_probs_backward(const bns_token_log_probs* shape, const 
  * heads of q, or of k.  k_heads may be 0: then everything of k may be NULL (dk_weight, if not, becomes zero).  position is
  * [batch][length]; one outside [0, positions) is padding: its outputs and gradients are zeros, whatever is there.
  * Backward, with d = R_p^T dy:   dx = rstd (weight d - n mean(weight d n))     dweight = sum over positions, heads of d n
- * from the inputs of the forward call; rstd is found again.  Sums are taken in fp32 in a fixed order.
+ * from the inputs of the forward call; rstd is found again.  Sums are taken in fp32 in a fixed order; a head whose squares' sum
+ * leaves fp32 (elements of 10^18 and more) counts as infinitely long: rstd is 0.
  * head_dim <= 1024, 2 <= rotary <= head_dim, even.  Any alignment of the element type; 16-byte vectors are used where pointers,
  * strides, rotary / 2 and the rest of a head allow them.  batch * length = 0 is allowed (weights' gradients become zero).
  */

@@ -3,8 +3,8 @@
 //   q = softmax of z / tau;  logp = log q_token;  H = - sum_v q_v log q_v;  alternatives: the K largest (z_v, lowest v first)
 //   dz_v = (dlogp ([v = token] - q_v) - dH q_v (log q_v + H)) / tau
 //
-// Bound by HBM: forward reads the logits once (4096 x 131072 bf16: 167 us, 6.4 TB/s), backward reads them and writes the gradient
-// (319 us, 6.7 TB/s).  With c = log2(e) / tau and a reference m, the largest z c so far, a pass keeps
+// Bound by HBM: forward reads the logits once (4096 x 131072 bf16: 168 us, 6.4 TB/s), backward reads them and writes the gradient
+// (317 us, 6.8 TB/s).  With c = log2(e) / tau and a reference m, the largest z c so far, a pass keeps
 //   s = sum 2^(z c - m)  and  t = sum 2^(z c - m) (z c - m);  then  log2 q_v = z_v c - m - log2 s,  H = ln 2 (log2 s - t / s)
 // t is a sum of terms of one sign, and a change of the reference by d scales both by 2^d after t has got d s.
 // Small blocks (128 or 256 threads, 1024 an SM) with eight 16-byte loads in flight a thread: a row's reductions lie under the
