@@ -444,7 +444,8 @@ bns_status bns_linear_cross_entropy_backward(const bns_head* shape, const void* 
  *   loss_t = temperature^2 sum_k p_k (log p_k - log q_{index_k})     lse_t = log sum_v exp(logits_tv / temperature)
  *   dlogits_tv = dloss_t temperature (q_v - sum over k with index_k = v of p_k)
  * A row without entries (or whose entries are all -inf) has loss 0 and gradient 0.  _backward takes the
- * lse of _forward; _step gives loss and gradient in one launch where dloss is known beforehand.
+ * lse of _forward, whose rounding (2^-24 of it) its q carry; _step gives loss and gradient in one launch where dloss is known
+ * beforehand, without that.
  * 1 <= entries <= 1024, 10^-38 <= temperature <= 10^30.  Any alignment of the element type.
  */
 typedef struct {

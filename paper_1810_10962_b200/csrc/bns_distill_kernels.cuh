@@ -97,10 +97,10 @@ constexpr int kDistillOwn = 2;                                      // entries t
 static_assert(kDistillThreads * kDistillOwn == kDistillMaxEntries);
 constexpr int kDistillDepth = 8;                                    // vectors in flight per thread
 
-// The student's maximum and sum as the forward call's log-sum tells them: lse tau c = m + rest with the same c as in
-// z c, so that only z - lse tau feels its rounding; 2^rest stands in for the sum.
-__device__ __forceinline__ TopSum student_of(const Distill& a, float lse) {
-    const double exponent = static_cast<double>(lse) * a.tau * a.c;
+// The student's maximum and sum as the forward call's log-sum tells them: its m + log2 s = m' + rest, which was found with the same rounded c
+// as z c is; 2^rest stands in for the sum.
+__device__ __forceinline__ TopSum student_of(float lse) {
+    const double exponent = static_cast<double>(lse) * (1. / kLn2Exact);
     const float m = static_cast<float>(exponent);
     return {m, exp2_fast(static_cast<float>(exponent - m))};
 }
@@ -338,13 +338,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
             for (int q = 1; q < a.parts; ++q) st = join(st, of_part[q]);
         }
     } else {
-        st = student_of(a, lse);
+        st = student_of(lse);
     }
     const bool any = teacher.s != 0.f;             // false: no entry, or all at -inf
 
     // the log-sum of a backward call tells -inf (nothing to do again) from far down
     if (tid == 0) far = (!(fabsf(st.m) <= kNear) && (kLoss || lse != -inf)) || (fabsf(teacher.m) > kNear && teacher.m != -inf);
-    if (kLoss && tid == 0 && part == 0 && a.lse) a.lse[row] = (st.m + log2f(st.s)) * kLn2;
+    if (kLoss && tid == 0 && part == 0 && a.lse) a.lse[row] = static_cast<float>((static_cast<double>(st.m) + log2f(st.s)) * kLn2Exact);
 
     // p_k, and the loss of differences to the two maxima: log p_k - log q_k in units of ln 2
     float loss = 0.f;

@@ -6,6 +6,7 @@
 namespace bns {
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr double kLn2Exact = 0.693147180559945309;
 constexpr float kFar = 0x1p29f;       // beyond it the rounding of max c, 2^-24 of it, is too much for an exponent
 constexpr float kNear = 0x1p28f;      // beside a maximum within it, what lies below -kFar is 0
 

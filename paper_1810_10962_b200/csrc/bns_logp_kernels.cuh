@@ -29,7 +29,6 @@ constexpr int kLogpSegments = 8;                        // of a thread
 constexpr int kLogpFound = 1024;                        // values that reach the bound, before the slow way is taken
 constexpr int kLogpQueue = 512;                         // segments that reach it, likewise
 constexpr int kLogpLooks = 4;                           // vectors of queued segments in flight per thread
-constexpr double kLn2Exact = 0.693147180559945309;
 constexpr float kLogpFloor = -0x1p60f;                  // stands in for anything lower: 2^(floor c - m) = 0, and 0 times it is 0
 static_assert(kLogpParts * kLogpMaxTop <= kLogpFound);
 
